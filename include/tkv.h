@@ -437,6 +437,70 @@ int tkv_decode_attention_static(const tkv_desc *desc, const void *pool, const ui
                                 int32_t *status, void *stream /* hipStream_t */);
 
 /* ------------------------------------------------------------------ */
+/* R1: norm and rotation of queries and keys (device), its table (host).*/
+/* ------------------------------------------------------------------ */
+/*
+ * What stands between the projections and the cache, which takes keys with
+ * their positions encoded (Sec. 3.2.3).  A position has one to four axes
+ * (text: one; images and video: time, height, width); each pair of channels
+ * turns with one of them.
+ *
+ * tkv_rope_table (host): one word per pair of channels, table_out[i] = the
+ * turns per position of pair i, inv_freq[i] / 2 pi, modulo 1, in units of
+ * 2^-64, its lowest two bits replaced by the pair's axis.
+ *   rotary_dim  channels 0 .. rotary_dim-1 of a head turn, a multiple of 16,
+ *               0 .. 128; the others keep their place
+ *   sections    host i32[n_axes], pairs of each axis, summing to rotary_dim/2;
+ *               NULL for one axis
+ *   interleaved 0: the first sections[0] pairs turn with axis 0, the next
+ *               sections[1] with axis 1, ...; 1: pairs are dealt out in turn
+ *               (pair i to axis i mod n_axes), and an axis whose section is
+ *               used up passes its turn to axis 0
+ *   inv_freq    host f64[rotary_dim/2], angle per position of each pair, or
+ *               NULL for theta^(-2 i / rotary_dim)
+ *   table_out   host u64[rotary_dim/2]
+ * Errors: TKV_ERR_BAD_SHAPE (rotary_dim, n_axes not in 1..4, sections that do
+ * not fit), TKV_ERR_INVALID_ARG (null table, theta <= 0 or a frequency that is
+ * not finite).
+ */
+typedef struct tkv_rope {
+    int32_t rotary_dim;
+    int32_t n_axes;
+    int32_t adjacent;       /* 0: pair i is channels (i, i + rotary_dim/2); 1: channels (2i, 2i+1) */
+    float scale;            /* factor of cosine and sine, 1 unless the frequencies were stretched with one */
+    const uint64_t *table;  /* device, u64[rotary_dim/2] as written by tkv_rope_table, 8-byte aligned */
+} tkv_rope;
+int tkv_rope_table(int32_t rotary_dim, int32_t n_axes, const int32_t *sections, int32_t interleaved,
+                   double theta, const double *inv_freq, uint64_t *table_out);
+/*
+ * For every token t and head h of q and k: the RMS norm over the head's 128
+ * channels, x * rsqrt(mean(x^2) + eps) * weight, where a weight is given, then
+ * the rotation of its pairs: (a, b) becomes (a cos - b sin, a sin + b cos) *
+ * scale with angle positions[axis][t] * frequency.  Values v, if given, are
+ * copied.  All in 32 bits (angles: 2^-32 turns at any position), rounded once.
+ *   q, k, v      device bf16, 16-byte aligned; token t, head h, channel c at
+ *                t * stride + h * 128 + c with the tensor's own stride in
+ *                elements (a multiple of 8): parts of a packed projection, or
+ *                tensors of their own.  q may be NULL if n_q_heads = 0; k and v
+ *                if n_kv_heads = 0; v may be NULL at any time
+ *   positions    device i32[n_axes][n_tokens], any value; unused (may be NULL)
+ *                if rotary_dim = 0
+ *   q_weight,    device bf16[128], 16-byte aligned, or NULL: no norm
+ *   k_weight
+ *   q_out, k_out, device bf16 [n_tokens, heads, 128], contiguous, 16-byte
+ *   v_out        aligned; an output may be its input, if that is contiguous,
+ *                and overlaps no other buffer of the call
+ * The sum of a row's squares must be finite in 32 bits (a row beyond that gives
+ * zeros, one that holds NaN or infinities NaN; other rows are left alone), and
+ * with eps = 0 a row of zeros gives NaN.  At most 2^31 - 4096 rows of heads in
+ * all.  n_tokens = 0 is a no-op.  One launch on `stream`.
+ */
+int tkv_norm_rope(const tkv_rope *rope, const void *q, int64_t q_stride, const void *k, int64_t k_stride,
+                  const void *v, int64_t v_stride, int32_t n_tokens, int32_t n_q_heads, int32_t n_kv_heads,
+                  const int32_t *positions, const void *q_weight, const void *k_weight, float eps,
+                  void *q_out, void *k_out, void *v_out, void *stream /* hipStream_t */);
+
+/* ------------------------------------------------------------------ */
 /* Measurement aid (device).                                            */
 /* ------------------------------------------------------------------ */
 /*

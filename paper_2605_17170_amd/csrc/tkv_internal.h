@@ -1,6 +1,6 @@
 // Internal interface between the host-side validation (tkv_host.cpp) and the
 // kernel launchers (tkv_append.hip, tkv_gather.hip, tkv_decode.hip,
-// tkv_probe.hip).  Arguments are already
+// tkv_rope.hip, tkv_probe.hip).  Arguments are already
 // validated; the launchers return TKV_OK or TKV_ERR_HIP.
 #ifndef TKV_INTERNAL_H
 #define TKV_INTERNAL_H
@@ -29,6 +29,9 @@ int tkv_launch_decode_split(const tkv_desc *desc, const void *pool, const uint8_
 int tkv_launch_decode_reduce(const tkv_desc *desc, const int32_t *seq_item_indptr, int32_t n_items, int32_t batch,
                              int32_t n_q_heads, float *out, const void *workspace, void *stream);
 
+int tkv_launch_norm_rope(const tkv_rope *rope, const void *q, int64_t q_stride, const void *k, int64_t k_stride, const void *v,
+                         int64_t v_stride, int32_t n_tokens, int32_t n_q_heads, int32_t n_kv_heads, const int32_t *positions,
+                         const void *q_weight, const void *k_weight, float eps, void *q_out, void *k_out, void *v_out, void *stream);
 
 // Argument checks shared by the decode entry points (tkv_host.cpp); TKV_OK or a negative status.
 int tkv_decode_check_args(const tkv_desc *desc, int32_t n_items, int32_t batch, int32_t n_q_heads,

@@ -43,7 +43,7 @@ EXPORTS = [
     "tkv_seq_page_ids", "tkv_route_residual", "tkv_plan_append_max_work", "tkv_plan_append", "tkv_quantize_append", "tkv_gather_dequant",
     "tkv_plan_decode_capacity", "tkv_plan_decode", "tkv_decode_workspace_bytes", "tkv_decode_attention",
     "tkv_decode_split", "tkv_decode_reduce", "tkv_decode_attention_static", "tkv_allocate_bits_greedy", "tkv_allocate_bits_exhaustive",
-    "tkv_tag_tokens", "tkv_tags_to_bits", "tkv_tag_counts", "tkv_probe_stream_read",
+    "tkv_tag_tokens", "tkv_tags_to_bits", "tkv_tag_counts", "tkv_rope_table", "tkv_norm_rope", "tkv_probe_stream_read",
     "tkv_probe_decode_reads", "tkv_probe_stream_mix",
 ]
 
@@ -63,6 +63,13 @@ class tkv_desc(C.Structure):
     def make(cls, n_kv_heads, n_pages_int2, n_pages_int4, head_dim=HEAD_DIM, group_size=GROUP_SIZE,
              page_tokens=PAGE_TOKENS, int2_key_axis=0):
         return cls(n_kv_heads, head_dim, group_size, page_tokens, n_pages_int2, n_pages_int4, int2_key_axis)
+
+
+class tkv_rope(C.Structure):
+    """How q and k are rotated; `table` (device) comes from tkv_rope_table.  Made by tkv_rope_make, which keeps the
+    table's tensor alive in `table_tensor`."""
+    _fields_ = [("rotary_dim", C.c_int32), ("n_axes", C.c_int32), ("adjacent", C.c_int32), ("scale", C.c_float),
+                ("table", C.c_void_p)]
 
 
 _lib = None
@@ -124,6 +131,9 @@ def lib():
                                                   vp, vp, vp]
         L.tkv_decode_split.argtypes = [dp, vp, vp, vp, vp, vp, vp, vp, vp, i32, i32, i32, C.c_float, vp, sz, vp, vp]
         L.tkv_decode_reduce.argtypes = [dp, vp, i32, i32, i32, vp, vp, sz, vp]
+        L.tkv_rope_table.argtypes = [i32, i32, vp, i32, C.c_double, vp, vp]
+        L.tkv_norm_rope.argtypes = [C.POINTER(tkv_rope), vp, C.c_int64, vp, C.c_int64, vp, C.c_int64, i32, i32, i32, vp, vp, vp, C.c_float,
+                                    vp, vp, vp, vp]
         L.tkv_probe_stream_read.argtypes = [vp, sz, vp, vp]
         L.tkv_probe_decode_reads.argtypes = [dp, vp, vp, vp, vp, vp, vp, i32, i32, i32, vp, vp]
         L.tkv_probe_stream_mix.argtypes = [vp, vp, sz, i32, i32, vp]
@@ -488,6 +498,58 @@ def tkv_tag_counts(tags) -> np.ndarray:
     counts = np.zeros(N_TAGS, np.int64)
     _check(lib().tkv_tag_counts(pt, tg.size, C.c_void_p(counts.ctypes.data)), "tkv_tag_counts")
     return counts
+
+
+# ---------------------------------------------------------------- R1 (host table, device)
+def tkv_rope_table(rotary_dim: int, theta: float = 10000.0, sections=None, interleaved: bool = False, inv_freq=None) -> np.ndarray:
+    """Words of the rotation table u64[rotary_dim/2]; sections: pairs of each axis (None: one axis)."""
+    out = np.zeros(max(0, rotary_dim // 2), np.uint64)
+    sec, ps = _np(sections if sections is not None else [rotary_dim // 2], np.int32)
+    pf = None
+    if inv_freq is not None:
+        freq, pf = _np(inv_freq, np.float64)
+        if freq.size != out.size:
+            raise ValueError("inv_freq has one entry per pair of channels")
+    _check(lib().tkv_rope_table(rotary_dim, sec.size, ps, 1 if interleaved else 0, float(theta), pf,
+                                C.c_void_p(out.ctypes.data if out.size else None)), "tkv_rope_table")
+    return out
+
+
+def tkv_rope_make(rotary_dim: int, theta: float = 10000.0, sections=None, interleaved: bool = False, adjacent: bool = False, inv_freq=None,
+                  scale: float = 1.0, device="cuda") -> tkv_rope:
+    """tkv_rope_table, moved to the device."""
+    import torch
+    table = tkv_rope_table(rotary_dim, theta, sections, interleaved, inv_freq)
+    rope = tkv_rope(rotary_dim, 1 if sections is None else len(sections), 1 if adjacent else 0, float(scale), None)
+    rope.table_tensor = torch.from_numpy(table.view(np.int64)).to(device)
+    rope.table = _dev(rope.table_tensor) if table.size else None
+    return rope
+
+
+def _rows(t, heads: str):
+    """(device pointer, token stride in elements, heads) of a bf16 tensor [T, heads, 128] whose heads lie densely."""
+    if t is None:
+        return None, 0, 0
+    assert t.dim() == 3 and int(t.shape[2]) == HEAD_DIM and t.element_size() == 2, heads + " is bf16 [tokens, heads, 128]"
+    assert t.stride(2) == 1 and (t.shape[1] <= 1 or t.stride(1) == HEAD_DIM), "the heads of a token lie one behind the other"
+    return t.data_ptr(), t.stride(0) if t.shape[0] > 1 else int(t.shape[1]) * HEAD_DIM, int(t.shape[1])
+
+
+def tkv_norm_rope(rope: tkv_rope, q, k, v, positions, q_weight, k_weight, eps: float, q_out, k_out, v_out=None, stream=None, prepare=False):
+    """Device tensors: q [T,Hq,128], k and v [T,Hkv,128] bf16, each with a token stride of its own (parts of a packed
+    projection), or None; positions i32[n_axes,T]; weights bf16[128] or None; outputs contiguous, v_out only with v."""
+    (pq, sq, hq), (pk, sk, hk), (pv, sv, hv) = _rows(q, "q"), _rows(k, "k"), _rows(v, "v")
+    n = int((q if q is not None else k).shape[0]) if q is not None or k is not None else 0
+    for t, o in ((q, q_out), (k, k_out), (v, v_out)):
+        assert t is None or (o is not None and tuple(o.shape) == tuple(t.shape) and o.element_size() == 2 and int(t.shape[0]) == n)
+    assert v is None or (k is not None and hv == hk)
+    assert rope.rotary_dim == 0 or positions.numel() == rope.n_axes * n and positions.element_size() == 4
+    for w in (q_weight, k_weight):
+        assert w is None or (w.numel() == HEAD_DIM and w.element_size() == 2)
+    return _run(lib().tkv_norm_rope,
+                (C.byref(rope), pq, sq, pk, sk, pv, sv, n, hq, hk, _dev(positions), _dev(q_weight), _dev(k_weight), float(eps),
+                 _dev(q_out if q is not None else None), _dev(k_out if k is not None else None), _dev(v_out if v is not None else None), _stream(stream)),
+                "tkv_norm_rope", (rope, q, k, v, positions, q_weight, k_weight, q_out, k_out, v_out, stream), prepare)
 
 
 # ---------------------------------------------------------------- measurement aid (device)

@@ -1,0 +1,196 @@
+"""tkv_norm_rope against a 64-bit evaluation of its formulas.
+
+Tolerance: the result is rounded to bf16 once, at most half a step, 2^-8 of the value.  Before that, in 32 bits, a
+product x * r * w is off by at most 14 half steps (twenty additions of squares count half through the root, the root,
+two products), cosine and sine by 4 (polynomial 3e-8, conversion of the angle, its evaluation), the rotation by 3: less
+than 2^-19 of |a| + |b| of the pair, times the scale."""
+import numpy as np
+import pytest
+import torch
+
+from paper_2605_17170_amd import tkv
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+
+
+def reference(x, weight, eps, pos, table_axes, freq, rotary, adjacent, scale):
+    """Value and tolerance, 64 bits; table_axes: axis of each pair."""
+    y = x.double()
+    if weight is not None:
+        y = y / torch.sqrt(y.square().mean(-1, keepdim=True) + eps) * weight.double()
+    out, size = y.clone(), y.abs()
+    half = rotary // 2
+    for i in range(half):
+        a, b = (2 * i, 2 * i + 1) if adjacent else (i, i + half)
+        angle = (pos[table_axes[i]].double() * freq[i])[:, None]
+        c, s = torch.cos(angle) * scale, torch.sin(angle) * scale
+        out[..., a], out[..., b] = y[..., a] * c - y[..., b] * s, y[..., a] * s + y[..., b] * c
+        size[..., a] = size[..., b] = (y[..., a].abs() + y[..., b].abs()) * max(1.0, abs(scale))
+    return out, 2.0 ** -8 * out.abs() + 2.0 ** -18 * size
+
+
+def check(got, want, what):
+    ref, tol = want
+    off = (got.double() - ref).abs()
+    worst = float((off / tol.clamp_min(1e-30)).max()) if off.numel() else 0.0
+    assert torch.isfinite(got.float()).all() and worst <= 1.0, "%s: %.3f of the tolerance" % (what, worst)
+
+
+def inputs(seed, tokens, hq, hk, packed, pad=0):
+    g = torch.Generator(device=DEV)
+    g.manual_seed(seed)
+    heads = hq + 2 * hk
+    row = torch.randn((tokens, heads * 128 + pad), device=DEV, generator=g)
+    row = (row * torch.where(torch.rand((heads * 128 + pad,), device=DEV, generator=g) < 0.05, 30.0, 1.0)).to(torch.bfloat16)
+    rows = row[:, :heads * 128].unflatten(1, (heads, 128))
+    parts = [rows[:, :hq], rows[:, hq:hq + hk], rows[:, hq + hk:]]
+    if not packed:
+        parts = [p.contiguous() for p in parts]
+    weights = [(1.0 + 0.3 * torch.randn((128,), device=DEV, generator=g)).to(torch.bfloat16) for _ in range(2)]
+    return parts, weights
+
+
+def axes_of(rope):
+    return [int(w) & 3 for w in rope.table_tensor.cpu().numpy().view(np.uint64)]
+
+
+def run_and_check(seed, tokens, hq, hk, rotary, theta=1e6, sections=None, interleaved=False, adjacent=False, norm=(True, True), packed=True, pad=0,
+                  scale=1.0, eps=1e-6, with_v=True, first=0, pos=None):
+    parts, weights = inputs(seed, tokens, hq, hk, packed, pad)
+    rope = tkv.tkv_rope_make(rotary, theta, sections, interleaved, adjacent, scale=scale, device=DEV)
+    if pos is None:
+        g = torch.Generator(device=DEV)
+        g.manual_seed(seed + 1)
+        pos = first + torch.randint(0, 5000, (rope.n_axes, tokens), device=DEV, generator=g, dtype=torch.int32)
+    w = [x if n else None for x, n in zip(weights, norm)]
+    guard = 7.0
+    outs = [torch.full((tokens + 1, p.shape[1], 128), guard, dtype=torch.bfloat16, device=DEV) for p in parts]
+    tkv.tkv_norm_rope(rope, parts[0] if hq else None, parts[1] if hk else None, parts[2] if hk and with_v else None, pos, w[0], w[1], eps,
+                      *[o[:tokens] for o in outs])
+    torch.cuda.synchronize()
+    freq = [theta ** (-2.0 * i / rotary) for i in range(rotary // 2)]
+    axes = axes_of(rope) if rotary else []
+    for p, o, wt, what in zip(parts, outs, w, "qk"):
+        if p.shape[1]:
+            check(o[:tokens], reference(p, wt, eps, pos, axes, freq, rotary, adjacent, scale), what)
+    if hk:
+        assert torch.equal(outs[2][:tokens], parts[2]) if with_v else bool((outs[2] == guard).all())
+    assert all(bool((o[tokens:] == guard).all()) for o in outs)
+
+
+@pytest.mark.parametrize("tokens", [1, 2, 3, 31, 257])
+@pytest.mark.parametrize("hq,hk", [(1, 1), (3, 1), (8, 8), (64, 8), (0, 2), (5, 0)])
+def test_heads_and_lengths(tokens, hq, hk):
+    run_and_check(tokens * 131 + hq, tokens, hq, hk, 128)
+
+
+@pytest.mark.parametrize("adjacent", [False, True])
+@pytest.mark.parametrize("rotary", [0, 16, 48, 64, 96, 112, 128])
+def test_part_of_the_head_turns(rotary, adjacent):
+    run_and_check(rotary, 37, 6, 2, rotary, theta=1e4, adjacent=adjacent)
+
+
+@pytest.mark.parametrize("norm", [(True, False), (False, True), (False, False)])
+def test_norms_of_either(norm):
+    run_and_check(5, 41, 7, 2, 64, norm=norm, packed=False, with_v=False)
+
+
+@pytest.mark.parametrize("sections,interleaved", [([16, 24, 24], False), ([24, 20, 20], True), ([32, 32], True), ([1, 2, 3, 58], False), ([64, 0, 0], False)])
+@pytest.mark.parametrize("adjacent", [False, True])
+def test_axes(sections, interleaved, adjacent):
+    run_and_check(9, 53, 8, 2, 128, sections=sections, interleaved=interleaved, adjacent=adjacent, pad=72)
+
+
+def test_scale_and_eps():
+    run_and_check(11, 29, 4, 1, 128, scale=1.3465735, eps=0.25)
+
+
+@pytest.mark.parametrize("adjacent", [False, True])
+def test_far_and_negative_positions(adjacent):
+    # the reference's own angle is position * frequency in 64 bits: off by 2^-53 of 2^31, far below the tolerance
+    pos = torch.tensor([[0, 1, -1, 2 ** 20, 2 ** 24 + 1, 2 ** 31 - 1, -2 ** 31, -12345678]], dtype=torch.int32, device=DEV)
+    run_and_check(13, 8, 2, 2, 128, theta=1e4, adjacent=adjacent, pos=pos)
+
+
+def test_many_tokens_of_many_heads():
+    run_and_check(15, 4099, 32, 8, 128, sections=[24, 20, 20], interleaved=True)
+
+
+def test_in_place_and_alone_on_a_stream():
+    parts, weights = inputs(17, 300, 8, 4, False)
+    rope = tkv.tkv_rope_make(128, 1e6, device=DEV)
+    pos = torch.arange(300, dtype=torch.int32, device=DEV)[None]
+    outs = [torch.empty_like(p) for p in parts]
+    tkv.tkv_norm_rope(rope, *parts, pos, *weights, 1e-6, *outs)
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    tkv.tkv_norm_rope(rope, *parts, pos, *weights, 1e-6, *parts, stream=s)
+    torch.cuda.synchronize()
+    assert all(torch.equal(p, o) for p, o in zip(parts, outs))
+
+
+def test_a_row_of_nan_or_infinities_leaves_the_others():
+    parts, weights = inputs(19, 5, 4, 1, False)
+    rope = tkv.tkv_rope_make(96, 1e6, device=DEV)
+    pos = torch.arange(5, dtype=torch.int32, device=DEV)[None]
+    outs, clean = [torch.empty_like(p) for p in parts], [torch.empty_like(p) for p in parts]
+    tkv.tkv_norm_rope(rope, *parts, pos, *weights, 1e-6, *clean)
+    parts[0][2, 1, 7], parts[0][4, 3, 127] = float("nan"), float("inf")
+    parts[1][0, 0, 3] = float("-inf")
+    tkv.tkv_norm_rope(rope, *parts, pos, *weights, 1e-6, *outs)
+    torch.cuda.synchronize()
+    for o, c, bad in ((outs[0], clean[0], [(2, 1), (4, 3)]), (outs[1], clean[1], [(0, 0)])):
+        same = torch.ones(o.shape[:2], dtype=torch.bool, device=DEV)
+        for t, h in bad:
+            same[t, h] = False
+            assert torch.isnan(o[t, h]).any()
+        assert torch.equal(o[same], c[same])
+    # without a norm, what does not turn stays what it is
+    plain = torch.empty_like(parts[0])
+    tkv.tkv_norm_rope(rope, parts[0], None, None, pos, None, None, 0.0, plain, None)
+    torch.cuda.synchronize()
+    assert torch.equal(plain[4, 3, 96:], parts[0][4, 3, 96:]) and torch.isfinite(plain[4, 3, :96].float()).all()
+
+
+def test_no_tokens():
+    parts, weights = inputs(21, 1, 4, 1, False)
+    rope = tkv.tkv_rope_make(128, 1e6, device=DEV)
+    none = [p[:0] for p in parts]
+    tkv.tkv_norm_rope(rope, *none, torch.zeros((1, 0), dtype=torch.int32, device=DEV), *weights, 1e-6, *none)
+    torch.cuda.synchronize()
+
+
+def test_more_than_two_to_the_31_values():
+    tokens = (1 << 24) + 5
+    x = torch.zeros((tokens, 1, 128), dtype=torch.bfloat16, device=DEV)
+    at = [0, 1, 8191, (1 << 23) - 1, 1 << 23, (1 << 24) - 1, 1 << 24, tokens - 1]
+    g = torch.Generator(device=DEV)
+    g.manual_seed(3)
+    x[at] = torch.randn((len(at), 1, 128), device=DEV, generator=g).to(torch.bfloat16)
+    keep = x[at].clone()
+    pos = torch.arange(tokens, dtype=torch.int32, device=DEV)[None]
+    rope = tkv.tkv_rope_make(128, 1e6, device=DEV)
+    tkv.tkv_norm_rope(rope, x, None, None, pos, None, None, 0.0, x, None)
+    torch.cuda.synchronize()
+    freq = [1e6 ** (-2.0 * i / 128) for i in range(64)]
+    check(x[at], reference(keep, None, 0.0, pos[:, at], [0] * 64, freq, 128, False, 1.0), "far rows")
+
+
+def test_captured_and_replayed():
+    parts, weights = inputs(23, 32, 64, 8, True)
+    rope = tkv.tkv_rope_make(128, 1e6, device=DEV)
+    pos = torch.arange(32, dtype=torch.int32, device=DEV)[None].contiguous()
+    outs, eager = [torch.empty(p.shape, dtype=p.dtype, device=DEV) for p in parts], [torch.empty(p.shape, dtype=p.dtype, device=DEV) for p in parts]
+    call = lambda o: tkv.tkv_norm_rope(rope, *parts, pos, *weights, 1e-6, *o)  # noqa: E731
+    call(outs)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        call(outs)
+    for step in range(4):
+        pos += 3
+        call(eager)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(outs, eager)), step
