@@ -52,8 +52,11 @@ enum {
     TKV_STATUS_BLOCK_PARTIAL = 16,   /* append, per-channel INT2 keys: a 32-token block arrived incomplete (block skipped) */
     TKV_STATUS_SCALE_SATURATED = 32, /* decode: a stored V scale above 255, or a per-channel INT2 key scale above 1023, was
                                         clamped: the output is finite but not the attention over the stored values */
-    TKV_STATUS_BAD_ITEM = 64         /* decode: a work item names a sequence outside the batch (it contributes nothing)
+    TKV_STATUS_BAD_ITEM = 64,        /* decode: a work item names a sequence outside the batch (it contributes nothing)
                                         or a partial slot outside the workspace (its partial is not stored) */
+    TKV_STATUS_TABLE_REFUSED = 128,  /* tkv_table_append: lengths, widths or a table that cannot be (nothing was changed) */
+    TKV_STATUS_POOL_EXHAUSTED = 256, /* tkv_table_append: too few free pages (nothing was changed) */
+    TKV_STATUS_CAPACITY = 512        /* tkv_table_append: max_pages or max_work is too small (nothing was changed) */
 };
 
 const char *tkv_strerror(int status);
@@ -435,6 +438,83 @@ int tkv_decode_attention_static(const tkv_desc *desc, const void *pool, const ui
                                 const int32_t *items, const int32_t *seq_item_indptr, int32_t n_items,
                                 int32_t batch, int32_t n_q_heads, float sm_scale, float *out,
                                 int32_t *status, void *stream /* hipStream_t */);
+
+/* ------------------------------------------------------------------ */
+/* Q1 on the GPU: page tables of a batch in device memory.              */
+/* ------------------------------------------------------------------ */
+/*
+ * The page tables, token counts and free lists of n_seqs sequences, all in
+ * device memory that the caller owns (4-byte aligned), for loops that the host
+ * does not take part in: a captured decode step, drafting and rejecting.  The
+ * same page streams as a tkv_seq has: row b of page_ids holds the sequence's
+ * INT2 pages, then its INT4 pages, then -1; with page_indptr[b] = b * max_pages
+ * (i32[n_seqs+1]) it is what tkv_decode_attention and tkv_decode_split take.
+ * Free lists are stacks, the next page to hand out last: free_pages[0 ..
+ * n_free[0]) those of the INT2 pool, free_pages[n_pages_int2 .. n_pages_int2 +
+ * n_free[1]) those of the INT4 pool; behind them anything.
+ * A decode plan (tkv_plan_decode) made for more INT4 pages than a sequence has
+ * yet stays valid while it grows into them: what an item names beyond the
+ * sequence's pages is not read.
+ */
+typedef struct tkv_table {
+    int32_t n_seqs;
+    int32_t max_pages;      /* entries of a row, at most 2^24; n_seqs * max_pages < 2^31 */
+    int32_t *page_ids;      /* i32[n_seqs * max_pages] */
+    int32_t *n_tok_int2;    /* i32[n_seqs] */
+    int32_t *n_tok_int4;    /* i32[n_seqs] */
+    int32_t *free_pages;    /* i32[n_pages_int2 + n_pages_int4] */
+    int32_t *n_free;        /* i32[2] */
+} tkv_table;
+
+/* No sequence has tokens and all pages are free, handed out in increasing order (one launch). */
+int tkv_table_reset(const tkv_desc *desc, const tkv_table *table, void *stream /* hipStream_t */);
+/* Upper bound of the pages that n_tokens tokens for n_seqs sequences can touch. */
+int32_t tkv_table_max_work(int32_t n_seqs, int32_t n_tokens);
+/* Bytes of workspace of tkv_table_append; 0 on a bad count. */
+size_t tkv_table_workspace_bytes(int32_t n_seqs, int32_t n_tokens);
+/*
+ * First cuts every sequence b back to its first keep_int2[b] tokens of the INT2
+ * stream and keep_int4[b] of the INT4 stream (0: a request that has ended; a
+ * few less: rejected drafts; as many or more than there are: nothing); pages
+ * that hold none of them return to the free lists, the first page of the first
+ * sequence on top, so that the same tokens appended again get the same pages.
+ * Then appends n_new[b] tokens to sequence b: the next ones of tag_bits (the
+ * sequences' tokens lie one behind the other), each to the stream of its width,
+ * pages from the top of the free lists, sequences in order: what one
+ * tkv_plan_append per sequence does.
+ *   keep_int2/4   device i32[n_seqs], or NULL: nothing is cut
+ *   n_new         device i32[n_seqs], or NULL: nothing arrives
+ *   tag_bits      device u8[n_tokens], 2 or 4; may be NULL if n_tokens = 0.  The
+ *                 lengths sum to at most n_tokens; tokens behind the last
+ *                 sequence (a padded batch) are no tokens
+ *   token_indptr  device i32[n_seqs+1] or NULL: first token of each sequence
+ *   positions     device i32[n_tokens] or NULL: place of each token in its
+ *                 sequence, over both widths; -1 behind the last sequence
+ *   slot_ids      device i32[n_tokens] or NULL: page * 64 + slot; -1 behind
+ *   work_pages, work_src   device i32[max_work], i32[max_work*64]: as written by
+ *                 tkv_plan_append (of each sequence INT2 pages, then INT4 pages);
+ *                 entries behind the last are page 0 with no slot named, which
+ *                 tkv_quantize_append passes over: it can be called with
+ *                 n_work = max_work from code that does not know n_work.
+ *                 max_work: see tkv_table_max_work
+ *   n_work        device i32: number of pages listed
+ *   workspace     device, >= tkv_table_workspace_bytes(...), 16-byte aligned,
+ *                 needs no initialisation, may be shared by calls on one stream
+ *   status        device i32, may be NULL
+ * All or nothing: where lengths are negative or sum to more than n_tokens, a
+ * width is neither 2 nor 4, counts of per-channel INT2 keys are no multiples of
+ * 32 (arriving or kept) or the table contradicts itself
+ * (TKV_STATUS_TABLE_REFUSED), a pool has too few pages
+ * (TKV_STATUS_POOL_EXHAUSTED), or max_pages or max_work does not suffice
+ * (TKV_STATUS_CAPACITY), the table stays as it is, n_work and token_indptr are
+ * 0, no slot is named, and slot_ids and positions are -1.
+ * One launch for up to 1024 sequences and 8192 tokens, else up to four.
+ */
+int tkv_table_append(const tkv_desc *desc, const tkv_table *table, const int32_t *keep_int2, const int32_t *keep_int4,
+                     const int32_t *n_new, const uint8_t *tag_bits, int32_t n_tokens,
+                     int32_t *token_indptr, int32_t *positions, int32_t *slot_ids,
+                     int32_t *work_pages, int32_t *work_src, int32_t max_work, int32_t *n_work,
+                     void *workspace, size_t workspace_bytes, int32_t *status, void *stream /* hipStream_t */);
 
 /* ------------------------------------------------------------------ */
 /* R1: norm and rotation of queries and keys (device), its table (host).*/

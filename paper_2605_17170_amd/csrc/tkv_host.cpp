@@ -3,7 +3,7 @@
 // INT2 keys, the triaxial tagger and the tag -> bitwidth allocation, and
 // argument validation in front of the kernel launchers.  Nothing here touches
 // the GPU; the launchers live in tkv_append.hip, tkv_gather.hip,
-// tkv_decode.hip, tkv_rope.hip and tkv_probe.hip.
+// tkv_decode.hip, tkv_table.hip, tkv_rope.hip and tkv_probe.hip.
 //
 // Paper passages: offset-split shared address space and one allocator per
 // pool, Sec. 3.2.2; per-token bitwidth array routing tokens to the pools and
@@ -525,6 +525,56 @@ int tkv_tag_counts(const uint8_t *tags, int32_t n_tokens, int64_t *counts)
         if (tags[t] >= TKV_N_TAGS) return TKV_ERR_INVALID_ARG;
     for (int32_t t = 0; t < n_tokens; ++t) ++counts[tags[t]];
     return TKV_OK;
+}
+
+/* ---------------------------------------------------------------- Q1 on the GPU: page tables in device memory */
+
+namespace {
+constexpr int32_t kMaxTableTokens = 1 << 28, kMaxTablePages = 1 << 24;
+int table_status(const tkv_desc *desc, const tkv_table *t)
+{
+    if (int st = desc_status(desc)) return st;
+    if (!t || t->n_seqs < 0 || t->max_pages < 0 || t->max_pages > kMaxTablePages || (int64_t)t->n_seqs * t->max_pages > INT32_MAX) return TKV_ERR_INVALID_ARG;
+    if (!t->n_free || (desc->n_pages_int2 + desc->n_pages_int4 > 0 && !t->free_pages)) return TKV_ERR_INVALID_ARG;
+    if (t->n_seqs > 0 && (!t->n_tok_int2 || !t->n_tok_int4 || (t->max_pages > 0 && !t->page_ids))) return TKV_ERR_INVALID_ARG;
+    const uintptr_t all = (uintptr_t)t->page_ids | (uintptr_t)t->n_tok_int2 | (uintptr_t)t->n_tok_int4 | (uintptr_t)t->free_pages | (uintptr_t)t->n_free;
+    return all & 3 ? TKV_ERR_INVALID_ARG : TKV_OK;
+}
+} // namespace
+
+int tkv_table_reset(const tkv_desc *desc, const tkv_table *table, void *stream)
+{
+    if (int st = table_status(desc, table)) return st;
+    return tkv_launch_table_reset(desc, table, stream);
+}
+
+int32_t tkv_table_max_work(int32_t n_seqs, int32_t n_tokens)
+{
+    if (n_seqs < 0 || n_tokens < 0 || n_tokens > kMaxTableTokens) return TKV_ERR_INVALID_ARG;
+    // n tokens of a sequence touch at most n pages, and at most n / 64 + 4 (tkv_plan_append_max_work)
+    return (int32_t)std::min<int64_t>(n_tokens, n_tokens / kPageTokens + 4 * (int64_t)std::min(n_seqs, n_tokens));
+}
+
+size_t tkv_table_workspace_bytes(int32_t n_seqs, int32_t n_tokens)
+{
+    if (n_seqs < 0 || n_tokens < 0 || n_tokens > kMaxTableTokens) return 0;
+    return 4 * tkv_table_words(n_seqs, n_tokens);
+}
+
+int tkv_table_append(const tkv_desc *desc, const tkv_table *table, const int32_t *keep_int2, const int32_t *keep_int4,
+                     const int32_t *n_new, const uint8_t *tag_bits, int32_t n_tokens, int32_t *token_indptr, int32_t *positions,
+                     int32_t *slot_ids, int32_t *work_pages, int32_t *work_src, int32_t max_work, int32_t *n_work,
+                     void *workspace, size_t workspace_bytes, int32_t *status, void *stream)
+{
+    if (int st = table_status(desc, table)) return st;
+    if (n_tokens < 0 || n_tokens > kMaxTableTokens || max_work < 0 || max_work > kMaxTableTokens) return TKV_ERR_INVALID_ARG;
+    if ((n_tokens > 0 && !tag_bits) || (max_work > 0 && (!work_pages || !work_src)) || !n_work || !workspace) return TKV_ERR_INVALID_ARG;
+    const uintptr_t words = (uintptr_t)keep_int2 | (uintptr_t)keep_int4 | (uintptr_t)n_new | (uintptr_t)token_indptr | (uintptr_t)positions |
+                            (uintptr_t)slot_ids | (uintptr_t)work_pages | (uintptr_t)work_src | (uintptr_t)n_work | (uintptr_t)status;
+    if ((words & 3) || ((uintptr_t)workspace & 15)) return TKV_ERR_INVALID_ARG;
+    if (workspace_bytes < tkv_table_workspace_bytes(table->n_seqs, n_tokens)) return TKV_ERR_WORKSPACE_TOO_SMALL;
+    return tkv_launch_table_append(desc, table, keep_int2, keep_int4, n_new, tag_bits, n_tokens, token_indptr, positions, slot_ids, work_pages,
+                                   work_src, max_work, n_work, workspace, status, stream);
 }
 
 /* ---------------------------------------------------------------- R1: rotation table, norm and rotation */

@@ -1,6 +1,6 @@
 // Internal interface between the host-side validation (tkv_host.cpp) and the
 // kernel launchers (tkv_append.hip, tkv_gather.hip, tkv_decode.hip,
-// tkv_rope.hip, tkv_probe.hip).  Arguments are already
+// tkv_table.hip, tkv_rope.hip, tkv_probe.hip).  Arguments are already
 // validated; the launchers return TKV_OK or TKV_ERR_HIP.
 #ifndef TKV_INTERNAL_H
 #define TKV_INTERNAL_H
@@ -32,6 +32,12 @@ int tkv_launch_decode_reduce(const tkv_desc *desc, const int32_t *seq_item_indpt
 int tkv_launch_norm_rope(const tkv_rope *rope, const void *q, int64_t q_stride, const void *k, int64_t k_stride, const void *v,
                          int64_t v_stride, int32_t n_tokens, int32_t n_q_heads, int32_t n_kv_heads, const int32_t *positions,
                          const void *q_weight, const void *k_weight, float eps, void *q_out, void *k_out, void *v_out, void *stream);
+
+size_t tkv_table_words(int32_t n_seqs, int32_t n_tokens);
+int tkv_launch_table_reset(const tkv_desc *desc, const tkv_table *table, void *stream);
+int tkv_launch_table_append(const tkv_desc *desc, const tkv_table *table, const int32_t *keep_int2, const int32_t *keep_int4, const int32_t *n_new,
+                            const uint8_t *tag_bits, int32_t n_tokens, int32_t *token_indptr, int32_t *positions, int32_t *slot_ids,
+                            int32_t *work_pages, int32_t *work_src, int32_t max_work, int32_t *n_work, void *workspace, int32_t *status, void *stream);
 
 // Argument checks shared by the decode entry points (tkv_host.cpp); TKV_OK or a negative status.
 int tkv_decode_check_args(const tkv_desc *desc, int32_t n_items, int32_t batch, int32_t n_q_heads,

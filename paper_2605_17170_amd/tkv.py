@@ -29,6 +29,9 @@ TKV_STATUS_DST_RANGE = 8
 TKV_STATUS_BLOCK_PARTIAL = 16
 TKV_STATUS_SCALE_SATURATED = 32
 TKV_STATUS_BAD_ITEM = 64
+TKV_STATUS_TABLE_REFUSED = 128
+TKV_STATUS_POOL_EXHAUSTED = 256
+TKV_STATUS_CAPACITY = 512
 TKV_KEYS_PER_TOKEN = 0
 TKV_KEYS_PER_CHANNEL = 1
 
@@ -43,7 +46,8 @@ EXPORTS = [
     "tkv_seq_page_ids", "tkv_route_residual", "tkv_plan_append_max_work", "tkv_plan_append", "tkv_quantize_append", "tkv_gather_dequant",
     "tkv_plan_decode_capacity", "tkv_plan_decode", "tkv_decode_workspace_bytes", "tkv_decode_attention",
     "tkv_decode_split", "tkv_decode_reduce", "tkv_decode_attention_static", "tkv_allocate_bits_greedy", "tkv_allocate_bits_exhaustive",
-    "tkv_tag_tokens", "tkv_tags_to_bits", "tkv_tag_counts", "tkv_rope_table", "tkv_norm_rope", "tkv_probe_stream_read",
+    "tkv_tag_tokens", "tkv_tags_to_bits", "tkv_tag_counts", "tkv_table_reset", "tkv_table_max_work",
+    "tkv_table_workspace_bytes", "tkv_table_append", "tkv_rope_table", "tkv_norm_rope", "tkv_probe_stream_read",
     "tkv_probe_decode_reads", "tkv_probe_stream_mix",
 ]
 
@@ -63,6 +67,22 @@ class tkv_desc(C.Structure):
     def make(cls, n_kv_heads, n_pages_int2, n_pages_int4, head_dim=HEAD_DIM, group_size=GROUP_SIZE,
              page_tokens=PAGE_TOKENS, int2_key_axis=0):
         return cls(n_kv_heads, head_dim, group_size, page_tokens, n_pages_int2, n_pages_int4, int2_key_axis)
+
+
+class tkv_table(C.Structure):
+    """Page tables of a batch in device memory; `make` keeps the tensors alive."""
+    _fields_ = [("n_seqs", C.c_int32), ("max_pages", C.c_int32), ("page_ids", C.c_void_p), ("n_tok_int2", C.c_void_p),
+                ("n_tok_int4", C.c_void_p), ("free_pages", C.c_void_p), ("n_free", C.c_void_p)]
+
+    @classmethod
+    def make(cls, page_ids, n_tok_int2, n_tok_int4, free_pages, n_free):
+        """i32 device tensors: page_ids [n_seqs, max_pages], n_tok_int2/4 [n_seqs], free_pages [pages of both pools], n_free [2]."""
+        tensors = (page_ids, n_tok_int2, n_tok_int4, free_pages, n_free)
+        n, m = int(page_ids.shape[0]), int(page_ids.shape[1])
+        assert all(t.element_size() == 4 for t in tensors) and n_tok_int2.numel() == n_tok_int4.numel() == n and n_free.numel() == 2
+        table = cls(n, m, *(_dev(t) for t in tensors))
+        table.tensors = tensors
+        return table
 
 
 class tkv_rope(C.Structure):
@@ -131,6 +151,13 @@ def lib():
                                                   vp, vp, vp]
         L.tkv_decode_split.argtypes = [dp, vp, vp, vp, vp, vp, vp, vp, vp, i32, i32, i32, C.c_float, vp, sz, vp, vp]
         L.tkv_decode_reduce.argtypes = [dp, vp, i32, i32, i32, vp, vp, sz, vp]
+        tp = C.POINTER(tkv_table)
+        L.tkv_table_reset.argtypes = [dp, tp, vp]
+        L.tkv_table_max_work.restype = i32
+        L.tkv_table_max_work.argtypes = [i32, i32]
+        L.tkv_table_workspace_bytes.restype = sz
+        L.tkv_table_workspace_bytes.argtypes = [i32, i32]
+        L.tkv_table_append.argtypes = [dp, tp, vp, vp, vp, vp, i32, vp, vp, vp, vp, vp, i32, vp, vp, sz, vp, vp]
         L.tkv_rope_table.argtypes = [i32, i32, vp, i32, C.c_double, vp, vp]
         L.tkv_norm_rope.argtypes = [C.POINTER(tkv_rope), vp, C.c_int64, vp, C.c_int64, vp, C.c_int64, i32, i32, i32, vp, vp, vp, C.c_float,
                                     vp, vp, vp, vp]
@@ -498,6 +525,41 @@ def tkv_tag_counts(tags) -> np.ndarray:
     counts = np.zeros(N_TAGS, np.int64)
     _check(lib().tkv_tag_counts(pt, tg.size, C.c_void_p(counts.ctypes.data)), "tkv_tag_counts")
     return counts
+
+
+# ---------------------------------------------------------------- Q1 on the GPU (device)
+def tkv_table_reset(desc, table: tkv_table, stream=None):
+    assert table.tensors[3].numel() >= desc.n_pages_int2 + desc.n_pages_int4
+    _check(lib().tkv_table_reset(C.byref(desc), C.byref(table), _stream(stream)), "tkv_table_reset")
+
+
+def tkv_table_max_work(n_seqs: int, n_tokens: int) -> int:
+    return _check(lib().tkv_table_max_work(n_seqs, n_tokens), "tkv_table_max_work")
+
+
+def tkv_table_workspace_bytes(n_seqs: int, n_tokens: int) -> int:
+    return int(lib().tkv_table_workspace_bytes(n_seqs, n_tokens))
+
+
+def tkv_table_append(desc, table: tkv_table, keep_int2, keep_int4, n_new, tag_bits, token_indptr, positions, slot_ids, work_pages, work_src,
+                     n_work, workspace, status=None, stream=None, prepare=False):
+    """Device tensors: keep_int2/4, n_new i32[n_seqs] or None; tag_bits u8[n_tokens] or None; token_indptr i32[n_seqs+1],
+    positions, slot_ids i32[n_tokens], each or None; work_pages i32[max_work], work_src i32[max_work, 64]; n_work i32[1];
+    workspace u8."""
+    n, n_tokens = table.n_seqs, int(tag_bits.numel()) if tag_bits is not None else 0
+    max_work = int(work_pages.numel()) if work_pages is not None else 0
+    for t, count in ((keep_int2, n), (keep_int4, n), (n_new, n), (token_indptr, n + 1), (positions, n_tokens), (slot_ids, n_tokens), (n_work, 1)):
+        assert t is None or (t.numel() == count and t.element_size() == 4)
+    assert tag_bits is None or tag_bits.element_size() == 1
+    assert max_work == 0 or (work_src.numel() == max_work * PAGE_TOKENS and work_src.element_size() == work_pages.element_size() == 4)
+    assert table.tensors[3].numel() >= desc.n_pages_int2 + desc.n_pages_int4
+    ws_bytes = int(workspace.numel() * workspace.element_size()) if workspace is not None else 0
+    return _run(lib().tkv_table_append,
+                (C.byref(desc), C.byref(table), _dev(keep_int2), _dev(keep_int4), _dev(n_new), _dev(tag_bits), n_tokens, _dev(token_indptr),
+                 _dev(positions), _dev(slot_ids), _dev(work_pages), _dev(work_src), max_work, _dev(n_work), _dev(workspace), ws_bytes,
+                 _dev(status), _stream(stream)),
+                "tkv_table_append", (desc, table, keep_int2, keep_int4, n_new, tag_bits, token_indptr, positions, slot_ids, work_pages, work_src,
+                                     n_work, workspace, status, stream), prepare)
 
 
 # ---------------------------------------------------------------- R1 (host table, device)
