@@ -39,7 +39,8 @@ int tkv_launch_table_append(const tkv_desc *desc, const tkv_table *table, const 
                             const uint8_t *tag_bits, int32_t n_tokens, int32_t *token_indptr, int32_t *positions, int32_t *slot_ids,
                             int32_t *work_pages, int32_t *work_src, int32_t max_work, int32_t *n_work, void *workspace, int32_t *status, void *stream);
 
-// Argument checks shared by the decode entry points (tkv_host.cpp); TKV_OK or a negative status.
+// Argument checks shared by the entry points (tkv_host.cpp); TKV_OK or a negative status.
+int tkv_desc_status(const tkv_desc *desc);
 int tkv_decode_check_args(const tkv_desc *desc, int32_t n_items, int32_t batch, int32_t n_q_heads,
                           const void *workspace, size_t workspace_bytes);
 
