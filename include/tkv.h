@@ -440,6 +440,89 @@ int tkv_decode_attention_static(const tkv_desc *desc, const void *pool, const ui
                                 int32_t *status, void *stream /* hipStream_t */);
 
 /* ------------------------------------------------------------------ */
+/* D8: decode attention over shared prefixes (host plan, device).       */
+/* ------------------------------------------------------------------ */
+/*
+ * Groups of sequences whose contexts begin with the same tokens (a system
+ * prompt with its tools, a document) list the pages of that prefix once, as a
+ * page list of the group; the sequences' own page lists hold what follows.  A
+ * sequence may be a member of several groups (a prompt of all, a document of
+ * some) or of none.  Attention does not depend on the order of tokens, so
+ * several prefixes need none.
+ *   n_groups, n_members   groups; entries of member_seqs
+ *   max_members           members of the largest group, at least (rows of the launch)
+ *   n_items               prefix work items
+ *   page_indptr  device i32[n_groups+1] page-list offsets of the groups
+ *   page_ids     device i32: per group INT2 pages, then INT4 pages, of the same pool as the sequences' own
+ *   n_tok_int2/4 device i32[n_groups] valid tokens per width
+ *   member_indptr device i32[n_groups+1], member_seqs device i32[n_members]: sequences of each group
+ *   member_slots device i32[n_members], items device i32[4*n_items]: as written by tkv_plan_decode_shared
+ */
+typedef struct tkv_prefix {
+    int32_t n_groups, n_members, max_members, n_items;
+    const int32_t *page_indptr;
+    const int32_t *page_ids;
+    const int32_t *n_tok_int2;
+    const int32_t *n_tok_int4;
+    const int32_t *member_indptr;
+    const int32_t *member_seqs;
+    const int32_t *member_slots;
+    const int32_t *items;
+} tkv_prefix;
+
+/* Upper bound of the items that tkv_plan_decode_shared makes. */
+int32_t tkv_plan_shared_capacity(int32_t n_groups, int32_t target_cus);
+/*
+ * Cuts the groups' page lists into work items and gives every (item, member) a
+ * partial slot behind the n_own_items slots of the sequences' own items
+ * (tkv_plan_decode).  An item is read by one workgroup per kv head and 64 rows
+ * (16 or 32 if no group has more; a row is one query head of one member), whose
+ * four wavefronts take its pages in turn: items are equal parts of whole fours
+ * of pages, as small as still gives no more workgroups than target_cus compute
+ * units hold at once (one of 64 rows each, two of 32, three of 16).  Depends on the page counts and members only.
+ *   n_tok_int2/4   host i32[n_groups]
+ *   member_indptr  host i32[n_groups+1], from 0; member_seqs host i32[member_indptr[n_groups]],
+ *                  below batch, each at most once in a group
+ *   target_cus     compute units to fill (>= 1)
+ *   items_out      host i32[4*capacity]: {group, first page, end page, number in the group}
+ *   member_slots_out  host i32[members]: slot of the member's partial of the group's first item, the others follow
+ *   seq_slot_indptr_out  host i32[batch+1]: slots of each sequence, from n_own_items on
+ * Returns the number of items (>= 0) or a negative status.
+ */
+int32_t tkv_plan_decode_shared(const tkv_desc *desc, int32_t batch, int32_t n_q_heads, int32_t n_groups,
+                               const int32_t *n_tok_int2, const int32_t *n_tok_int4,
+                               const int32_t *member_indptr, const int32_t *member_seqs, int32_t target_cus,
+                               int32_t n_own_items, int32_t *items_out, int32_t capacity,
+                               int32_t *member_slots_out, int32_t *seq_slot_indptr_out);
+/*
+ * tkv_decode_attention over each sequence's prefixes and its own tokens
+ * together.  The prefix's pages are dequantised to fp16 as tkv_gather_dequant
+ * does (the values that a prefill over the prefix saw) and attended to with
+ * fp16 softmax weights and 32-bit sums; own tokens as in tkv_decode_split.  The
+ * output is bf16, as the projection behind it takes it.  A sequence without
+ * tokens gives zeros.
+ *   q, page_indptr .. n_items, sm_scale   as for tkv_decode_attention (own tokens; n_items may be 0)
+ *   prefix         host struct of device arrays, above; n_items may be 0
+ *   slot_indptr    device i32[2*(batch+1)]: seq_item_indptr_out of tkv_plan_decode, then seq_slot_indptr_out
+ *   n_slots        seq_slot_indptr_out[batch]
+ *   out            device bf16 [batch, n_q_heads, head_dim], 16-byte aligned
+ *   workspace      device, >= tkv_decode_workspace_bytes(desc, n_slots, n_q_heads), 16-byte aligned
+ *   status         device i32, may be NULL; bits as for tkv_decode_attention.  Members outside the batch, slots outside
+ *                  [n_items, n_slots) and groups with more members than max_members raise TKV_STATUS_BAD_ITEM: what they
+ *                  name is not stored, and the sequence reads what the workspace held before
+ * Preconditions on cache and q as for tkv_decode_attention; NaN and infinities
+ * in a query head leave the others alone.  n_q_heads / n_kv_heads is 1, 2, 4 or
+ * 8; at most 65535 prefix items.  Up to three launches on `stream`.
+ */
+int tkv_decode_attention_shared(const tkv_desc *desc, const void *pool, const uint8_t *bit_map, const void *q,
+                                const int32_t *page_indptr, const int32_t *page_ids,
+                                const int32_t *n_tok_int2, const int32_t *n_tok_int4,
+                                const int32_t *items, int32_t n_items, const tkv_prefix *prefix,
+                                const int32_t *slot_indptr, int32_t n_slots, int32_t batch, int32_t n_q_heads,
+                                float sm_scale, void *out, void *workspace, size_t workspace_bytes,
+                                int32_t *status, void *stream /* hipStream_t */);
+
+/* ------------------------------------------------------------------ */
 /* Q1 on the GPU: page tables of a batch in device memory.              */
 /* ------------------------------------------------------------------ */
 /*

@@ -1,14 +1,16 @@
-// Host side of what stands around append and decode in a step of a serving loop: the rotation table, and argument validation
-// in front of the launchers of tkv_rope.hip (norm and rotation) and tkv_table.hip (page tables in device memory).  Nothing
-// here touches the GPU.
+// Host side of what stands around append and decode in a step of a serving loop: the rotation table, the plan of shared
+// prefixes, and argument validation in front of the launchers of tkv_rope.hip (norm and rotation), tkv_table.hip (page tables
+// in device memory) and tkv_shared.hip (attention over shared prefixes).  Nothing here touches the GPU.
 #include "tkv.h"
 #include "tkv_internal.h"
 
 #include <algorithm>
 #include <cmath>
+#include <new>
+#include <vector>
 
 namespace {
-constexpr int kHeadDim = 128, kPageTokens = 64;
+constexpr int kHeadDim = 128, kGroup = 32, kPageTokens = 64;
 }
 
 extern "C" {
@@ -126,6 +128,141 @@ int tkv_norm_rope(const tkv_rope *rope, const void *q, int64_t q_stride, const v
     if (((uintptr_t)q_weight & 15) || ((uintptr_t)k_weight & 15)) return TKV_ERR_INVALID_ARG;
     return tkv_launch_norm_rope(rope, q, q_stride, k, k_stride, n_kv_heads > 0 ? v : nullptr, v_stride, n_tokens, n_q_heads, n_kv_heads, positions, q_weight, k_weight,
                                 eps, q_out, k_out, v_out, stream);
+}
+
+/* ---------------------------------------------------------------- D8: shared prefixes */
+
+int32_t tkv_plan_shared_capacity(int32_t n_groups, int32_t target_cus)
+{
+    // three workgroups a compute unit at most, and an item for every group
+    if (n_groups < 0 || target_cus < 1 || n_groups + 3 * (int64_t)target_cus > INT32_MAX) return TKV_ERR_INVALID_ARG;
+    return n_groups + 3 * target_cus;
+}
+
+int32_t tkv_plan_decode_shared(const tkv_desc *desc, int32_t batch, int32_t n_q_heads, int32_t n_groups, const int32_t *n_tok_int2,
+                               const int32_t *n_tok_int4, const int32_t *member_indptr, const int32_t *member_seqs, int32_t target_cus,
+                               int32_t n_own_items, int32_t *items_out, int32_t capacity, int32_t *member_slots_out, int32_t *seq_slot_indptr_out)
+{
+    if (int st = tkv_desc_status(desc)) return st;
+    if (batch < 0 || n_groups < 0 || n_own_items < 0 || capacity < 0 || n_q_heads <= 0 || !seq_slot_indptr_out || !member_indptr) return TKV_ERR_INVALID_ARG;
+    if (tkv_plan_shared_capacity(n_groups, target_cus) < 0) return TKV_ERR_INVALID_ARG;
+    if (n_groups > 0 && (!n_tok_int2 || !n_tok_int4)) return TKV_ERR_INVALID_ARG;
+    if (n_q_heads % desc->n_kv_heads) return TKV_ERR_BAD_SHAPE;
+    const int32_t r = n_q_heads / desc->n_kv_heads;
+    if (r != 1 && r != 2 && r != 4 && r != 8) return TKV_ERR_BAD_SHAPE;
+    if (member_indptr[0] != 0) return TKV_ERR_INVALID_ARG;
+    int32_t largest = 0;
+    int64_t longest = 1;
+    for (int32_t g = 0; g < n_groups; ++g) {
+        const int64_t members = (int64_t)member_indptr[g + 1] - member_indptr[g];
+        if (members < 0 || members > batch || n_tok_int2[g] < 0 || n_tok_int4[g] < 0) return TKV_ERR_INVALID_ARG;
+        if (desc->int2_key_axis == TKV_KEYS_PER_CHANNEL && n_tok_int2[g] % kGroup) return TKV_ERR_INVALID_ARG;
+        largest = std::max(largest, (int32_t)members);
+    }
+    const int32_t n_members = member_indptr[n_groups];
+    if (n_members > 0 && (!member_seqs || !member_slots_out)) return TKV_ERR_INVALID_ARG;
+    if (capacity > 0 && !items_out) return TKV_ERR_INVALID_ARG;
+    if ((int64_t)largest * r > INT32_MAX) return TKV_ERR_INVALID_ARG;
+    try {
+        std::vector<int32_t> seen((size_t)batch, -1), next((size_t)batch + 1, 0);
+        for (int32_t g = 0; g < n_groups; ++g)
+            for (int32_t m = member_indptr[g]; m < member_indptr[g + 1]; ++m) {
+                const int32_t b = member_seqs[m];
+                if (b < 0 || b >= batch || seen[(size_t)b] == g) return TKV_ERR_INVALID_ARG;
+                seen[(size_t)b] = g;
+            }
+        const int32_t rows = tkv_prefix_rows(largest * r);
+        const int64_t target = (int64_t)target_cus * (rows == 64 ? 1 : rows == 32 ? 2 : 3);
+        auto fours = [&](int32_t g) -> int64_t {   // of pages, a page for each wavefront
+            if (member_indptr[g + 1] == member_indptr[g]) return 0;
+            const int64_t pages = ((int64_t)n_tok_int2[g] + kPageTokens - 1) / kPageTokens + ((int64_t)n_tok_int4[g] + kPageTokens - 1) / kPageTokens;
+            return (pages + 3) / 4;
+        };
+        auto blocks = [&](int32_t g) -> int64_t {   // workgroups of an item
+            return (((int64_t)(member_indptr[g + 1] - member_indptr[g]) * r + rows - 1) / rows) * desc->n_kv_heads;
+        };
+        for (int32_t g = 0; g < n_groups; ++g) longest = std::max(longest, fours(g));
+        auto workgroups = [&](int64_t per) {
+            int64_t n = 0;
+            for (int32_t g = 0; g < n_groups; ++g) n += (fours(g) + per - 1) / per * blocks(g);
+            return n;
+        };
+        int64_t lo = 1, hi = longest;
+        while (lo < hi) {
+            const int64_t mid = lo + (hi - lo) / 2;
+            if (workgroups(mid) <= target) hi = mid;
+            else lo = mid + 1;
+        }
+        int64_t n_items = 0, n_slots = n_own_items;
+        std::vector<int32_t> parts((size_t)n_groups, 0);
+        for (int32_t g = 0; g < n_groups; ++g) {
+            const int64_t all = fours(g), n = (all + lo - 1) / lo;
+            const int64_t pages = ((int64_t)n_tok_int2[g] + kPageTokens - 1) / kPageTokens + ((int64_t)n_tok_int4[g] + kPageTokens - 1) / kPageTokens;
+            parts[(size_t)g] = (int32_t)n;
+            if (n_items + n > capacity) return TKV_ERR_CAPACITY;
+            for (int64_t k = 0; k < n; ++k) {
+                int32_t *it = items_out + 4 * n_items++;
+                it[0] = g;
+                it[1] = (int32_t)(4 * (all * k / n));
+                it[2] = (int32_t)std::min(pages, 4 * (all * (k + 1) / n));
+                it[3] = (int32_t)k;
+            }
+            for (int32_t m = member_indptr[g]; m < member_indptr[g + 1]; ++m) next[(size_t)member_seqs[m]] += (int32_t)n;
+            n_slots += n * (member_indptr[g + 1] - member_indptr[g]);
+            if (n_slots > INT32_MAX) return TKV_ERR_INVALID_ARG;
+        }
+        int32_t at = n_own_items;
+        for (int32_t b = 0; b < batch; ++b) {
+            seq_slot_indptr_out[b] = at;
+            const int32_t n = next[(size_t)b];
+            next[(size_t)b] = at;
+            at += n;
+        }
+        seq_slot_indptr_out[batch] = at;
+        for (int32_t g = 0; g < n_groups; ++g)
+            for (int32_t m = member_indptr[g]; m < member_indptr[g + 1]; ++m) {
+                int32_t &slot = next[(size_t)member_seqs[m]];
+                member_slots_out[m] = slot;
+                slot += parts[(size_t)g];
+            }
+        return (int32_t)n_items;
+    } catch (const std::bad_alloc &) {
+        return TKV_ERR_INVALID_ARG;
+    }
+}
+
+int tkv_decode_attention_shared(const tkv_desc *desc, const void *pool, const uint8_t *bit_map, const void *q, const int32_t *page_indptr,
+                                const int32_t *page_ids, const int32_t *n_tok_int2, const int32_t *n_tok_int4, const int32_t *items,
+                                int32_t n_items, const tkv_prefix *prefix, const int32_t *slot_indptr, int32_t n_slots, int32_t batch,
+                                int32_t n_q_heads, float sm_scale, void *out, void *workspace, size_t workspace_bytes, int32_t *status,
+                                void *stream)
+{
+    if (!prefix || n_items < 0 || n_slots < n_items) return tkv_desc_status(desc) ? tkv_desc_status(desc) : TKV_ERR_INVALID_ARG;
+    if (int st = tkv_decode_check_args(desc, n_slots, batch, n_q_heads, workspace, workspace_bytes)) return st;
+    const tkv_prefix &p = *prefix;
+    if (p.n_groups < 0 || p.n_members < 0 || p.max_members < 0 || p.n_items < 0 || p.n_items > 65535) return TKV_ERR_INVALID_ARG;
+    if (batch == 0) return TKV_OK;
+    if (!(sm_scale > 0.0f) || !(sm_scale < 3.0e38f)) return TKV_ERR_INVALID_ARG;
+    if (!q || !out || !slot_indptr) return TKV_ERR_INVALID_ARG;
+    if ((n_items > 0 || p.n_items > 0) && (!pool || !bit_map)) return TKV_ERR_INVALID_ARG;
+    if (n_items > 0 && (!page_indptr || !page_ids || !n_tok_int2 || !n_tok_int4 || !items)) return TKV_ERR_INVALID_ARG;
+    if (((uintptr_t)pool & 255) || ((uintptr_t)q & 15) || ((uintptr_t)out & 15)) return TKV_ERR_INVALID_ARG;
+    const int32_t r = n_q_heads / desc->n_kv_heads;
+    if (p.n_items > 0) {
+        if (!p.page_indptr || !p.page_ids || !p.n_tok_int2 || !p.n_tok_int4 || !p.member_indptr || !p.member_seqs || !p.member_slots || !p.items ||
+            p.n_groups == 0 || p.n_members == 0 || p.max_members == 0)
+            return TKV_ERR_INVALID_ARG;
+        const int64_t rows = (int64_t)p.max_members * r;
+        if (rows > INT32_MAX / 2 || (int64_t)p.n_members * r > INT32_MAX / 2 || (rows + 63) / 64 > 65535) return TKV_ERR_INVALID_ARG;
+    }
+    float *own = (float *)workspace, *shared = own + (size_t)n_items * n_q_heads * (kHeadDim + 2);
+    if (p.n_items > 0)
+        if (int st = tkv_launch_prefix(desc, pool, bit_map, q, prefix, n_items, n_slots, batch, n_q_heads, sm_scale, shared, status, stream)) return st;
+    if (n_items > 0)
+        if (int st = tkv_launch_decode_split(desc, pool, bit_map, q, page_indptr, page_ids, n_tok_int2, n_tok_int4, items, n_items, batch, n_q_heads,
+                                             sm_scale, own, status, stream))
+            return st;
+    return tkv_launch_merge_shared(slot_indptr, n_items, n_slots - n_items, batch, n_q_heads, out, own, shared, stream);
 }
 
 } // extern "C"

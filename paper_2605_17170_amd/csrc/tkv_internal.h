@@ -1,6 +1,6 @@
 // Internal interface between the host-side validation (tkv_host.cpp) and the
 // kernel launchers (tkv_append.hip, tkv_gather.hip, tkv_decode.hip,
-// tkv_table.hip, tkv_rope.hip, tkv_probe.hip).  Arguments are already
+// tkv_shared.hip, tkv_table.hip, tkv_rope.hip, tkv_probe.hip).  Arguments are already
 // validated; the launchers return TKV_OK or TKV_ERR_HIP.
 #ifndef TKV_INTERNAL_H
 #define TKV_INTERNAL_H
@@ -32,6 +32,12 @@ int tkv_launch_decode_reduce(const tkv_desc *desc, const int32_t *seq_item_indpt
 int tkv_launch_norm_rope(const tkv_rope *rope, const void *q, int64_t q_stride, const void *k, int64_t k_stride, const void *v,
                          int64_t v_stride, int32_t n_tokens, int32_t n_q_heads, int32_t n_kv_heads, const int32_t *positions,
                          const void *q_weight, const void *k_weight, float eps, void *q_out, void *k_out, void *v_out, void *stream);
+
+int32_t tkv_prefix_rows(int32_t rows);   // rows of a workgroup of the prefix kernel in a launch with groups of up to so many rows
+int tkv_launch_prefix(const tkv_desc *desc, const void *pool, const uint8_t *bit_map, const void *q, const tkv_prefix *prefix, int32_t first_slot,
+                      int32_t n_slots, int32_t batch, int32_t n_q_heads, float sm_scale, void *workspace, int32_t *status, void *stream);
+int tkv_launch_merge_shared(const int32_t *indptr, int32_t n_own, int32_t n_prefix, int32_t batch, int32_t n_q_heads, void *out, const void *own_ws,
+                            const void *prefix_ws, void *stream);
 
 size_t tkv_table_words(int32_t n_seqs, int32_t n_tokens);
 int tkv_launch_table_reset(const tkv_desc *desc, const tkv_table *table, void *stream);

@@ -167,6 +167,35 @@ class PagedCache:
                                     self.d_page_ids, self.d_n_tok2, self.d_n_tok4, d_items, float(sm_scale), workspace,
                                     self.status, stream, prepare=prepare)
 
+    # -- D8
+    def plan_shared(self, groups: list, n_q_heads: int, target_items: int, target_cus: int) -> tkv.SharedPlan:
+        """The first len(groups) sequences of the cache are prefixes, the others the batch; groups[g]: the sequences of the
+        batch that prefix g is shared by."""
+        n = len(groups)
+        batch = len(self.seq_bits) - n
+        items, sip = tkv.tkv_plan_decode(self.desc, self.page_indptr[n:] - self.page_indptr[n], self.n_tok2[n:], self.n_tok4[n:], target_items)
+        indptr = np.concatenate([[0], np.cumsum([len(g) for g in groups])]).astype(np.int32)
+        members = np.array([b for g in groups for b in g], np.int32)
+        plan = tkv.tkv_plan_decode_shared(self.desc, batch, n_q_heads, self.n_tok2[:n], self.n_tok4[:n], indptr, members, target_cus, items, sip)
+        d = lambda a: torch.from_numpy(np.ascontiguousarray(a)).to(self.device)  # noqa: E731
+        prefix = tkv.tkv_prefix.make(self.d_page_indptr[:n + 1], self.d_page_ids, self.d_n_tok2[:n], self.d_n_tok4[:n], d(indptr), d(members),
+                                     d(plan.member_slots), d(plan.prefix_items), plan.max_members)
+        self._shared = (n, plan, prefix, d(plan.items), d(plan.seq_item_indptr))
+        return plan
+
+    def decode_shared(self, q: torch.Tensor, out: torch.Tensor | None = None, workspace=None, pool=None, stream=None, prepare=False):
+        """Attention of the batch of plan_shared over prefixes and own tokens, bf16; arguments as for decode."""
+        n, plan, prefix, d_items, d_indptr = self._shared
+        if out is None:
+            out = torch.empty(q.shape, dtype=torch.bfloat16, device=self.device)
+        if workspace is None:
+            workspace = torch.empty(max(16, tkv.tkv_decode_workspace_bytes(self.desc, plan.n_slots, int(q.shape[1]))), dtype=torch.uint8, device=self.device)
+        sm_scale = np.float32(1.0 / math.sqrt(tkv.HEAD_DIM))
+        call = tkv.tkv_decode_attention_shared(self.desc, self.pool if pool is None else pool, self.bit_map, q, self.d_page_indptr[n:], self.d_page_ids,
+                                               self.d_n_tok2[n:], self.d_n_tok4[n:], d_items, prefix, d_indptr, plan.n_slots, float(sm_scale), out, workspace,
+                                               self.status, stream, prepare=prepare)
+        return call if prepare else out
+
     def workspace(self, n_q_heads: int) -> torch.Tensor:
         n_items = self._plan[2].shape[0]
         nbytes = max(16, tkv.tkv_decode_workspace_bytes(self.desc, n_items, n_q_heads))
@@ -185,3 +214,8 @@ def default_target_items(n_kv_heads: int, device=None) -> int:
     props = torch.cuda.get_device_properties(device if device is not None else torch.cuda.current_device())
     waves = props.multi_processor_count * 4 * 3
     return max(1, waves // n_kv_heads)
+
+
+def default_shared_units(device=None) -> int:
+    """Compute units that tkv_plan_decode_shared fills with the workgroups of the prefix kernel."""
+    return torch.cuda.get_device_properties(device if device is not None else torch.cuda.current_device()).multi_processor_count

@@ -5,6 +5,7 @@ the library's HIP kernels -- there is no fallback: if the library has not been
 built, importing a function here raises."""
 from __future__ import annotations
 
+import collections
 import ctypes as C
 import os
 
@@ -46,7 +47,8 @@ EXPORTS = [
     "tkv_seq_page_ids", "tkv_route_residual", "tkv_plan_append_max_work", "tkv_plan_append", "tkv_quantize_append", "tkv_gather_dequant",
     "tkv_plan_decode_capacity", "tkv_plan_decode", "tkv_decode_workspace_bytes", "tkv_decode_attention",
     "tkv_decode_split", "tkv_decode_reduce", "tkv_decode_attention_static", "tkv_allocate_bits_greedy", "tkv_allocate_bits_exhaustive",
-    "tkv_tag_tokens", "tkv_tags_to_bits", "tkv_tag_counts", "tkv_table_reset", "tkv_table_max_work",
+    "tkv_tag_tokens", "tkv_tags_to_bits", "tkv_tag_counts", "tkv_plan_shared_capacity",
+    "tkv_plan_decode_shared", "tkv_decode_attention_shared", "tkv_table_reset", "tkv_table_max_work",
     "tkv_table_workspace_bytes", "tkv_table_append", "tkv_rope_table", "tkv_norm_rope", "tkv_probe_stream_read",
     "tkv_probe_decode_reads", "tkv_probe_stream_mix",
 ]
@@ -67,6 +69,25 @@ class tkv_desc(C.Structure):
     def make(cls, n_kv_heads, n_pages_int2, n_pages_int4, head_dim=HEAD_DIM, group_size=GROUP_SIZE,
              page_tokens=PAGE_TOKENS, int2_key_axis=0):
         return cls(n_kv_heads, head_dim, group_size, page_tokens, n_pages_int2, n_pages_int4, int2_key_axis)
+
+
+class tkv_prefix(C.Structure):
+    """Shared prefixes of groups of sequences: device arrays; `make` keeps the tensors alive."""
+    _fields_ = [("n_groups", C.c_int32), ("n_members", C.c_int32), ("max_members", C.c_int32), ("n_items", C.c_int32),
+                ("page_indptr", C.c_void_p), ("page_ids", C.c_void_p), ("n_tok_int2", C.c_void_p), ("n_tok_int4", C.c_void_p),
+                ("member_indptr", C.c_void_p), ("member_seqs", C.c_void_p), ("member_slots", C.c_void_p), ("items", C.c_void_p)]
+
+    @classmethod
+    def make(cls, page_indptr, page_ids, n_tok_int2, n_tok_int4, member_indptr, member_seqs, member_slots, items, max_members: int):
+        """i32 device tensors: page_indptr, member_indptr [n_groups+1]; page_ids; n_tok_int2/4 [n_groups]; member_seqs,
+        member_slots [n_members]; items [n_items, 4] (the last two and max_members from tkv_plan_decode_shared)."""
+        tensors = (page_indptr, page_ids, n_tok_int2, n_tok_int4, member_indptr, member_seqs, member_slots, items)
+        n = n_tok_int2.numel()
+        assert all(t.element_size() == 4 for t in tensors) and n_tok_int4.numel() == n and page_indptr.numel() == member_indptr.numel() == n + 1
+        assert member_seqs.numel() == member_slots.numel() and items.numel() % 4 == 0
+        prefix = cls(n, member_seqs.numel(), max_members, items.numel() // 4, *(_dev(t) for t in tensors))
+        prefix.tensors = tensors
+        return prefix
 
 
 class tkv_table(C.Structure):
@@ -151,6 +172,12 @@ def lib():
                                                   vp, vp, vp]
         L.tkv_decode_split.argtypes = [dp, vp, vp, vp, vp, vp, vp, vp, vp, i32, i32, i32, C.c_float, vp, sz, vp, vp]
         L.tkv_decode_reduce.argtypes = [dp, vp, i32, i32, i32, vp, vp, sz, vp]
+        L.tkv_plan_shared_capacity.restype = i32
+        L.tkv_plan_shared_capacity.argtypes = [i32, i32]
+        L.tkv_plan_decode_shared.restype = i32
+        L.tkv_plan_decode_shared.argtypes = [dp, i32, i32, i32, vp, vp, vp, vp, i32, i32, vp, i32, vp, vp]
+        L.tkv_decode_attention_shared.argtypes = [dp, vp, vp, vp, vp, vp, vp, vp, vp, i32, C.POINTER(tkv_prefix), vp, i32, i32, i32, C.c_float,
+                                                  vp, vp, sz, vp, vp]
         tp = C.POINTER(tkv_table)
         L.tkv_table_reset.argtypes = [dp, tp, vp]
         L.tkv_table_max_work.restype = i32
@@ -525,6 +552,55 @@ def tkv_tag_counts(tags) -> np.ndarray:
     counts = np.zeros(N_TAGS, np.int64)
     _check(lib().tkv_tag_counts(pt, tg.size, C.c_void_p(counts.ctypes.data)), "tkv_tag_counts")
     return counts
+
+
+# ---------------------------------------------------------------- D8 (host plan, device)
+SharedPlan = collections.namedtuple("SharedPlan", "items seq_item_indptr n_slots prefix_items member_slots max_members")
+
+
+def tkv_plan_decode_shared(desc, batch: int, n_q_heads: int, n_tok_int2, n_tok_int4, member_indptr, member_seqs, target_cus: int, items,
+                           seq_item_indptr) -> SharedPlan:
+    """Plan over the groups' prefixes (host arrays, per group) beside the plan (items, seq_item_indptr) of the sequences' own
+    tokens from tkv_plan_decode.  SharedPlan: items i32[n_items, 4] and seq_item_indptr i32[2*(batch+1)] of the sequences,
+    n_slots, prefix_items i32[n, 4], member_slots i32[n_members], max_members."""
+    n2, p2 = _np(n_tok_int2, np.int32)
+    n4, p4 = _np(n_tok_int4, np.int32)
+    ip, pip = _np(member_indptr, np.int32)
+    sq, psq = _np(member_seqs, np.int32)
+    sip, _ = _np(seq_item_indptr, np.int32)
+    if n2.size != n4.size or ip.size != n2.size + 1 or sip.size != batch + 1 or sq.size != ip[-1]:
+        raise ValueError("one count per group, group offsets, members and sequence offsets")
+    cap = _check(lib().tkv_plan_shared_capacity(n2.size, target_cus), "tkv_plan_shared_capacity")
+    prefix_items, slots, indptr = np.empty((cap, 4), np.int32), np.empty(sq.size, np.int32), np.empty(batch + 1, np.int32)
+    n_own = int(np.asarray(items).reshape(-1, 4).shape[0])
+    n = _check(lib().tkv_plan_decode_shared(C.byref(desc), batch, n_q_heads, n2.size, p2, p4, pip, psq, target_cus, n_own,
+                                            C.c_void_p(prefix_items.ctypes.data), cap, C.c_void_p(slots.ctypes.data if slots.size else None),
+                                            C.c_void_p(indptr.ctypes.data)), "tkv_plan_decode_shared")
+    return SharedPlan(np.asarray(items, np.int32).reshape(-1, 4), np.concatenate([sip, indptr]), int(indptr[-1]), prefix_items[:n].copy(), slots,
+                      int(np.diff(ip).max()) if n2.size else 0)
+
+
+def tkv_decode_attention_shared(desc, pool, bit_map, q, page_indptr, page_ids, n_tok_int2, n_tok_int4, items, prefix: tkv_prefix, slot_indptr,
+                                n_slots: int, sm_scale: float, out, workspace, status=None, stream=None, prepare=False):
+    """Device tensors: q bf16 [B,Hq,D]; page_indptr i32[B+1], page_ids, n_tok_int2/4 i32[B], items i32[n_items,4] of the
+    sequences' own tokens; slot_indptr i32[2*(B+1)] (SharedPlan.seq_item_indptr); out bf16 [B,Hq,D]; workspace u8."""
+    batch, n_q_heads = int(q.shape[0]), int(q.shape[1])
+    n_items = int(items.shape[0]) if items is not None else 0
+    ws_bytes = int(workspace.numel() * workspace.element_size()) if workspace is not None else 0
+    assert q.element_size() == 2 and int(q.shape[2]) == desc.head_dim
+    assert out.numel() == q.numel() and out.element_size() == 2
+    assert slot_indptr.numel() == 2 * (batch + 1) and slot_indptr.element_size() == 4
+    if n_items:
+        assert items.numel() == 4 * n_items and page_indptr.numel() == batch + 1 and n_tok_int2.numel() == batch and n_tok_int4.numel() == batch
+    if n_items or prefix.n_items:
+        assert pool.numel() * pool.element_size() >= tkv_pool_bytes(desc) and bit_map.numel() >= desc.n_pages_int2 + desc.n_pages_int4
+    return _run(lib().tkv_decode_attention_shared,
+                (C.byref(desc), _dev(pool), _dev(bit_map), _dev(q), _dev(page_indptr), _dev(page_ids), _dev(n_tok_int2), _dev(n_tok_int4),
+                 _dev(items), n_items, C.byref(prefix), _dev(slot_indptr), n_slots, batch, n_q_heads, float(sm_scale), _dev(out), _dev(workspace),
+                 ws_bytes, _dev(status), _stream(stream)),
+                "tkv_decode_attention_shared",
+                (desc, pool, bit_map, q, page_indptr, page_ids, n_tok_int2, n_tok_int4, items, prefix, slot_indptr, out, workspace, status, stream),
+                prepare)
 
 
 # ---------------------------------------------------------------- Q1 on the GPU (device)
