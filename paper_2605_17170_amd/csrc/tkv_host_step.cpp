@@ -134,9 +134,9 @@ int tkv_norm_rope(const tkv_rope *rope, const void *q, int64_t q_stride, const v
 
 int32_t tkv_plan_shared_capacity(int32_t n_groups, int32_t target_cus)
 {
-    // three workgroups a compute unit at most, and an item for every group
-    if (n_groups < 0 || target_cus < 1 || n_groups + 3 * (int64_t)target_cus > INT32_MAX) return TKV_ERR_INVALID_ARG;
-    return n_groups + 3 * target_cus;
+    // a workgroup for a compute unit at most, or an item for every group
+    if (n_groups < 0 || target_cus < 1 || n_groups + (int64_t)target_cus > INT32_MAX) return TKV_ERR_INVALID_ARG;
+    return n_groups + target_cus;
 }
 
 int32_t tkv_plan_decode_shared(const tkv_desc *desc, int32_t batch, int32_t n_q_heads, int32_t n_groups, const int32_t *n_tok_int2,
@@ -172,19 +172,19 @@ int32_t tkv_plan_decode_shared(const tkv_desc *desc, int32_t batch, int32_t n_q_
                 seen[(size_t)b] = g;
             }
         const int32_t rows = tkv_prefix_rows(largest * r);
-        const int64_t target = (int64_t)target_cus * (rows == 64 ? 1 : rows == 32 ? 2 : 3);
-        auto fours = [&](int32_t g) -> int64_t {   // of pages, a page for each wavefront
+        const int64_t target = target_cus, unit = rows == 16 ? 8 : 4;
+        auto units = [&](int32_t g) -> int64_t {
             if (member_indptr[g + 1] == member_indptr[g]) return 0;
             const int64_t pages = ((int64_t)n_tok_int2[g] + kPageTokens - 1) / kPageTokens + ((int64_t)n_tok_int4[g] + kPageTokens - 1) / kPageTokens;
-            return (pages + 3) / 4;
+            return (pages + unit - 1) / unit;
         };
         auto blocks = [&](int32_t g) -> int64_t {   // workgroups of an item
             return (((int64_t)(member_indptr[g + 1] - member_indptr[g]) * r + rows - 1) / rows) * desc->n_kv_heads;
         };
-        for (int32_t g = 0; g < n_groups; ++g) longest = std::max(longest, fours(g));
+        for (int32_t g = 0; g < n_groups; ++g) longest = std::max(longest, units(g));
         auto workgroups = [&](int64_t per) {
             int64_t n = 0;
-            for (int32_t g = 0; g < n_groups; ++g) n += (fours(g) + per - 1) / per * blocks(g);
+            for (int32_t g = 0; g < n_groups; ++g) n += (units(g) + per - 1) / per * blocks(g);
             return n;
         };
         int64_t lo = 1, hi = longest;
@@ -196,15 +196,15 @@ int32_t tkv_plan_decode_shared(const tkv_desc *desc, int32_t batch, int32_t n_q_
         int64_t n_items = 0, n_slots = n_own_items;
         std::vector<int32_t> parts((size_t)n_groups, 0);
         for (int32_t g = 0; g < n_groups; ++g) {
-            const int64_t all = fours(g), n = (all + lo - 1) / lo;
+            const int64_t all = units(g), n = (all + lo - 1) / lo;
             const int64_t pages = ((int64_t)n_tok_int2[g] + kPageTokens - 1) / kPageTokens + ((int64_t)n_tok_int4[g] + kPageTokens - 1) / kPageTokens;
             parts[(size_t)g] = (int32_t)n;
             if (n_items + n > capacity) return TKV_ERR_CAPACITY;
             for (int64_t k = 0; k < n; ++k) {
                 int32_t *it = items_out + 4 * n_items++;
                 it[0] = g;
-                it[1] = (int32_t)(4 * (all * k / n));
-                it[2] = (int32_t)std::min(pages, 4 * (all * (k + 1) / n));
+                it[1] = (int32_t)(unit * (all * k / n));
+                it[2] = (int32_t)std::min(pages, unit * (all * (k + 1) / n));
                 it[3] = (int32_t)k;
             }
             for (int32_t m = member_indptr[g]; m < member_indptr[g + 1]; ++m) next[(size_t)member_seqs[m]] += (int32_t)n;
@@ -255,14 +255,8 @@ int tkv_decode_attention_shared(const tkv_desc *desc, const void *pool, const ui
         const int64_t rows = (int64_t)p.max_members * r;
         if (rows > INT32_MAX / 2 || (int64_t)p.n_members * r > INT32_MAX / 2 || (rows + 63) / 64 > 65535) return TKV_ERR_INVALID_ARG;
     }
-    float *own = (float *)workspace, *shared = own + (size_t)n_items * n_q_heads * (kHeadDim + 2);
-    if (p.n_items > 0)
-        if (int st = tkv_launch_prefix(desc, pool, bit_map, q, prefix, n_items, n_slots, batch, n_q_heads, sm_scale, shared, status, stream)) return st;
-    if (n_items > 0)
-        if (int st = tkv_launch_decode_split(desc, pool, bit_map, q, page_indptr, page_ids, n_tok_int2, n_tok_int4, items, n_items, batch, n_q_heads,
-                                             sm_scale, own, status, stream))
-            return st;
-    return tkv_launch_merge_shared(slot_indptr, n_items, n_slots - n_items, batch, n_q_heads, out, own, shared, stream);
+    return tkv_launch_shared(desc, pool, bit_map, q, page_indptr, page_ids, n_tok_int2, n_tok_int4, items, n_items, prefix, slot_indptr, n_slots,
+                             batch, n_q_heads, sm_scale, out, workspace, status, stream);
 }
 
 } // extern "C"

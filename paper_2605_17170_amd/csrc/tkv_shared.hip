@@ -20,6 +20,8 @@
 // bf16, which has 8.
 #include <hip/hip_runtime.h>
 
+#include <type_traits>
+
 #include "tkv_internal.h"
 #include "tkv_layout.h"
 
@@ -36,7 +38,7 @@ typedef const __attribute__((address_space(4))) int32_t *ConstWords;   // words 
 
 constexpr float kTau = 4.0f;   // a row's reference moves when a logit exceeds it by this much (log2 units)
 constexpr int kPExp = 8;       // weights and their sums carry 2^8, as the partials of the split kernel do
-constexpr int kWaves = 4;
+constexpr int kWaves = 8;
 
 __device__ __forceinline__ half8 as_half8(uint32_t a, uint32_t b, uint32_t c, uint32_t d)
 {
@@ -51,14 +53,37 @@ __device__ __forceinline__ uint32_t pack_h2(float a, float b)
 }
 __device__ __forceinline__ float bf16_lo(uint32_t v) { return __uint_as_float(v << 16); }
 __device__ __forceinline__ float bf16_hi(uint32_t v) { return __uint_as_float(v & 0xffff0000u); }
-// Two codes in bits 0.. and 16.. of x as fp16 numbers, times s plus z with one rounding per value.  (A code under the bit pattern
-// 0x6400 is 1024 + code, and subtracting 1024 is exact.)
-template <int BITS> __device__ __forceinline__ uint32_t dequant2(uint32_t x, uint32_t s, uint32_t z)
+// Two codes in bits POS .. POS + BITS - 1 of the halves of x as fp16 numbers, times s plus z with one rounding per value.  A field
+// of the mantissa under the exponent 25 - POS is 2^(10 - POS) + code, and subtracting the power of two is exact.
+struct Magic {   // the exponents, in vector registers: v_and_or_b32 takes one constant besides
+    uint32_t e[4];
+    __device__ __forceinline__ Magic()
+    {
+        asm("v_mov_b32 %0, 0x64006400" : "=v"(e[0]));
+        asm("v_mov_b32 %0, 0x5c005c00" : "=v"(e[1]));
+        asm("v_mov_b32 %0, 0x54005400" : "=v"(e[2]));
+        asm("v_mov_b32 %0, 0x4c004c00" : "=v"(e[3]));
+    }
+};
+template <int BITS, int POS> __device__ __forceinline__ uint32_t dequant2(uint32_t x, uint32_t s, uint32_t z, const Magic &mg)
 {
-    constexpr uint32_t m = ((1u << BITS) - 1u) * 0x00010001u;
-    const half2_t k = {(_Float16)1024.0f, (_Float16)1024.0f};
-    const half2_t c = __builtin_bit_cast(half2_t, (x & m) | 0x64006400u) - k;
+    static_assert(POS % 2 == 0 && POS + BITS <= 8, "a field of the mantissa");
+    constexpr uint32_t m = ((1u << BITS) - 1u) * 0x00010001u << POS;
+    constexpr float base = 1024 >> POS;
+    const half2_t k = {(_Float16)base, (_Float16)base};
+    const half2_t c = __builtin_bit_cast(half2_t, (x & m) | mg.e[POS / 2]) - k;
     return __builtin_bit_cast(uint32_t, __builtin_elementwise_fma(c, __builtin_bit_cast(half2_t, s), __builtin_bit_cast(half2_t, z)));
+}
+// Eight codes: fields k of the halves of x (BITS wide) are register k.
+template <int BITS> __device__ __forceinline__ half8 dequant8(uint32_t x, uint32_t s0, uint32_t s1, uint32_t s2, uint32_t s3, uint32_t z0, uint32_t z1,
+                                                              uint32_t z2, uint32_t z3, const Magic &mg)
+{
+    if constexpr (BITS == 2) {
+        return as_half8(dequant2<2, 0>(x, s0, z0, mg), dequant2<2, 2>(x, s1, z1, mg), dequant2<2, 4>(x, s2, z2, mg), dequant2<2, 6>(x, s3, z3, mg));
+    } else {
+        const uint32_t y = x >> 8;
+        return as_half8(dequant2<4, 0>(x, s0, z0, mg), dequant2<4, 4>(x, s1, z1, mg), dequant2<4, 0>(y, s2, z2, mg), dequant2<4, 4>(y, s3, z3, mg));
+    }
 }
 // Half i & 1 of v, twice.
 __device__ __forceinline__ uint32_t twice(uint32_t v, int i) { return __builtin_amdgcn_perm(v, v, (i & 1) ? 0x07060706u : 0x05040504u); }
@@ -75,29 +100,244 @@ __device__ __forceinline__ uint4 load16(Record r, uint32_t offset)
     return make_uint4(v.x, v.y, v.z, v.w);
 }
 
-struct PrefixArgs {
+__device__ __forceinline__ uint2 load8(Record r, uint32_t offset)
+{
+    typedef uint32_t u32x2_t __attribute__((ext_vector_type(2)));
+    const u32x2_t v = __builtin_amdgcn_raw_buffer_load_b64(r, (int)offset, 0, 0);
+    return make_uint2(v.x, v.y);
+}
+__device__ __forceinline__ uint32_t load4(Record r, uint32_t offset) { return __builtin_amdgcn_raw_buffer_load_b32(r, (int)offset, 0, 0); }
+
+struct SharedArgs {
     const uint8_t *pool;
     const uint8_t *bit_map;
     const uint16_t *q;
+    const int32_t *page_indptr;   // the sequences' own tokens
+    const int32_t *page_ids;
+    const int32_t *n_tok_int2;
+    const int32_t *n_tok_int4;
+    const int32_t *items;
+    int n_items;      // own items: slots [0, n_items); the prefixes' partials have [n_items, n_slots)
+    int own_blocks;   // the first workgroups, a wavefront for each (own item, kv head)
     tkv_prefix p;
+    int row_blocks;   // workgroups of a (prefix item, kv head)
     int n_kv_heads;
     int log2_r;
     int n_pages_int2;
     int n_pages_int4;
     int batch;
-    int first_slot;   // slots [first_slot, n_slots) hold the prefixes' partials
     int n_slots;
     float kappa;      // sm_scale * log2(e)
-    float *acc_ws;    // of slot first_slot
-    float *ml_ws;
+    float *acc_ws[2]; // partials of the own items, of the prefixes
+    float *ml_ws[2];
     int32_t *status;
 };
 
-// What a lane loads of one (page, kv head) record.
-template <int BITS> struct PageRegs {
+template <int NT> struct Rows {   // NT tiles of 16 query rows
+    half8 q[NT][4];        // operand of QK^T for a group of channels: row lane % 16, channels (k, k + 4) of octet lane / 16
+    floatx4 acc[NT][8];    // row 4 * (lane / 16) + i, channel 16 * tile + lane % 16
+    floatx4 sum[NT];       // denominators, rows as in acc
+    float m[NT];           // reference of row lane % 16, log2 units, -inf at first
+    float shift[NT];       // kPExp less the reference, or less 0 for -inf
+    float kappa[NT];       // of row lane % 16
+    bool huge;             // whether some row's reference is so large that rounding it moves a weight by more than 2^-4
+};
+template <int NT> __device__ __forceinline__ void clear(Rows<NT> &rows)
+{
+    rows.huge = false;
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+        rows.m[n] = -INFINITY;
+        rows.shift[n] = INFINITY;   // any logit moves the reference
+        rows.sum[n] = floatx4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int c = 0; c < 8; ++c) rows.acc[n][c] = floatx4{0.f, 0.f, 0.f, 0.f};
+    }
+}
+// q of one tile; `row`: this lane's row of q, lane % 16 of the tile.
+template <int NT> __device__ __forceinline__ void load_q(Rows<NT> &rows, int n, const uint16_t *__restrict__ row, float kappa, int lane)
+{
+    const uint4 *src = reinterpret_cast<const uint4 *>(row) + (lane >> 4);
+    uint4 x[4];
+#pragma unroll
+    for (int g = 0; g < 4; ++g) x[g] = src[4 * g];
+    // the largest exponent of the row, from |x| as integers plus one in the exponent, which makes NaN and infinities negative
+    typedef short short2_t __attribute__((ext_vector_type(2)));
+    short2_t big = {0, 0};
+#pragma unroll
+    for (int g = 0; g < 4; ++g) {
+        const uint32_t d[4] = {x[g].x, x[g].y, x[g].z, x[g].w};
+#pragma unroll
+        for (int k = 0; k < 4; ++k) big = __builtin_elementwise_max(big, __builtin_bit_cast(short2_t, (d[k] & 0x7fff7fffu) + 0x00800080u));
+    }
+    int top = big[0] > big[1] ? big[0] : big[1];
+    top = max(top, __shfl_xor(top, 16));
+    top = max(top, __shfl_xor(top, 32));
+    int E = top <= 0x80 ? 0 : 15 - ((top >> 7) - 127);   // the largest lies in [2^14, 2^15)
+    E = E > 100 ? 100 : (E < -100 ? -100 : E);
+    const float f = ldexpf(1.0f, E);
+    rows.kappa[n] = kappa * ldexpf(1.0f, -E);
+#pragma unroll
+    for (int g = 0; g < 4; ++g)
+        rows.q[n][g] = as_half8(pack_h2(bf16_lo(x[g].x) * f, bf16_lo(x[g].z) * f), pack_h2(bf16_hi(x[g].x) * f, bf16_hi(x[g].z) * f),
+                                pack_h2(bf16_lo(x[g].y) * f, bf16_lo(x[g].w) * f), pack_h2(bf16_hi(x[g].y) * f, bf16_hi(x[g].w) * f));
+}
+
+// ---- codes to operands -----------------------------------------------------------------------------------------------
+// K of this lane's token for a group of channels: octet lane / 16, register k holds channels (k, k + 4).  w: the group's word;
+// s, z: scales and zero-points of the four registers.
+template <int BITS> __device__ __forceinline__ half8 k_operand(uint32_t w, const uint32_t (&s)[4], const uint32_t (&z)[4], int q4, const Magic &mg)
+{
+    // INT4: codes k and k + 4 lie in the halves of the word; INT2: the bytes of this lane's octet move there
+    const uint32_t x = BITS == 4 ? w : __builtin_amdgcn_perm(w, w, (q4 & 1) ? 0x0c070c06u : 0x0c050c04u);
+    return dequant8<BITS>(x, s[0], s[1], s[2], s[3], z[0], z[1], z[2], z[3], mg);
+}
+// Scales (or zero-points) of per-channel INT2 keys in that order; `plane`: 32 chunks of 8, [block][group][quarter].
+__device__ __forceinline__ void channel_meta(const uint4 *plane, int blk, int g, int q4, uint32_t (&s)[4])
+{
+    const uint4 a = plane[(blk * 4 + g) * 4 + 2 * (q4 >> 1)], b = plane[(blk * 4 + g) * 4 + 2 * (q4 >> 1) + 1];
+    const uint32_t sel = (q4 & 1) ? 0x07060302u : 0x05040100u;
+    s[0] = __builtin_amdgcn_perm(b.x, a.x, sel);
+    s[1] = __builtin_amdgcn_perm(b.y, a.y, sel);
+    s[2] = __builtin_amdgcn_perm(b.z, a.z, sel);
+    s[3] = __builtin_amdgcn_perm(b.w, a.w, sel);
+}
+// V of this lane's channel for the eight tokens 32 b + 16 (j >> 2) + 4 (lane / 16) + (j & 3): register k holds j = (2k, 2k + 1).
+template <int BITS> __device__ __forceinline__ half8 v_operand(uint32_t w, int b, uint4 s, uint4 z, const Magic &mg)
+{
+    const uint32_t x = BITS == 4 ? w : w >> (8 * b);   // INT2 words hold both blocks
+    return dequant8<BITS>(x, s.x, s.y, s.z, s.w, z.x, z.y, z.z, z.w, mg);
+}
+// What was never written counts nothing, whatever stands there: chunk (b, quad) of the V planes with the tokens from n_valid on zero.
+__device__ __forceinline__ uint4 mask_meta(uint4 v, int b, int quad, int n_valid)
+{
+    const int t0 = 32 * b + 4 * quad;
+    auto mask = [&](int t) { return (t < n_valid ? 0xffffu : 0u) | (t + 1 < n_valid ? 0xffff0000u : 0u); };
+    return make_uint4(v.x & mask(t0), v.y & mask(t0 + 2), v.z & mask(t0 + 16), v.w & mask(t0 + 18));
+}
+__device__ __forceinline__ uint32_t word_of(uint4 v, int i) { return i == 0 ? v.x : i == 1 ? v.y : i == 2 ? v.z : v.w; }
+
+// Softmax weights of a page.  S: logits of its 16-token tiles (token 16 e + 4 (lane / 16) + i, row lane % 16), P: operands of PV for
+// its 32-token blocks.  One test for all tiles whether a reference has to move.
+template <int NT> __device__ __forceinline__ void weigh(Rows<NT> &rows, floatx4 (&S)[NT][4], int n_valid, int q4, half8 (&P)[NT][2])
+{
+    if (__builtin_expect(n_valid < kPageTokens, 0)) {
+#pragma unroll
+        for (int n = 0; n < NT; ++n)
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) S[n][e][i] = 16 * e + 4 * q4 + i < n_valid ? S[n][e][i] : -INFINITY;
+    }
+    float mx[NT], factor[NT], shift[NT];
+    bool move = rows.huge;
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+        mx[n] = S[n][0][0];
+#pragma unroll
+        for (int k = 1; k < 16; ++k) mx[n] = __builtin_elementwise_maximum(mx[n], S[n][k >> 2][k & 3]);
+        factor[n] = rows.kappa[n];
+        shift[n] = rows.shift[n];
+        // (a row of NaN compares false and keeps its reference: its weights are NaN)
+        move = move || mx[n] * factor[n] + shift[n] > kTau + (float)kPExp;
+    }
+    if (__any(move)) {
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+            float top = fmaxf(mx[n], __shfl_xor(mx[n], 16));
+            top = fmaxf(top, __shfl_xor(top, 32));
+            const float old = rows.m[n], m_new = fmaxf(old, top * factor[n]);
+            const float alpha = m_new == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(old - m_new);
+            rows.m[n] = m_new;
+            rows.huge = rows.huge || __any(fabsf(m_new) > 0x1p20f && m_new != -INFINITY);
+            const float ref = m_new == -INFINITY ? 0.0f : m_new;
+            rows.shift[n] = shift[n] = (float)kPExp - ref;
+            floatx4 av;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) av[i] = __shfl(alpha, 4 * q4 + i);
+#pragma unroll
+            for (int c = 0; c < 8; ++c) rows.acc[n][c] *= av;
+            rows.sum[n] *= av;
+        }
+        if (rows.huge) {
+            // factor * logit with one rounding, as the reference has it, then the difference: the largest weight is 2^8
+#pragma unroll
+            for (int n = 0; n < NT; ++n) {
+                const float ref = rows.m[n] == -INFINITY ? 0.0f : rows.m[n];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) S[n][e] = S[n][e] * factor[n] - ref;
+                factor[n] = 1.0f;
+                shift[n] = (float)kPExp;
+            }
+        }
+    }
+#pragma unroll
+    for (int n = 0; n < NT; ++n)
+#pragma unroll
+        for (int b = 0; b < 2; ++b) {
+            uint32_t w[4];
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                const floatx4 x = S[n][2 * b + (k >> 1)];
+                w[k] = pack_h2(__builtin_amdgcn_exp2f(fmaf(x[2 * (k & 1)], factor[n], shift[n])), __builtin_amdgcn_exp2f(fmaf(x[2 * (k & 1) + 1], factor[n], shift[n])));
+            }
+            P[n][b] = as_half8(w[0], w[1], w[2], w[3]);
+        }
+}
+__device__ __forceinline__ half8 ones() { return as_half8(0x3c003c00u, 0x3c003c00u, 0x3c003c00u, 0x3c003c00u); }
+
+// ---- the pages of a list, 64 at a time in registers: lane l holds page number base + l ------------------------------------
+struct PageList {
+    int base;
+    uint32_t at;   // where the record starts in the pool, in units of kUnit
+    int valid;     // tokens of the page that count
+};
+constexpr int kUnitLog2 = 11;   // record and arena sizes are multiples of it
+static_assert(Rec<2>::kBytes % (1 << kUnitLog2) == 0 && Rec<4>::kBytes % (1 << kUnitLog2) == 0, "record unit");
+struct ListCtx {
+    const uint8_t *pool;
+    const uint8_t *bit_map;
+    const int32_t *pages;
+    int first, step, n;                  // page number i stands at list position first + step * i; n of them
+    int np2, np4, last2, last4;          // pages of either width of the list, tokens of the last ones
+    int kvh, n_kv_heads, n_pages_int2, n_pages_total, lane;
+    int32_t *status;
+    __device__ __forceinline__ bool is2(int i) const { return first + step * i < np2; }
+};
+__device__ __forceinline__ void fetch_list(const ListCtx &cx, PageList &l, int base)
+{
+    l.base = base;
+    const int i = base + cx.lane < cx.n ? base + cx.lane : cx.n - 1;
+    const int pos = cx.first + cx.step * i;
+    const int page = cx.pages[pos];
+    const bool is2 = pos < cx.np2;
+    const int lo = is2 ? 0 : cx.n_pages_int2, hi = is2 ? cx.n_pages_int2 : cx.n_pages_total;
+    const bool ok = page >= lo && page < hi;
+    if (!ok && cx.status) atomicOr(cx.status, page < 0 || page >= cx.n_pages_total ? TKV_STATUS_PAGE_RANGE : TKV_STATUS_BITMAP_MISMATCH);
+    // a page that cannot be read counts no tokens, and nothing is read in its place (the record's size is 0, see record_of)
+    const uint32_t rec = (uint32_t)(is2 ? page : page - cx.n_pages_int2) * (uint32_t)cx.n_kv_heads + (uint32_t)cx.kvh;
+    constexpr uint32_t kUnits2 = Rec<2>::kBytes >> kUnitLog2, kUnits4 = Rec<4>::kBytes >> kUnitLog2;
+    l.at = !ok ? 0 : (is2 ? rec * kUnits2 : (uint32_t)cx.n_pages_int2 * (uint32_t)cx.n_kv_heads * kUnits2 + rec * kUnits4);   // (pools below 8 TB: 32 bits)
+    const bool written = ok && cx.bit_map[ok ? page : 0] == (is2 ? 2 : 4);
+    if (ok && !written && cx.status) atomicOr(cx.status, TKV_STATUS_BITMAP_MISMATCH);
+    l.valid = !written ? 0 : (pos == cx.np2 - 1 ? cx.last2 : pos == cx.np2 + cx.np4 - 1 ? cx.last4 : kPageTokens);
+}
+__device__ __forceinline__ int valid_of(const PageList &l, int i) { return __builtin_amdgcn_readlane(l.valid, i - l.base); }
+__device__ __forceinline__ Record record_of(const ListCtx &cx, const PageList &l, int i, bool wanted)
+{
+    const uint64_t at = (uint32_t)__builtin_amdgcn_readlane((int)l.at, i - l.base);
+    const int bytes = cx.is2(i) ? Rec<2>::kBytes : Rec<4>::kBytes;
+    return __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t *>(cx.pool) + (at << kUnitLog2), 0, wanted && valid_of(l, i) > 0 ? bytes : 0, 0x00027000);
+}
+
+// ---- few rows: a wavefront works on pages of its own -------------------------------------------------------------------
+template <int BITS> struct PageRegs {   // what a lane loads of one (page, kv head) record
     uint4 kw[4];      // K codes: four group words of this lane's token of each 16-token tile
     uint4 vw[BITS];   // V codes: chunk 64 i + lane of the plane
     uint4 km, vm;     // 16 bytes of the K scale | K zero planes, of the V scale | V zero planes
+};
+struct alignas(16) Meta {   // of one wavefront's page
+    uint4 k[64], v[64];
 };
 template <int BITS> __device__ __forceinline__ void load_k(PageRegs<BITS> &r, Record rec, int lane)
 {
@@ -114,271 +354,319 @@ template <int BITS> __device__ __forceinline__ void load_v(PageRegs<BITS> &r, Re
 #pragma unroll
     for (int i = 0; i < BITS; ++i) r.vw[i] = load16(rec, R::kVCodes + 1024 * i + 16 * lane);
 }
-
-template <int NT> struct Rows {   // NT tiles of 16 query rows
-    half8 q[NT][4];        // operand of QK^T for a group of channels: row lane % 16, eight channels
-    floatx4 acc[NT][8];    // row 4 * (lane / 16) + i, channel 16 * tile + lane % 16
-    floatx4 sum[NT];       // denominators, rows as in acc
-    float m[NT];           // reference of row lane % 16, log2 units, -inf at first
-    float kappa[NT];       // of row lane % 16
-    int at[NT];            // its row of q
-    bool huge;             // whether some row's reference is so large that rounding it moves a weight by more than 2^-4
-};
-struct alignas(16) Meta {   // of one wavefront's page
-    uint4 k[64], v[64];
-};
-
-// q of the lane's rows in the channel order of the codes: register k of a lane holds channels (k, k + 4) of octet lane / 16 of
-// the group; SPREAD (per-channel INT2 keys): channels (k, k + 8) from 16 * (lane / 32) + 4 * (lane / 16 % 2) on.
-template <int NT, bool SPREAD> __device__ __forceinline__ void load_q(Rows<NT> &rows, const uint16_t *__restrict__ q, float kappa, int lane)
-{
-    const int q4 = lane >> 4;
-#pragma unroll
-    for (int n = 0; n < NT; ++n) {
-        const uint16_t *row = q + (size_t)rows.at[n] * kHeadDim;
-        uint2 x[4], y[4];
-#pragma unroll
-        for (int g = 0; g < 4; ++g) {
-            const int c = 32 * g + (SPREAD ? 16 * (q4 >> 1) + 4 * (q4 & 1) : 8 * q4);
-            x[g] = *reinterpret_cast<const uint2 *>(row + c);
-            y[g] = *reinterpret_cast<const uint2 *>(row + c + (SPREAD ? 8 : 4));
-        }
-        // the largest exponent of the row; NaN and infinities do not count
-        uint32_t top = 0;
-#pragma unroll
-        for (int g = 0; g < 4; ++g) {
-            const uint32_t d[4] = {x[g].x, x[g].y, y[g].x, y[g].y};
-#pragma unroll
-            for (int k = 0; k < 4; ++k) {
-                const uint32_t a = d[k] & 0x7f80u, b = (d[k] >> 16) & 0x7f80u;
-                top = max(top, a == 0x7f80u ? 0 : a);
-                top = max(top, b == 0x7f80u ? 0 : b);
-            }
-        }
-        top = max(top, (uint32_t)__shfl_xor((int)top, 16));
-        top = max(top, (uint32_t)__shfl_xor((int)top, 32));
-        int E = top == 0 ? 0 : 14 - ((int)(top >> 7) - 127);   // the largest lies in [2^14, 2^15)
-        E = E > 100 ? 100 : (E < -100 ? -100 : E);
-        const float f = ldexpf(1.0f, E);
-        rows.kappa[n] = kappa * ldexpf(1.0f, -E);
-#pragma unroll
-        for (int g = 0; g < 4; ++g)
-            rows.q[n][g] = as_half8(pack_h2(bf16_lo(x[g].x) * f, bf16_lo(y[g].x) * f), pack_h2(bf16_hi(x[g].x) * f, bf16_hi(y[g].x) * f),
-                                    pack_h2(bf16_lo(x[g].y) * f, bf16_lo(y[g].y) * f), pack_h2(bf16_hi(x[g].y) * f, bf16_hi(y[g].y) * f));
-    }
-}
-
 // One page.  The K registers are free behind after_qk, the V registers behind the function.
 template <int NT, int BITS, bool KC, class AfterQK>
-__device__ __forceinline__ void attend_page(const PageRegs<BITS> &r, int n_valid, int lane, Rows<NT> &rows, Meta &meta, AfterQK after_qk)
+__device__ __forceinline__ void attend_page(const PageRegs<BITS> &r, int n_valid, int lane, Rows<NT> &rows, Meta &meta, const Magic &mg, AfterQK after_qk)
 {
-    constexpr bool kPerChannel = KC && BITS == 2;
     const int r16 = lane & 15, q4 = lane >> 4;
-    const bool partial = n_valid < kPageTokens;
     meta.k[lane] = r.km;
-    {
-        uint4 vm = r.vm;
-        if (partial) {
-            // what was never written counts nothing, whatever stands there: chunk lane % 32 = (block, quad, group) of eight tokens
-            const int t0 = 32 * ((lane >> 4) & 1) + 4 * ((lane >> 2) & 3);
-            auto mask = [&](int t) { return (t < n_valid ? 0xffffu : 0u) | (t + 1 < n_valid ? 0xffff0000u : 0u); };
-            vm.x &= mask(t0);
-            vm.y &= mask(t0 + 2);
-            vm.z &= mask(t0 + 16);
-            vm.w &= mask(t0 + 18);
-        }
-        meta.v[lane] = vm;
-    }
+    // this lane's chunk of the V planes: lane % 32 = (block, quad, group)
+    meta.v[lane] = n_valid < kPageTokens ? mask_meta(r.vm, (lane >> 4) & 1, (lane >> 2) & 3, n_valid) : r.vm;
     lds_order();
-
     floatx4 S[NT][4];   // token 16 e + 4 q4 + i, row r16
 #pragma unroll
     for (int n = 0; n < NT; ++n)
 #pragma unroll
         for (int e = 0; e < 4; ++e) S[n][e] = floatx4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-    for (int e = 0; e < 4; ++e) {
-        uint2 sc, zc;
-        if constexpr (!kPerChannel) {
-            sc = reinterpret_cast<const uint2 *>(meta.k)[16 * e + r16];
-            zc = reinterpret_cast<const uint2 *>(meta.k + 32)[16 * e + r16];
-        }
+    for (int b = 0; b < 2; ++b) {
+        uint2 sc[2], zc[2];
+        if constexpr (!(KC && BITS == 2))
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                sc[e] = reinterpret_cast<const uint2 *>(meta.k)[32 * b + 16 * e + r16];
+                zc[e] = reinterpret_cast<const uint2 *>(meta.k + 32)[32 * b + 16 * e + r16];
+            }
 #pragma unroll
         for (int g = 0; g < 4; ++g) {
-            const uint32_t w = g == 0 ? r.kw[e].x : g == 1 ? r.kw[e].y : g == 2 ? r.kw[e].z : r.kw[e].w;
-            uint32_t a[4];
-            if constexpr (kPerChannel) {
-                const uint4 s = meta.k[((e >> 1) * 4 + g) * 4 + q4], z = meta.k[32 + ((e >> 1) * 4 + g) * 4 + q4];
-                const uint32_t x = w >> (8 * (q4 & 1));
-                a[0] = dequant2<2>(x, s.x, z.x);
-                a[1] = dequant2<2>(x >> 2, s.y, z.y);
-                a[2] = dequant2<2>(x >> 4, s.z, z.z);
-                a[3] = dequant2<2>(x >> 6, s.w, z.w);
-            } else {
-                const uint32_t s = twice(g < 2 ? sc.x : sc.y, g), z = twice(g < 2 ? zc.x : zc.y, g);
-                // INT4: codes k and k + 4 lie in the halves of the word; INT2: the bytes of this lane's octet move there
-                const uint32_t x = BITS == 4 ? w : __builtin_amdgcn_perm(w, w, (q4 & 1) ? 0x0c070c06u : 0x0c050c04u);
-#pragma unroll
-                for (int k = 0; k < 4; ++k) a[k] = dequant2<BITS>(x >> (BITS * k), s, z);
+            uint32_t s[4], z[4];
+            if constexpr (KC && BITS == 2) {
+                channel_meta(meta.k, b, g, q4, s);
+                channel_meta(meta.k + 32, b, g, q4, z);
             }
-            const half8 A = as_half8(a[0], a[1], a[2], a[3]);
 #pragma unroll
-            for (int n = 0; n < NT; ++n) S[n][e] = mfma(A, rows.q[n][g], S[n][e]);
+            for (int e = 0; e < 2; ++e) {
+                if constexpr (!(KC && BITS == 2)) {
+                    s[0] = s[1] = s[2] = s[3] = twice(g < 2 ? sc[e].x : sc[e].y, g);
+                    z[0] = z[1] = z[2] = z[3] = twice(g < 2 ? zc[e].x : zc[e].y, g);
+                }
+                const half8 A = k_operand<BITS>(word_of(r.kw[2 * b + e], g), s, z, q4, mg);
+#pragma unroll
+                for (int n = 0; n < NT; ++n) S[n][2 * b + e] = mfma(A, rows.q[n][g], S[n][2 * b + e]);
+            }
         }
     }
     after_qk();
-
-    // softmax weights, operands of PV: tokens 32 b + 16 (j >> 2) + 4 q4 + (j & 3), j = 0..7, of row r16
     half8 P[NT][2];
-#pragma unroll
-    for (int n = 0; n < NT; ++n) {
-        if (partial) {
-#pragma unroll
-            for (int e = 0; e < 4; ++e)
-#pragma unroll
-                for (int i = 0; i < 4; ++i) S[n][e][i] = 16 * e + 4 * q4 + i < n_valid ? S[n][e][i] : -INFINITY;
-        }
-        float mx = S[n][0][0];
-#pragma unroll
-        for (int k = 1; k < 16; ++k) mx = fmaxf(mx, S[n][k >> 2][k & 3]);
-        if (__any(mx * rows.kappa[n] > rows.m[n] + kTau)) {
-            mx = fmaxf(mx, __shfl_xor(mx, 16));
-            mx = fmaxf(mx, __shfl_xor(mx, 32));
-            const float m_new = fmaxf(rows.m[n], mx * rows.kappa[n]);
-            const float alpha = m_new == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(rows.m[n] - m_new);
-            rows.m[n] = m_new;
-            rows.huge = rows.huge || __any(fabsf(m_new) > 0x1p20f && m_new != -INFINITY);
-            floatx4 av;
-#pragma unroll
-            for (int i = 0; i < 4; ++i) av[i] = __shfl(alpha, 4 * q4 + i);
-#pragma unroll
-            for (int c = 0; c < 8; ++c) rows.acc[n][c] *= av;
-            rows.sum[n] *= av;
-        }
-        float factor = rows.kappa[n], shift = (float)kPExp - (rows.m[n] == -INFINITY ? 0.0f : rows.m[n]);
-        if (__builtin_expect(rows.huge, 0)) {
-            // factor * logit with one rounding, as the reference has it, then the difference: the largest weight is 2^8
-#pragma unroll
-            for (int e = 0; e < 4; ++e) S[n][e] = S[n][e] * factor - (rows.m[n] == -INFINITY ? 0.0f : rows.m[n]);
-            factor = 1.0f;
-            shift = (float)kPExp;
-        }
-        uint32_t w[8];
-#pragma unroll
-        for (int k = 0; k < 8; ++k) {
-            const float a = __builtin_amdgcn_exp2f(fmaf(S[n][k >> 1][2 * (k & 1)], factor, shift));
-            const float b = __builtin_amdgcn_exp2f(fmaf(S[n][k >> 1][2 * (k & 1) + 1], factor, shift));
-            w[k] = pack_h2(a, b);
-        }
-        P[n][0] = as_half8(w[0], w[1], w[2], w[3]);
-        P[n][1] = as_half8(w[4], w[5], w[6], w[7]);
-    }
-
-    const half8 ones = as_half8(0x3c003c00u, 0x3c003c00u, 0x3c003c00u, 0x3c003c00u);
+    weigh(rows, S, n_valid, q4, P);
 #pragma unroll
     for (int b = 0; b < 2; ++b) {
 #pragma unroll
-        for (int n = 0; n < NT; ++n) rows.sum[n] = mfma(P[n][b], ones, rows.sum[n]);
+        for (int n = 0; n < NT; ++n) rows.sum[n] = mfma(P[n][b], ones(), rows.sum[n]);
 #pragma unroll
         for (int g = 0; g < 4; ++g) {
             const uint4 s = meta.v[(b * 4 + q4) * 4 + g], z = meta.v[32 + (b * 4 + q4) * 4 + g];
 #pragma unroll
             for (int c = 0; c < 2; ++c) {
-                const int tile = 2 * g + c, half = tile >> 2, comp = tile & 3;
-                const uint4 v4 = r.vw[BITS == 4 ? b * 2 + half : half];
-                const uint32_t w = comp == 0 ? v4.x : comp == 1 ? v4.y : comp == 2 ? v4.z : v4.w;
-                const uint32_t x = BITS == 4 ? w : w >> (8 * b);
-                const half8 B = as_half8(dequant2<BITS>(x, s.x, z.x), dequant2<BITS>(x >> BITS, s.y, z.y), dequant2<BITS>(x >> (2 * BITS), s.z, z.z),
-                                         dequant2<BITS>(x >> (3 * BITS), s.w, z.w));
+                const int tile = 2 * g + c, half = tile >> 2;
+                const half8 B = v_operand<BITS>(word_of(r.vw[BITS == 4 ? b * 2 + half : half], tile & 3), b, s, z, mg);
 #pragma unroll
                 for (int n = 0; n < NT; ++n) rows.acc[n][tile] = mfma(P[n][b], B, rows.acc[n][tile]);
             }
         }
     }
 }
-
-// The pages of a wavefront, 64 at a time in registers: lane l holds the wavefront's page number base + l.
-struct PageList {
-    int base;
-    uint32_t at;   // where the record starts in the pool, in units of kUnit
-    int valid;     // tokens of the page that count
-};
-constexpr int kUnitLog2 = 11;   // record and arena sizes are multiples of it
-static_assert(Rec<2>::kBytes % (1 << kUnitLog2) == 0 && Rec<4>::kBytes % (1 << kUnitLog2) == 0, "record unit");
-struct ItemCtx {
-    const uint8_t *pool;
-    const uint8_t *bit_map;
-    const int32_t *pages;
-    int first, n;                        // list position of the wavefront's first page; how many it has, every kWaves-th
-    int np2, np4, last2, last4;          // pages of either width of the list, tokens of the last ones
-    int kvh, n_kv_heads, n_pages_int2, n_pages_total, lane;
-    int32_t *status;
-};
-__device__ __forceinline__ void fetch_list(const ItemCtx &cx, PageList &l, int base)
-{
-    l.base = base;
-    const int i = base + cx.lane < cx.n ? base + cx.lane : cx.n - 1;
-    const int pos = cx.first + kWaves * i;
-    const int page = cx.pages[pos];
-    const bool is2 = pos < cx.np2;
-    const int lo = is2 ? 0 : cx.n_pages_int2, hi = is2 ? cx.n_pages_int2 : cx.n_pages_total;
-    const bool ok = page >= lo && page < hi;
-    if (!ok && cx.status) atomicOr(cx.status, page < 0 || page >= cx.n_pages_total ? TKV_STATUS_PAGE_RANGE : TKV_STATUS_BITMAP_MISMATCH);
-    // a page that cannot be read counts no tokens; nothing is read in its place (the record's size is 0, see record_of)
-    const uint32_t rec = (uint32_t)(is2 ? page : page - cx.n_pages_int2) * (uint32_t)cx.n_kv_heads + (uint32_t)cx.kvh;
-    constexpr uint32_t kUnits2 = Rec<2>::kBytes >> kUnitLog2, kUnits4 = Rec<4>::kBytes >> kUnitLog2;
-    l.at = !ok ? 0 : (is2 ? rec * kUnits2 : (uint32_t)cx.n_pages_int2 * (uint32_t)cx.n_kv_heads * kUnits2 + rec * kUnits4);   // (pools below 8 TB: 32 bits)
-    const bool written = ok && cx.bit_map[ok ? page : 0] == (is2 ? 2 : 4);
-    if (ok && !written && cx.status) atomicOr(cx.status, TKV_STATUS_BITMAP_MISMATCH);
-    l.valid = !written ? 0 : (pos == cx.np2 - 1 ? cx.last2 : pos == cx.np2 + cx.np4 - 1 ? cx.last4 : kPageTokens);
-}
-template <int BITS> __device__ __forceinline__ Record record_of(const ItemCtx &cx, const PageList &l, int i, bool wanted)
-{
-    const uint64_t at = (uint32_t)__builtin_amdgcn_readlane((int)l.at, i - l.base);
-    const int valid = __builtin_amdgcn_readlane(l.valid, i - l.base);
-    return __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t *>(cx.pool) + (at << kUnitLog2), 0, wanted && valid > 0 ? Rec<BITS>::kBytes : 0, 0x00027000);
-}
-
-// Pages [i, end) of the wavefront, all of one width.
+// Pages [i, end), all of one width.
 template <int NT, int BITS, bool KC>
-__device__ __forceinline__ void run_pages(const ItemCtx &cx, PageList &list, int i, int end, Rows<NT> &rows, Meta &meta)
+__device__ __forceinline__ void run_pages(const ListCtx &cx, PageList &list, int i, int end, Rows<NT> &rows, Meta &meta)
 {
+    const Magic mg;
     PageRegs<BITS> r;
-    Record rec = record_of<BITS>(cx, list, i, true);
+    Record rec = record_of(cx, list, i, true);
     load_k(r, rec, cx.lane);
     load_v(r, rec, cx.lane);
     for (; i < end; ++i) {
-        const int valid = __builtin_amdgcn_readlane(list.valid, i - list.base);
+        const int valid = valid_of(list, i);
         const bool more = i + 1 < end;
         if (more && i + 1 - list.base >= 64) fetch_list(cx, list, i + 1);
-        rec = record_of<BITS>(cx, list, more ? i + 1 : i, more);
-        attend_page<NT, BITS, KC>(r, valid, cx.lane, rows, meta, [&]() {
-            __builtin_amdgcn_sched_barrier(0);
+        rec = record_of(cx, list, more ? i + 1 : i, more);
+        if (valid > 0) {
+            attend_page<NT, BITS, KC>(r, valid, cx.lane, rows, meta, mg, [&]() {
+                __builtin_amdgcn_sched_barrier(0);
+                load_k(r, rec, cx.lane);
+            });
+        } else {
             load_k(r, rec, cx.lane);
-        });
+        }
         __builtin_amdgcn_sched_barrier(0);
         load_v(r, rec, cx.lane);
     }
 }
+template <int NT, bool KC> __device__ __forceinline__ void run_list(const ListCtx &cx, Rows<NT> &rows, Meta &meta)
+{
+    if (cx.n <= 0) return;
+    PageList list;
+    fetch_list(cx, list, 0);
+    int n2 = cx.first < cx.np2 ? (cx.np2 - cx.first + cx.step - 1) / cx.step : 0;   // INT2 pages: they come first
+    n2 = n2 < cx.n ? n2 : cx.n;
+    if (n2 > 0) run_pages<NT, 2, KC>(cx, list, 0, n2, rows, meta);
+    if (n2 < cx.n) {
+        if (n2 - list.base >= 64) fetch_list(cx, list, n2);
+        run_pages<NT, 4, KC>(cx, list, n2, cx.n, rows, meta);
+    }
+}
 
+// ---- many rows: four wavefronts expand a page together, and each attends to it with rows of its own ------------------------
+// Wavefront (rw, th) = (wave % 4, wave / 4) owns row tiles rw * NT ... and every second page, th first.  The operands of a page
+// stand in LDS as the MFMAs take them, 1 KiB each: K (token tile e, group g), V (block b, channel tile).  Of its next page
+// it expands K tile rw and the V operands of chunk rw = (block, channel half) of the plane, while the others of its four
+// wavefronts expand theirs.
+struct alignas(16) Operands {
+    uint4 k[16][64], v[16][64];
+};
+struct RawPage {   // this lane's part of a page as stored
+    uint4 kw, vw;         // four group words of its token, four channel words of its tokens
+    uint4 km;             // K scales (x, y) and zeros (z, w) of its token; per-channel INT2 keys: chunk `lane` of the K planes
+    uint4 vs[2], vz[2];   // V scales and zero-points of its eight tokens, two groups
+};
+template <int BITS, bool KC> __device__ __forceinline__ void load_raw(RawPage &r, Record rec, int rw, int lane)
+{
+    using R = Rec<BITS>;
+    const int r16 = lane & 15;
+    r.kw = load16(rec, R::kKCodes + 16 * (BITS == 4 ? rw * 64 + lane : rw * 32 + (lane >> 5) * 16 + r16));
+    if constexpr (KC && BITS == 2) {
+        r.km = load16(rec, R::kKScale + 16 * lane);
+    } else {
+        const uint2 s = load8(rec, R::kKScale + 8 * (16 * rw + r16)), z = load8(rec, R::kKZero + 8 * (16 * rw + r16));
+        r.km = make_uint4(s.x, s.y, z.x, z.y);
+    }
+    r.vw = load16(rec, R::kVCodes + 16 * ((BITS == 4 ? rw : rw & 1) * 64 + lane));
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        const int chunk = ((rw >> 1) * 4 + (lane >> 4)) * 4 + 2 * (rw & 1) + i;
+        r.vs[i] = load16(rec, R::kVScale + 16 * chunk);
+        r.vz[i] = load16(rec, R::kVZero + 16 * chunk);
+    }
+}
+template <int BITS, bool KC> __device__ __forceinline__ void expand(RawPage &r, int n_valid, int rw, int lane, Operands &o, uint4 *stage, const Magic &mg)
+{
+    const int q4 = lane >> 4, b = rw >> 1;
+    if constexpr (KC && BITS == 2) {
+        stage[lane] = r.km;
+        lds_order();
+    }
+    if (__builtin_expect(n_valid < kPageTokens, 0))
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            r.vs[i] = mask_meta(r.vs[i], b, q4, n_valid);
+            r.vz[i] = mask_meta(r.vz[i], b, q4, n_valid);
+        }
+#pragma unroll
+    for (int g = 0; g < 4; ++g) {
+        uint32_t s[4], z[4];
+        if constexpr (KC && BITS == 2) {
+            channel_meta(stage, b, g, q4, s);
+            channel_meta(stage + 32, b, g, q4, z);
+        } else {
+            s[0] = s[1] = s[2] = s[3] = twice(g < 2 ? r.km.x : r.km.y, g);
+            z[0] = z[1] = z[2] = z[3] = twice(g < 2 ? r.km.z : r.km.w, g);
+        }
+        o.k[rw * 4 + g][lane] = __builtin_bit_cast(uint4, k_operand<BITS>(word_of(r.kw, g), s, z, q4, mg));
+    }
+#pragma unroll
+    for (int c = 0; c < 4; ++c)
+        o.v[b * 8 + 4 * (rw & 1) + c][lane] = __builtin_bit_cast(uint4, v_operand<BITS>(word_of(r.vw, c), b, r.vs[c >> 1], r.vz[c >> 1], mg));
+}
+// The logits of a page, what `between` does, and the rest.
+template <int NT, class Between> __device__ __forceinline__ void attend_operands(const Operands &o, int n_valid, int lane, Rows<NT> &rows, Between between)
+{
+    const int q4 = lane >> 4;
+    floatx4 S[NT][4];
+#pragma unroll
+    for (int n = 0; n < NT; ++n)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) S[n][e] = floatx4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int g = 0; g < 4; ++g)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const half8 A = __builtin_bit_cast(half8, o.k[e * 4 + g][lane]);
+#pragma unroll
+            for (int n = 0; n < NT; ++n) S[n][e] = mfma(A, rows.q[n][g], S[n][e]);
+        }
+    between();
+    half8 P[NT][2];
+    weigh(rows, S, n_valid, q4, P);
+#pragma unroll
+    for (int b = 0; b < 2; ++b) {
+#pragma unroll
+        for (int n = 0; n < NT; ++n) rows.sum[n] = mfma(P[n][b], ones(), rows.sum[n]);
+#pragma unroll
+        for (int c = 0; c < 8; ++c) {
+            const half8 B = __builtin_bit_cast(half8, o.v[b * 8 + c][lane]);
+#pragma unroll
+            for (int n = 0; n < NT; ++n) rows.acc[n][c] = mfma(P[n][b], B, rows.acc[n][c]);
+        }
+    }
+}
+struct TileLds {
+    Operands page[2][2];   // [step % 2][th]
+    uint4 stage[kWaves][64];
+};
+// Pages [i0, end) of the list, all of one width; the same number of steps, and barriers, in all wavefronts.
+template <int NT, int BITS, bool KC>
+__device__ __forceinline__ void run_tiles(const ListCtx &cx, PageList &list, int i0, int end, bool active, int wave, Rows<NT> &rows, TileLds &lds)
+{
+    const int rw = wave & 3, th = wave >> 2, lane = cx.lane;
+    const Magic mg;
+    RawPage raw;
+    int valid = 0, valid_next = 0;   // tokens of this step's page and of the next one's; 0: none
+    auto request = [&](int i) -> int {
+        if (i >= end) return 0;
+        if (i - list.base >= 64) fetch_list(cx, list, i);
+        const int v = valid_of(list, i);
+        load_raw<BITS, KC>(raw, record_of(cx, list, i, true), rw, lane);
+        return v;
+    };
+    int i = i0 + th;
+    valid = request(i);
+    if (valid > 0) expand<BITS, KC>(raw, valid, rw, lane, lds.page[0][th], lds.stage[wave], mg);
+    valid_next = request(i + 2);
+    __syncthreads();
+    for (int step = 0, n = (end - i0 + 1) / 2; step < n; ++step, i += 2) {
+        Operands &now = lds.page[step & 1][th], &next = lds.page[(step + 1) & 1][th];
+        int valid_after = 0;
+        auto prepare_next = [&]() {
+            if (valid_next > 0) expand<BITS, KC>(raw, valid_next, rw, lane, next, lds.stage[wave], mg);
+            valid_after = request(i + 4);
+        };
+        if (active && valid > 0) attend_operands<NT>(now, valid, lane, rows, prepare_next);
+        else prepare_next();
+        __syncthreads();   // this step's pages are read, the next ones stand there
+        valid = valid_next;
+        valid_next = valid_after;
+    }
+}
+
+// ---- work items ----------------------------------------------------------------------------------------------------------
+// MODE 0: one row tile, every wavefront with pages of its own; 1, 2: MODE row tiles a wavefront, pages expanded together.
+constexpr int tiles_of(int mode) { return mode == 0 ? 1 : mode; }
+constexpr int rows_of(int mode) { return mode == 0 ? 16 : 64 * mode; }
 constexpr int kOutRow = kHeadDim + 4;   // floats: rows 4 q4 + i of a store fall on different banks
-template <int NT> struct Shared {
+template <int SETS, int ROWS> struct Results {   // of SETS wavefronts for the same rows, on their way out
+    float acc[SETS][ROWS][kOutRow];
+    float m[SETS][ROWS], sum[SETS][ROWS];
+};
+template <int MODE> struct Shared {
+    static constexpr int kSets = MODE == 0 ? kWaves : 2;
     union {
         Meta meta[kWaves];
-        float acc[kWaves][16 * NT][kOutRow];
+        std::conditional_t<MODE == 0, Meta, TileLds> tile;
+        Results<kSets, rows_of(MODE)> out;
+        union {
+            Meta meta;
+            float acc[8][kOutRow];
+        } own[kWaves];
     };
-    float m[kWaves][16 * NT], sum[kWaves][16 * NT];
 };
 
-template <int NT, bool KC> __device__ __forceinline__ void prefix_item(const PrefixArgs &a)
+// The own tokens of a sequence: a wavefront for each (item, kv head), whose rows are the query heads of the kv head.
+template <bool KC, class L> __device__ __forceinline__ void own_item(const SharedArgs &a, L &lds, int wave, int lane)
 {
-    __shared__ Shared<NT> lds;
-    const int tid = threadIdx.x, lane = tid & 63, r16 = lane & 15, q4 = lane >> 4, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int kvh = blockIdx.x, item = blockIdx.y, R = 1 << a.log2_r, n_q_heads = a.n_kv_heads << a.log2_r;
+    const int r16 = lane & 15, q4 = lane >> 4, R = 1 << a.log2_r, n_q_heads = a.n_kv_heads << a.log2_r;
+    const int64_t unit = (int64_t)blockIdx.x * kWaves + wave;
+    if (unit >= (int64_t)a.n_items * a.n_kv_heads) return;
+    const int item = (int)(unit / a.n_kv_heads), kvh = (int)(unit % a.n_kv_heads);
+    const ConstWords words = (ConstWords)(a.items + 4 * (size_t)item);
+    const int seq = words[0], item_pb = words[1], item_pe = words[2], slot = words[3];
+    const bool seq_ok = seq >= 0 && seq < a.batch, slot_ok = slot >= 0 && slot < a.n_items;
+    if (!(seq_ok && slot_ok) && a.status && lane == 0) atomicOr(a.status, TKV_STATUS_BAD_ITEM);
+    if (!slot_ok) return;
+    const int sq = seq_ok ? seq : 0;
+    const int n2 = ((ConstWords)a.n_tok_int2)[sq], n4 = ((ConstWords)a.n_tok_int4)[sq];
+    const int list0 = ((ConstWords)a.page_indptr)[sq], list1 = ((ConstWords)a.page_indptr)[sq + 1];
+    const int np2 = (n2 + kPageTokens - 1) / kPageTokens, np4 = (n4 + kPageTokens - 1) / kPageTokens;
+    const int np = np2 + np4 < list1 - list0 ? np2 + np4 : list1 - list0;
+    const int pb = item_pb > 0 ? item_pb : 0, pe = item_pe < np ? item_pe : np;
+    Rows<1> rows;
+    clear(rows);
+    if (seq_ok && pb < pe) {
+        load_q(rows, 0, a.q + ((size_t)sq * n_q_heads + kvh * R + (r16 & (R - 1))) * kHeadDim, a.kappa, lane);
+        const ListCtx cx = {a.pool, a.bit_map, a.page_ids + list0, pb, 1, pe - pb, np2, np4, n2 - (np2 - 1) * kPageTokens, n4 - (np4 - 1) * kPageTokens,
+                            kvh, a.n_kv_heads, a.n_pages_int2, a.n_pages_int2 + a.n_pages_int4, lane, a.status};
+        run_list<1, KC>(cx, rows, lds.own[wave].meta);
+    }
+    const size_t at = (size_t)slot * n_q_heads + kvh * R;
+    if (q4 == 0 && r16 < R) a.ml_ws[0][2 * (at + r16)] = rows.m[0];
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+        if (r16 == 0 && 4 * q4 + i < R) a.ml_ws[0][2 * (at + 4 * q4 + i) + 1] = rows.sum[0][i];
+    lds_order();   // the metadata is read
+    if (q4 < 2)
+#pragma unroll
+        for (int c = 0; c < 8; ++c)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) lds.own[wave].acc[4 * q4 + i][16 * c + r16] = rows.acc[0][c][i];
+    lds_order();
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        const int r = 2 * k + (lane >> 5), c4 = lane & 31;
+        if (r < R) reinterpret_cast<float4 *>(a.acc_ws[0] + (at + r) * kHeadDim)[c4] = *reinterpret_cast<const float4 *>(&lds.own[wave].acc[r][4 * c4]);
+    }
+}
+
+// A prefix's pages [item_pb, item_pe) for rows_of(MODE) query rows of its members.
+template <int MODE, bool KC> __device__ __forceinline__ void prefix_item(const SharedArgs &a, Shared<MODE> &lds, int wave, int lane)
+{
+    constexpr int NT = tiles_of(MODE), ROWS = rows_of(MODE), SETS = Shared<MODE>::kSets;
+    const int r16 = lane & 15, q4 = lane >> 4, R = 1 << a.log2_r, n_q_heads = a.n_kv_heads << a.log2_r;
+    // the workgroups of an (item, kv head) lie a multiple of items x kv heads apart: with eight kv heads on one XCD, whose L2 they share
+    const int per = a.p.n_items * a.n_kv_heads, block = blockIdx.x - a.own_blocks, z = block / per, unit = block - z * per;
+    const int item = unit / a.n_kv_heads, kvh = unit - item * a.n_kv_heads;
     const ConstWords words = (ConstWords)(a.p.items + 4 * (size_t)item);
     const int group = words[0], item_pb = words[1], item_pe = words[2], part = words[3];
     if (group < 0 || group >= a.p.n_groups || part < 0) {
-        if (a.status && tid == 0) atomicOr(a.status, TKV_STATUS_BAD_ITEM);
+        if (a.status && threadIdx.x == 0) atomicOr(a.status, TKV_STATUS_BAD_ITEM);
         return;
     }
     int m0 = ((ConstWords)a.p.member_indptr)[group], m1 = ((ConstWords)a.p.member_indptr)[group + 1];
@@ -386,107 +674,101 @@ template <int NT, bool KC> __device__ __forceinline__ void prefix_item(const Pre
     const int list0 = ((ConstWords)a.p.page_indptr)[group], list1 = ((ConstWords)a.p.page_indptr)[group + 1];
     m0 = m0 > 0 ? m0 : 0;
     m1 = m1 < a.p.n_members ? m1 : a.p.n_members;
-    const int n_rows = (m1 - m0) << a.log2_r, row0 = blockIdx.z * 16 * NT;
+    const int n_rows = (m1 - m0) << a.log2_r, row0 = z * ROWS;
     if (row0 >= n_rows) return;
-    if (m1 - m0 > a.p.max_members && a.status && tid == 0) atomicOr(a.status, TKV_STATUS_BAD_ITEM);   // more rows than the launch has workgroups for
+    if (m1 - m0 > a.p.max_members && a.status && threadIdx.x == 0) atomicOr(a.status, TKV_STATUS_BAD_ITEM);   // more rows than the launch has workgroups for
     const int np2 = (n2 + kPageTokens - 1) / kPageTokens, np4 = (n4 + kPageTokens - 1) / kPageTokens;
     const int np = np2 + np4 < list1 - list0 ? np2 + np4 : list1 - list0;
     const int pb = item_pb > 0 ? item_pb : 0, pe = item_pe < np ? item_pe : np;
 
+    const int wave_row = MODE == 0 ? 0 : (wave & 3) * 16 * NT;   // this wavefront's first row of the workgroup
+    const bool active = row0 + wave_row < n_rows;
     Rows<NT> rows;
-    rows.huge = false;
+    clear(rows);
+    if (active) {
 #pragma unroll
-    for (int n = 0; n < NT; ++n) {
-        const int row = row0 + 16 * n + r16, member = m0 + (row >> a.log2_r);
-        int seq = row < n_rows ? a.p.member_seqs[member] : 0;
-        if (seq < 0 || seq >= a.batch) seq = 0;   // nothing of it is stored
-        rows.at[n] = seq * n_q_heads + kvh * R + (row & (R - 1));
-        rows.m[n] = -INFINITY;
-        rows.sum[n] = floatx4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-        for (int c = 0; c < 8; ++c) rows.acc[n][c] = floatx4{0.f, 0.f, 0.f, 0.f};
+        for (int n = 0; n < NT; ++n) {
+            const int row = row0 + wave_row + 16 * n + r16;
+            int seq = row < n_rows ? a.p.member_seqs[m0 + (row >> a.log2_r)] : 0;
+            if (seq < 0 || seq >= a.batch) seq = 0;   // nothing of it is stored
+            load_q(rows, n, a.q + ((size_t)seq * n_q_heads + kvh * R + (row & (R - 1))) * kHeadDim, a.kappa, lane);
+        }
     }
-    const int first = pb + wave, n = first < pe ? (pe - first + kWaves - 1) / kWaves : 0;   // this wavefront's pages
-    if (n > 0) {
-        const ItemCtx cx = {a.pool, a.bit_map, a.p.page_ids + list0, first, n, np2, np4, n2 - (np2 - 1) * kPageTokens, n4 - (np4 - 1) * kPageTokens,
-                            kvh, a.n_kv_heads, a.n_pages_int2, a.n_pages_int2 + a.n_pages_int4, lane, a.status};
+    const int first = MODE == 0 ? pb + wave : pb, step = MODE == 0 ? kWaves : 1;
+    const ListCtx cx = {a.pool, a.bit_map, a.p.page_ids + list0, first, step, first < pe ? (pe - first + step - 1) / step : 0, np2, np4,
+                        n2 - (np2 - 1) * kPageTokens, n4 - (np4 - 1) * kPageTokens,
+                        kvh, a.n_kv_heads, a.n_pages_int2, a.n_pages_int2 + a.n_pages_int4, lane, a.status};
+    if constexpr (MODE == 0) {
+        run_list<NT, KC>(cx, rows, lds.meta[wave]);
+    } else if (cx.n > 0) {
         PageList list;
         fetch_list(cx, list, 0);
-        const int n_2 = first < np2 ? ((np2 < pe ? np2 : pe) - first + kWaves - 1) / kWaves : 0;   // INT2 pages among them: they come first
-        if (n_2 > 0) {
-            load_q<NT, KC>(rows, a.q, a.kappa, lane);
-            run_pages<NT, 2, KC>(cx, list, 0, n_2, rows, lds.meta[wave]);
-        }
-        if (n_2 < n) {
-            if (n_2 == 0 || KC) load_q<NT, false>(rows, a.q, a.kappa, lane);
-            if (n_2 - list.base >= 64) fetch_list(cx, list, n_2);
-            run_pages<NT, 4, KC>(cx, list, n_2, n, rows, lds.meta[wave]);
-        }
+        int n2 = first < np2 ? np2 - first : 0;   // INT2 pages: they come first
+        n2 = n2 < cx.n ? n2 : cx.n;
+        if (n2 > 0) run_tiles<NT, 2, KC>(cx, list, 0, n2, active, wave, rows, lds.tile);
+        if (n2 < cx.n) run_tiles<NT, 4, KC>(cx, list, n2, cx.n, active, wave, rows, lds.tile);
     }
 
-    // ---- the four wavefronts' results are brought to a common reference, added and stored --------------------------------
-    if (q4 == 0)
+    // ---- results of the wavefronts for the same rows are brought to a common reference, added and stored ------------------
+    if constexpr (MODE == 0) __syncthreads();   // no page is being worked on
+    const int set = MODE == 0 ? wave : wave >> 2;
+    if (active) {
 #pragma unroll
-        for (int k = 0; k < NT; ++k) lds.m[wave][16 * k + r16] = rows.m[k];
-    __syncthreads();   // the references are there, and no page is being worked on
+        for (int n = 0; n < NT; ++n) {
+            const int r = wave_row + 16 * n;
+            if (q4 == 0) lds.out.m[set][r + r16] = rows.m[n];
 #pragma unroll
-    for (int k = 0; k < NT; ++k) {
-        floatx4 f;
+            for (int i = 0; i < 4; ++i) {
+                if (r16 == 0) lds.out.sum[set][r + 4 * q4 + i] = rows.sum[n][i];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const int row = 16 * k + 4 * q4 + i;
-            const float own = lds.m[wave][row];
-            const float top = fmaxf(fmaxf(lds.m[0][row], lds.m[1][row]), fmaxf(lds.m[2][row], lds.m[3][row]));
-            f[i] = own == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(own - top);
+                for (int c = 0; c < 8; ++c) lds.out.acc[set][r + 4 * q4 + i][16 * c + r16] = rows.acc[n][c][i];
+            }
         }
-        rows.sum[k] *= f;
-#pragma unroll
-        for (int c = 0; c < 8; ++c) {
-            rows.acc[k][c] *= f;
-#pragma unroll
-            for (int i = 0; i < 4; ++i) lds.acc[wave][16 * k + 4 * q4 + i][16 * c + r16] = rows.acc[k][c][i];
-        }
-        if (r16 == 0)
-#pragma unroll
-            for (int i = 0; i < 4; ++i) lds.sum[wave][16 * k + 4 * q4 + i] = rows.sum[k][i];
     }
     __syncthreads();
-    const int c4 = tid & 31;   // 32 lanes store a row
-#pragma unroll 4
-    for (int r = tid >> 5; r < 16 * NT; r += 8) {
+    const int c4 = threadIdx.x & 31;   // 32 lanes store a row
+#pragma unroll 2
+    for (int r = threadIdx.x >> 5; r < ROWS; r += 2 * kWaves) {
         const int row = row0 + r;
         if (row >= n_rows) break;
         const int member = m0 + (row >> a.log2_r), seq = a.p.member_seqs[member];
         const int64_t slot = (int64_t)a.p.member_slots[member] + part;
-        if (seq < 0 || seq >= a.batch || slot < a.first_slot || slot >= a.n_slots) {
+        if (seq < 0 || seq >= a.batch || slot < a.n_items || slot >= a.n_slots) {
             if (a.status) atomicOr(a.status, TKV_STATUS_BAD_ITEM);
             continue;
         }
-        float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+        float top = lds.out.m[0][r];
 #pragma unroll
-        for (int w = 0; w < kWaves; ++w) {
-            const float4 t = *reinterpret_cast<const float4 *>(&lds.acc[w][r][4 * c4]);
-            v.x += t.x;
-            v.y += t.y;
-            v.z += t.z;
-            v.w += t.w;
+        for (int k = 1; k < SETS; ++k) top = fmaxf(top, lds.out.m[k][r]);
+        float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+        float sum = 0.0f;
+#pragma unroll
+        for (int k = 0; k < SETS; ++k) {
+            const float m = lds.out.m[k][r], w = m == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(m - top);
+            const float4 t = *reinterpret_cast<const float4 *>(&lds.out.acc[k][r][4 * c4]);
+            v.x = fmaf(w, t.x, v.x);
+            v.y = fmaf(w, t.y, v.y);
+            v.z = fmaf(w, t.z, v.z);
+            v.w = fmaf(w, t.w, v.w);
+            sum = fmaf(w, lds.out.sum[k][r], sum);
         }
-        const size_t at = (size_t)(slot - a.first_slot) * n_q_heads + kvh * R + (row & (R - 1));
-        reinterpret_cast<float4 *>(a.acc_ws + at * kHeadDim)[c4] = v;
-        if (c4 == 0)
-            reinterpret_cast<float2 *>(a.ml_ws)[at] = make_float2(fmaxf(fmaxf(lds.m[0][r], lds.m[1][r]), fmaxf(lds.m[2][r], lds.m[3][r])),
-                                                                  (lds.sum[0][r] + lds.sum[1][r]) + (lds.sum[2][r] + lds.sum[3][r]));
+        const size_t at = (size_t)(slot - a.n_items) * n_q_heads + kvh * R + (row & (R - 1));
+        reinterpret_cast<float4 *>(a.acc_ws[1] + at * kHeadDim)[c4] = v;
+        if (c4 == 0) reinterpret_cast<float2 *>(a.ml_ws[1])[at] = make_float2(top, sum);
     }
 }
-template <int NT, bool KC>
-__global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(NT == 4 ? 1 : NT == 2 ? 2 : 3, NT == 4 ? 1 : NT == 2 ? 2 : 3)))
-void tkv_prefix_kernel(PrefixArgs a)
+template <int MODE, bool KC>
+__global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2, 2))) void tkv_shared_kernel(SharedArgs a)
 {
-    prefix_item<NT, KC>(a);
+    __shared__ Shared<MODE> lds;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    if ((int)blockIdx.x < a.own_blocks) own_item<KC>(a, lds, wave, lane);
+    else prefix_item<MODE, KC>(a, lds, wave, lane);
 }
 
 // out = sum_i 2^(m_i - M) acc_i / sum_i 2^(m_i - M) l_i over a sequence's own items and its prefixes'.  One workgroup of four
 // wavefronts per (sequence, query head); a wavefront takes every fourth partial, a lane two channels.
+constexpr int kMergeWaves = 4;
 struct MergeArgs {
     const float *ws[2];              // partials of the own items, of the prefixes
     int n[2];                        // slots of either
@@ -508,10 +790,10 @@ __device__ __forceinline__ float wave_sum(float v)
     for (int d = 1; d < 64; d <<= 1) v += __shfl_xor(v, d);
     return v;
 }
-__global__ __launch_bounds__(64 * kWaves) void tkv_merge_shared_kernel(MergeArgs a)
+__global__ __launch_bounds__(64 * kMergeWaves) void tkv_merge_shared_kernel(MergeArgs a)
 {
-    __shared__ float2 num_s[kWaves][64];
-    __shared__ float2 ml_s[kWaves];
+    __shared__ float2 num_s[kMergeWaves][64];
+    __shared__ float2 ml_s[kMergeWaves];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int h = blockIdx.x, b = blockIdx.y + blockIdx.z * gridDim.y;
     if (b >= a.batch) return;
@@ -535,8 +817,8 @@ __global__ __launch_bounds__(64 * kWaves) void tkv_merge_shared_kernel(MergeArgs
         ml = ws + (size_t)(k ? a.n[1] : a.n[0]) * a.n_q_heads * kHeadDim + 2 * at;
     };
     // 64 of the wavefront's partials at a time: lane l weighs the l-th
-    for (int base = wave; base < all; base += kWaves * 64) {
-        const int mine = base + kWaves * lane;
+    for (int base = wave; base < all; base += kMergeWaves * 64) {
+        const int mine = base + kMergeWaves * lane;
         const float *acc, *mlp;
         float2 ml = make_float2(-INFINITY, 0.0f);
         if (mine < all) {
@@ -550,10 +832,10 @@ __global__ __launch_bounds__(64 * kWaves) void tkv_merge_shared_kernel(MergeArgs
         den = den * so + wave_sum(mine < all ? w * ml.y : 0.0f);
         num.x *= so;
         num.y *= so;
-        const int count = (all - base + kWaves - 1) / kWaves < 64 ? (all - base + kWaves - 1) / kWaves : 64;
+        const int count = (all - base + kMergeWaves - 1) / kMergeWaves < 64 ? (all - base + kMergeWaves - 1) / kMergeWaves : 64;
 #pragma unroll 8
         for (int k = 0; k < count; ++k) {
-            row_of(base + kWaves * k, acc, mlp);
+            row_of(base + kMergeWaves * k, acc, mlp);
             const float2 v = reinterpret_cast<const float2 *>(acc)[lane];
             const float wk = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(w), k));
             num.x = fmaf(wk, v.x, num.x);
@@ -567,11 +849,11 @@ __global__ __launch_bounds__(64 * kWaves) void tkv_merge_shared_kernel(MergeArgs
     if (wave > 0) return;
     float Mg = M;
 #pragma unroll
-    for (int k = 1; k < kWaves; ++k) Mg = fmaxf(Mg, ml_s[k].x);
+    for (int k = 1; k < kMergeWaves; ++k) Mg = fmaxf(Mg, ml_s[k].x);
     float d = 0.0f;
     float2 o = make_float2(0.f, 0.f);
 #pragma unroll
-    for (int k = 0; k < kWaves; ++k) {
+    for (int k = 0; k < kMergeWaves; ++k) {
         const float wk = merge_weight(ml_s[k].x, Mg);
         d += wk * ml_s[k].y;
         o.x = fmaf(wk, num_s[k][lane].x, o.x);
@@ -583,59 +865,71 @@ __global__ __launch_bounds__(64 * kWaves) void tkv_merge_shared_kernel(MergeArgs
     reinterpret_cast<uint32_t *>(a.out + ((size_t)b * a.n_q_heads + h) * kHeadDim)[lane] = __builtin_bit_cast(uint32_t, v);
 }
 
-template <int NT> void launch_prefix(bool kc, dim3 grid, hipStream_t s, const PrefixArgs &a)
+template <int MODE> void launch_shared(bool kc, unsigned blocks, hipStream_t s, const SharedArgs &a)
 {
-    hipLaunchKernelGGL((kc ? tkv_prefix_kernel<NT, true> : tkv_prefix_kernel<NT, false>), grid, dim3(64 * kWaves), 0, s, a);
+    hipLaunchKernelGGL((kc ? tkv_shared_kernel<MODE, true> : tkv_shared_kernel<MODE, false>), dim3(blocks), dim3(64 * kWaves), 0, s, a);
 }
 
 } // namespace
 
-int tkv_prefix_rows(int32_t rows) { return rows <= 16 ? 16 : rows <= 32 ? 32 : 64; }
+int32_t tkv_prefix_rows(int32_t rows) { return rows <= 16 ? 16 : rows <= 64 ? 64 : 128; }
 
-int tkv_launch_prefix(const tkv_desc *desc, const void *pool, const uint8_t *bit_map, const void *q, const tkv_prefix *prefix, int32_t first_slot,
-                      int32_t n_slots, int32_t batch, int32_t n_q_heads, float sm_scale, void *workspace, int32_t *status, void *stream)
+int tkv_launch_shared(const tkv_desc *desc, const void *pool, const uint8_t *bit_map, const void *q, const int32_t *page_indptr,
+                      const int32_t *page_ids, const int32_t *n_tok_int2, const int32_t *n_tok_int4, const int32_t *items, int32_t n_items,
+                      const tkv_prefix *prefix, const int32_t *slot_indptr, int32_t n_slots, int32_t batch, int32_t n_q_heads, float sm_scale,
+                      void *out, void *workspace, int32_t *status, void *stream)
 {
     int log2_r = 0;
     while ((desc->n_kv_heads << log2_r) < n_q_heads) ++log2_r;
-    PrefixArgs a = {};
+    const size_t row_floats = (size_t)n_q_heads * (kHeadDim + 2);
+    float *const ws[2] = {(float *)workspace, (float *)workspace + (size_t)n_items * row_floats};
+    const int n[2] = {n_items, n_slots - n_items};
+    SharedArgs a = {};
     a.pool = (const uint8_t *)pool;
     a.bit_map = bit_map;
     a.q = (const uint16_t *)q;
+    a.page_indptr = page_indptr;
+    a.page_ids = page_ids;
+    a.n_tok_int2 = n_tok_int2;
+    a.n_tok_int4 = n_tok_int4;
+    a.items = items;
+    a.n_items = n_items;
     a.p = *prefix;
     a.n_kv_heads = desc->n_kv_heads;
     a.log2_r = log2_r;
     a.n_pages_int2 = desc->n_pages_int2;
     a.n_pages_int4 = desc->n_pages_int4;
     a.batch = batch;
-    a.first_slot = first_slot;
     a.n_slots = n_slots;
     a.kappa = sm_scale * 1.44269504088896340736f;
-    a.acc_ws = (float *)workspace;
-    a.ml_ws = a.acc_ws + (size_t)(n_slots - first_slot) * n_q_heads * kHeadDim;
+    for (int k = 0; k < 2; ++k) {
+        a.acc_ws[k] = ws[k];
+        a.ml_ws[k] = ws[k] + (size_t)n[k] * n_q_heads * kHeadDim;
+    }
     a.status = status;
-    const int rows = prefix->max_members << log2_r, per = tkv_prefix_rows(rows);
-    const dim3 grid((unsigned)desc->n_kv_heads, (unsigned)prefix->n_items, (unsigned)((rows + per - 1) / per));
-    const bool kc = desc->int2_key_axis == TKV_KEYS_PER_CHANNEL;
-    if (per == 16) launch_prefix<1>(kc, grid, (hipStream_t)stream, a);
-    else if (per == 32) launch_prefix<2>(kc, grid, (hipStream_t)stream, a);
-    else launch_prefix<4>(kc, grid, (hipStream_t)stream, a);
-    return hipGetLastError() == hipSuccess ? TKV_OK : TKV_ERR_HIP;
-}
-
-int tkv_launch_merge_shared(const int32_t *indptr, int32_t n_own, int32_t n_prefix, int32_t batch, int32_t n_q_heads, void *out, const void *own_ws,
-                            const void *prefix_ws, void *stream)
-{
-    MergeArgs a = {};
-    a.ws[0] = (const float *)own_ws;
-    a.ws[1] = (const float *)prefix_ws;
-    a.n[0] = n_own;
-    a.n[1] = n_prefix;
-    a.indptr = indptr;
-    a.batch = batch;
-    a.n_q_heads = n_q_heads;
-    a.out = (uint16_t *)out;
+    a.own_blocks = (int)(((int64_t)n_items * desc->n_kv_heads + kWaves - 1) / kWaves);
+    const int rows = prefix->n_items > 0 ? prefix->max_members << log2_r : 1, per = tkv_prefix_rows(rows);
+    a.row_blocks = (rows + per - 1) / per;
+    const int64_t blocks = a.own_blocks + (int64_t)prefix->n_items * desc->n_kv_heads * a.row_blocks;
+    if (blocks > INT32_MAX) return TKV_ERR_INVALID_ARG;
+    if (blocks > 0) {
+        const bool kc = desc->int2_key_axis == TKV_KEYS_PER_CHANNEL;
+        if (per == 16) launch_shared<0>(kc, (unsigned)blocks, (hipStream_t)stream, a);
+        else if (per == 64) launch_shared<1>(kc, (unsigned)blocks, (hipStream_t)stream, a);
+        else launch_shared<2>(kc, (unsigned)blocks, (hipStream_t)stream, a);
+        if (hipGetLastError() != hipSuccess) return TKV_ERR_HIP;
+    }
+    MergeArgs m = {};
+    for (int k = 0; k < 2; ++k) {
+        m.ws[k] = ws[k];
+        m.n[k] = n[k];
+    }
+    m.indptr = slot_indptr;
+    m.batch = batch;
+    m.n_q_heads = n_q_heads;
+    m.out = (uint16_t *)out;
     constexpr int kMaxY = 65535;
     const dim3 grid((unsigned)n_q_heads, (unsigned)(batch < kMaxY ? batch : kMaxY), (unsigned)((batch + kMaxY - 1) / kMaxY));
-    hipLaunchKernelGGL(tkv_merge_shared_kernel, grid, dim3(64 * kWaves), 0, (hipStream_t)stream, a);
+    hipLaunchKernelGGL(tkv_merge_shared_kernel, grid, dim3(64 * kMergeWaves), 0, (hipStream_t)stream, m);
     return hipGetLastError() == hipSuccess ? TKV_OK : TKV_ERR_HIP;
 }

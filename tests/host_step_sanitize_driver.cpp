@@ -27,10 +27,10 @@ size_t tkv_table_words(int32_t n_seqs, int32_t n_tokens) { return (size_t)n_seqs
 int tkv_launch_table_reset(const tkv_desc *, const tkv_table *, void *) { return TKV_OK; }
 int tkv_launch_table_append(const tkv_desc *, const tkv_table *, const int32_t *, const int32_t *, const int32_t *, const uint8_t *, int32_t, int32_t *,
                             int32_t *, int32_t *, int32_t *, int32_t *, int32_t, int32_t *, void *, int32_t *, void *) { return TKV_OK; }
-int32_t tkv_prefix_rows(int32_t rows) { return rows <= 16 ? 16 : rows <= 32 ? 32 : 64; }
-int tkv_launch_prefix(const tkv_desc *, const void *, const uint8_t *, const void *, const tkv_prefix *, int32_t, int32_t, int32_t, int32_t, float, void *,
-                      int32_t *, void *) { return TKV_OK; }
-int tkv_launch_merge_shared(const int32_t *, int32_t, int32_t, int32_t, int32_t, void *, const void *, const void *, void *) { return TKV_OK; }
+int32_t tkv_prefix_rows(int32_t rows) { return rows <= 16 ? 16 : rows <= 64 ? 64 : 128; }
+int tkv_launch_shared(const tkv_desc *, const void *, const uint8_t *, const void *, const int32_t *, const int32_t *, const int32_t *, const int32_t *,
+                      const int32_t *, int32_t, const tkv_prefix *, const int32_t *, int32_t, int32_t, int32_t, float, void *, void *, int32_t *,
+                      void *) { return TKV_OK; }
 
 #define CHECK(x) do { if (!(x)) { std::printf("FAILED line %d: %s\n", __LINE__, #x); return 1; } } while (0)
 

@@ -137,11 +137,8 @@ def test_queries_of_very_different_size():
         out = cache.decode_shared(harness.bf16_tensor(bits, DEV))
         torch.cuda.synchronize()
         assert int(cache.status.item()) == 0
-        # the own tokens' kernel takes no sums of q over a group of channels beyond 65504: NaN in that head (its header says so)
-        sums = np.abs(wl.bf16_bits_to_f32(bits)[0].astype(np.float64).reshape(8, 4, 32).sum(-1)).max(-1)
-        assert (sums > 65504).all() and torch.isnan(out[0]).all()
         ref, tol = reference(bits, Ks, Vs, [[0, 1, 2, 3]], 2)
-        check(out[1:], (ref[1:], tol[1:]), "scaled")
+        check(out, (ref, tol), "scaled")
     finally:
         cache.close()
 
@@ -166,7 +163,6 @@ def test_a_query_head_of_nan_or_infinities_leaves_the_others():
         for b, h in ((0, 1), (1, 4), (2, 7)):
             same[b, h] = False
             assert torch.isnan(out[b, h]).all(), (b, h)
-        # (the own tokens' kernel rounds the other heads of a kv head against the largest finite one: unchanged here)
         assert torch.equal(out[same], clean[same])
     finally:
         cache.close()

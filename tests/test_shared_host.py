@@ -26,8 +26,8 @@ def test_items_cover_the_pages_and_slots_are_the_sequences(seed):
     p = plan(batch, 4 * r, n2, n4, groups, target, n_own)
     pages = -(-n2 // 64) + -(-n4 // 64)
     rows = max([len(g) for g in groups], default=0) * r
-    tile = 16 if rows <= 16 else 32 if rows <= 32 else 64
-    most, per_group = target * {16: 3, 32: 2, 64: 1}[tile], []
+    tile = next((x for x in (16, 64) if rows <= x), 128)
+    unit, per_group = 8 if tile == 16 else 4, []
     launched = 0
     for g in range(n):
         items = p.prefix_items[p.prefix_items[:, 0] == g]
@@ -38,10 +38,10 @@ def test_items_cover_the_pages_and_slots_are_the_sequences(seed):
             continue
         assert items[0, 1] == 0 and items[-1, 2] == pages[g] and np.array_equal(items[1:, 1], items[:-1, 2]) and np.all(items[:, 2] > items[:, 1])
         assert np.array_equal(items[:, 3], np.arange(len(items)))
-        quads = -(-(items[:, 2] - items[:, 1]) // 4)
-        assert quads.max() - quads.min() <= 1 and np.all(items[:-1, 2] % 4 == 0)
+        units = -(-(items[:, 2] - items[:, 1]) // unit)
+        assert units.max() - units.min() <= 1 and np.all(items[:-1, 2] % unit == 0)
     fewest = sum(4 * -(-len(groups[g]) * r // tile) for g in range(n) if per_group[g])
-    assert launched <= max(most, fewest)
+    assert launched <= max(target, fewest)
     # slots of a sequence: one of each item of each of its groups, all different, side by side, behind the own ones
     indptr = p.seq_item_indptr[batch + 1:]
     assert indptr[0] == n_own and indptr[-1] == p.n_slots and p.max_members == max([len(g) for g in groups], default=0)
@@ -72,7 +72,7 @@ def raw(**kw):
 @pytest.mark.parametrize("kw,status", [
     (dict(desc=tkv.tkv_desc.make(0, 1, 1)), tkv.TKV_ERR_BAD_SHAPE), (dict(batch=-1), tkv.TKV_ERR_INVALID_ARG), (dict(n=-1), tkv.TKV_ERR_INVALID_ARG),
     (dict(heads=0), tkv.TKV_ERR_INVALID_ARG), (dict(heads=6), tkv.TKV_ERR_BAD_SHAPE), (dict(heads=12), tkv.TKV_ERR_BAD_SHAPE), (dict(heads=64), tkv.TKV_ERR_BAD_SHAPE),
-    (dict(target=0), tkv.TKV_ERR_INVALID_ARG), (dict(target=1 << 30), tkv.TKV_ERR_INVALID_ARG), (dict(own=-1), tkv.TKV_ERR_INVALID_ARG),
+    (dict(target=0), tkv.TKV_ERR_INVALID_ARG), (dict(target=(1 << 31) - 1), tkv.TKV_ERR_INVALID_ARG), (dict(own=-1), tkv.TKV_ERR_INVALID_ARG),
     (dict(n2=[-1]), tkv.TKV_ERR_INVALID_ARG), (dict(n4=None), tkv.TKV_ERR_INVALID_ARG), (dict(indptr=[1, 2]), tkv.TKV_ERR_INVALID_ARG),
     (dict(indptr=[0, -1]), tkv.TKV_ERR_INVALID_ARG), (dict(seqs=[0, 3]), tkv.TKV_ERR_INVALID_ARG), (dict(seqs=[-1, 2]), tkv.TKV_ERR_INVALID_ARG),
     (dict(seqs=[2, 2]), tkv.TKV_ERR_INVALID_ARG),                                      # a sequence twice in a group would count the prefix twice
