@@ -172,7 +172,7 @@ int32_t tkv_plan_decode_shared(const tkv_desc *desc, int32_t batch, int32_t n_q_
                 seen[(size_t)b] = g;
             }
         const int32_t rows = tkv_prefix_rows(largest * r);
-        const int64_t target = target_cus, unit = rows == 16 ? 8 : 4;
+        const int64_t target = target_cus, unit = rows == 16 ? 8 : 2;
         auto units = [&](int32_t g) -> int64_t {
             if (member_indptr[g + 1] == member_indptr[g]) return 0;
             const int64_t pages = ((int64_t)n_tok_int2[g] + kPageTokens - 1) / kPageTokens + ((int64_t)n_tok_int4[g] + kPageTokens - 1) / kPageTokens;

@@ -141,14 +141,16 @@ template <int NT> struct Rows {   // NT tiles of 16 query rows
     float shift[NT];       // kPExp less the reference, or less 0 for -inf
     float kappa[NT];       // of row lane % 16
     bool huge;             // whether some row's reference is so large that rounding it moves a weight by more than 2^-4
+    bool look;             // that, or some row has no reference yet
 };
 template <int NT> __device__ __forceinline__ void clear(Rows<NT> &rows)
 {
     rows.huge = false;
+    rows.look = true;
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
         rows.m[n] = -INFINITY;
-        rows.shift[n] = INFINITY;   // any logit moves the reference
+        rows.shift[n] = (float)kPExp;
         rows.sum[n] = floatx4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int c = 0; c < 8; ++c) rows.acc[n][c] = floatx4{0.f, 0.f, 0.f, 0.f};
@@ -230,7 +232,7 @@ template <int NT> __device__ __forceinline__ void weigh(Rows<NT> &rows, floatx4 
                 for (int i = 0; i < 4; ++i) S[n][e][i] = 16 * e + 4 * q4 + i < n_valid ? S[n][e][i] : -INFINITY;
     }
     float mx[NT], factor[NT], shift[NT];
-    bool move = rows.huge;
+    bool move = rows.look;
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
         mx[n] = S[n][0][0];
@@ -242,6 +244,7 @@ template <int NT> __device__ __forceinline__ void weigh(Rows<NT> &rows, floatx4 
         move = move || mx[n] * factor[n] + shift[n] > kTau + (float)kPExp;
     }
     if (__any(move)) {
+        bool none = false;
 #pragma unroll
         for (int n = 0; n < NT; ++n) {
             float top = fmaxf(mx[n], __shfl_xor(mx[n], 16));
@@ -250,6 +253,7 @@ template <int NT> __device__ __forceinline__ void weigh(Rows<NT> &rows, floatx4 
             const float alpha = m_new == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(old - m_new);
             rows.m[n] = m_new;
             rows.huge = rows.huge || __any(fabsf(m_new) > 0x1p20f && m_new != -INFINITY);
+            none = none || m_new == -INFINITY;
             const float ref = m_new == -INFINITY ? 0.0f : m_new;
             rows.shift[n] = shift[n] = (float)kPExp - ref;
             floatx4 av;
@@ -259,6 +263,7 @@ template <int NT> __device__ __forceinline__ void weigh(Rows<NT> &rows, floatx4 
             for (int c = 0; c < 8; ++c) rows.acc[n][c] *= av;
             rows.sum[n] *= av;
         }
+        rows.look = rows.huge || __any(none);
         if (rows.huge) {
             // factor * logit with one rounding, as the reference has it, then the difference: the largest weight is 2^8
 #pragma unroll
@@ -289,9 +294,10 @@ __device__ __forceinline__ half8 ones() { return as_half8(0x3c003c00u, 0x3c003c0
 // ---- the pages of a list, 64 at a time in registers: lane l holds page number base + l ------------------------------------
 struct PageList {
     int base;
-    uint32_t at;   // where the record starts in the pool, in units of kUnit
+    uint32_t at;   // where the record starts in the pool, in units of kUnit; kNowhere: it cannot be read
     int valid;     // tokens of the page that count
 };
+constexpr uint32_t kNowhere = 0xffffffffu;
 constexpr int kUnitLog2 = 11;   // record and arena sizes are multiples of it
 static_assert(Rec<2>::kBytes % (1 << kUnitLog2) == 0 && Rec<4>::kBytes % (1 << kUnitLog2) == 0, "record unit");
 struct ListCtx {
@@ -314,10 +320,11 @@ __device__ __forceinline__ void fetch_list(const ListCtx &cx, PageList &l, int b
     const int lo = is2 ? 0 : cx.n_pages_int2, hi = is2 ? cx.n_pages_int2 : cx.n_pages_total;
     const bool ok = page >= lo && page < hi;
     if (!ok && cx.status) atomicOr(cx.status, page < 0 || page >= cx.n_pages_total ? TKV_STATUS_PAGE_RANGE : TKV_STATUS_BITMAP_MISMATCH);
-    // a page that cannot be read counts no tokens, and nothing is read in its place (the record's size is 0, see record_of)
+    // a page that cannot be read counts no tokens, and nothing is read in its place (the record's size is 0, see record_of); one that
+    // was never written is read, and counts none either: its request does not wait for bit_map
     const uint32_t rec = (uint32_t)(is2 ? page : page - cx.n_pages_int2) * (uint32_t)cx.n_kv_heads + (uint32_t)cx.kvh;
     constexpr uint32_t kUnits2 = Rec<2>::kBytes >> kUnitLog2, kUnits4 = Rec<4>::kBytes >> kUnitLog2;
-    l.at = !ok ? 0 : (is2 ? rec * kUnits2 : (uint32_t)cx.n_pages_int2 * (uint32_t)cx.n_kv_heads * kUnits2 + rec * kUnits4);   // (pools below 8 TB: 32 bits)
+    l.at = !ok ? kNowhere : (is2 ? rec * kUnits2 : (uint32_t)cx.n_pages_int2 * (uint32_t)cx.n_kv_heads * kUnits2 + rec * kUnits4);   // (pools below 8 TB: 32 bits)
     const bool written = ok && cx.bit_map[ok ? page : 0] == (is2 ? 2 : 4);
     if (ok && !written && cx.status) atomicOr(cx.status, TKV_STATUS_BITMAP_MISMATCH);
     l.valid = !written ? 0 : (pos == cx.np2 - 1 ? cx.last2 : pos == cx.np2 + cx.np4 - 1 ? cx.last4 : kPageTokens);
@@ -325,9 +332,10 @@ __device__ __forceinline__ void fetch_list(const ListCtx &cx, PageList &l, int b
 __device__ __forceinline__ int valid_of(const PageList &l, int i) { return __builtin_amdgcn_readlane(l.valid, i - l.base); }
 __device__ __forceinline__ Record record_of(const ListCtx &cx, const PageList &l, int i, bool wanted)
 {
-    const uint64_t at = (uint32_t)__builtin_amdgcn_readlane((int)l.at, i - l.base);
+    const uint32_t at = (uint32_t)__builtin_amdgcn_readlane((int)l.at, i - l.base);
+    const bool there = wanted && at != kNowhere;
     const int bytes = cx.is2(i) ? Rec<2>::kBytes : Rec<4>::kBytes;
-    return __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t *>(cx.pool) + (at << kUnitLog2), 0, wanted && valid_of(l, i) > 0 ? bytes : 0, 0x00027000);
+    return __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t *>(cx.pool) + ((uint64_t)(there ? at : 0) << kUnitLog2), 0, there ? bytes : 0, 0x00027000);
 }
 
 // ---- few rows: a wavefront works on pages of its own -------------------------------------------------------------------
@@ -442,11 +450,9 @@ __device__ __forceinline__ void run_pages(const ListCtx &cx, PageList &list, int
         load_v(r, rec, cx.lane);
     }
 }
-template <int NT, bool KC> __device__ __forceinline__ void run_list(const ListCtx &cx, Rows<NT> &rows, Meta &meta)
+template <int NT, bool KC> __device__ __forceinline__ void run_list(const ListCtx &cx, PageList &list, Rows<NT> &rows, Meta &meta)
 {
     if (cx.n <= 0) return;
-    PageList list;
-    fetch_list(cx, list, 0);
     int n2 = cx.first < cx.np2 ? (cx.np2 - cx.first + cx.step - 1) / cx.step : 0;   // INT2 pages: they come first
     n2 = n2 < cx.n ? n2 : cx.n;
     if (n2 > 0) run_pages<NT, 2, KC>(cx, list, 0, n2, rows, meta);
@@ -517,24 +523,36 @@ template <int BITS, bool KC> __device__ __forceinline__ void expand(RawPage &r, 
     for (int c = 0; c < 4; ++c)
         o.v[b * 8 + 4 * (rw & 1) + c][lane] = __builtin_bit_cast(uint4, v_operand<BITS>(word_of(r.vw, c), b, r.vs[c >> 1], r.vz[c >> 1], mg));
 }
-// The logits of a page, what `between` does, and the rest.
+// The logits of a page, what `between` does, and the rest.  Operands are asked for eight MFMAs ahead of the first that takes them, those
+// of V ahead of the exponentials: left to the compiler's order, each read stood right in front of its MFMAs.
 template <int NT, class Between> __device__ __forceinline__ void attend_operands(const Operands &o, int n_valid, int lane, Rows<NT> &rows, Between between)
 {
     const int q4 = lane >> 4;
+    auto k_at = [&](int g, int e) { return __builtin_bit_cast(half8, o.k[e * 4 + g][lane]); };
+    auto v_at = [&](int b, int c) { return __builtin_bit_cast(half8, o.v[b * 8 + c][lane]); };
     floatx4 S[NT][4];
+    half8 A[2][4];
 #pragma unroll
-    for (int n = 0; n < NT; ++n)
+    for (int g = 0; g < 2; ++g)
 #pragma unroll
-        for (int e = 0; e < 4; ++e) S[n][e] = floatx4{0.f, 0.f, 0.f, 0.f};
+        for (int e = 0; e < 4; ++e) A[g][e] = k_at(g, e);
 #pragma unroll
-    for (int g = 0; g < 4; ++g)
+    for (int g = 0; g < 4; ++g) {
+        __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            const half8 A = __builtin_bit_cast(half8, o.k[e * 4 + g][lane]);
+        for (int e = 0; e < 4; ++e)
 #pragma unroll
-            for (int n = 0; n < NT; ++n) S[n][e] = mfma(A, rows.q[n][g], S[n][e]);
-        }
+            for (int n = 0; n < NT; ++n) S[n][e] = mfma(A[g & 1][e], rows.q[n][g], g == 0 ? floatx4{0.f, 0.f, 0.f, 0.f} : S[n][e]);
+        __builtin_amdgcn_sched_barrier(0);
+        if (g < 2)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) A[g & 1][e] = k_at(g + 2, e);
+    }
     between();
+    half8 B[8];
+#pragma unroll
+    for (int c = 0; c < 8; ++c) B[c] = v_at(0, c);
+    __builtin_amdgcn_sched_barrier(0);
     half8 P[NT][2];
     weigh(rows, S, n_valid, q4, P);
 #pragma unroll
@@ -543,9 +561,13 @@ template <int NT, class Between> __device__ __forceinline__ void attend_operands
         for (int n = 0; n < NT; ++n) rows.sum[n] = mfma(P[n][b], ones(), rows.sum[n]);
 #pragma unroll
         for (int c = 0; c < 8; ++c) {
-            const half8 B = __builtin_bit_cast(half8, o.v[b * 8 + c][lane]);
 #pragma unroll
-            for (int n = 0; n < NT; ++n) rows.acc[n][c] = mfma(P[n][b], B, rows.acc[n][c]);
+            for (int n = 0; n < NT; ++n) rows.acc[n][c] = mfma(P[n][b], B[c], rows.acc[n][c]);
+            if (b == 0) {
+                __builtin_amdgcn_sched_barrier(0);
+                B[c] = v_at(1, c);
+                __builtin_amdgcn_sched_barrier(0);
+            }
         }
     }
 }
@@ -561,31 +583,37 @@ __device__ __forceinline__ void run_tiles(const ListCtx &cx, PageList &list, int
     const Magic mg;
     RawPage raw;
     int valid = 0, valid_next = 0;   // tokens of this step's page and of the next one's; 0: none
+    // (behind the last page an empty record: zeros, without a branch around the loads)
     auto request = [&](int i) -> int {
-        if (i >= end) return 0;
-        if (i - list.base >= 64) fetch_list(cx, list, i);
-        const int v = valid_of(list, i);
-        load_raw<BITS, KC>(raw, record_of(cx, list, i, true), rw, lane);
-        return v;
+        const bool wanted = i < end;
+        const int k = wanted ? i : end - 1;
+        if (k - list.base >= 64) fetch_list(cx, list, k);
+        load_raw<BITS, KC>(raw, record_of(cx, list, k, wanted), rw, lane);
+        return wanted ? valid_of(list, k) : 0;
     };
     int i = i0 + th;
     valid = request(i);
-    if (valid > 0) expand<BITS, KC>(raw, valid, rw, lane, lds.page[0][th], lds.stage[wave], mg);
+    expand<BITS, KC>(raw, valid, rw, lane, lds.page[0][th], lds.stage[wave], mg);
     valid_next = request(i + 2);
     __syncthreads();
-    for (int step = 0, n = (end - i0 + 1) / 2; step < n; ++step, i += 2) {
-        Operands &now = lds.page[step & 1][th], &next = lds.page[(step + 1) & 1][th];
-        int valid_after = 0;
-        auto prepare_next = [&]() {
-            if (valid_next > 0) expand<BITS, KC>(raw, valid_next, rw, lane, next, lds.stage[wave], mg);
-            valid_after = request(i + 4);
-        };
-        if (active && valid > 0) attend_operands<NT>(now, valid, lane, rows, prepare_next);
-        else prepare_next();
-        __syncthreads();   // this step's pages are read, the next ones stand there
-        valid = valid_next;
-        valid_next = valid_after;
-    }
+    // (two loops: with wavefronts with and without rows in one, the registers of either wait for the other's loads)
+    auto steps = [&](auto rows_here) {
+        for (int step = 0, n = (end - i0 + 1) / 2; step < n; ++step, i += 2) {
+            Operands &now = lds.page[step & 1][th], &next = lds.page[(step + 1) & 1][th];
+            int valid_after = 0;
+            auto prepare_next = [&]() {
+                expand<BITS, KC>(raw, valid_next, rw, lane, next, lds.stage[wave], mg);
+                valid_after = request(i + 4);
+            };
+            if constexpr (decltype(rows_here)::value) attend_operands<NT>(now, valid, lane, rows, prepare_next);
+            else prepare_next();
+            __syncthreads();   // this step's pages are read, the next ones stand there
+            valid = valid_next;
+            valid_next = valid_after;
+        }
+    };
+    if (active) steps(std::true_type());
+    else steps(std::false_type());
 }
 
 // ---- work items ----------------------------------------------------------------------------------------------------------
@@ -598,6 +626,7 @@ template <int SETS, int ROWS> struct Results {   // of SETS wavefronts for the s
     float m[SETS][ROWS], sum[SETS][ROWS];
 };
 template <int MODE> struct Shared {
+    int64_t dest[rows_of(MODE)];   // row of each query row's partial, or -1
     static constexpr int kSets = MODE == 0 ? kWaves : 2;
     union {
         Meta meta[kWaves];
@@ -631,10 +660,12 @@ template <bool KC, class L> __device__ __forceinline__ void own_item(const Share
     Rows<1> rows;
     clear(rows);
     if (seq_ok && pb < pe) {
-        load_q(rows, 0, a.q + ((size_t)sq * n_q_heads + kvh * R + (r16 & (R - 1))) * kHeadDim, a.kappa, lane);
         const ListCtx cx = {a.pool, a.bit_map, a.page_ids + list0, pb, 1, pe - pb, np2, np4, n2 - (np2 - 1) * kPageTokens, n4 - (np4 - 1) * kPageTokens,
                             kvh, a.n_kv_heads, a.n_pages_int2, a.n_pages_int2 + a.n_pages_int4, lane, a.status};
-        run_list<1, KC>(cx, rows, lds.own[wave].meta);
+        PageList list;
+        fetch_list(cx, list, 0);
+        load_q(rows, 0, a.q + ((size_t)sq * n_q_heads + kvh * R + (r16 & (R - 1))) * kHeadDim, a.kappa, lane);
+        run_list<1, KC>(cx, list, rows, lds.own[wave].meta);
     }
     const size_t at = (size_t)slot * n_q_heads + kvh * R;
     if (q4 == 0 && r16 < R) a.ml_ws[0][2 * (at + r16)] = rows.m[0];
@@ -681,6 +712,26 @@ template <int MODE, bool KC> __device__ __forceinline__ void prefix_item(const S
     const int np = np2 + np4 < list1 - list0 ? np2 + np4 : list1 - list0;
     const int pb = item_pb > 0 ? item_pb : 0, pe = item_pe < np ? item_pe : np;
 
+    const int first = MODE == 0 ? pb + wave : pb, step = MODE == 0 ? kWaves : 1;
+    const ListCtx cx = {a.pool, a.bit_map, a.p.page_ids + list0, first, step, first < pe ? (pe - first + step - 1) / step : 0, np2, np4,
+                        n2 - (np2 - 1) * kPageTokens, n4 - (np4 - 1) * kPageTokens,
+                        kvh, a.n_kv_heads, a.n_pages_int2, a.n_pages_int2 + a.n_pages_int4, lane, a.status};
+    PageList list = {0, kNowhere, 0};
+    if (cx.n > 0) fetch_list(cx, list, 0);
+    // where the rows' partials go, while the pages' ids are under way
+    if (threadIdx.x < ROWS) {
+        const int row = row0 + threadIdx.x;
+        int64_t dest = -1;
+        if (row < n_rows) {
+            const int member = m0 + (row >> a.log2_r), seq = a.p.member_seqs[member];
+            const int64_t slot = (int64_t)a.p.member_slots[member] + part;
+            if (seq >= 0 && seq < a.batch && slot >= a.n_items && slot < a.n_slots)
+                dest = (slot - a.n_items) * n_q_heads + kvh * R + (row & (R - 1));
+            else if (a.status)
+                atomicOr(a.status, TKV_STATUS_BAD_ITEM);
+        }
+        lds.dest[threadIdx.x] = dest;
+    }
     const int wave_row = MODE == 0 ? 0 : (wave & 3) * 16 * NT;   // this wavefront's first row of the workgroup
     const bool active = row0 + wave_row < n_rows;
     Rows<NT> rows;
@@ -694,15 +745,9 @@ template <int MODE, bool KC> __device__ __forceinline__ void prefix_item(const S
             load_q(rows, n, a.q + ((size_t)seq * n_q_heads + kvh * R + (row & (R - 1))) * kHeadDim, a.kappa, lane);
         }
     }
-    const int first = MODE == 0 ? pb + wave : pb, step = MODE == 0 ? kWaves : 1;
-    const ListCtx cx = {a.pool, a.bit_map, a.p.page_ids + list0, first, step, first < pe ? (pe - first + step - 1) / step : 0, np2, np4,
-                        n2 - (np2 - 1) * kPageTokens, n4 - (np4 - 1) * kPageTokens,
-                        kvh, a.n_kv_heads, a.n_pages_int2, a.n_pages_int2 + a.n_pages_int4, lane, a.status};
     if constexpr (MODE == 0) {
-        run_list<NT, KC>(cx, rows, lds.meta[wave]);
+        run_list<NT, KC>(cx, list, rows, lds.meta[wave]);
     } else if (cx.n > 0) {
-        PageList list;
-        fetch_list(cx, list, 0);
         int n2 = first < np2 ? np2 - first : 0;   // INT2 pages: they come first
         n2 = n2 < cx.n ? n2 : cx.n;
         if (n2 > 0) run_tiles<NT, 2, KC>(cx, list, 0, n2, active, wave, rows, lds.tile);
@@ -727,32 +772,26 @@ template <int MODE, bool KC> __device__ __forceinline__ void prefix_item(const S
     }
     __syncthreads();
     const int c4 = threadIdx.x & 31;   // 32 lanes store a row
-#pragma unroll 2
-    for (int r = threadIdx.x >> 5; r < ROWS; r += 2 * kWaves) {
-        const int row = row0 + r;
-        if (row >= n_rows) break;
-        const int member = m0 + (row >> a.log2_r), seq = a.p.member_seqs[member];
-        const int64_t slot = (int64_t)a.p.member_slots[member] + part;
-        if (seq < 0 || seq >= a.batch || slot < a.n_items || slot >= a.n_slots) {
-            if (a.status) atomicOr(a.status, TKV_STATUS_BAD_ITEM);
-            continue;
-        }
+#pragma unroll
+    for (int k = 0; k < (ROWS + 2 * kWaves - 1) / (2 * kWaves); ++k) {
+        const int r = 2 * kWaves * k + (threadIdx.x >> 5);
+        const int64_t at = lds.dest[r];
+        if (at < 0) continue;
         float top = lds.out.m[0][r];
 #pragma unroll
-        for (int k = 1; k < SETS; ++k) top = fmaxf(top, lds.out.m[k][r]);
+        for (int i = 1; i < SETS; ++i) top = fmaxf(top, lds.out.m[i][r]);
         float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
         float sum = 0.0f;
 #pragma unroll
-        for (int k = 0; k < SETS; ++k) {
-            const float m = lds.out.m[k][r], w = m == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(m - top);
-            const float4 t = *reinterpret_cast<const float4 *>(&lds.out.acc[k][r][4 * c4]);
+        for (int i = 0; i < SETS; ++i) {
+            const float m = lds.out.m[i][r], w = m == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(m - top);
+            const float4 t = *reinterpret_cast<const float4 *>(&lds.out.acc[i][r][4 * c4]);
             v.x = fmaf(w, t.x, v.x);
             v.y = fmaf(w, t.y, v.y);
             v.z = fmaf(w, t.z, v.z);
             v.w = fmaf(w, t.w, v.w);
-            sum = fmaf(w, lds.out.sum[k][r], sum);
+            sum = fmaf(w, lds.out.sum[i][r], sum);
         }
-        const size_t at = (size_t)(slot - a.n_items) * n_q_heads + kvh * R + (row & (R - 1));
         reinterpret_cast<float4 *>(a.acc_ws[1] + at * kHeadDim)[c4] = v;
         if (c4 == 0) reinterpret_cast<float2 *>(a.ml_ws[1])[at] = make_float2(top, sum);
     }

@@ -27,7 +27,7 @@ def test_items_cover_the_pages_and_slots_are_the_sequences(seed):
     pages = -(-n2 // 64) + -(-n4 // 64)
     rows = max([len(g) for g in groups], default=0) * r
     tile = next((x for x in (16, 64) if rows <= x), 128)
-    unit, per_group = 8 if tile == 16 else 4, []
+    unit, per_group = 8 if tile == 16 else 2, []
     launched = 0
     for g in range(n):
         items = p.prefix_items[p.prefix_items[:, 0] == g]
