@@ -451,6 +451,7 @@ int tkv_decode_attention_static(const tkv_desc *desc, const void *pool, const ui
  * several prefixes need none.
  *   n_groups, n_members   groups; entries of member_seqs
  *   max_members           members of the largest group, at least (rows of the launch)
+ *   tile_rows             query rows of a workgroup, 16, 64 or 128, as tkv_plan_decode_shared chooses them (any gives the same attention)
  *   n_items               prefix work items
  *   page_indptr  device i32[n_groups+1] page-list offsets of the groups
  *   page_ids     device i32: per group INT2 pages, then INT4 pages, of the same pool as the sequences' own
@@ -459,7 +460,7 @@ int tkv_decode_attention_static(const tkv_desc *desc, const void *pool, const ui
  *   member_slots device i32[n_members], items device i32[4*n_items]: as written by tkv_plan_decode_shared
  */
 typedef struct tkv_prefix {
-    int32_t n_groups, n_members, max_members, n_items;
+    int32_t n_groups, n_members, max_members, tile_rows, n_items;
     const int32_t *page_indptr;
     const int32_t *page_ids;
     const int32_t *n_tok_int2;
@@ -475,11 +476,14 @@ int32_t tkv_plan_shared_capacity(int32_t n_groups, int32_t target_cus);
 /*
  * Cuts the groups' page lists into work items and gives every (item, member) a
  * partial slot behind the n_own_items slots of the sequences' own items
- * (tkv_plan_decode).  An item is read by one workgroup per kv head and 64 rows
- * (16 or 32 if no group has more; a row is one query head of one member), whose
- * four wavefronts take its pages in turn: items are equal parts of whole fours
- * of pages, as small as still gives no more workgroups than target_cus compute
- * units hold at once (one of 64 rows each, two of 32, three of 16).  Depends on the page counts and members only.
+ * (tkv_plan_decode).  An item is read by one workgroup per kv head and tile_rows
+ * rows (a row is one query head of one member); with 16 rows its eight
+ * wavefronts work on a page each at a time, with 64 and 128 on two pages
+ * together.  The number of rows is the one that is expected to take least time,
+ * and items are equal parts of whole steps, as small as still gives no more
+ * workgroups than target_cus compute units, less those that the own items take
+ * (or none, where these are few beside the prefixes).  Depends on the page
+ * counts and members only, and ages as a decode plan does.
  *   n_tok_int2/4   host i32[n_groups]
  *   member_indptr  host i32[n_groups+1], from 0; member_seqs host i32[member_indptr[n_groups]],
  *                  below batch, each at most once in a group
@@ -487,20 +491,20 @@ int32_t tkv_plan_shared_capacity(int32_t n_groups, int32_t target_cus);
  *   items_out      host i32[4*capacity]: {group, first page, end page, number in the group}
  *   member_slots_out  host i32[members]: slot of the member's partial of the group's first item, the others follow
  *   seq_slot_indptr_out  host i32[batch+1]: slots of each sequence, from n_own_items on
+ *   tile_rows_out  host i32
  * Returns the number of items (>= 0) or a negative status.
  */
 int32_t tkv_plan_decode_shared(const tkv_desc *desc, int32_t batch, int32_t n_q_heads, int32_t n_groups,
                                const int32_t *n_tok_int2, const int32_t *n_tok_int4,
                                const int32_t *member_indptr, const int32_t *member_seqs, int32_t target_cus,
                                int32_t n_own_items, int32_t *items_out, int32_t capacity,
-                               int32_t *member_slots_out, int32_t *seq_slot_indptr_out);
+                               int32_t *member_slots_out, int32_t *seq_slot_indptr_out, int32_t *tile_rows_out);
 /*
  * tkv_decode_attention over each sequence's prefixes and its own tokens
- * together.  The prefix's pages are dequantised to fp16 as tkv_gather_dequant
- * does (the values that a prefill over the prefix saw) and attended to with
- * fp16 softmax weights and 32-bit sums; own tokens as in tkv_decode_split.  The
- * output is bf16, as the projection behind it takes it.  A sequence without
- * tokens gives zeros.
+ * together.  Pages are dequantised to fp16 as tkv_gather_dequant does (the
+ * values that a prefill over them saw) and attended to with fp16 softmax
+ * weights and 32-bit sums.  The output is bf16, as the projection behind it
+ * takes it.  A sequence without tokens gives zeros.
  *   q, page_indptr .. n_items, sm_scale   as for tkv_decode_attention (own tokens; n_items may be 0)
  *   prefix         host struct of device arrays, above; n_items may be 0
  *   slot_indptr    device i32[2*(batch+1)]: seq_item_indptr_out of tkv_plan_decode, then seq_slot_indptr_out
@@ -510,9 +514,11 @@ int32_t tkv_plan_decode_shared(const tkv_desc *desc, int32_t batch, int32_t n_q_
  *   status         device i32, may be NULL; bits as for tkv_decode_attention.  Members outside the batch, slots outside
  *                  [n_items, n_slots) and groups with more members than max_members raise TKV_STATUS_BAD_ITEM: what they
  *                  name is not stored, and the sequence reads what the workspace held before
- * Preconditions on cache and q as for tkv_decode_attention; NaN and infinities
- * in a query head leave the others alone.  n_q_heads / n_kv_heads is 1, 2, 4 or
- * 8; at most 65535 prefix items.  Up to three launches on `stream`.
+ * Preconditions: stored scales and zeros finite, and values within fp16; with
+ * TKV_KEYS_PER_CHANNEL every n_tok_int2 a multiple of 32.  q may hold any
+ * finite values; a query head of NaN or infinities gives NaN and leaves the
+ * others alone.  n_q_heads / n_kv_heads is 1, 2, 4 or 8; at most 65535 prefix
+ * items.  Two launches on `stream`: attention, then the merge.
  */
 int tkv_decode_attention_shared(const tkv_desc *desc, const void *pool, const uint8_t *bit_map, const void *q,
                                 const int32_t *page_indptr, const int32_t *page_ids,

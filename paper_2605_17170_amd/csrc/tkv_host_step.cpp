@@ -141,10 +141,11 @@ int32_t tkv_plan_shared_capacity(int32_t n_groups, int32_t target_cus)
 
 int32_t tkv_plan_decode_shared(const tkv_desc *desc, int32_t batch, int32_t n_q_heads, int32_t n_groups, const int32_t *n_tok_int2,
                                const int32_t *n_tok_int4, const int32_t *member_indptr, const int32_t *member_seqs, int32_t target_cus,
-                               int32_t n_own_items, int32_t *items_out, int32_t capacity, int32_t *member_slots_out, int32_t *seq_slot_indptr_out)
+                               int32_t n_own_items, int32_t *items_out, int32_t capacity, int32_t *member_slots_out, int32_t *seq_slot_indptr_out,
+                               int32_t *tile_rows_out)
 {
     if (int st = tkv_desc_status(desc)) return st;
-    if (batch < 0 || n_groups < 0 || n_own_items < 0 || capacity < 0 || n_q_heads <= 0 || !seq_slot_indptr_out || !member_indptr) return TKV_ERR_INVALID_ARG;
+    if (batch < 0 || n_groups < 0 || n_own_items < 0 || capacity < 0 || n_q_heads <= 0 || !seq_slot_indptr_out || !tile_rows_out || !member_indptr) return TKV_ERR_INVALID_ARG;
     if (tkv_plan_shared_capacity(n_groups, target_cus) < 0) return TKV_ERR_INVALID_ARG;
     if (n_groups > 0 && (!n_tok_int2 || !n_tok_int4)) return TKV_ERR_INVALID_ARG;
     if (n_q_heads % desc->n_kv_heads) return TKV_ERR_BAD_SHAPE;
@@ -171,13 +172,35 @@ int32_t tkv_plan_decode_shared(const tkv_desc *desc, int32_t batch, int32_t n_q_
                 if (b < 0 || b >= batch || seen[(size_t)b] == g) return TKV_ERR_INVALID_ARG;
                 seen[(size_t)b] = g;
             }
-        const int32_t rows = tkv_prefix_rows(largest * r);
-        const int64_t target = target_cus, unit = rows == 16 ? 8 : 2;
-        auto units = [&](int32_t g) -> int64_t {
-            if (member_indptr[g + 1] == member_indptr[g]) return 0;
-            const int64_t pages = ((int64_t)n_tok_int2[g] + kPageTokens - 1) / kPageTokens + ((int64_t)n_tok_int4[g] + kPageTokens - 1) / kPageTokens;
-            return (pages + unit - 1) / unit;
-        };
+        // The own items' workgroups (a wavefront for each item and kv head) are launched first.  Either the prefixes' fill the compute units
+        // that are left, or all, and begin behind them.
+        const int64_t own = std::min(((int64_t)n_own_items * desc->n_kv_heads + 7) / 8, (int64_t)target_cus), spare = target_cus - own;
+        auto pages = [&](int32_t g) { return ((int64_t)n_tok_int2[g] + kPageTokens - 1) / kPageTokens + ((int64_t)n_tok_int4[g] + kPageTokens - 1) / kPageTokens; };
+        // Rows of a workgroup.  With 16 its wavefronts work on a page each, eight a step; with 64 and 128 they expand pages together, two
+        // a step.  us, 16 / 64 / 128 rows: 32 rows over 32000 tokens, 8 kv heads 21 / 26 / 33; 64 over 4000 12 / 16 / 18, 11000 18.0 / 18.4 / 21.6,
+        // 32000 36 / 30 / 38; 128 over 1000 10 / 15 / 19, 8000 28 / 23 / 25; 256 over 1000 19 / 17 / 18, 8000 37 / 34 / 36, 32768 - / - / 61: about
+        // 3.1 us a step, 3 + 2.1 and 9 + 2.5 beside what all have in common.  (Steps of a workgroup: those of all, over the compute units.)
+        static const struct { int32_t rows, pages; double begin, step; } kinds[3] = {{16, 8, 0.0, 3.1}, {64, 2, 3.0, 2.1}, {128, 2, 9.0, 2.5}};
+        int32_t rows = 0;
+        int64_t unit = 1, target = target_cus;
+        double least = 0.0;
+        for (const auto &k : kinds) {
+            int64_t all = 0;
+            for (int32_t g = 0; g < n_groups; ++g)
+                all += (pages(g) + k.pages - 1) / k.pages * (((int64_t)(member_indptr[g + 1] - member_indptr[g]) * r + k.rows - 1) / k.rows) * desc->n_kv_heads;
+            // 6 us later, if own items come first on the same compute units
+            const double with_own = spare > 0 ? k.step * (double)((all + spare - 1) / spare) : INFINITY;
+            const double behind = k.step * (double)((all + target_cus - 1) / target_cus) + (own > 0 ? 6.0 : 0.0);
+            const double time = k.begin + std::min(with_own, behind);
+            if (rows == 0 || time < least) {
+                rows = k.rows;
+                unit = k.pages;
+                target = with_own <= behind ? spare : target_cus;
+                least = time;
+            }
+        }
+        *tile_rows_out = rows;
+        auto units = [&](int32_t g) -> int64_t { return member_indptr[g + 1] == member_indptr[g] ? 0 : (pages(g) + unit - 1) / unit; };
         auto blocks = [&](int32_t g) -> int64_t {   // workgroups of an item
             return (((int64_t)(member_indptr[g + 1] - member_indptr[g]) * r + rows - 1) / rows) * desc->n_kv_heads;
         };
@@ -197,14 +220,13 @@ int32_t tkv_plan_decode_shared(const tkv_desc *desc, int32_t batch, int32_t n_q_
         std::vector<int32_t> parts((size_t)n_groups, 0);
         for (int32_t g = 0; g < n_groups; ++g) {
             const int64_t all = units(g), n = (all + lo - 1) / lo;
-            const int64_t pages = ((int64_t)n_tok_int2[g] + kPageTokens - 1) / kPageTokens + ((int64_t)n_tok_int4[g] + kPageTokens - 1) / kPageTokens;
             parts[(size_t)g] = (int32_t)n;
             if (n_items + n > capacity) return TKV_ERR_CAPACITY;
             for (int64_t k = 0; k < n; ++k) {
                 int32_t *it = items_out + 4 * n_items++;
                 it[0] = g;
                 it[1] = (int32_t)(unit * (all * k / n));
-                it[2] = (int32_t)std::min(pages, unit * (all * (k + 1) / n));
+                it[2] = (int32_t)std::min(pages(g), unit * (all * (k + 1) / n));
                 it[3] = (int32_t)k;
             }
             for (int32_t m = member_indptr[g]; m < member_indptr[g + 1]; ++m) next[(size_t)member_seqs[m]] += (int32_t)n;
@@ -252,8 +274,9 @@ int tkv_decode_attention_shared(const tkv_desc *desc, const void *pool, const ui
         if (!p.page_indptr || !p.page_ids || !p.n_tok_int2 || !p.n_tok_int4 || !p.member_indptr || !p.member_seqs || !p.member_slots || !p.items ||
             p.n_groups == 0 || p.n_members == 0 || p.max_members == 0)
             return TKV_ERR_INVALID_ARG;
+        if (p.tile_rows != 16 && p.tile_rows != 64 && p.tile_rows != 128) return TKV_ERR_INVALID_ARG;
         const int64_t rows = (int64_t)p.max_members * r;
-        if (rows > INT32_MAX / 2 || (int64_t)p.n_members * r > INT32_MAX / 2 || (rows + 63) / 64 > 65535) return TKV_ERR_INVALID_ARG;
+        if (rows > INT32_MAX / 2 || (int64_t)p.n_members * r > INT32_MAX / 2 || (rows + p.tile_rows - 1) / p.tile_rows > 65535) return TKV_ERR_INVALID_ARG;
     }
     return tkv_launch_shared(desc, pool, bit_map, q, page_indptr, page_ids, n_tok_int2, n_tok_int4, items, n_items, prefix, slot_indptr, n_slots,
                              batch, n_q_heads, sm_scale, out, workspace, status, stream);

@@ -33,7 +33,6 @@ int tkv_launch_norm_rope(const tkv_rope *rope, const void *q, int64_t q_stride, 
                          int64_t v_stride, int32_t n_tokens, int32_t n_q_heads, int32_t n_kv_heads, const int32_t *positions,
                          const void *q_weight, const void *k_weight, float eps, void *q_out, void *k_out, void *v_out, void *stream);
 
-int32_t tkv_prefix_rows(int32_t rows);   // rows of a workgroup of the prefix kernel in a launch with groups of up to so many rows
 int tkv_launch_shared(const tkv_desc *desc, const void *pool, const uint8_t *bit_map, const void *q, const int32_t *page_indptr,
                       const int32_t *page_ids, const int32_t *n_tok_int2, const int32_t *n_tok_int4, const int32_t *items, int32_t n_items,
                       const tkv_prefix *prefix, const int32_t *slot_indptr, int32_t n_slots, int32_t batch, int32_t n_q_heads, float sm_scale,

@@ -617,7 +617,8 @@ __device__ __forceinline__ void run_tiles(const ListCtx &cx, PageList &list, int
 }
 
 // ---- work items ----------------------------------------------------------------------------------------------------------
-// MODE 0: one row tile, every wavefront with pages of its own; 1, 2: MODE row tiles a wavefront, pages expanded together.
+// MODE 0: one row tile, every wavefront with pages of its own; 1, 2: MODE row tiles a wavefront, pages expanded together.  (Two row tiles
+// with pages of their own do not fit the registers of two wavefronts a SIMD.)
 constexpr int tiles_of(int mode) { return mode == 0 ? 1 : mode; }
 constexpr int rows_of(int mode) { return mode == 0 ? 16 : 64 * mode; }
 constexpr int kOutRow = kHeadDim + 4;   // floats: rows 4 q4 + i of a store fall on different banks
@@ -911,8 +912,6 @@ template <int MODE> void launch_shared(bool kc, unsigned blocks, hipStream_t s, 
 
 } // namespace
 
-int32_t tkv_prefix_rows(int32_t rows) { return rows <= 16 ? 16 : rows <= 64 ? 64 : 128; }
-
 int tkv_launch_shared(const tkv_desc *desc, const void *pool, const uint8_t *bit_map, const void *q, const int32_t *page_indptr,
                       const int32_t *page_ids, const int32_t *n_tok_int2, const int32_t *n_tok_int4, const int32_t *items, int32_t n_items,
                       const tkv_prefix *prefix, const int32_t *slot_indptr, int32_t n_slots, int32_t batch, int32_t n_q_heads, float sm_scale,
@@ -947,7 +946,7 @@ int tkv_launch_shared(const tkv_desc *desc, const void *pool, const uint8_t *bit
     }
     a.status = status;
     a.own_blocks = (int)(((int64_t)n_items * desc->n_kv_heads + kWaves - 1) / kWaves);
-    const int rows = prefix->n_items > 0 ? prefix->max_members << log2_r : 1, per = tkv_prefix_rows(rows);
+    const int rows = prefix->n_items > 0 ? prefix->max_members << log2_r : 1, per = prefix->n_items > 0 ? prefix->tile_rows : 16;
     a.row_blocks = (rows + per - 1) / per;
     const int64_t blocks = a.own_blocks + (int64_t)prefix->n_items * desc->n_kv_heads * a.row_blocks;
     if (blocks > INT32_MAX) return TKV_ERR_INVALID_ARG;

@@ -73,7 +73,7 @@ class tkv_desc(C.Structure):
 
 class tkv_prefix(C.Structure):
     """Shared prefixes of groups of sequences: device arrays; `make` keeps the tensors alive."""
-    _fields_ = [("n_groups", C.c_int32), ("n_members", C.c_int32), ("max_members", C.c_int32), ("n_items", C.c_int32),
+    _fields_ = [("n_groups", C.c_int32), ("n_members", C.c_int32), ("max_members", C.c_int32), ("tile_rows", C.c_int32), ("n_items", C.c_int32),
                 ("page_indptr", C.c_void_p), ("page_ids", C.c_void_p), ("n_tok_int2", C.c_void_p), ("n_tok_int4", C.c_void_p),
                 ("member_indptr", C.c_void_p), ("member_seqs", C.c_void_p), ("member_slots", C.c_void_p), ("items", C.c_void_p)]
 
@@ -85,7 +85,7 @@ class tkv_prefix(C.Structure):
         n = n_tok_int2.numel()
         assert all(t.element_size() == 4 for t in tensors) and n_tok_int4.numel() == n and page_indptr.numel() == member_indptr.numel() == n + 1
         assert member_seqs.numel() == member_slots.numel() and items.numel() % 4 == 0
-        prefix = cls(n, member_seqs.numel(), max_members, items.numel() // 4, *(_dev(t) for t in tensors))
+        prefix = cls(n, member_seqs.numel(), max_members, getattr(max_members, "tile_rows", 16), items.numel() // 4, *(_dev(t) for t in tensors))
         prefix.tensors = tensors
         return prefix
 
@@ -175,7 +175,7 @@ def lib():
         L.tkv_plan_shared_capacity.restype = i32
         L.tkv_plan_shared_capacity.argtypes = [i32, i32]
         L.tkv_plan_decode_shared.restype = i32
-        L.tkv_plan_decode_shared.argtypes = [dp, i32, i32, i32, vp, vp, vp, vp, i32, i32, vp, i32, vp, vp]
+        L.tkv_plan_decode_shared.argtypes = [dp, i32, i32, i32, vp, vp, vp, vp, i32, i32, vp, i32, vp, vp, C.POINTER(i32)]
         L.tkv_decode_attention_shared.argtypes = [dp, vp, vp, vp, vp, vp, vp, vp, vp, i32, C.POINTER(tkv_prefix), vp, i32, i32, i32, C.c_float,
                                                   vp, vp, sz, vp, vp]
         tp = C.POINTER(tkv_table)
@@ -555,6 +555,10 @@ def tkv_tag_counts(tags) -> np.ndarray:
 
 
 # ---------------------------------------------------------------- D8 (host plan, device)
+class MaxMembers(int):
+    """Members of the largest group, with the rows of a workgroup that a plan was made for (`tile_rows`)."""
+
+
 SharedPlan = collections.namedtuple("SharedPlan", "items seq_item_indptr n_slots prefix_items member_slots max_members")
 
 
@@ -573,11 +577,13 @@ def tkv_plan_decode_shared(desc, batch: int, n_q_heads: int, n_tok_int2, n_tok_i
     cap = _check(lib().tkv_plan_shared_capacity(n2.size, target_cus), "tkv_plan_shared_capacity")
     prefix_items, slots, indptr = np.empty((cap, 4), np.int32), np.empty(sq.size, np.int32), np.empty(batch + 1, np.int32)
     n_own = int(np.asarray(items).reshape(-1, 4).shape[0])
+    tile_rows = C.c_int32(0)
     n = _check(lib().tkv_plan_decode_shared(C.byref(desc), batch, n_q_heads, n2.size, p2, p4, pip, psq, target_cus, n_own,
                                             C.c_void_p(prefix_items.ctypes.data), cap, C.c_void_p(slots.ctypes.data if slots.size else None),
-                                            C.c_void_p(indptr.ctypes.data)), "tkv_plan_decode_shared")
-    return SharedPlan(np.asarray(items, np.int32).reshape(-1, 4), np.concatenate([sip, indptr]), int(indptr[-1]), prefix_items[:n].copy(), slots,
-                      int(np.diff(ip).max()) if n2.size else 0)
+                                            C.c_void_p(indptr.ctypes.data), C.byref(tile_rows)), "tkv_plan_decode_shared")
+    members = MaxMembers(np.diff(ip).max() if n2.size else 0)
+    members.tile_rows = tile_rows.value
+    return SharedPlan(np.asarray(items, np.int32).reshape(-1, 4), np.concatenate([sip, indptr]), int(indptr[-1]), prefix_items[:n].copy(), slots, members)
 
 
 def tkv_decode_attention_shared(desc, pool, bit_map, q, page_indptr, page_ids, n_tok_int2, n_tok_int4, items, prefix: tkv_prefix, slot_indptr,

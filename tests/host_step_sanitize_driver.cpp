@@ -27,7 +27,6 @@ size_t tkv_table_words(int32_t n_seqs, int32_t n_tokens) { return (size_t)n_seqs
 int tkv_launch_table_reset(const tkv_desc *, const tkv_table *, void *) { return TKV_OK; }
 int tkv_launch_table_append(const tkv_desc *, const tkv_table *, const int32_t *, const int32_t *, const int32_t *, const uint8_t *, int32_t, int32_t *,
                             int32_t *, int32_t *, int32_t *, int32_t *, int32_t, int32_t *, void *, int32_t *, void *) { return TKV_OK; }
-int32_t tkv_prefix_rows(int32_t rows) { return rows <= 16 ? 16 : rows <= 64 ? 64 : 128; }
 int tkv_launch_shared(const tkv_desc *, const void *, const uint8_t *, const void *, const int32_t *, const int32_t *, const int32_t *, const int32_t *,
                       const int32_t *, int32_t, const tkv_prefix *, const int32_t *, int32_t, int32_t, int32_t, float, void *, void *, int32_t *,
                       void *) { return TKV_OK; }
@@ -63,14 +62,15 @@ int main()
                 if (rnd() & 1) seqs.push_back(b);
             indptr.push_back((int32_t)seqs.size());
         }
+        int32_t tile = 0;
         const int target = 1 + (int)(rnd() % 400), cap = tkv_plan_shared_capacity(n, target);
         std::vector<int32_t> items(4 * (size_t)cap), slots(seqs.size()), out((size_t)batch + 1);
         const int got = tkv_plan_decode_shared(&d, batch, d.n_kv_heads * r, n, n2.data(), n4.data(), indptr.data(), seqs.data(), target, 5, items.data(), cap,
-                                               slots.data(), out.data());
+                                               slots.data(), out.data(), &tile);
         CHECK(got >= 0 && got <= cap && out[0] == 5);
         if (got > 0)
             CHECK(tkv_plan_decode_shared(&d, batch, d.n_kv_heads * r, n, n2.data(), n4.data(), indptr.data(), seqs.data(), target, 5, items.data(), got - 1,
-                                         slots.data(), out.data()) == TKV_ERR_CAPACITY);
+                                         slots.data(), out.data(), &tile) == TKV_ERR_CAPACITY);
     }
     CHECK(tkv_plan_shared_capacity(INT32_MAX, INT32_MAX) == TKV_ERR_INVALID_ARG);
     CHECK(tkv_table_max_work(INT32_MAX, 1 << 28) == 1 << 28);

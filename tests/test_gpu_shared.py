@@ -72,10 +72,13 @@ def run(seed, prefixes, own, groups, kv_heads, r, key_axis=0, f4=0.4, target_ite
     try:
         q = wl.make_q(np.random.SeedSequence([seed, 5]), len(own), kv_heads * r) if q is None else q
         cache.plan_shared(groups, kv_heads * r, target_items, target_cus)
-        out = cache.decode_shared(harness.bf16_tensor(q, DEV))
-        torch.cuda.synchronize()
-        assert int(cache.status.item()) == 0
-        check(out, reference(q, Ks, Vs, groups, kv_heads), "%s %s" % (prefixes, own))
+        want = reference(q, Ks, Vs, groups, kv_heads)
+        for rows in (16, 64, 128):     # the plan chooses one by the sizes; each has to hold at every size
+            cache._shared[2].tile_rows = rows
+            out = cache.decode_shared(harness.bf16_tensor(q, DEV))
+            torch.cuda.synchronize()
+            assert int(cache.status.item()) == 0
+            check(out, want, "%s %s in %d rows" % (prefixes, own, rows))
         return out
     finally:
         cache.close()
