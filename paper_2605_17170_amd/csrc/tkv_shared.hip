@@ -806,9 +806,10 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2, 
     else prefix_item<MODE, KC>(a, lds, wave, lane);
 }
 
-// out = sum_i 2^(m_i - M) acc_i / sum_i 2^(m_i - M) l_i over a sequence's own items and its prefixes'.  One workgroup of four
-// wavefronts per (sequence, query head); a wavefront takes every fourth partial, a lane two channels.
-constexpr int kMergeWaves = 4;
+// out = sum_i 2^(m_i - M) acc_i / sum_i 2^(m_i - M) l_i over a sequence's own items and its prefixes'.  One workgroup per (sequence,
+// query head); 32 lanes take every eighth partial, four channels a lane, and ask for eight of them at a time with their m and l: nothing
+// waits for anything but the workspace, and that once for up to 64 partials.
+constexpr int kMergeWaves = 4, kMergeSets = 2 * kMergeWaves, kMergeBatch = 8;
 struct MergeArgs {
     const float *ws[2];              // partials of the own items, of the prefixes
     int n[2];                        // slots of either
@@ -818,23 +819,11 @@ struct MergeArgs {
     uint16_t *out;
 };
 __device__ __forceinline__ float merge_weight(float m, float M) { return m == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(m - M); }
-__device__ __forceinline__ float wave_max(float v)
-{
-#pragma unroll
-    for (int d = 1; d < 64; d <<= 1) v = fmaxf(v, __shfl_xor(v, d));
-    return v;
-}
-__device__ __forceinline__ float wave_sum(float v)
-{
-#pragma unroll
-    for (int d = 1; d < 64; d <<= 1) v += __shfl_xor(v, d);
-    return v;
-}
 __global__ __launch_bounds__(64 * kMergeWaves) void tkv_merge_shared_kernel(MergeArgs a)
 {
-    __shared__ float2 num_s[kMergeWaves][64];
-    __shared__ float2 ml_s[kMergeWaves];
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    __shared__ float4 num_s[kMergeSets][kHeadDim / 4];
+    __shared__ float2 ml_s[kMergeSets];
+    const int c4 = threadIdx.x & 31, set = threadIdx.x >> 5;
     const int h = blockIdx.x, b = blockIdx.y + blockIdx.z * gridDim.y;
     if (b >= a.batch) return;
     int i0[2], n[2];
@@ -848,56 +837,57 @@ __global__ __launch_bounds__(64 * kMergeWaves) void tkv_merge_shared_kernel(Merg
     }
     const int all = n[0] + n[1];
     float M = -INFINITY, den = 0.0f;
-    float2 num = make_float2(0.f, 0.f);
-    auto row_of = [&](int i, const float *&acc, const float *&ml) {   // partial i of the sequence
-        const int k = i < n[0] ? 0 : 1;
-        const size_t at = (size_t)(k ? i0[1] + i - n[0] : i0[0] + i) * a.n_q_heads + h;
-        const float *ws = k ? a.ws[1] : a.ws[0];
-        acc = ws + at * kHeadDim;
-        ml = ws + (size_t)(k ? a.n[1] : a.n[0]) * a.n_q_heads * kHeadDim + 2 * at;
-    };
-    // 64 of the wavefront's partials at a time: lane l weighs the l-th
-    for (int base = wave; base < all; base += kMergeWaves * 64) {
-        const int mine = base + kMergeWaves * lane;
-        const float *acc, *mlp;
-        float2 ml = make_float2(-INFINITY, 0.0f);
-        if (mine < all) {
-            row_of(mine, acc, mlp);
-            ml = *reinterpret_cast<const float2 *>(mlp);
+    float4 num = make_float4(0.f, 0.f, 0.f, 0.f);
+    for (int base = set; base < all; base += kMergeSets * kMergeBatch) {
+        float4 v[kMergeBatch];
+        float2 ml[kMergeBatch];
+#pragma unroll
+        for (int j = 0; j < kMergeBatch; ++j) {
+            const int i = base + kMergeSets * j, k = i < n[0] ? 0 : 1;
+            v[j] = make_float4(0.f, 0.f, 0.f, 0.f);
+            ml[j] = make_float2(-INFINITY, 0.0f);
+            if (i < all) {
+                const size_t at = (size_t)(k ? i0[1] + i - n[0] : i0[0] + i) * a.n_q_heads + h;
+                const float *ws = k ? a.ws[1] : a.ws[0];
+                v[j] = reinterpret_cast<const float4 *>(ws + at * kHeadDim)[c4];
+                ml[j] = reinterpret_cast<const float2 *>(ws + (size_t)(k ? a.n[1] : a.n[0]) * a.n_q_heads * kHeadDim)[at];
+            }
         }
-        const float Mn = fmaxf(M, wave_max(ml.x));
+        float Mn = M;
+#pragma unroll
+        for (int j = 0; j < kMergeBatch; ++j) Mn = fmaxf(Mn, ml[j].x);
         const float so = merge_weight(M, Mn);
-        float w = merge_weight(ml.x, Mn);
-        if (ml.y != ml.y) w = ml.y;   // NaN stays
-        den = den * so + wave_sum(mine < all ? w * ml.y : 0.0f);
-        num.x *= so;
-        num.y *= so;
-        const int count = (all - base + kMergeWaves - 1) / kMergeWaves < 64 ? (all - base + kMergeWaves - 1) / kMergeWaves : 64;
-#pragma unroll 8
-        for (int k = 0; k < count; ++k) {
-            row_of(base + kMergeWaves * k, acc, mlp);
-            const float2 v = reinterpret_cast<const float2 *>(acc)[lane];
-            const float wk = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(w), k));
-            num.x = fmaf(wk, v.x, num.x);
-            num.y = fmaf(wk, v.y, num.y);
+        den *= so;
+        num = make_float4(num.x * so, num.y * so, num.z * so, num.w * so);
+#pragma unroll
+        for (int j = 0; j < kMergeBatch; ++j) {
+            float w = merge_weight(ml[j].x, Mn);
+            if (ml[j].y != ml[j].y) w = ml[j].y;   // NaN stays
+            den = fmaf(w, ml[j].y, den);
+            num.x = fmaf(w, v[j].x, num.x);
+            num.y = fmaf(w, v[j].y, num.y);
+            num.z = fmaf(w, v[j].z, num.z);
+            num.w = fmaf(w, v[j].w, num.w);
         }
         M = Mn;
     }
-    num_s[wave][lane] = num;
-    if (lane == 0) ml_s[wave] = make_float2(M, den);
+    num_s[set][c4] = num;
+    if (c4 == 0) ml_s[set] = make_float2(M, den);
     __syncthreads();
-    if (wave > 0) return;
-    float Mg = M;
+    const int lane = threadIdx.x;
+    if (lane >= kHeadDim / 2) return;   // two channels a lane
+    float Mg = ml_s[0].x;
 #pragma unroll
-    for (int k = 1; k < kMergeWaves; ++k) Mg = fmaxf(Mg, ml_s[k].x);
+    for (int k = 1; k < kMergeSets; ++k) Mg = fmaxf(Mg, ml_s[k].x);
     float d = 0.0f;
     float2 o = make_float2(0.f, 0.f);
 #pragma unroll
-    for (int k = 0; k < kMergeWaves; ++k) {
+    for (int k = 0; k < kMergeSets; ++k) {
         const float wk = merge_weight(ml_s[k].x, Mg);
-        d += wk * ml_s[k].y;
-        o.x = fmaf(wk, num_s[k][lane].x, o.x);
-        o.y = fmaf(wk, num_s[k][lane].y, o.y);
+        const float2 x = reinterpret_cast<const float2 *>(num_s[k])[lane];
+        d = fmaf(wk, ml_s[k].y, d);
+        o.x = fmaf(wk, x.x, o.x);
+        o.y = fmaf(wk, x.y, o.y);
     }
     const float r = d == 0.0f ? 0.0f : 1.0f / d;   // no tokens: zeros; NaN stays
     typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
