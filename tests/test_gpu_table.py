@@ -77,7 +77,8 @@ def trace(rng, n, share4=0.4):
 
 
 @pytest.mark.parametrize("n_seqs,longest,steps", [(1, 1, 3), (1, 700, 4), (3, 64, 4), (17, 129, 3), (300, 5, 4), (1024, 7, 2),   # one workgroup
-                                                  (1025, 3, 3), (2500, 9, 3), (5, 4000, 3), (1, 20000, 2), (64, 1500, 2)])        # four launches
+                                                  (5, 4000, 3), (1, 20000, 2), (64, 900, 3), (1000, 60, 2),      # sums in one
+                                                  (1025, 3, 3), (2500, 9, 3), (64, 2500, 2), (2, 70000, 2)])                     # four launches
 def test_lengths_cuts_and_widths(n_seqs, longest, steps):
     rng = np.random.default_rng(n_seqs * 31 + longest)
     pages = n_seqs * (longest * steps // 64 + 2) + 3
@@ -94,6 +95,38 @@ def test_lengths_cuts_and_widths(n_seqs, longest, steps):
             keep[rng.random(n_seqs) < 0.3] = 1 << 30       # everything
             keep[rng.random(n_seqs) < 0.1] = 0             # a request that has ended
         dev.check(*dev.append(keep, lens, trace(rng, int(lens.sum())), tag_offset=step))
+
+
+@pytest.mark.parametrize("n_seqs,max_pages", [(1024, 64), (1024, 65), (41, 2000)])
+def test_pages_given_back_by_many_rows(n_seqs, max_pages):
+    """Rows of 65536 entries together and of more: their pages go back in the launch of the sums or in one of their own."""
+    rng = np.random.default_rng(max_pages)
+    dev = Device(n_seqs, max_pages, 50 * n_seqs, 50 * n_seqs, seed=7)
+    for step in range(4):
+        count = np.array(dev.model.count)
+        keep = np.maximum(0, count - rng.integers(0, 64 * 7, (n_seqs, 2)))
+        lens = rng.integers(0, 120000 // n_seqs, n_seqs) if step < 3 else np.full(n_seqs, 9)
+        while lens.sum() > 65536:
+            lens //= 2
+        keep[(count + lens[:, None]).sum(1) > 40 * 64] = 0
+        dev.check(*dev.append(keep, lens, np.concatenate([trace(rng, int(lens.sum())), np.full(65536 - int(lens.sum()), 1, np.uint8)])))
+
+
+def test_refusals_with_many_tokens():
+    n_seqs, n = 7, 20000
+    dev = Device(n_seqs, 60, 300, 40)
+    dev.check(*dev.append(None, [100] * n_seqs, np.full(n, 2, np.uint8)))
+    refused, exhausted, capacity = tkv.TKV_STATUS_TABLE_REFUSED, tkv.TKV_STATUS_POOL_EXHAUSTED, tkv.TKV_STATUS_CAPACITY
+    lens, tags = np.full(n_seqs, 2500), np.full(n, 2, np.uint8)
+    full = [(tags, lens + 1000, None, refused), (tags, np.array([5, -1] + [0] * 5), None, refused), (tags, np.array([1 << 29] * n_seqs), None, refused),
+            (np.where(np.arange(n) == 17499, 3, tags), lens, None, refused), (np.where(np.arange(n) < 2561, 4, tags), lens, None, exhausted),   # 41 pages
+            (tags, np.array([60 * 64] + [0] * 6), None, capacity), (tags, lens, 100, capacity)]
+    for tags_, lens_, max_work, bits in full:
+        got, status, want = dev.append(None, lens_, tags_.astype(np.uint8), max_work=max_work)
+        assert isinstance(want, str)
+        dev.check_refused(got, status, bits)
+    dev.check(*dev.append([[64, 64]] * n_seqs, lens, np.where(np.arange(n) == 17500, 3, tags).astype(np.uint8)))
+    dev.check(*dev.append([[64, 64]] * n_seqs, lens, np.where(np.arange(n) < 2500, 4, tags).astype(np.uint8)))             # all 40 pages
 
 
 @pytest.mark.parametrize("n_seqs", [6, 1100])
