@@ -16,10 +16,9 @@
 //   up to 1024 sequences, 8192 tokens and 1024 work entries: one launch, which also updates rows and places tokens.  32 sequences
 //     with a token each 5.7 us (an empty kernel 4.4), 200 with five 6.9; with launches of their own for sums, pages given back,
 //     rows and tokens such calls take 17.
-//   up to 1024 sequences and 65536 tokens: rows and tokens in a second launch over many workgroups, since one would write for 20 us and more.
-//     6 prompts with 63 thousand tokens 11.7 us, 12 with 9 thousand 10.9.  Pages given back by rows of more than 65536 entries
-//     together, some 10 us of one workgroup, have a launch in between (3.9 us).
-//   beyond: four launches; tags to bit masks, sums in a loop, pages given back, rows and tokens (64 sequences, 63 thousand tokens: 17.5).
+//   up to 1024 sequences and 65536 tokens: rows and tokens in a second launch over many workgroups.  6 prompts with 63 thousand tokens
+//     11.6 us (in four launches 15.6), 12 with 9 thousand 10.9 (15.2).
+//   beyond: four launches; tags to bit masks, sums in a loop, pages given back, rows and tokens.
 #include <hip/hip_runtime.h>
 
 #include "tkv_internal.h"
@@ -677,8 +676,9 @@ int tkv_launch_table_append(const tkv_desc *desc, const tkv_table *table, const 
     const int64_t lists = (int64_t)max_work * kPageTokens;
     bool push = keep_int2 || keep_int4;
     if (a.n_seqs <= kPlanSeqs && n_tokens <= kPlanTokens) {
-        // one workgroup gives as many pages back as it can read while another launch would begin
-        const bool inside = (int64_t)a.n_seqs * a.max_pages <= 65536;
+        // Pages given back in the launch of the sums, by its one workgroup, or in one of their own.  Few of them: a launch (3.9 us) less.
+        // 8000: 17.6 us inside and 14.4 in a launch of their own, 64000: 39 and 16.  How many there are is known on the GPU only.
+        const bool inside = (int64_t)a.n_seqs * a.max_pages <= 8192;
         hipLaunchKernelGGL(tkv_table_plan_kernel<false>, dim3(1 + blocks_for(lists / 16, 255)), dim3(kThreads), 0, s, a, inside ? 1 : 0);
         push = push && !inside;
     } else {

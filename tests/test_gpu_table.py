@@ -97,9 +97,9 @@ def test_lengths_cuts_and_widths(n_seqs, longest, steps):
         dev.check(*dev.append(keep, lens, trace(rng, int(lens.sum())), tag_offset=step))
 
 
-@pytest.mark.parametrize("n_seqs,max_pages", [(1024, 64), (1024, 65), (41, 2000)])
+@pytest.mark.parametrize("n_seqs,max_pages", [(128, 64), (128, 65), (1024, 64), (41, 2000)])
 def test_pages_given_back_by_many_rows(n_seqs, max_pages):
-    """Rows of 65536 entries together and of more: their pages go back in the launch of the sums or in one of their own."""
+    """Rows of 8192 entries together and of more: their pages go back in the launch of the sums or in one of their own."""
     rng = np.random.default_rng(max_pages)
     dev = Device(n_seqs, max_pages, 50 * n_seqs, 50 * n_seqs, seed=7)
     for step in range(4):
