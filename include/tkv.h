@@ -450,17 +450,16 @@ int tkv_decode_attention_static(const tkv_desc *desc, const void *pool, const ui
  * some) or of none.  Attention does not depend on the order of tokens, so
  * several prefixes need none.
  *   n_groups, n_members   groups; entries of member_seqs
- *   max_members           members of the largest group, at least (rows of the launch)
- *   tile_rows             query rows of a workgroup, 16, 64 or 128, as tkv_plan_decode_shared chooses them (any gives the same attention)
+ *   tile_rows             query rows of an item, 16, 64 or 128, as tkv_plan_decode_shared chooses them
  *   n_items               prefix work items
  *   page_indptr  device i32[n_groups+1] page-list offsets of the groups
  *   page_ids     device i32: per group INT2 pages, then INT4 pages, of the same pool as the sequences' own
  *   n_tok_int2/4 device i32[n_groups] valid tokens per width
  *   member_indptr device i32[n_groups+1], member_seqs device i32[n_members]: sequences of each group
- *   member_slots device i32[n_members], items device i32[4*n_items]: as written by tkv_plan_decode_shared
+ *   member_slots device i32[n_members], items device i32[5*n_items]: as written by tkv_plan_decode_shared
  */
 typedef struct tkv_prefix {
-    int32_t n_groups, n_members, max_members, tile_rows, n_items;
+    int32_t n_groups, n_members, tile_rows, n_items;
     const int32_t *page_indptr;
     const int32_t *page_ids;
     const int32_t *n_tok_int2;
@@ -472,24 +471,25 @@ typedef struct tkv_prefix {
 } tkv_prefix;
 
 /* Upper bound of the items that tkv_plan_decode_shared makes. */
-int32_t tkv_plan_shared_capacity(int32_t n_groups, int32_t target_cus);
+int32_t tkv_plan_shared_capacity(int32_t n_groups, int32_t n_members, int32_t target_cus);
 /*
- * Cuts the groups' page lists into work items and gives every (item, member) a
- * partial slot behind the n_own_items slots of the sequences' own items
- * (tkv_plan_decode).  An item is read by one workgroup per kv head and tile_rows
- * rows (a row is one query head of one member); with 16 rows its eight
- * wavefronts work on a page each at a time, with 64 and 128 on two pages
- * together.  The number of rows is the one that is expected to take least time,
- * and items are equal parts of whole steps, as small as still gives no more
- * workgroups than target_cus compute units, less those that the own items take
- * (or none, where these are few beside the prefixes).  Depends on the page
- * counts and members only, and ages as a decode plan does.
+ * Cuts the groups' page lists into parts, and those and the groups' query rows
+ * (of one kv head: n_q_heads / n_kv_heads of each member) into work items, and
+ * gives every (part, member) a partial slot behind the n_own_items slots of the
+ * sequences' own items (tkv_plan_decode).  An item is one workgroup per kv head
+ * for tile_rows rows: with 16 its eight wavefronts work on a page each at a
+ * time, with 64 and 128 on two pages together.  The number of rows is the one
+ * that is expected to take least time, and parts are equal numbers of whole
+ * steps, as small as still gives no more workgroups than target_cus compute
+ * units, less those that the own items take (or none, where these are few
+ * beside the prefixes).  Depends on the page counts and members only, and ages
+ * as a decode plan does.
  *   n_tok_int2/4   host i32[n_groups]
  *   member_indptr  host i32[n_groups+1], from 0; member_seqs host i32[member_indptr[n_groups]],
  *                  below batch, each at most once in a group
  *   target_cus     compute units to fill (>= 1)
- *   items_out      host i32[4*capacity]: {group, first page, end page, number in the group}
- *   member_slots_out  host i32[members]: slot of the member's partial of the group's first item, the others follow
+ *   items_out      host i32[5*capacity]: {group, first page, end page, number of the part in the group, first row}
+ *   member_slots_out  host i32[members]: slot of the member's partial of the group's first part, the others follow
  *   seq_slot_indptr_out  host i32[batch+1]: slots of each sequence, from n_own_items on
  *   tile_rows_out  host i32
  * Returns the number of items (>= 0) or a negative status.
@@ -512,13 +512,13 @@ int32_t tkv_plan_decode_shared(const tkv_desc *desc, int32_t batch, int32_t n_q_
  *   out            device bf16 [batch, n_q_heads, head_dim], 16-byte aligned
  *   workspace      device, >= tkv_decode_workspace_bytes(desc, n_slots, n_q_heads), 16-byte aligned
  *   status         device i32, may be NULL; bits as for tkv_decode_attention.  Members outside the batch, slots outside
- *                  [n_items, n_slots) and groups with more members than max_members raise TKV_STATUS_BAD_ITEM: what they
- *                  name is not stored, and the sequence reads what the workspace held before
+ *                  [n_items, n_slots) and items outside the groups raise TKV_STATUS_BAD_ITEM: what they name is not stored,
+ *                  and the sequence reads what the workspace held before
  * Preconditions: stored scales and zeros finite, and values within fp16; with
  * TKV_KEYS_PER_CHANNEL every n_tok_int2 a multiple of 32.  q may hold any
  * finite values; a query head of NaN or infinities gives NaN and leaves the
- * others alone.  n_q_heads / n_kv_heads is 1, 2, 4 or 8; at most 65535 prefix
- * items.  Two launches on `stream`: attention, then the merge.
+ * others alone.  n_q_heads / n_kv_heads is 1, 2, 4 or 8.  Two launches on
+ * `stream`: attention, then the merge.
  */
 int tkv_decode_attention_shared(const tkv_desc *desc, const void *pool, const uint8_t *bit_map, const void *q,
                                 const int32_t *page_indptr, const int32_t *page_ids,

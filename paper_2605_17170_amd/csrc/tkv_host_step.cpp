@@ -132,11 +132,11 @@ int tkv_norm_rope(const tkv_rope *rope, const void *q, int64_t q_stride, const v
 
 /* ---------------------------------------------------------------- D8: shared prefixes */
 
-int32_t tkv_plan_shared_capacity(int32_t n_groups, int32_t target_cus)
+int32_t tkv_plan_shared_capacity(int32_t n_groups, int32_t n_members, int32_t target_cus)
 {
-    // a workgroup for a compute unit at most, or an item for every group
-    if (n_groups < 0 || target_cus < 1 || n_groups + (int64_t)target_cus > INT32_MAX) return TKV_ERR_INVALID_ARG;
-    return n_groups + target_cus;
+    // a workgroup for a compute unit at most, or the workgroups for the rows of every group: up to eight rows a member, at least 16 a workgroup
+    const int64_t n = n_groups + (int64_t)target_cus + ((int64_t)n_members + 1) / 2;
+    return n_groups < 0 || n_members < 0 || target_cus < 1 || n > INT32_MAX ? (int32_t)TKV_ERR_INVALID_ARG : (int32_t)n;
 }
 
 int32_t tkv_plan_decode_shared(const tkv_desc *desc, int32_t batch, int32_t n_q_heads, int32_t n_groups, const int32_t *n_tok_int2,
@@ -146,7 +146,7 @@ int32_t tkv_plan_decode_shared(const tkv_desc *desc, int32_t batch, int32_t n_q_
 {
     if (int st = tkv_desc_status(desc)) return st;
     if (batch < 0 || n_groups < 0 || n_own_items < 0 || capacity < 0 || n_q_heads <= 0 || !seq_slot_indptr_out || !tile_rows_out || !member_indptr) return TKV_ERR_INVALID_ARG;
-    if (tkv_plan_shared_capacity(n_groups, target_cus) < 0) return TKV_ERR_INVALID_ARG;
+    if (tkv_plan_shared_capacity(n_groups, 0, target_cus) < 0) return TKV_ERR_INVALID_ARG;
     if (n_groups > 0 && (!n_tok_int2 || !n_tok_int4)) return TKV_ERR_INVALID_ARG;
     if (n_q_heads % desc->n_kv_heads) return TKV_ERR_BAD_SHAPE;
     const int32_t r = n_q_heads / desc->n_kv_heads;
@@ -201,13 +201,11 @@ int32_t tkv_plan_decode_shared(const tkv_desc *desc, int32_t batch, int32_t n_q_
         }
         *tile_rows_out = rows;
         auto units = [&](int32_t g) -> int64_t { return member_indptr[g + 1] == member_indptr[g] ? 0 : (pages(g) + unit - 1) / unit; };
-        auto blocks = [&](int32_t g) -> int64_t {   // workgroups of an item
-            return (((int64_t)(member_indptr[g + 1] - member_indptr[g]) * r + rows - 1) / rows) * desc->n_kv_heads;
-        };
+        auto row_blocks = [&](int32_t g) { return ((int64_t)(member_indptr[g + 1] - member_indptr[g]) * r + rows - 1) / rows; };
         for (int32_t g = 0; g < n_groups; ++g) longest = std::max(longest, units(g));
         auto workgroups = [&](int64_t per) {
             int64_t n = 0;
-            for (int32_t g = 0; g < n_groups; ++g) n += (units(g) + per - 1) / per * blocks(g);
+            for (int32_t g = 0; g < n_groups; ++g) n += (units(g) + per - 1) / per * row_blocks(g) * desc->n_kv_heads;
             return n;
         };
         int64_t lo = 1, hi = longest;
@@ -221,14 +219,17 @@ int32_t tkv_plan_decode_shared(const tkv_desc *desc, int32_t batch, int32_t n_q_
         for (int32_t g = 0; g < n_groups; ++g) {
             const int64_t all = units(g), n = (all + lo - 1) / lo;
             parts[(size_t)g] = (int32_t)n;
-            if (n_items + n > capacity) return TKV_ERR_CAPACITY;
-            for (int64_t k = 0; k < n; ++k) {
-                int32_t *it = items_out + 4 * n_items++;
-                it[0] = g;
-                it[1] = (int32_t)(unit * (all * k / n));
-                it[2] = (int32_t)std::min(pages(g), unit * (all * (k + 1) / n));
-                it[3] = (int32_t)k;
-            }
+            if (n_items + n * row_blocks(g) > capacity) return TKV_ERR_CAPACITY;
+            // workgroups of the same pages follow one another: with eight kv heads they lie on one XCD, whose L2 they share
+            for (int64_t k = 0; k < n; ++k)
+                for (int64_t z = 0; z < row_blocks(g); ++z) {
+                    int32_t *it = items_out + 5 * n_items++;
+                    it[0] = g;
+                    it[1] = (int32_t)(unit * (all * k / n));
+                    it[2] = (int32_t)std::min(pages(g), unit * (all * (k + 1) / n));
+                    it[3] = (int32_t)k;
+                    it[4] = (int32_t)(rows * z);
+                }
             for (int32_t m = member_indptr[g]; m < member_indptr[g + 1]; ++m) next[(size_t)member_seqs[m]] += (int32_t)n;
             n_slots += n * (member_indptr[g + 1] - member_indptr[g]);
             if (n_slots > INT32_MAX) return TKV_ERR_INVALID_ARG;
@@ -262,7 +263,7 @@ int tkv_decode_attention_shared(const tkv_desc *desc, const void *pool, const ui
     if (!prefix || n_items < 0 || n_slots < n_items) return tkv_desc_status(desc) ? tkv_desc_status(desc) : TKV_ERR_INVALID_ARG;
     if (int st = tkv_decode_check_args(desc, n_slots, batch, n_q_heads, workspace, workspace_bytes)) return st;
     const tkv_prefix &p = *prefix;
-    if (p.n_groups < 0 || p.n_members < 0 || p.max_members < 0 || p.n_items < 0 || p.n_items > 65535) return TKV_ERR_INVALID_ARG;
+    if (p.n_groups < 0 || p.n_members < 0 || p.n_items < 0) return TKV_ERR_INVALID_ARG;
     if (batch == 0) return TKV_OK;
     if (!(sm_scale > 0.0f) || !(sm_scale < 3.0e38f)) return TKV_ERR_INVALID_ARG;
     if (!q || !out || !slot_indptr) return TKV_ERR_INVALID_ARG;
@@ -272,11 +273,10 @@ int tkv_decode_attention_shared(const tkv_desc *desc, const void *pool, const ui
     const int32_t r = n_q_heads / desc->n_kv_heads;
     if (p.n_items > 0) {
         if (!p.page_indptr || !p.page_ids || !p.n_tok_int2 || !p.n_tok_int4 || !p.member_indptr || !p.member_seqs || !p.member_slots || !p.items ||
-            p.n_groups == 0 || p.n_members == 0 || p.max_members == 0)
+            p.n_groups == 0 || p.n_members == 0)
             return TKV_ERR_INVALID_ARG;
         if (p.tile_rows != 16 && p.tile_rows != 64 && p.tile_rows != 128) return TKV_ERR_INVALID_ARG;
-        const int64_t rows = (int64_t)p.max_members * r;
-        if (rows > INT32_MAX / 2 || (int64_t)p.n_members * r > INT32_MAX / 2 || (rows + p.tile_rows - 1) / p.tile_rows > 65535) return TKV_ERR_INVALID_ARG;
+        if ((int64_t)p.n_members * r > INT32_MAX / 2 || (int64_t)p.n_items * desc->n_kv_heads > INT32_MAX / 2) return TKV_ERR_INVALID_ARG;
     }
     return tkv_launch_shared(desc, pool, bit_map, q, page_indptr, page_ids, n_tok_int2, n_tok_int4, items, n_items, prefix, slot_indptr, n_slots,
                              batch, n_q_heads, sm_scale, out, workspace, status, stream);

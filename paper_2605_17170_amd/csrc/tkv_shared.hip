@@ -120,7 +120,6 @@ struct SharedArgs {
     int n_items;      // own items: slots [0, n_items); the prefixes' partials have [n_items, n_slots)
     int own_blocks;   // the first workgroups, a wavefront for each (own item, kv head)
     tkv_prefix p;
-    int row_blocks;   // workgroups of a (prefix item, kv head)
     int n_kv_heads;
     int log2_r;
     int n_pages_int2;
@@ -692,12 +691,10 @@ template <int MODE, bool KC> __device__ __forceinline__ void prefix_item(const S
 {
     constexpr int NT = tiles_of(MODE), ROWS = rows_of(MODE), SETS = Shared<MODE>::kSets;
     const int r16 = lane & 15, q4 = lane >> 4, R = 1 << a.log2_r, n_q_heads = a.n_kv_heads << a.log2_r;
-    // the workgroups of an (item, kv head) lie a multiple of items x kv heads apart: with eight kv heads on one XCD, whose L2 they share
-    const int per = a.p.n_items * a.n_kv_heads, block = blockIdx.x - a.own_blocks, z = block / per, unit = block - z * per;
-    const int item = unit / a.n_kv_heads, kvh = unit - item * a.n_kv_heads;
-    const ConstWords words = (ConstWords)(a.p.items + 4 * (size_t)item);
-    const int group = words[0], item_pb = words[1], item_pe = words[2], part = words[3];
-    if (group < 0 || group >= a.p.n_groups || part < 0) {
+    const int block = blockIdx.x - a.own_blocks, item = block / a.n_kv_heads, kvh = block - item * a.n_kv_heads;
+    const ConstWords words = (ConstWords)(a.p.items + 5 * (size_t)item);
+    const int group = words[0], item_pb = words[1], item_pe = words[2], part = words[3], row0 = words[4];
+    if (group < 0 || group >= a.p.n_groups || part < 0 || row0 < 0) {
         if (a.status && threadIdx.x == 0) atomicOr(a.status, TKV_STATUS_BAD_ITEM);
         return;
     }
@@ -706,9 +703,8 @@ template <int MODE, bool KC> __device__ __forceinline__ void prefix_item(const S
     const int list0 = ((ConstWords)a.p.page_indptr)[group], list1 = ((ConstWords)a.p.page_indptr)[group + 1];
     m0 = m0 > 0 ? m0 : 0;
     m1 = m1 < a.p.n_members ? m1 : a.p.n_members;
-    const int n_rows = (m1 - m0) << a.log2_r, row0 = z * ROWS;
+    const int n_rows = (m1 - m0) << a.log2_r;
     if (row0 >= n_rows) return;
-    if (m1 - m0 > a.p.max_members && a.status && threadIdx.x == 0) atomicOr(a.status, TKV_STATUS_BAD_ITEM);   // more rows than the launch has workgroups for
     const int np2 = (n2 + kPageTokens - 1) / kPageTokens, np4 = (n4 + kPageTokens - 1) / kPageTokens;
     const int np = np2 + np4 < list1 - list0 ? np2 + np4 : list1 - list0;
     const int pb = item_pb > 0 ? item_pb : 0, pe = item_pe < np ? item_pe : np;
@@ -936,9 +932,8 @@ int tkv_launch_shared(const tkv_desc *desc, const void *pool, const uint8_t *bit
     }
     a.status = status;
     a.own_blocks = (int)(((int64_t)n_items * desc->n_kv_heads + kWaves - 1) / kWaves);
-    const int rows = prefix->n_items > 0 ? prefix->max_members << log2_r : 1, per = prefix->n_items > 0 ? prefix->tile_rows : 16;
-    a.row_blocks = (rows + per - 1) / per;
-    const int64_t blocks = a.own_blocks + (int64_t)prefix->n_items * desc->n_kv_heads * a.row_blocks;
+    const int per = prefix->n_items > 0 ? prefix->tile_rows : 16;
+    const int64_t blocks = a.own_blocks + (int64_t)prefix->n_items * desc->n_kv_heads;
     if (blocks > INT32_MAX) return TKV_ERR_INVALID_ARG;
     if (blocks > 0) {
         const bool kc = desc->int2_key_axis == TKV_KEYS_PER_CHANNEL;

@@ -73,19 +73,20 @@ class tkv_desc(C.Structure):
 
 class tkv_prefix(C.Structure):
     """Shared prefixes of groups of sequences: device arrays; `make` keeps the tensors alive."""
-    _fields_ = [("n_groups", C.c_int32), ("n_members", C.c_int32), ("max_members", C.c_int32), ("tile_rows", C.c_int32), ("n_items", C.c_int32),
+    _fields_ = [("n_groups", C.c_int32), ("n_members", C.c_int32), ("tile_rows", C.c_int32), ("n_items", C.c_int32),
                 ("page_indptr", C.c_void_p), ("page_ids", C.c_void_p), ("n_tok_int2", C.c_void_p), ("n_tok_int4", C.c_void_p),
                 ("member_indptr", C.c_void_p), ("member_seqs", C.c_void_p), ("member_slots", C.c_void_p), ("items", C.c_void_p)]
 
     @classmethod
-    def make(cls, page_indptr, page_ids, n_tok_int2, n_tok_int4, member_indptr, member_seqs, member_slots, items, max_members: int):
+    def make(cls, page_indptr, page_ids, n_tok_int2, n_tok_int4, member_indptr, member_seqs, member_slots, items, max_members):
         """i32 device tensors: page_indptr, member_indptr [n_groups+1]; page_ids; n_tok_int2/4 [n_groups]; member_seqs,
-        member_slots [n_members]; items [n_items, 4] (the last two and max_members from tkv_plan_decode_shared)."""
+        member_slots [n_members]; items [n_items, 5] (the last two and max_members from tkv_plan_decode_shared, whose
+        max_members also names the rows of an item)."""
         tensors = (page_indptr, page_ids, n_tok_int2, n_tok_int4, member_indptr, member_seqs, member_slots, items)
         n = n_tok_int2.numel()
         assert all(t.element_size() == 4 for t in tensors) and n_tok_int4.numel() == n and page_indptr.numel() == member_indptr.numel() == n + 1
-        assert member_seqs.numel() == member_slots.numel() and items.numel() % 4 == 0
-        prefix = cls(n, member_seqs.numel(), max_members, getattr(max_members, "tile_rows", 16), items.numel() // 4, *(_dev(t) for t in tensors))
+        assert member_seqs.numel() == member_slots.numel() and items.numel() % 5 == 0
+        prefix = cls(n, member_seqs.numel(), max_members.tile_rows, items.numel() // 5, *(_dev(t) for t in tensors))
         prefix.tensors = tensors
         return prefix
 
@@ -173,7 +174,7 @@ def lib():
         L.tkv_decode_split.argtypes = [dp, vp, vp, vp, vp, vp, vp, vp, vp, i32, i32, i32, C.c_float, vp, sz, vp, vp]
         L.tkv_decode_reduce.argtypes = [dp, vp, i32, i32, i32, vp, vp, sz, vp]
         L.tkv_plan_shared_capacity.restype = i32
-        L.tkv_plan_shared_capacity.argtypes = [i32, i32]
+        L.tkv_plan_shared_capacity.argtypes = [i32, i32, i32]
         L.tkv_plan_decode_shared.restype = i32
         L.tkv_plan_decode_shared.argtypes = [dp, i32, i32, i32, vp, vp, vp, vp, i32, i32, vp, i32, vp, vp, C.POINTER(i32)]
         L.tkv_decode_attention_shared.argtypes = [dp, vp, vp, vp, vp, vp, vp, vp, vp, i32, C.POINTER(tkv_prefix), vp, i32, i32, i32, C.c_float,
@@ -556,7 +557,7 @@ def tkv_tag_counts(tags) -> np.ndarray:
 
 # ---------------------------------------------------------------- D8 (host plan, device)
 class MaxMembers(int):
-    """Members of the largest group, with the rows of a workgroup that a plan was made for (`tile_rows`)."""
+    """Members of the largest group, with the rows of the plan's items (`tile_rows`)."""
 
 
 SharedPlan = collections.namedtuple("SharedPlan", "items seq_item_indptr n_slots prefix_items member_slots max_members")
@@ -566,7 +567,7 @@ def tkv_plan_decode_shared(desc, batch: int, n_q_heads: int, n_tok_int2, n_tok_i
                            seq_item_indptr) -> SharedPlan:
     """Plan over the groups' prefixes (host arrays, per group) beside the plan (items, seq_item_indptr) of the sequences' own
     tokens from tkv_plan_decode.  SharedPlan: items i32[n_items, 4] and seq_item_indptr i32[2*(batch+1)] of the sequences,
-    n_slots, prefix_items i32[n, 4], member_slots i32[n_members], max_members."""
+    n_slots, prefix_items i32[n, 5], member_slots i32[n_members], max_members."""
     n2, p2 = _np(n_tok_int2, np.int32)
     n4, p4 = _np(n_tok_int4, np.int32)
     ip, pip = _np(member_indptr, np.int32)
@@ -574,8 +575,8 @@ def tkv_plan_decode_shared(desc, batch: int, n_q_heads: int, n_tok_int2, n_tok_i
     sip, _ = _np(seq_item_indptr, np.int32)
     if n2.size != n4.size or ip.size != n2.size + 1 or sip.size != batch + 1 or sq.size != ip[-1]:
         raise ValueError("one count per group, group offsets, members and sequence offsets")
-    cap = _check(lib().tkv_plan_shared_capacity(n2.size, target_cus), "tkv_plan_shared_capacity")
-    prefix_items, slots, indptr = np.empty((cap, 4), np.int32), np.empty(sq.size, np.int32), np.empty(batch + 1, np.int32)
+    cap = _check(lib().tkv_plan_shared_capacity(n2.size, sq.size, target_cus), "tkv_plan_shared_capacity")
+    prefix_items, slots, indptr = np.empty((cap, 5), np.int32), np.empty(sq.size, np.int32), np.empty(batch + 1, np.int32)
     n_own = int(np.asarray(items).reshape(-1, 4).shape[0])
     tile_rows = C.c_int32(0)
     n = _check(lib().tkv_plan_decode_shared(C.byref(desc), batch, n_q_heads, n2.size, p2, p4, pip, psq, target_cus, n_own,

@@ -63,8 +63,8 @@ int main()
             indptr.push_back((int32_t)seqs.size());
         }
         int32_t tile = 0;
-        const int target = 1 + (int)(rnd() % 400), cap = tkv_plan_shared_capacity(n, target);
-        std::vector<int32_t> items(4 * (size_t)cap), slots(seqs.size()), out((size_t)batch + 1);
+        const int target = 1 + (int)(rnd() % 400), cap = tkv_plan_shared_capacity(n, (int)seqs.size(), target);
+        std::vector<int32_t> items(5 * (size_t)cap), slots(seqs.size()), out((size_t)batch + 1);
         const int got = tkv_plan_decode_shared(&d, batch, d.n_kv_heads * r, n, n2.data(), n4.data(), indptr.data(), seqs.data(), target, 5, items.data(), cap,
                                                slots.data(), out.data(), &tile);
         CHECK(got >= 0 && got <= cap && out[0] == 5);
@@ -72,7 +72,7 @@ int main()
             CHECK(tkv_plan_decode_shared(&d, batch, d.n_kv_heads * r, n, n2.data(), n4.data(), indptr.data(), seqs.data(), target, 5, items.data(), got - 1,
                                          slots.data(), out.data(), &tile) == TKV_ERR_CAPACITY);
     }
-    CHECK(tkv_plan_shared_capacity(INT32_MAX, INT32_MAX) == TKV_ERR_INVALID_ARG);
+    CHECK(tkv_plan_shared_capacity(INT32_MAX, 0, INT32_MAX) == TKV_ERR_INVALID_ARG);
     CHECK(tkv_table_max_work(INT32_MAX, 1 << 28) == 1 << 28);
     CHECK(tkv_table_max_work(1 << 20, 1 << 28) == (1 << 22) + (1 << 22));
     std::printf("host step sanitizer run ok\n");

@@ -67,6 +67,17 @@ def check(out, want, what=""):
     assert worst <= 1.0, (what, worst)
 
 
+def cut_rows(cache, rows, rows_of_group):
+    """The plan's parts with items of another number of rows."""
+    prefix = cache._shared[2]
+    parts = np.unique(prefix.tensors[7].cpu().numpy().reshape(-1, 5)[:, :4], axis=0)
+    items = np.array([[*p, row] for p in parts for row in range(0, rows_of_group[p[0]], rows)], np.int32).reshape(-1, 5)
+    cache._shared = (*cache._shared[:2], tkv.tkv_prefix(prefix.n_groups, prefix.n_members, rows, len(items), *[t.data_ptr() for t in prefix.tensors[:7]], 0),
+                     *cache._shared[3:])
+    cache._shared[2].tensors = (*prefix.tensors[:7], torch.from_numpy(items).to(DEV))
+    cache._shared[2].items = cache._shared[2].tensors[7].data_ptr()
+
+
 def run(seed, prefixes, own, groups, kv_heads, r, key_axis=0, f4=0.4, target_items=40, target_cus=8, q=None):
     cache, Ks, Vs = build(seed, prefixes, own, kv_heads, key_axis, f4)
     try:
@@ -74,7 +85,7 @@ def run(seed, prefixes, own, groups, kv_heads, r, key_axis=0, f4=0.4, target_ite
         cache.plan_shared(groups, kv_heads * r, target_items, target_cus)
         want = reference(q, Ks, Vs, groups, kv_heads)
         for rows in (16, 64, 128):     # the plan chooses one by the sizes; each has to hold at every size
-            cache._shared[2].tile_rows = rows
+            cut_rows(cache, rows, [len(g) * r for g in groups])
             out = cache.decode_shared(harness.bf16_tensor(q, DEV))
             torch.cuda.synchronize()
             assert int(cache.status.item()) == 0
@@ -229,12 +240,9 @@ def test_members_slots_and_items_that_cannot_be():
         flagged(items, 0, -1)
         flagged(items, 0, 1)
         flagged(items, 3, -1)
+        flagged(items, 4, -1)
+        flagged(items, 4, -(1 << 31))
         flagged(items, 3, (1 << 31) - 1)
-        cache.status.zero_()
-        prefix.max_members = 1       # four rows: a launch of one tile of 16, which holds all three members
-        assert torch.equal(cache.decode_shared(q), clean)
-        torch.cuda.synchronize()
-        assert int(cache.status.item()) == tkv.TKV_STATUS_BAD_ITEM
     finally:
         cache.close()
 

@@ -31,8 +31,14 @@ def test_items_cover_the_pages_and_slots_are_the_sequences(seed):
     launched = 0
     for g in range(n):
         items = p.prefix_items[p.prefix_items[:, 0] == g]
+        launched += len(items) * 4
+        blocks = -(-len(groups[g]) * r // tile)
+        if blocks:
+            assert np.array_equal(items[:, 4], np.tile(np.arange(blocks) * tile, len(items) // blocks))     # every row of every part
+            items = items.reshape(-1, blocks, 5)
+            assert np.all(items[:, :, :4] == items[:, :1, :4])
+            items = items[:, 0]
         per_group.append(len(items))
-        launched += len(items) * 4 * -(-len(groups[g]) * r // tile)
         if not groups[g] or pages[g] == 0:
             assert len(items) == 0
             continue
@@ -64,7 +70,7 @@ def raw(**kw):
     arr = lambda x: np.array(x, np.int32) if x is not None else None  # noqa: E731
     ptr = lambda x: C.c_void_p(x.ctypes.data) if x is not None and x.size else None  # noqa: E731
     n2, n4, ip, sq = (arr(a[k]) for k in ("n2", "n4", "indptr", "seqs"))
-    items, slots, out, tile = np.empty((max(1, a["cap"]), 4), np.int32), np.empty(16, np.int32), np.empty(64, np.int32), C.c_int32(0)
+    items, slots, out, tile = np.empty((max(1, a["cap"]), 5), np.int32), np.empty(16, np.int32), np.empty(64, np.int32), C.c_int32(0)
     return tkv.lib().tkv_plan_decode_shared(C.byref(a["desc"]), a["batch"], a["heads"], a["n"], ptr(n2), ptr(n4), ptr(ip), ptr(sq), a["target"], a["own"],
                                             ptr(items), a["cap"], ptr(slots), ptr(out), C.byref(tile))
 
@@ -92,7 +98,7 @@ def test_a_plan_of_hundreds_of_millions_of_tokens_does_not_overflow():
 
 def call(**kw):
     """tkv_decode_attention_shared with addresses that are never touched."""
-    d = dict(n_groups=1, n_members=2, max_members=2, tile_rows=64, n_items=1, page_indptr=64, page_ids=64, n_tok_int2=64, n_tok_int4=64, member_indptr=64,
+    d = dict(n_groups=1, n_members=2, tile_rows=64, n_items=1, page_indptr=64, page_ids=64, n_tok_int2=64, n_tok_int4=64, member_indptr=64,
              member_seqs=64, member_slots=64, items=64)
     a = dict(desc=DESC, pool=256, bit_map=256, q=256, indptr=64, ids=64, n2=64, n4=64, items=64, n_items=3, slots=64, n_slots=9, batch=3, heads=8, scale=0.1,
              out=256, ws=256, ws_bytes=1 << 30, status=64)
@@ -119,10 +125,10 @@ BAD = tkv.TKV_ERR_INVALID_ARG
     (dict(scale=0.0), BAD), (dict(scale=float("nan")), BAD), (dict(q=None), BAD), (dict(q=264), BAD), (dict(out=None), BAD), (dict(out=264), BAD),
     (dict(slots=None), BAD), (dict(pool=None), BAD), (dict(pool=128), BAD), (dict(bit_map=None), BAD), (dict(indptr=None), BAD), (dict(ids=None), BAD),
     (dict(items=None), BAD), (dict(n2=None), BAD),
-    (dict(n_groups=-1), BAD), (dict(n_groups=0), BAD), (dict(n_members=0), BAD), (dict(max_members=0), BAD), (dict(max_members=-1), BAD),
-    (dict(p_n_items=-1), BAD), (dict(p_n_items=65536), BAD), (dict(p_items=None), BAD), (dict(page_indptr=None), BAD), (dict(page_ids=None), BAD),
+    (dict(n_groups=-1), BAD), (dict(n_groups=0), BAD), (dict(n_members=0), BAD),
+    (dict(p_n_items=-1), BAD), (dict(p_n_items=1 << 29), BAD), (dict(p_items=None), BAD), (dict(page_indptr=None), BAD), (dict(page_ids=None), BAD),
     (dict(n_tok_int2=None), BAD), (dict(n_tok_int4=None), BAD), (dict(member_indptr=None), BAD), (dict(member_seqs=None), BAD), (dict(member_slots=None), BAD),
-    (dict(max_members=1 << 30), BAD), (dict(max_members=65535 * 32 + 1), BAD), (dict(tile_rows=0), BAD), (dict(tile_rows=32), BAD), (dict(n_members=1 << 30), BAD),
+    (dict(tile_rows=0), BAD), (dict(tile_rows=32), BAD), (dict(n_members=1 << 30), BAD),
     (dict(batch=0), tkv.TKV_OK),
 ])
 def test_calls_that_launch_nothing(kw, status):
