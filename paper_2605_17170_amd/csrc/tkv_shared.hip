@@ -1,15 +1,13 @@
 // tkv_decode_attention_shared: decode attention for sequences that share a long prefix (a system prompt, tool definitions, a
-// document).  The prefix's pages are attended to once for all of its sequences (tkv_prefix_kernel), each sequence's own pages
-// by the split kernel of tkv_decode.hip, and the partials of both are merged by log-sum-exp (tkv_merge_shared_kernel).
+// document).  One launch attends to the prefixes' pages for all sequences of a group together and to each sequence's own pages
+// (tkv_shared_kernel), and one merges the partials by log-sum-exp (tkv_merge_shared_kernel).
 //
 // With one sequence, a page is read for the eight query rows at most that share its kv head, and memory bounds the kernel.
 // With S sequences there are S times as many rows for the same page: arithmetic bounds it, and the page's codes are
-// worth expanding.  A workgroup of four wavefronts owns (work item, kv head, up to 64 query rows); the wavefronts take the
-// item's pages in turn, all rows each, and their results are added in LDS at the end.
+// worth expanding.
 //
 //   K, V  code * scale + zero in fp16, one rounding: the values that tkv_gather_dequant gives a prefill kernel.  The page layout
-//         is that of the matrix operands, so a lane expands exactly what it feeds to the MFMAs, and nothing but the scales and
-//         zero-points goes through LDS.
+//         is that of the matrix operands, so a lane expands exactly what some lane feeds to the MFMAs.
 //   QK^T  D[token, row] = sum_c K[token, c] q[row, c] (v_mfma_f32_16x16x32_f16), q in fp16, each row scaled by a power of two
 //         of its own that its softmax factor takes back: bf16 has 8 bits, so q is exact down to 2^-31 of the row's largest.
 //   PV    D[row, channel] = sum_token W[row, token] V[token, channel]: the results of QK^T lie where PV wants its operand.
@@ -18,6 +16,23 @@
 //         against ones: of the rounded weights, as the numerators.
 // All sums are 32 bits.  K, V and W carry 11 bits where the split kernel carries what its fp32 results need; the output is
 // bf16, which has 8.
+//
+// Workgroups of eight wavefronts, one a compute unit (196 to 256 registers), do one of three things:
+//   own pages       a wavefront for each (work item, kv head), operands in registers, rows = the query heads of the kv head
+//   16 rows         the wavefronts take an item's pages in turn, operands in registers; their results are added in LDS
+//   64, 128 rows    two pages a step, each expanded once into LDS by the four wavefronts that attend to it with 16 or 32 rows each;
+//                   the next two are expanded and the ones after them requested between QK^T and the softmax of a step
+// Which of the latter two is planned by size (tkv_plan_decode_shared).
+//
+// What bounds it: 128 rows, a step 2.5 us, of which the SIMD's MFMAs take 1.09, its other vector instructions 1.0 (expansion and
+// softmax about half each) and LDS 0.9 (256 KiB read, 64 written).  MFMAs and vector instructions of two wavefronts overlap
+// by a third at most (16 MFMAs beside 64 multiply-adds 202 ns, alone 128 and 120).  256 rows over 32768 tokens, 8 kv heads: 55 us of
+// steps and some 12 of loads that wait for one another, first expansion, and results on their way out; 63.7 us with the merge, 544 TFLOP/s
+// (a large product of the library reaches 1100).  16 rows: the chain item -> group -> page ids -> codes -> softmax -> sums in LDS; a page for
+// each wavefront takes 8 us.
+// Tried and not kept: 64 rows a wavefront in registers (copies between register files, 85 us instead of 63.7), 32 rows a wavefront with pages
+// of its own (130 registers spilled, 23 us instead of 12 to 15), the wavefronts of a SIMD half a step apart and raised priorities
+// (no change), MFMAs and vector instructions interleaved by hand (66 to 70 us).
 #include <hip/hip_runtime.h>
 
 #include <type_traits>
@@ -943,9 +958,10 @@ int tkv_launch_shared(const tkv_desc *desc, const void *pool, const uint8_t *bit
         a.ml_ws[k] = ws[k] + (size_t)n[k] * n_q_heads * kHeadDim;
     }
     a.status = status;
-    a.own_blocks = (int)(((int64_t)n_items * desc->n_kv_heads + kWaves - 1) / kWaves);
+    const int64_t own_blocks = ((int64_t)n_items * desc->n_kv_heads + kWaves - 1) / kWaves;
+    a.own_blocks = (int)own_blocks;
     const int per = prefix->n_items > 0 ? prefix->tile_rows : 16;
-    const int64_t blocks = a.own_blocks + (int64_t)prefix->n_items * desc->n_kv_heads;
+    const int64_t blocks = own_blocks + (int64_t)prefix->n_items * desc->n_kv_heads;
     if (blocks > INT32_MAX) return TKV_ERR_INVALID_ARG;
     if (blocks > 0) {
         const bool kc = desc->int2_key_axis == TKV_KEYS_PER_CHANNEL;

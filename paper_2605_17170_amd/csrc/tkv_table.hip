@@ -14,8 +14,7 @@
 // What bounds it is latency: a few hundred KiB move at most.  One workgroup forms the sums, a sequence and 64 tokens a thread, and
 // asks for everything it may need (open pages, tops of the free lists) before the first of them.
 //   up to 1024 sequences, 8192 tokens and 1024 work entries: one launch, which also updates rows and places tokens.  32 sequences
-//     with a token each 5.7 us (an empty kernel 4.4), 200 with five 6.9; with launches of their own for sums, pages given back,
-//     rows and tokens such calls take 17.
+//     with a token each 5.7 us (an empty kernel 3.9 to 4.4), 200 with five 6.9.
 //   up to 1024 sequences and 65536 tokens: rows and tokens in a second launch over many workgroups.  6 prompts with 63 thousand tokens
 //     11.6 us (in four launches 15.6), 12 with 9 thousand 10.9 (15.2).
 //   beyond: four launches; tags to bit masks, sums in a loop, pages given back, rows and tokens.

@@ -86,6 +86,8 @@ class tkv_prefix(C.Structure):
         n = n_tok_int2.numel()
         assert all(t.element_size() == 4 for t in tensors) and n_tok_int4.numel() == n and page_indptr.numel() == member_indptr.numel() == n + 1
         assert member_seqs.numel() == member_slots.numel() and items.numel() % 5 == 0
+        if not hasattr(max_members, "tile_rows"):
+            raise ValueError("max_members: as tkv_plan_decode_shared gives it, with the rows of the items")
         prefix = cls(n, member_seqs.numel(), max_members.tile_rows, items.numel() // 5, *(_dev(t) for t in tensors))
         prefix.tensors = tensors
         return prefix

@@ -133,3 +133,13 @@ BAD = tkv.TKV_ERR_INVALID_ARG
 ])
 def test_calls_that_launch_nothing(kw, status):
     assert call(**kw) == status
+
+
+def test_a_prefix_wants_the_plan_s_own_number_of_members():
+    import torch
+    i32 = lambda n: torch.zeros(n, dtype=torch.int32)  # noqa: E731
+    p = plan(2, 4, [100], [100], [[0, 1]], 10)
+    prefix = tkv.tkv_prefix.make(i32(2), i32(4), i32(1), i32(1), i32(2), i32(2), i32(2), torch.from_numpy(p.prefix_items), p.max_members)
+    assert prefix.n_items == len(p.prefix_items) and prefix.tile_rows == p.max_members.tile_rows
+    with pytest.raises(ValueError):
+        tkv.tkv_prefix.make(i32(2), i32(4), i32(1), i32(1), i32(2), i32(2), i32(2), torch.from_numpy(p.prefix_items), 2)
