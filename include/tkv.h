@@ -597,7 +597,7 @@ size_t tkv_table_workspace_bytes(int32_t n_seqs, int32_t n_tokens);
  * (TKV_STATUS_POOL_EXHAUSTED), or max_pages or max_work does not suffice
  * (TKV_STATUS_CAPACITY), the table stays as it is, n_work and token_indptr are
  * 0, no slot is named, and slot_ids and positions are -1.
- * One launch for up to 1024 sequences and 8192 tokens, else up to four.
+ * One launch for up to 1024 sequences and 6144 tokens, else up to four.
  */
 int tkv_table_append(const tkv_desc *desc, const tkv_table *table, const int32_t *keep_int2, const int32_t *keep_int4,
                      const int32_t *n_new, const uint8_t *tag_bits, int32_t n_tokens,

@@ -13,8 +13,8 @@
 //
 // What bounds it is latency: a few hundred KiB move at most.  One workgroup forms the sums, a sequence and 64 tokens a thread, and
 // asks for everything it may need (open pages, tops of the free lists) before the first of them.
-//   up to 1024 sequences, 8192 tokens and 1024 work entries: one launch, which also updates rows and places tokens.  32 sequences
-//     with a token each 5.7 us (an empty kernel 3.9 to 4.4), 200 with five 6.9.
+//   up to 1024 sequences, 6144 tokens and 1024 work entries: one launch, which also updates rows and places tokens.  32 sequences
+//     with a token each 5.7 us (an empty kernel 3.9 to 4.4), 200 with five 6.9; 9 thousand tokens would take 12.7, and 11.0 in two launches.
 //   up to 1024 sequences and 65536 tokens: rows and tokens in a second launch over many workgroups.  6 prompts with 63 thousand tokens
 //     11.6 us (in four launches 15.6), 12 with 9 thousand 10.9 (15.2).
 //   beyond: four launches; tags to bit masks, sums in a loop, pages given back, rows and tokens.
@@ -245,7 +245,7 @@ __device__ __forceinline__ Workspace workspace_of(const TableArgs &a)
 // ---- one workgroup for the sums --------------------------------------------------------------------------------------
 // PLACE: the same workgroup updates the rows and places the tokens.  Otherwise tkv_table_place_kernel does, from the workspace, the
 // other workgroups of this launch clear the lists, and with `push` 0 a launch between the two gives the pages back.
-constexpr int kPlanSeqs = kThreads, kPlanTokens = 64 * kThreads, kSmallTokens = 8 * kThreads, kSmallWork = kThreads;
+constexpr int kPlanSeqs = kThreads, kPlanTokens = 64 * kThreads, kSmallTokens = 6 * kThreads, kSmallWork = kThreads;
 __device__ __forceinline__ void clear_lists(const TableArgs &a, int64_t i, int64_t step)
 {
     const int64_t n = (int64_t)a.max_work * kPageTokens;
