@@ -153,7 +153,6 @@ int32_t tkv_plan_decode_shared(const tkv_desc *desc, int32_t batch, int32_t n_q_
     if (r != 1 && r != 2 && r != 4 && r != 8) return TKV_ERR_BAD_SHAPE;
     if (member_indptr[0] != 0) return TKV_ERR_INVALID_ARG;
     int32_t largest = 0;
-    int64_t longest = 1;
     for (int32_t g = 0; g < n_groups; ++g) {
         const int64_t members = (int64_t)member_indptr[g + 1] - member_indptr[g];
         if (members < 0 || members > batch || n_tok_int2[g] < 0 || n_tok_int4[g] < 0) return TKV_ERR_INVALID_ARG;
@@ -175,7 +174,8 @@ int32_t tkv_plan_decode_shared(const tkv_desc *desc, int32_t batch, int32_t n_q_
         // The own items' workgroups (a wavefront for each item and kv head) are launched first.  Either the prefixes' fill the compute units
         // that are left, or all, and begin behind them.
         const int64_t own = std::min(((int64_t)n_own_items * desc->n_kv_heads + 7) / 8, (int64_t)target_cus), spare = target_cus - own;
-        auto pages = [&](int32_t g) { return ((int64_t)n_tok_int2[g] + kPageTokens - 1) / kPageTokens + ((int64_t)n_tok_int4[g] + kPageTokens - 1) / kPageTokens; };
+        auto pages_of = [](int32_t n) { return ((int64_t)n + kPageTokens - 1) / kPageTokens; };
+        auto pages = [&](int32_t g) { return pages_of(n_tok_int2[g]) + pages_of(n_tok_int4[g]); };
         // Rows of a workgroup.  With 16 its wavefronts work on a page each, eight a step; with 64 and 128 they expand pages together, two
         // a step.  us, 16 / 64 / 128 rows: 32 rows over 32000 tokens, 8 kv heads 21 / 26 / 33; 64 over 4000 12 / 16 / 18, 11000 18.0 / 18.4 / 21.6,
         // 32000 36 / 30 / 38; 128 over 1000 10 / 15 / 19, 8000 28 / 23 / 25; 256 over 1000 19 / 17 / 18, 8000 37 / 34 / 36, 32768 - / - / 61: about
@@ -200,36 +200,58 @@ int32_t tkv_plan_decode_shared(const tkv_desc *desc, int32_t batch, int32_t n_q_
             }
         }
         *tile_rows_out = rows;
-        auto units = [&](int32_t g) -> int64_t { return member_indptr[g + 1] == member_indptr[g] ? 0 : (pages(g) + unit - 1) / unit; };
         auto row_blocks = [&](int32_t g) { return ((int64_t)(member_indptr[g + 1] - member_indptr[g]) * r + rows - 1) / rows; };
-        for (int32_t g = 0; g < n_groups; ++g) longest = std::max(longest, units(g));
-        auto workgroups = [&](int64_t per) {
-            int64_t n = 0;
-            for (int32_t g = 0; g < n_groups; ++g) n += (units(g) + per - 1) / per * row_blocks(g) * desc->n_kv_heads;
-            return n;
+        // Steps of a group, of either width by themselves or of the whole list.
+        auto units = [&](int32_t g, int w, bool split) -> int64_t {
+            const int64_t p2 = pages_of(n_tok_int2[g]), p4 = pages_of(n_tok_int4[g]), n = split ? (w ? p4 : p2) : (w ? 0 : p2 + p4);
+            return member_indptr[g + 1] == member_indptr[g] ? 0 : (n + unit - 1) / unit;
         };
-        int64_t lo = 1, hi = longest;
-        while (lo < hi) {
-            const int64_t mid = lo + (hi - lo) / 2;
-            if (workgroups(mid) <= target) hi = mid;
-            else lo = mid + 1;
+        // The fewest steps of an item with which the workgroups fit.
+        auto shortest = [&](bool split) {
+            int64_t lo = 1, hi = 1;
+            for (int32_t g = 0; g < n_groups; ++g) hi = std::max({hi, units(g, 0, split), units(g, 1, split)});
+            while (lo < hi) {
+                const int64_t mid = lo + (hi - lo) / 2;
+                int64_t n = 0;
+                for (int32_t g = 0; g < n_groups; ++g)
+                    n += ((units(g, 0, split) + mid - 1) / mid + (units(g, 1, split) + mid - 1) / mid) * row_blocks(g) * desc->n_kv_heads;
+                if (n <= target) hi = mid;
+                else lo = mid + 1;
+            }
+            return lo;
+        };
+        // An item with pages of both widths begins twice, which takes about as long as a step; parts of one width each may be longer, or more
+        // than the target has compute units for.
+        const int64_t whole = shortest(false), apart = shortest(true);
+        bool split = apart <= whole + 1;
+        if (split) {
+            int64_t n = 0;
+            for (int32_t g = 0; g < n_groups; ++g)
+                n += ((units(g, 0, true) + apart - 1) / apart + (units(g, 1, true) + apart - 1) / apart) * row_blocks(g) * desc->n_kv_heads;
+            split = n <= target;
         }
+        const int64_t most = split ? apart : whole;
         int64_t n_items = 0, n_slots = n_own_items;
         std::vector<int32_t> parts((size_t)n_groups, 0);
         for (int32_t g = 0; g < n_groups; ++g) {
-            const int64_t all = units(g), n = (all + lo - 1) / lo;
+            int64_t n = 0;   // parts so far
+            for (int w = 0; w < 2; ++w) {
+                const int64_t all = units(g, w, split), count = (all + most - 1) / most;
+                const int64_t begin = w ? pages_of(n_tok_int2[g]) : 0, end = split && w == 0 ? pages_of(n_tok_int2[g]) : pages(g);
+                if (n_items + count * row_blocks(g) > capacity) return TKV_ERR_CAPACITY;
+                // workgroups of the same pages follow one another: with eight kv heads they lie on one XCD, whose L2 they share
+                for (int64_t k = 0; k < count; ++k)
+                    for (int64_t z = 0; z < row_blocks(g); ++z) {
+                        int32_t *it = items_out + 5 * n_items++;
+                        it[0] = g;
+                        it[1] = (int32_t)(begin + unit * (all * k / count));
+                        it[2] = (int32_t)std::min(end, begin + unit * (all * (k + 1) / count));
+                        it[3] = (int32_t)(n + k);
+                        it[4] = (int32_t)(rows * z);
+                    }
+                n += count;
+            }
             parts[(size_t)g] = (int32_t)n;
-            if (n_items + n * row_blocks(g) > capacity) return TKV_ERR_CAPACITY;
-            // workgroups of the same pages follow one another: with eight kv heads they lie on one XCD, whose L2 they share
-            for (int64_t k = 0; k < n; ++k)
-                for (int64_t z = 0; z < row_blocks(g); ++z) {
-                    int32_t *it = items_out + 5 * n_items++;
-                    it[0] = g;
-                    it[1] = (int32_t)(unit * (all * k / n));
-                    it[2] = (int32_t)std::min(pages(g), unit * (all * (k + 1) / n));
-                    it[3] = (int32_t)k;
-                    it[4] = (int32_t)(rows * z);
-                }
             for (int32_t m = member_indptr[g]; m < member_indptr[g + 1]; ++m) next[(size_t)member_seqs[m]] += (int32_t)n;
             n_slots += n * (member_indptr[g + 1] - member_indptr[g]);
             if (n_slots > INT32_MAX) return TKV_ERR_INVALID_ARG;

@@ -28,7 +28,7 @@ def test_items_cover_the_pages_and_slots_are_the_sequences(seed):
     tile = p.max_members.tile_rows
     assert tile in (16, 64, 128)
     unit, per_group = 8 if tile == 16 else 2, []
-    launched = 0
+    launched, split = 0, []
     for g in range(n):
         items = p.prefix_items[p.prefix_items[:, 0] == g]
         launched += len(items) * 4
@@ -44,8 +44,11 @@ def test_items_cover_the_pages_and_slots_are_the_sequences(seed):
             continue
         assert items[0, 1] == 0 and items[-1, 2] == pages[g] and np.array_equal(items[1:, 1], items[:-1, 2]) and np.all(items[:, 2] > items[:, 1])
         assert np.array_equal(items[:, 3], np.arange(len(items)))
-        units = -(-(items[:, 2] - items[:, 1]) // unit)
-        assert units.max() - units.min() <= 1 and np.all(items[:-1, 2] % unit == 0)
+        wide = -(-n2[g] // 64)      # first page of the second width
+        split.append(not np.any((items[:, 1] < wide) & (items[:, 2] > wide)) and 0 < wide < pages[g])
+        for part in [items[items[:, 1] < wide], items[items[:, 1] >= wide]] if split[-1] else [items]:
+            units = -(-(part[:, 2] - part[:, 1]) // unit)
+            assert units.max() - units.min() <= 1 and np.all((part[:-1, 2] - part[0, 1]) % unit == 0)
     fewest = sum(4 * -(-len(groups[g]) * r // tile) for g in range(n) if per_group[g])
     assert launched <= max(target, fewest)
     # slots of a sequence: one of each item of each of its groups, all different, side by side, behind the own ones
