@@ -501,10 +501,10 @@ int32_t tkv_plan_decode_shared(const tkv_desc *desc, int32_t batch, int32_t n_q_
                                int32_t *member_slots_out, int32_t *seq_slot_indptr_out, int32_t *tile_rows_out);
 /*
  * tkv_decode_attention over each sequence's prefixes and its own tokens
- * together.  Pages are dequantised to fp16 as tkv_gather_dequant does (the
- * values that a prefill over them saw) and attended to with fp16 softmax
- * weights and 32-bit sums.  The output is bf16, as the projection behind it
- * takes it.  A sequence without tokens gives zeros.
+ * together.  Values, and the keys of items of 64 and 128 rows, are dequantised
+ * to fp16 as tkv_gather_dequant does (as a prefill over them saw them); other
+ * keys are not rounded.  Softmax weights are fp16, sums 32 bits.  The output is
+ * bf16, as the projection behind it takes it.  A sequence without tokens gives zeros.
  *   q, page_indptr .. n_items, sm_scale   as for tkv_decode_attention (own tokens; n_items may be 0)
  *   prefix         host struct of device arrays, above; n_items may be 0
  *   slot_indptr    device i32[2*(batch+1)]: seq_item_indptr_out of tkv_plan_decode, then seq_slot_indptr_out
@@ -514,11 +514,12 @@ int32_t tkv_plan_decode_shared(const tkv_desc *desc, int32_t batch, int32_t n_q_
  *   status         device i32, may be NULL; bits as for tkv_decode_attention.  Members outside the batch, slots outside
  *                  [n_items, n_slots) and items outside the groups raise TKV_STATUS_BAD_ITEM: what they name is not stored,
  *                  and the sequence reads what the workspace held before
- * Preconditions: stored scales and zeros finite, and values within fp16; with
- * TKV_KEYS_PER_CHANNEL every n_tok_int2 a multiple of 32.  q may hold any
- * finite values; a query head of NaN or infinities gives NaN and leaves the
- * others alone.  n_q_heads / n_kv_heads is 1, 2, 4 or 8.  Two launches on
- * `stream`: attention, then the merge.
+ * Preconditions: stored scales and zeros finite, values within fp16, and so 14
+ * times the scales of INT4 keys and twice those of INT2 keys; with
+ * TKV_KEYS_PER_CHANNEL every n_tok_int2 a multiple of 32.  q may hold any finite
+ * values; a query head of NaN or infinities gives NaN and leaves the others
+ * alone.  n_q_heads / n_kv_heads is 1, 2, 4 or 8.  Two launches on `stream`:
+ * attention, then the merge.
  */
 int tkv_decode_attention_shared(const tkv_desc *desc, const void *pool, const uint8_t *bit_map, const void *q,
                                 const int32_t *page_indptr, const int32_t *page_ids,

@@ -8,13 +8,18 @@
 //
 //   K, V  code * scale + zero in fp16, one rounding: the values that tkv_gather_dequant gives a prefill kernel.  The page layout
 //         is that of the matrix operands, so a lane expands exactly what some lane feeds to the MFMAs.
+//         Own pages and items of 16 rows hold K exactly: (code - 1) * scale + (zero + scale), the products in one fp16 number (INT2)
+//         or two (INT4), zero and scale as stored against the sums of q, or as keys of their own.  Logits of 20 and more make
+//         2^-12 of a key up to 2^-8 of a weight, and with few rows one such row is seen in the result: 4 sequences over 1500 tokens
+//         were off by up to 0.0027 in norm where bf16 alone gives 0.0019, and are by 0.0019 (10.1 -> 10.4 us; 13 over 5000 12.5 -> 12.9).
+//         With 64 and 128 rows it would cost 5 % of a step for INT2 and 45 % for INT4, where the results are off by 0.0017 to 0.0018.
 //   QK^T  D[token, row] = sum_c K[token, c] q[row, c] (v_mfma_f32_16x16x32_f16), q in fp16, each row scaled by a power of two
-//         of its own that its softmax factor takes back: bf16 has 8 bits, so q is exact down to 2^-31 of the row's largest.
+//         of its own that its softmax factor takes back: bf16 has 8 bits, so q is exact down to 2^-26 of the row's largest.
 //   PV    D[row, channel] = sum_token W[row, token] V[token, channel]: the results of QK^T lie where PV wants its operand.
 //         W = 2^(logit - m + 8) in fp16, m a reference that follows the row's maximum lazily (within 2^4), so that W stays
 //         below 2^12 and weights down to 2^-22 of the largest are exact to half a step.  The denominators are one more MFMA
 //         against ones: of the rounded weights, as the numerators.
-// All sums are 32 bits.  K, V and W carry 11 bits where the split kernel carries what its fp32 results need; the output is
+// All sums are 32 bits.  V, W and the expanded K carry 11 bits where the split kernel carries what its fp32 results need; the output is
 // bf16, which has 8.
 //
 // Workgroups of eight wavefronts, one a compute unit (196 to 256 registers), do one of three things:
@@ -100,6 +105,16 @@ template <int BITS> __device__ __forceinline__ half8 dequant8(uint32_t x, uint32
         return as_half8(dequant2<4, 0>(x, s0, z0, mg), dequant2<4, 4>(x, s1, z1, mg), dequant2<4, 0>(y, s2, z2, mg), dequant2<4, 4>(y, s3, z3, mg));
     }
 }
+// Codes less one times s, rounded to fp16, and in `rest` what the rounding took, which is exact; with two bits nothing: -s, 0, s, 2 s.
+template <int BITS, int POS> __device__ __forceinline__ uint32_t times2(uint32_t x, uint32_t s, const Magic &mg, uint32_t &rest)
+{
+    constexpr uint32_t m = ((1u << BITS) - 1u) * 0x00010001u << POS;
+    constexpr float base = (1024 >> POS) + 1;
+    const half2_t k = {(_Float16)base, (_Float16)base}, sv = __builtin_bit_cast(half2_t, s);
+    const half2_t c = __builtin_bit_cast(half2_t, (x & m) | mg.e[POS / 2]) - k, p = c * sv;
+    if constexpr (BITS == 4) rest = __builtin_bit_cast(uint32_t, __builtin_elementwise_fma(c, sv, -p));
+    return __builtin_bit_cast(uint32_t, p);
+}
 // Half i & 1 of v, twice.
 __device__ __forceinline__ uint32_t twice(uint32_t v, int i) { return __builtin_amdgcn_perm(v, v, (i & 1) ? 0x07060706u : 0x05040504u); }
 // Orders this wavefront's LDS writes before its later LDS reads: LDS operations of a wavefront execute in order.
@@ -149,6 +164,7 @@ struct SharedArgs {
 
 template <int NT> struct Rows {   // NT tiles of 16 query rows
     half8 q[NT][4];        // operand of QK^T for a group of channels: row lane % 16, channels (k, k + 4) of octet lane / 16
+    half8 sums[NT];        // of q over the four groups, row lane % 16, twice: rounded (lanes 0 .. 15), what that took (16 .. 31), 0
     floatx4 acc[NT][8];    // row 4 * (lane / 16) + i, channel 16 * tile + lane % 16
     floatx4 sum[NT];       // denominators, rows as in acc
     float m[NT];           // reference of row lane % 16, log2 units, -inf at first
@@ -189,7 +205,7 @@ template <int NT> __device__ __forceinline__ void load_q(Rows<NT> &rows, int n, 
     int top = big[0] > big[1] ? big[0] : big[1];
     top = max(top, __shfl_xor(top, 16));
     top = max(top, __shfl_xor(top, 32));
-    int E = top <= 0x80 ? 0 : 15 - ((top >> 7) - 127);   // the largest lies in [2^14, 2^15)
+    int E = top <= 0x80 ? 0 : 10 - ((top >> 7) - 127);   // the largest lies in [2^9, 2^10), and a sum over a group below 2^15
     E = E > 100 ? 100 : (E < -100 ? -100 : E);
     const float f = ldexpf(1.0f, E);
     rows.kappa[n] = kappa * ldexpf(1.0f, -E);
@@ -197,6 +213,27 @@ template <int NT> __device__ __forceinline__ void load_q(Rows<NT> &rows, int n, 
     for (int g = 0; g < 4; ++g)
         rows.q[n][g] = as_half8(pack_h2(bf16_lo(x[g].x) * f, bf16_lo(x[g].z) * f), pack_h2(bf16_hi(x[g].x) * f, bf16_hi(x[g].z) * f),
                                 pack_h2(bf16_lo(x[g].y) * f, bf16_lo(x[g].w) * f), pack_h2(bf16_hi(x[g].y) * f, bf16_hi(x[g].w) * f));
+}
+
+__device__ __forceinline__ half8 ones() { return as_half8(0x3c003c00u, 0x3c003c00u, 0x3c003c00u, 0x3c003c00u); }
+// Sums of q over the groups of channels, for what K's zero-points add.
+template <int NT> __device__ __forceinline__ void sum_q(Rows<NT> &rows, int n, int lane)
+{
+    float sum[4];
+#pragma unroll
+    for (int g = 0; g < 4; ++g) {
+        sum[g] = 0.0f;
+#pragma unroll
+        for (int k = 0; k < 8; ++k) sum[g] += (float)rows.q[n][g][k];
+        sum[g] += __shfl_xor(sum[g], 16);
+        sum[g] += __shfl_xor(sum[g], 32);
+    }
+    const int q4 = lane >> 4;
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+        const _Float16 hi = (_Float16)sum[k & 3], lo = (_Float16)(sum[k & 3] - (float)hi);
+        rows.sums[n][k] = q4 == 0 ? hi : (q4 == 1 ? lo : (_Float16)0.0f);
+    }
 }
 
 // ---- codes to operands -----------------------------------------------------------------------------------------------
@@ -207,6 +244,26 @@ template <int BITS> __device__ __forceinline__ half8 k_operand(uint32_t w, const
     // INT4: codes k and k + 4 lie in the halves of the word; INT2: the bytes of this lane's octet move there
     const uint32_t x = BITS == 4 ? w : __builtin_amdgcn_perm(w, w, (q4 & 1) ? 0x0c070c06u : 0x0c050c04u);
     return dequant8<BITS>(x, s[0], s[1], s[2], s[3], z[0], z[1], z[2], z[3], mg);
+}
+// The same without the zero-point, of codes less one; `rest`: see times2.
+template <int BITS> __device__ __forceinline__ half8 k_products(uint32_t w, const uint32_t (&s)[4], int q4, const Magic &mg, half8 &rest)
+{
+    uint32_t p[4], r[4] = {};
+    if constexpr (BITS == 2) {
+        const uint32_t x = __builtin_amdgcn_perm(w, w, (q4 & 1) ? 0x0c070c06u : 0x0c050c04u);
+        p[0] = times2<2, 0>(x, s[0], mg, r[0]);
+        p[1] = times2<2, 2>(x, s[1], mg, r[1]);
+        p[2] = times2<2, 4>(x, s[2], mg, r[2]);
+        p[3] = times2<2, 6>(x, s[3], mg, r[3]);
+    } else {
+        const uint32_t y = w >> 8;
+        p[0] = times2<4, 0>(w, s[0], mg, r[0]);
+        p[1] = times2<4, 4>(w, s[1], mg, r[1]);
+        p[2] = times2<4, 0>(y, s[2], mg, r[2]);
+        p[3] = times2<4, 4>(y, s[3], mg, r[3]);
+    }
+    rest = as_half8(r[0], r[1], r[2], r[3]);
+    return as_half8(p[0], p[1], p[2], p[3]);
 }
 // Scales (or zero-points) of per-channel INT2 keys in that order; `plane`: 32 chunks of 8, [block][group][quarter].
 __device__ __forceinline__ void channel_meta(const uint4 *plane, int blk, int g, int q4, uint32_t (&s)[4])
@@ -303,7 +360,6 @@ template <int NT> __device__ __forceinline__ void weigh(Rows<NT> &rows, floatx4 
             P[n][b] = as_half8(w[0], w[1], w[2], w[3]);
         }
 }
-__device__ __forceinline__ half8 ones() { return as_half8(0x3c003c00u, 0x3c003c00u, 0x3c003c00u, 0x3c003c00u); }
 
 // ---- the pages of a list, 64 at a time in registers: lane l holds page number base + l ------------------------------------
 struct PageList {
@@ -385,38 +441,52 @@ __device__ __forceinline__ void attend_page(const PageRegs<BITS> &r, int n_valid
     // this lane's chunk of the V planes: lane % 32 = (block, quad, group)
     meta.v[lane] = n_valid < kPageTokens ? mask_meta(r.vm, (lane >> 4) & 1, (lane >> 2) & 3, n_valid) : r.vm;
     lds_order();
+    // K = (code - 1) * s + (z + s): the products by themselves are exact, and so are z and s, which stand for a token and a group (one MFMA
+    // against the sums of q) or for a channel and 32 tokens (as keys of their own, of which all tokens have the same)
     floatx4 S[NT][4];   // token 16 e + 4 q4 + i, row r16
 #pragma unroll
-    for (int n = 0; n < NT; ++n)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) S[n][e] = floatx4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
     for (int b = 0; b < 2; ++b) {
+        uint32_t s[4][4];
         uint2 sc[2], zc[2];
-        if constexpr (!(KC && BITS == 2))
+        if constexpr (KC && BITS == 2) {
+#pragma unroll
+            for (int n = 0; n < NT; ++n) S[n][2 * b] = floatx4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int g = 0; g < 4; ++g) {
+                uint32_t z[4];
+                channel_meta(meta.k, b, g, q4, s[g]);
+                channel_meta(meta.k + 32, b, g, q4, z);
+#pragma unroll
+                for (int n = 0; n < NT; ++n) {
+                    S[n][2 * b] = mfma(as_half8(z[0], z[1], z[2], z[3]), rows.q[n][g], S[n][2 * b]);
+                    S[n][2 * b] = mfma(as_half8(s[g][0], s[g][1], s[g][2], s[g][3]), rows.q[n][g], S[n][2 * b]);
+                }
+            }
+#pragma unroll
+            for (int n = 0; n < NT; ++n) S[n][2 * b + 1] = S[n][2 * b];
+        } else {
 #pragma unroll
             for (int e = 0; e < 2; ++e) {
                 sc[e] = reinterpret_cast<const uint2 *>(meta.k)[32 * b + 16 * e + r16];
                 zc[e] = reinterpret_cast<const uint2 *>(meta.k + 32)[32 * b + 16 * e + r16];
-            }
 #pragma unroll
-        for (int g = 0; g < 4; ++g) {
-            uint32_t s[4], z[4];
-            if constexpr (KC && BITS == 2) {
-                channel_meta(meta.k, b, g, q4, s);
-                channel_meta(meta.k + 32, b, g, q4, z);
-            }
-#pragma unroll
-            for (int e = 0; e < 2; ++e) {
-                if constexpr (!(KC && BITS == 2)) {
-                    s[0] = s[1] = s[2] = s[3] = twice(g < 2 ? sc[e].x : sc[e].y, g);
-                    z[0] = z[1] = z[2] = z[3] = twice(g < 2 ? zc[e].x : zc[e].y, g);
-                }
-                const half8 A = k_operand<BITS>(word_of(r.kw[2 * b + e], g), s, z, q4, mg);
-#pragma unroll
-                for (int n = 0; n < NT; ++n) S[n][2 * b + e] = mfma(A, rows.q[n][g], S[n][2 * b + e]);
+                for (int n = 0; n < NT; ++n)
+                    S[n][2 * b + e] = mfma(as_half8(zc[e].x, zc[e].y, sc[e].x, sc[e].y), rows.sums[n], floatx4{0.f, 0.f, 0.f, 0.f});
             }
         }
+#pragma unroll
+        for (int g = 0; g < 4; ++g)
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                if constexpr (!(KC && BITS == 2)) s[g][0] = s[g][1] = s[g][2] = s[g][3] = twice(g < 2 ? sc[e].x : sc[e].y, g);
+                half8 rest;
+                const half8 A = k_products<BITS>(word_of(r.kw[2 * b + e], g), s[g], q4, mg, rest);
+#pragma unroll
+                for (int n = 0; n < NT; ++n) {
+                    S[n][2 * b + e] = mfma(A, rows.q[n][g], S[n][2 * b + e]);
+                    if constexpr (BITS == 4) S[n][2 * b + e] = mfma(rest, rows.q[n][g], S[n][2 * b + e]);
+                }
+            }
     }
     after_qk();
     half8 P[NT][2];
@@ -692,6 +762,7 @@ template <bool KC, bool THROUGH, class L> __device__ __forceinline__ void own_it
         PageList list;
         fetch_list(cx, list, 0);
         load_q(rows, 0, a.q + ((size_t)sq * n_q_heads + kvh * R + (r16 & (R - 1))) * kHeadDim, a.kappa, lane);
+        sum_q(rows, 0, lane);
         run_list<1, KC>(cx, list, rows, lds.own[wave].meta);
     }
     const size_t at = (size_t)slot * n_q_heads + kvh * R;
@@ -767,6 +838,7 @@ template <int MODE, bool KC> __device__ __forceinline__ void prefix_item(const S
             int seq = row < n_rows ? a.p.member_seqs[m0 + (row >> a.log2_r)] : 0;
             if (seq < 0 || seq >= a.batch) seq = 0;   // nothing of it is stored
             load_q(rows, n, a.q + ((size_t)seq * n_q_heads + kvh * R + (row & (R - 1))) * kHeadDim, a.kappa, lane);
+            if constexpr (MODE == 0) sum_q(rows, n, lane);
         }
     }
     if constexpr (MODE == 0) {

@@ -1,7 +1,7 @@
 """tkv_decode_attention_shared against attention in 64 bits over the values that stand in the cache.
 
 Tolerance.  With p the softmax weights and dl the largest error of a logit, a weighted mean of V is off by at most
-(e^(2 dl) - 1) * sum p |V - out| <= 2.2 dl (sum p |V| + |out|).  K is rounded to fp16, half a step 2^-11 of each value: dl <=
+(e^(2 dl) - 1) * sum p |V - out| <= 2.2 dl (sum p |V| + |out|).  K is rounded (not for own tokens and items of 16 rows) to fp16, half a step 2^-11 of each value: dl <=
 scale * sum |q K| * 2^-11 (the 32-bit sums add 2^-17 of the same sum).  Weights and V are rounded to fp16: 2 * 2^-11 of sum p |V|,
 the denominator by none of its own (it sums the rounded weights).  Then one rounding to bf16, 2^-8 of the result."""
 import numpy as np
@@ -22,9 +22,10 @@ def _oracle():
     tkv_oracle.build()
 
 
-def build(seed, prefixes, own, kv_heads, key_axis=0, f4=0.4, fill=0xFF, shuffle_seed=3):
+def build(seed, prefixes, own, kv_heads, key_axis=0, f4=0.4, fill=0xFF, shuffle_seed=3, k_exp=0):
     """A cache of prefix lists and own lists; (cache, K, V in 64 bits per list)."""
     _, K, V, bits = gc.random_case(seed, list(prefixes) + list(own), kv_heads, kv_heads, f4=f4)
+    K = ((wl.bf16_bits_to_f32(K).astype(np.float32) * np.float32(2.0 ** k_exp)).view(np.uint32) >> 16).astype(np.uint16)
     cache = harness.PagedCache(kv_heads, bits, DEV, pool_factor=1.3, shuffle_seed=shuffle_seed, fill=fill, key_axis=key_axis)
     gc.gpu_append(cache, K, V)
     if key_axis:
@@ -37,8 +38,10 @@ def build(seed, prefixes, own, kv_heads, key_axis=0, f4=0.4, fill=0xFF, shuffle_
     return cache, np.split(np.asarray(Kh, np.float64), ends), np.split(np.asarray(Vh, np.float64), ends)
 
 
-def reference(q, Ks, Vs, groups, kv_heads):
-    """(result, tolerance) [batch, heads, 128] in 64 bits; q bf16 bits."""
+def reference(q, Ks, Vs, groups, kv_heads, rounded=True):
+    """(result, tolerance) [batch, heads, 128] in 64 bits; q bf16 bits.  rounded: keys are fp16 numbers, and a logit is off by half
+    a step of each; otherwise by the 32-bit sums of (code - 1) s + (z + s), whose parts are at most three times the largest key of
+    a group or of a channel's block, 2^-24 for each of 128 channels."""
     n, f = len(groups), wl.bf16_bits_to_f32(q).astype(np.float64)
     batch, heads = f.shape[:2]
     r = heads // kv_heads
@@ -53,6 +56,9 @@ def reference(q, Ks, Vs, groups, kv_heads):
         p = torch.softmax(logits, -1)
         o, size = torch.matmul(p, V), torch.matmul(p, V.abs())
         dl = (torch.matmul(x.abs(), K.abs().transpose(1, 2).contiguous()).amax(-1, keepdim=True) * gc.SM) * (2.0 ** -11 + 2.0 ** -17)
+        if not rounded:
+            big = torch.maximum(K.abs().reshape(kv_heads, -1, 4, 32).amax(-1, keepdim=True).expand(-1, -1, 4, 32).reshape(K.shape), K.abs().amax(1, keepdim=True))
+            dl = 3.0 * 2.0 ** -17 * torch.matmul(x.abs(), big.transpose(1, 2).contiguous()).amax(-1, keepdim=True) * gc.SM
         t = 2.0 ** -8 * o.abs() + 2.2 * dl * (size + o.abs()) + 2.0 * 2.0 ** -11 * size + 1e-30
         out[b], tol[b] = o.reshape(heads, 128).numpy(), t.reshape(heads, 128).numpy()
     return out, tol
@@ -78,18 +84,18 @@ def cut_rows(cache, rows, rows_of_group):
     cache._shared[2].items = cache._shared[2].tensors[7].data_ptr()
 
 
-def run(seed, prefixes, own, groups, kv_heads, r, key_axis=0, f4=0.4, target_items=40, target_cus=8, q=None):
-    cache, Ks, Vs = build(seed, prefixes, own, kv_heads, key_axis, f4)
+def run(seed, prefixes, own, groups, kv_heads, r, key_axis=0, f4=0.4, target_items=40, target_cus=8, q=None, k_exp=0):
+    cache, Ks, Vs = build(seed, prefixes, own, kv_heads, key_axis, f4, k_exp=k_exp)
     try:
         q = wl.make_q(np.random.SeedSequence([seed, 5]), len(own), kv_heads * r) if q is None else q
         cache.plan_shared(groups, kv_heads * r, target_items, target_cus)
-        want = reference(q, Ks, Vs, groups, kv_heads)
+        want = {exact: reference(q, Ks, Vs, groups, kv_heads, not exact) for exact in (False, True)}
         for rows in (16, 64, 128):     # the plan chooses one by the sizes; each has to hold at every size
             cut_rows(cache, rows, [len(g) * r for g in groups])
             out = cache.decode_shared(harness.bf16_tensor(q, DEV))
             torch.cuda.synchronize()
             assert int(cache.status.item()) == 0
-            check(out, want, "%s %s in %d rows" % (prefixes, own, rows))
+            check(out, want[rows == 16], "%s %s in %d rows" % (prefixes, own, rows))
         return out
     finally:
         cache.close()
@@ -155,6 +161,14 @@ def test_queries_of_very_different_size():
         check(out, (ref, tol), "scaled")
     finally:
         cache.close()
+
+
+@pytest.mark.parametrize("key_axis", [0, 1])
+@pytest.mark.parametrize("k_exp", [7, -12])
+def test_keys_large_and_small(k_exp, key_axis):
+    # up to 2^14, and with scales down to the smallest normal numbers and below
+    q = wl.bf16_bits_to_f32(wl.make_q(np.random.SeedSequence([39, 5]), 3, 8)).astype(np.float32) * np.float32(2.0 ** -k_exp)
+    run(39, [700], [100, 3, 70], [[0, 1, 2]], 2, 4, key_axis, q=(q.view(np.uint32) >> 16).astype(np.uint16), k_exp=k_exp)
 
 
 def test_queries_beyond_fp16_over_a_prefix_alone():
