@@ -113,7 +113,7 @@ __device__ __forceinline__ int plan_sequence(const TableArgs &a, const int (&had
     return bad;
 }
 // Whether the whole call can be done.
-__device__ __forceinline__ int judge(const TableArgs &a, const Totals &t, const int (&n_free)[2])
+__device__ __forceinline__ int refusal(const TableArgs &a, const Totals &t, const int (&n_free)[2])
 {
     int bad = t.bad;
     if (t.tokens < 0) bad |= TKV_STATUS_TABLE_REFUSED;
@@ -349,7 +349,7 @@ template <bool PLACE> __global__ __launch_bounds__(kThreads) void tkv_table_plan
     int u[5] = {p.old[0] - p.kept[0], p.old[1] - p.kept[1], p.now[0] - p.kept[0], p.now[1] - p.kept[1], p.touch[0] + p.touch[1]}, sum[5];
     block_before(u, sum, sums + 2);
     Totals t = {{sum[0], sum[1]}, {sum[2], sum[3]}, sum[4], total, bad_s};
-    const int refused = judge(a, t, n_free);
+    const int refused = refusal(a, t, n_free);
     if constexpr (!PLACE)
         if (tid == 0) {
             ws.h->t = t;
@@ -543,7 +543,7 @@ __global__ __launch_bounds__(kThreads) void tkv_table_sums_kernel(TableArgs a)
     // (sums of pages fit 32 bits: each row has at most max_pages, and rows times max_pages do)
     Totals t = {{at[0], at[1]}, {at[2], at[3]}, at[4], tokens <= a.n_tokens ? (int)tokens : -1, bad_s};
     if (odd_s < t.tokens) t.bad |= TKV_STATUS_TABLE_REFUSED;
-    const int refused = judge(a, t, n_free);
+    const int refused = refusal(a, t, n_free);
     for (int b = tid; b < a.n_seqs; b += kThreads)
         if (a.token_indptr) a.token_indptr[b] = refused ? 0 : ws.s.at(kTok0, b);
     if (tid == 0) {
