@@ -12,7 +12,7 @@
 //         or two (INT4), zero and scale as stored against the sums of q, or as keys of their own.  Logits of 20 and more make
 //         2^-12 of a key up to 2^-8 of a weight, and with few rows one such row is seen in the result: 4 sequences over 1500 tokens
 //         were off by up to 0.0027 in norm where bf16 alone gives 0.0019, and are by 0.0019 (10.1 -> 10.4 us; 13 over 5000 12.5 -> 12.9).
-//         With 64 and 128 rows it would cost 5 % of a step for INT2 and 45 % for INT4, where the results are off by 0.0017 to 0.0018.
+//         With 64 and 128 rows, where results are off by 0.0017 to 0.0018, it would be 12 % more MFMAs for INT2 and 59 % for INT4.
 //   QK^T  D[token, row] = sum_c K[token, c] q[row, c] (v_mfma_f32_16x16x32_f16), q in fp16, each row scaled by a power of two
 //         of its own that its softmax factor takes back: bf16 has 8 bits, so q is exact down to 2^-26 of the row's largest.
 //   PV    D[row, channel] = sum_token W[row, token] V[token, channel]: the results of QK^T lie where PV wants its operand.
@@ -32,10 +32,10 @@
 // What bounds it: 128 rows, a step 2.5 us, of which the SIMD's MFMAs take 1.09, its other vector instructions 1.0 (expansion and
 // softmax about half each) and LDS 0.9 (256 KiB read, 64 written).  MFMAs and vector instructions of two wavefronts overlap
 // by a third at most (16 MFMAs beside 64 multiply-adds 202 ns, alone 128 and 120).  256 rows over 32768 tokens, 8 kv heads: 55 us of
-// steps and some 12 of loads that wait for one another, first expansion, and results on their way out; 63.7 us with the merge, 544 TFLOP/s
+// steps and some 12 of loads that wait for one another, first expansion, and results on their way out; 64.0 us with the merge, 542 TFLOP/s
 // (a large product of the library reaches 1100).  16 rows: the chain item -> group -> page ids -> codes -> softmax -> sums in LDS; a page for
 // each wavefront takes 8 us.
-// Tried and not kept: 64 rows a wavefront in registers (copies between register files, 85 us instead of 63.7), 32 rows a wavefront with pages
+// Tried and not kept: 64 rows a wavefront in registers (copies between register files, 85 us instead of 64), 32 rows a wavefront with pages
 // of its own (130 registers spilled, 23 us instead of 12 to 15), the wavefronts of a SIMD half a step apart and raised priorities
 // (no change), MFMAs and vector instructions interleaved by hand (66 to 70 us).
 #include <hip/hip_runtime.h>
