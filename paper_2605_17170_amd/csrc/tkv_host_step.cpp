@@ -177,10 +177,11 @@ int32_t tkv_plan_decode_shared(const tkv_desc *desc, int32_t batch, int32_t n_q_
         auto pages_of = [](int32_t n) { return ((int64_t)n + kPageTokens - 1) / kPageTokens; };
         auto pages = [&](int32_t g) { return pages_of(n_tok_int2[g]) + pages_of(n_tok_int4[g]); };
         // Rows of a workgroup.  With 16 its wavefronts work on a page each, eight a step; with 64 and 128 they expand pages together, two
-        // a step.  us, 16 / 64 / 128 rows: 32 rows over 32000 tokens, 8 kv heads 21 / 26 / 33; 64 over 4000 12 / 16 / 18, 11000 18.0 / 18.4 / 21.6,
-        // 32000 36 / 30 / 38; 128 over 1000 10 / 15 / 19, 8000 28 / 23 / 25; 256 over 1000 19 / 17 / 18, 8000 37 / 34 / 36, 32768 - / - / 61: about
-        // 3.1 us a step, 3 + 2.1 and 9 + 2.5 beside what all have in common.  (Steps of a workgroup: those of all, over the compute units.)
-        static const struct { int32_t rows, pages; double begin, step; } kinds[3] = {{16, 8, 0.0, 3.1}, {64, 2, 3.0, 2.1}, {128, 2, 9.0, 2.5}};
+        // a step.  us of a call, 16 / 64 / 128 rows, 8 kv heads of 8 query heads: 4 sequences over 4000 tokens 11.7 / 12.4 / 14.7, 16000
+        // 18.3 / 17.8 / 22.1; 8 over 1000 11.3 / 11.8 / 13.1, 16000 24.8 / 21.2 / 24.9; 16 over 1000 12.4 / 13.5 / 15.7, 4000 20.2 / 17.3 / 20.8,
+        // 16000 39.7 / 27.2 / 29.8, 32000 72.4 / 42.4 / 39.7; 32 over 1000 16.1 / 15.4 / 18.2, 16000 61.3 / 42.4 / 40.9: about 3.2, 1.9 and
+        // 2.8 us a step, and 2 and 5.5 more than with 16 rows once.  (Steps of a workgroup: those of all, over the compute units.)
+        static const struct { int32_t rows, pages; double begin, step; } kinds[3] = {{16, 8, 0.0, 3.2}, {64, 2, 2.0, 1.9}, {128, 2, 5.5, 2.8}};
         int32_t rows = 0;
         int64_t unit = 1, target = target_cus;
         double least = 0.0;
