@@ -117,6 +117,22 @@ def test_many_tokens_of_many_heads():
     run_and_check(15, 4099, 32, 8, 128, sections=[24, 20, 20], interleaved=True)
 
 
+def test_rows_beyond_offsets_of_32_bits():
+    """Tokens 2^30 elements apart, against the same tokens side by side."""
+    (q, k, v), weights = inputs(31, 3, 4, 2, True)
+    rope = tkv.tkv_rope_make(128, 1e6, device=DEV)
+    pos = torch.tensor([[5, 77, 1000]], dtype=torch.int32, device=DEV)
+    near, far = ([torch.empty((3, n, 128), dtype=torch.bfloat16, device=DEV) for n in (4, 2, 2)] for _ in range(2))
+    tkv.tkv_norm_rope(rope, q, k, v, pos, *weights, 1e-6, *near)
+    held = torch.empty(2 ** 31 + 1024, dtype=torch.bfloat16, device=DEV)
+    parts = [held.as_strided((3, n, 128), (2 ** 30, 128, 1), 128 * at) for n, at in ((4, 0), (2, 4), (2, 6))]
+    for a, b in zip(parts, (q, k, v)):
+        a.copy_(b)
+    tkv.tkv_norm_rope(rope, *parts, pos, *weights, 1e-6, *far)
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(near, far))
+
+
 def test_in_place_and_alone_on_a_stream():
     parts, weights = inputs(17, 300, 8, 4, False)
     rope = tkv.tkv_rope_make(128, 1e6, device=DEV)

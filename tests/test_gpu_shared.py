@@ -261,6 +261,41 @@ def test_members_slots_and_items_that_cannot_be():
         cache.close()
 
 
+def test_pages_beyond_offsets_of_32_bits():
+    """The same cache with its pages 5 GiB into either arena of a larger pool."""
+    kv_heads, heads = 2, 8
+    cache, Ks, Vs = build(61, [900], [30, 130, 0], kv_heads)
+    try:
+        q = harness.bf16_tensor(wl.make_q(np.random.SeedSequence([61, 5]), 3, heads), DEV)
+        plan = cache.plan_shared([[2, 0, 1]], heads, 8, 8)
+        p2, p4 = cache.desc.n_pages_int2, cache.desc.n_pages_int4
+        size2, size4 = (tkv.tkv_page_bytes(cache.desc, bits) for bits in (2, 4))
+        far2, far4 = (5 << 30) // size2, (5 << 30) // size4
+        desc = tkv.tkv_desc.make(kv_heads, p2 + far2, p4 + far4)
+        pool = torch.empty(tkv.tkv_pool_bytes(desc), dtype=torch.uint8, device=DEV)
+        bit_map = torch.zeros(p2 + far2 + p4 + far4, dtype=torch.uint8, device=DEV)
+        for page, far, n, size in ((0, far2, p2, size2), (p2, far2 + far4, p4, size4)):
+            a, b = tkv.tkv_record_offset(cache.desc, page, 0), tkv.tkv_record_offset(desc, page + far, 0)
+            pool[b:b + n * size] = cache.pool[a:a + n * size]
+            bit_map[page + far:page + far + n] = cache.bit_map[page:page + n]
+        ids = torch.where(cache.d_page_ids < p2, cache.d_page_ids + far2, cache.d_page_ids + far2 + far4)
+        assert tkv.tkv_record_offset(desc, int(ids.min()), 0) > 1 << 32
+        out = torch.empty(q.shape, dtype=torch.bfloat16, device=DEV)
+        ws = torch.empty(tkv.tkv_decode_workspace_bytes(desc, plan.n_slots, heads), dtype=torch.uint8, device=DEV)
+        for rows in (16, 64, 128):
+            cut_rows(cache, rows, [3 * heads // kv_heads])
+            want = cache.decode_shared(q)
+            _, _, near, d_items, d_indptr = cache._shared
+            prefix = tkv.tkv_prefix(*[getattr(near, f) for f, _ in tkv.tkv_prefix._fields_])
+            prefix.page_ids = ids.data_ptr()
+            tkv.tkv_decode_attention_shared(desc, pool, bit_map, q, cache.d_page_indptr[1:], ids, cache.d_n_tok2[1:], cache.d_n_tok4[1:], d_items, prefix,
+                                            d_indptr, plan.n_slots, float(gc.SM), out, ws, cache.status)
+            torch.cuda.synchronize()
+            assert int(cache.status.item()) == 0 and torch.equal(out, want), rows
+    finally:
+        cache.close()
+
+
 def test_captured_and_replayed_with_other_queries_and_counts():
     cache, Ks, Vs = build(53, [640], [100, 40, 64], 2)
     try:
