@@ -516,9 +516,10 @@ int32_t tkv_plan_decode_shared(const tkv_desc *desc, int32_t batch, int32_t n_q_
  *                  and the sequence reads what the workspace held before
  * Preconditions: stored scales and zeros finite, values within fp16, and so 14
  * times the scales of INT4 keys and twice those of INT2 keys; with
- * TKV_KEYS_PER_CHANNEL every n_tok_int2 a multiple of 32.  q may hold any finite
- * values; a query head of NaN or infinities gives NaN and leaves the others
- * alone.  n_q_heads / n_kv_heads is 1, 2, 4 or 8.  Two launches on `stream`:
+ * TKV_KEYS_PER_CHANNEL every n_tok_int2 a multiple of 32.  q may hold any values
+ * whose products with sm_scale, and the logits that they give (times log2 e), are
+ * finite in 32 bits; a query head of NaN or infinities gives NaN and leaves the
+ * others alone.  n_q_heads / n_kv_heads is 1, 2, 4 or 8.  Two launches on `stream`:
  * attention, then the merge.
  */
 int tkv_decode_attention_shared(const tkv_desc *desc, const void *pool, const uint8_t *bit_map, const void *q,

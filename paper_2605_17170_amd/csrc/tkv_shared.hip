@@ -205,14 +205,14 @@ template <int NT> __device__ __forceinline__ void load_q(Rows<NT> &rows, int n, 
     int top = big[0] > big[1] ? big[0] : big[1];
     top = max(top, __shfl_xor(top, 16));
     top = max(top, __shfl_xor(top, 32));
-    int E = top <= 0x80 ? 0 : 10 - ((top >> 7) - 127);   // the largest lies in [2^9, 2^10), and a sum over a group below 2^15
-    E = E > 100 ? 100 : (E < -100 ? -100 : E);
-    const float f = ldexpf(1.0f, E);
-    rows.kappa[n] = kappa * ldexpf(1.0f, -E);
+    // the largest lies in [2^9, 2^10), and a sum over a group below 2^15; from -118 to 136, beyond what a factor of 32 bits can be
+    const int E = top <= 0x80 ? 0 : 10 - ((top >> 7) - 127);
+    rows.kappa[n] = ldexpf(kappa, -E);
+    auto scaled = [&](float a, float b) { return pack_h2(ldexpf(a, E), ldexpf(b, E)); };
 #pragma unroll
     for (int g = 0; g < 4; ++g)
-        rows.q[n][g] = as_half8(pack_h2(bf16_lo(x[g].x) * f, bf16_lo(x[g].z) * f), pack_h2(bf16_hi(x[g].x) * f, bf16_hi(x[g].z) * f),
-                                pack_h2(bf16_lo(x[g].y) * f, bf16_lo(x[g].w) * f), pack_h2(bf16_hi(x[g].y) * f, bf16_hi(x[g].w) * f));
+        rows.q[n][g] = as_half8(scaled(bf16_lo(x[g].x), bf16_lo(x[g].z)), scaled(bf16_hi(x[g].x), bf16_hi(x[g].z)),
+                                scaled(bf16_lo(x[g].y), bf16_lo(x[g].w)), scaled(bf16_hi(x[g].y), bf16_hi(x[g].w)));
 }
 
 __device__ __forceinline__ half8 ones() { return as_half8(0x3c003c00u, 0x3c003c00u, 0x3c003c00u, 0x3c003c00u); }

@@ -1,0 +1,62 @@
+"""tkv_decode_attention_shared at the ends of what its arguments may be, in items of 16, 64 and 128 rows."""
+import numpy as np
+import pytest
+import torch
+
+import gpu_common as gc
+from paper_2605_17170_amd import harness, tkv
+from paper_2605_17170_amd import workloads as wl
+from test_gpu_shared import build, cut_rows
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+
+
+@pytest.fixture(scope="module", autouse=True)
+def _oracle():
+    from oracle import tkv_oracle
+    tkv_oracle.build()
+
+
+def attend(cache, q, sm_scale, workspace=None):
+    """The batch of cache.plan_shared with another factor of the logits."""
+    n, plan, prefix, d_items, d_indptr = cache._shared
+    out = torch.empty(q.shape, dtype=torch.bfloat16, device=DEV)
+    if workspace is None:
+        workspace = torch.empty(tkv.tkv_decode_workspace_bytes(cache.desc, plan.n_slots, int(q.shape[1])), dtype=torch.uint8, device=DEV)
+    tkv.tkv_decode_attention_shared(cache.desc, cache.pool, cache.bit_map, q, cache.d_page_indptr[n:], cache.d_page_ids, cache.d_n_tok2[n:], cache.d_n_tok4[n:],
+                                    d_items, prefix, d_indptr, plan.n_slots, float(sm_scale), out, workspace, cache.status)
+    torch.cuda.synchronize()
+    assert int(cache.status.item()) == 0
+    return out
+
+
+def times(q, factor):
+    """bf16 bits of q times a power of two, which is exact."""
+    f = wl.bf16_bits_to_f32(q).astype(np.float32) * np.float32(factor)
+    assert np.all(np.isfinite(f)) and not np.any(f.view(np.uint32) & 0xffff)
+    return harness.bf16_tensor((f.view(np.uint32) >> 16).astype(np.uint16), DEV)
+
+
+@pytest.mark.parametrize("key_axis", [0, 1])
+def test_queries_from_the_smallest_to_the_largest_exponent(key_axis):
+    """q times 2^k with a factor of the logits 2^-k as large: the same logits, and the same bits of the result."""
+    cache, _, _ = build(71, [700], [30, 0, 130], 2, key_axis)
+    try:
+        q = wl.make_q(np.random.SeedSequence([71, 5]), 3, 16)
+        f = np.clip(wl.bf16_bits_to_f32(q), -3.875, 3.875).astype(np.float32)
+        f = np.where(np.abs(f) < 2.0 ** -12, 0.0, f).astype(np.float32)     # (the rest stays clear of subnormal numbers)
+        f[2, 3] = 0.0
+        q = (f.view(np.uint32) >> 16).astype(np.uint16)
+        assert np.abs(f).max() >= 2.0
+        cache.plan_shared([[0, 1, 2]], 16, 8, 8)
+        scale = 16.0 * float(np.float32(gc.SM))     # (2^-126 of it is a normal number)
+        for rows in (16, 64, 128):
+            cut_rows(cache, rows, [3 * 8])
+            want = attend(cache, times(q, 1.0), scale)
+            assert torch.isfinite(want.float()).all()
+            for k in (40, 100, 110, 116, 118, 122, 126, -40, -100, -114):
+                got = attend(cache, times(q, 2.0 ** k), np.float32(scale) * np.float32(2.0 ** -k))
+                assert torch.equal(got, want), (rows, k)
+    finally:
+        cache.close()
