@@ -207,7 +207,8 @@ template <int NT> __device__ __forceinline__ void load_q(Rows<NT> &rows, int n, 
     top = max(top, __shfl_xor(top, 32));
     // the largest lies in [2^9, 2^10), and a sum over a group below 2^15; from -118 to 136, beyond what a factor of 32 bits can be
     const int E = top <= 0x80 ? 0 : 10 - ((top >> 7) - 127);
-    rows.kappa[n] = ldexpf(kappa, -E);
+    // (a smaller factor weighs all tokens alike too, and zero times the -inf of a token that does not count would be NaN)
+    rows.kappa[n] = fmaxf(ldexpf(kappa, -E), 0x1p-126f);
     auto scaled = [&](float a, float b) { return pack_h2(ldexpf(a, E), ldexpf(b, E)); };
 #pragma unroll
     for (int g = 0; g < 4; ++g)

@@ -6,7 +6,7 @@ import torch
 import gpu_common as gc
 from paper_2605_17170_amd import harness, tkv
 from paper_2605_17170_amd import workloads as wl
-from test_gpu_shared import build, cut_rows
+from test_gpu_shared import build, check, cut_rows, reference
 
 pytestmark = pytest.mark.gpu
 DEV = "cuda:0"
@@ -58,5 +58,22 @@ def test_queries_from_the_smallest_to_the_largest_exponent(key_axis):
             for k in (40, 100, 110, 116, 118, 122, 126, -40, -100, -114):
                 got = attend(cache, times(q, 2.0 ** k), np.float32(scale) * np.float32(2.0 ** -k))
                 assert torch.equal(got, want), (rows, k)
+    finally:
+        cache.close()
+
+
+@pytest.mark.parametrize("key_axis", [0, 1])
+def test_logits_too_small_for_32_bits_weigh_all_tokens_alike(key_axis):
+    """A factor of the logits below the smallest number of 32 bits: the mean of the values, of these tokens only."""
+    cache, Ks, Vs = build(73, [333], [20, 0, 65], 2, key_axis)
+    try:
+        q = wl.make_q(np.random.SeedSequence([73, 5]), 3, 8)
+        cache.plan_shared([[0, 1, 2]], 8, 8, 8)
+        want = reference(np.zeros_like(q), Ks, Vs, [[0, 1, 2]], 2)
+        for rows in (16, 64, 128):
+            cut_rows(cache, rows, [3 * 4])
+            for k, scale in ((-100, 2.0 ** -70), (-60, 2.0 ** -126), (0, 1e-45)):
+                f = wl.bf16_bits_to_f32(q).astype(np.float32) * np.float32(2.0 ** k)
+                check(attend(cache, harness.bf16_tensor((f.view(np.uint32) >> 16).astype(np.uint16), DEV), scale), want, "%d rows, 2^%d, %g" % (rows, k, scale))
     finally:
         cache.close()
