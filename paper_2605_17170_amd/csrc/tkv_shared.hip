@@ -321,7 +321,10 @@ template <int NT> __device__ __forceinline__ void weigh(Rows<NT> &rows, floatx4 
         for (int n = 0; n < NT; ++n) {
             float top = fmaxf(mx[n], __shfl_xor(mx[n], 16));
             top = fmaxf(top, __shfl_xor(top, 32));
-            const float old = rows.m[n], m_new = fmaxf(old, top * factor[n]);
+            // only a row that exceeds its own reference moves: its result does not depend on the wavefront's other rows
+            const float old = rows.m[n];
+            const bool moves = old == -INFINITY || top * factor[n] + shift[n] > kTau + (float)kPExp;
+            const float m_new = moves ? fmaxf(old, top * factor[n]) : old;
             const float alpha = m_new == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(old - m_new);
             rows.m[n] = m_new;
             rows.huge = rows.huge || __any(fabsf(m_new) > 0x1p20f && m_new != -INFINITY);
@@ -340,11 +343,12 @@ template <int NT> __device__ __forceinline__ void weigh(Rows<NT> &rows, floatx4 
             // factor * logit with one rounding, as the reference has it, then the difference: the largest weight is 2^8
 #pragma unroll
             for (int n = 0; n < NT; ++n) {
-                const float ref = rows.m[n] == -INFINITY ? 0.0f : rows.m[n];
+                const bool huge = fabsf(rows.m[n]) > 0x1p20f && rows.m[n] != -INFINITY;
+                const float ref = huge ? rows.m[n] : 0.0f, f = huge ? factor[n] : 1.0f;
 #pragma unroll
-                for (int e = 0; e < 4; ++e) S[n][e] = S[n][e] * factor[n] - ref;
-                factor[n] = 1.0f;
-                shift[n] = (float)kPExp;
+                for (int e = 0; e < 4; ++e) S[n][e] = S[n][e] * f - ref;
+                factor[n] = huge ? 1.0f : factor[n];
+                shift[n] = huge ? (float)kPExp : shift[n];
             }
         }
     }

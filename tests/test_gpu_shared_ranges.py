@@ -77,3 +77,26 @@ def test_logits_too_small_for_32_bits_weigh_all_tokens_alike(key_axis):
                 check(attend(cache, harness.bf16_tensor((f.view(np.uint32) >> 16).astype(np.uint16), DEV), scale), want, "%d rows, 2^%d, %g" % (rows, k, scale))
     finally:
         cache.close()
+
+
+@pytest.mark.parametrize("key_axis", [0, 1])
+@pytest.mark.parametrize("r", [2, 8])
+def test_a_head_does_not_depend_on_what_the_others_ask(r, key_axis):
+    """Other heads and sequences with other queries, small and huge ones and NaN: the same bits for those that stay."""
+    cache, _, _ = build(83, [1500], [130, 0, 40, 64, 9], 2, key_axis)
+    try:
+        heads = 2 * r
+        q = wl.make_q(np.random.SeedSequence([83, 5]), 5, heads)
+        other = wl.make_q(np.random.SeedSequence([84, 5]), 5, heads)
+        stay = np.random.default_rng(83).random((5, heads)) < 0.5
+        cache.plan_shared([[0, 1, 2, 4]], heads, 8, 8)
+        for rows in (16, 64, 128):
+            cut_rows(cache, rows, [4 * r])
+            want = attend(cache, harness.bf16_tensor(q, DEV), gc.SM)
+            for factor in (1.0, 2.0 ** -20, 2.0 ** 9, 2.0 ** 30, float("nan")):
+                f = np.where(stay[..., None], wl.bf16_bits_to_f32(q), wl.bf16_bits_to_f32(other) * np.float32(factor)).astype(np.float32)
+                got = attend(cache, harness.bf16_tensor((f.view(np.uint32) >> 16).astype(np.uint16), DEV), gc.SM)
+                mask = torch.from_numpy(stay).to(DEV)
+                assert torch.equal(got[mask], want[mask]), (rows, factor)
+    finally:
+        cache.close()
