@@ -193,14 +193,14 @@ template <int NT> __device__ __forceinline__ void load_q(Rows<NT> &rows, int n, 
     uint4 x[4];
 #pragma unroll
     for (int g = 0; g < 4; ++g) x[g] = src[4 * g];
-    // the largest exponent of the row, from |x| as integers plus one in the exponent, which makes NaN and infinities negative
-    typedef short short2_t __attribute__((ext_vector_type(2)));
-    short2_t big = {0, 0};
+    // the largest exponent of the row, from |x| as integers plus one in the exponent: NaN and infinities are 0x8000 and more
+    typedef unsigned short ushort2_t __attribute__((ext_vector_type(2)));
+    ushort2_t big = {0, 0};
 #pragma unroll
     for (int g = 0; g < 4; ++g) {
         const uint32_t d[4] = {x[g].x, x[g].y, x[g].z, x[g].w};
 #pragma unroll
-        for (int k = 0; k < 4; ++k) big = __builtin_elementwise_max(big, __builtin_bit_cast(short2_t, (d[k] & 0x7fff7fffu) + 0x00800080u));
+        for (int k = 0; k < 4; ++k) big = __builtin_elementwise_max(big, __builtin_bit_cast(ushort2_t, (d[k] & 0x7fff7fffu) + 0x00800080u));
     }
     int top = big[0] > big[1] ? big[0] : big[1];
     top = max(top, __shfl_xor(top, 16));
@@ -209,6 +209,11 @@ template <int NT> __device__ __forceinline__ void load_q(Rows<NT> &rows, int n, 
     const int E = top <= 0x80 ? 0 : 10 - ((top >> 7) - 127);
     // (a smaller factor weighs all tokens alike too, and zero times the -inf of a token that does not count would be NaN)
     rows.kappa[n] = fmaxf(ldexpf(kappa, -E), 0x1p-126f);
+    if (top >= 0x8000) {
+        // every weight of the row is NaN, also where all logits are -inf; with a reference, so that the wavefront's pages do not look for one
+        rows.kappa[n] = __builtin_nanf("");
+        rows.m[n] = 0.0f;
+    }
     auto scaled = [&](float a, float b) { return pack_h2(ldexpf(a, E), ldexpf(b, E)); };
 #pragma unroll
     for (int g = 0; g < 4; ++g)

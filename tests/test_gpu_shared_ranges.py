@@ -100,3 +100,33 @@ def test_a_head_does_not_depend_on_what_the_others_ask(r, key_axis):
                 assert torch.equal(got[mask], want[mask]), (rows, factor)
     finally:
         cache.close()
+
+
+@pytest.mark.parametrize("key_axis", [0, 1])
+def test_a_head_whose_logits_are_all_infinite_is_nan(key_axis):
+    """An infinity at a channel where all keys have one sign: every logit +inf or -inf, over a prefix alone, own tokens alone and both."""
+    prefixes, own, kv_heads, r = [400], [30, 0, 0], 2, 4
+    _, K, V, bits = gc.random_case(79, prefixes + own, kv_heads, kv_heads, f4=0.4)
+    f = wl.bf16_bits_to_f32(K).astype(np.float32)
+    f[..., 5] = 128.0 + np.abs(f[..., 5])     # the largest of its group of channels
+    K = (f.view(np.uint32) >> 16).astype(np.uint16)
+    cache = harness.PagedCache(kv_heads, bits, DEV, pool_factor=1.3, shuffle_seed=3, fill=0xFF, key_axis=key_axis)
+    try:
+        gc.gpu_append(cache, K, V)
+        q = wl.make_q(np.random.SeedSequence([79, 5]), 3, kv_heads * r)
+        bad = q.copy()
+        where = [(0, 1, 0xff80), (0, 6, 0x7f80), (1, 2, 0xff80), (1, 3, 0x7f80), (1, 4, 0x7fc0), (2, 7, 0xffc1)]
+        for b, h, bits_ in where:
+            bad[b, h, 5] = bits_
+        same = torch.ones((3, kv_heads * r), dtype=torch.bool, device=DEV)
+        for b, h, _ in where:
+            same[b, h] = False
+        for groups in ([[0, 1]], [[1]]):      # (sequence 2 has no tokens at all: zeros, whatever q holds)
+            cache.plan_shared(groups, kv_heads * r, 8, 8)
+            for rows in (16, 64, 128):
+                cut_rows(cache, rows, [len(groups[0]) * r])
+                clean, out = (attend(cache, harness.bf16_tensor(x, DEV), gc.SM) for x in (q, bad))
+                assert torch.isnan(out[:2][~same[:2]]).all(), (groups, rows)
+                assert torch.equal(out[same], clean[same]) and bool((out[2] == 0).all()), (groups, rows)
+    finally:
+        cache.close()
