@@ -916,7 +916,7 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2, 
 // waits for anything but the workspace, and that once for up to 64 partials.
 constexpr int kMergeWaves = 4, kMergeSets = 2 * kMergeWaves, kMergeBatch = 8;
 struct MergeArgs {
-    const float *ws[2];              // partials of the own items, of the prefixes
+    const float *acc[2], *ml[2];     // partials of the own items, of the prefixes
     int n[2];                        // slots of either
     const int32_t *indptr;           // [2][batch + 1] slots of the sequences
     int batch;
@@ -953,9 +953,8 @@ __global__ __launch_bounds__(64 * kMergeWaves) void tkv_merge_shared_kernel(Merg
             ml[j] = make_float2(-INFINITY, 0.0f);
             if (i < all) {
                 const size_t at = (size_t)(k ? i0[1] + i - n[0] : i0[0] + i) * a.n_q_heads + h;
-                const float *ws = k ? a.ws[1] : a.ws[0];
-                v[j] = reinterpret_cast<const float4 *>(ws + at * kHeadDim)[c4];
-                ml[j] = reinterpret_cast<const float2 *>(ws + (size_t)(k ? a.n[1] : a.n[0]) * a.n_q_heads * kHeadDim)[at];
+                v[j] = reinterpret_cast<const float4 *>((k ? a.acc[1] : a.acc[0]) + at * kHeadDim)[c4];
+                ml[j] = reinterpret_cast<const float2 *>(k ? a.ml[1] : a.ml[0])[at];
             }
         }
         float Mn = M;
@@ -1014,9 +1013,9 @@ int tkv_launch_shared(const tkv_desc *desc, const void *pool, const uint8_t *bit
 {
     int log2_r = 0;
     while ((desc->n_kv_heads << log2_r) < n_q_heads) ++log2_r;
-    const size_t row_floats = (size_t)n_q_heads * (kHeadDim + 2);
-    float *const ws[2] = {(float *)workspace, (float *)workspace + (size_t)n_items * row_floats};
-    const int n[2] = {n_items, n_slots - n_items};
+    // the rows of all slots, then their (m, l): every row begins a 128-byte line of its own, as far as the workspace does
+    const size_t own_rows = (size_t)n_items * n_q_heads, rows = (size_t)n_slots * n_q_heads;
+    float *const acc = (float *)workspace, *const ml = acc + rows * kHeadDim;
     SharedArgs a = {};
     a.pool = (const uint8_t *)pool;
     a.bit_map = bit_map;
@@ -1035,10 +1034,10 @@ int tkv_launch_shared(const tkv_desc *desc, const void *pool, const uint8_t *bit
     a.batch = batch;
     a.n_slots = n_slots;
     a.kappa = sm_scale * 1.44269504088896340736f;
-    for (int k = 0; k < 2; ++k) {
-        a.acc_ws[k] = ws[k];
-        a.ml_ws[k] = ws[k] + (size_t)n[k] * n_q_heads * kHeadDim;
-    }
+    a.acc_ws[0] = acc;
+    a.acc_ws[1] = acc + own_rows * kHeadDim;
+    a.ml_ws[0] = ml;
+    a.ml_ws[1] = ml + 2 * own_rows;
     a.status = status;
     const int64_t own_blocks = ((int64_t)n_items * desc->n_kv_heads + kWaves - 1) / kWaves;
     a.own_blocks = (int)own_blocks;
@@ -1054,9 +1053,11 @@ int tkv_launch_shared(const tkv_desc *desc, const void *pool, const uint8_t *bit
     }
     MergeArgs m = {};
     for (int k = 0; k < 2; ++k) {
-        m.ws[k] = ws[k];
-        m.n[k] = n[k];
+        m.acc[k] = a.acc_ws[k];
+        m.ml[k] = a.ml_ws[k];
     }
+    m.n[0] = n_items;
+    m.n[1] = n_slots - n_items;
     m.indptr = slot_indptr;
     m.batch = batch;
     m.n_q_heads = n_q_heads;

@@ -130,3 +130,30 @@ def test_a_head_whose_logits_are_all_infinite_is_nan(key_axis):
                 assert torch.equal(out[same], clean[same]) and bool((out[2] == 0).all()), (groups, rows)
     finally:
         cache.close()
+
+
+@pytest.mark.parametrize("kv_heads,r,own", [(1, 1, [70, 0, 5]), (3, 1, [70, 20, 5]), (1, 8, [64, 0, 0]), (2, 4, [0, 0, 0]), (3, 8, [200, 1, 65])])
+def test_partials_are_rows_of_512_bytes_behind_one_another(kv_heads, r, own):
+    """acc of slot s and query head h at row s * heads + h of the workspace, (m, l) of all of them behind: merged here in 64 bits,
+    off by the rounding to bf16, half a step of the result, and of the 32-bit sums."""
+    heads = kv_heads * r
+    cache, _, _ = build(89, [700], own, kv_heads)
+    try:
+        q = harness.bf16_tensor(wl.make_q(np.random.SeedSequence([89, 5]), 3, heads), DEV)
+        plan = cache.plan_shared([[0, 2, 1]], heads, 3, 4)
+        indptr = plan.seq_item_indptr.reshape(2, 4)
+        for rows in (16, 64, 128):
+            cut_rows(cache, rows, [3 * r])
+            ws = torch.full((tkv.tkv_decode_workspace_bytes(cache.desc, plan.n_slots, heads) // 4,), float("nan"), device=DEV)
+            out = attend(cache, q, gc.SM, ws).double().cpu()
+            assert torch.isfinite(ws).all()
+            n = plan.n_slots * heads
+            acc, ml = ws[:128 * n].view(plan.n_slots, heads, 128).double().cpu(), ws[128 * n:].view(plan.n_slots, heads, 2).double().cpu()
+            for b in range(3):
+                at = [s for k in range(2) for s in range(indptr[k, b], indptr[k, b + 1])]
+                w = torch.exp2(ml[at, :, 0] - ml[at, :, 0].amax(0))[..., None]
+                den = (w[..., 0] * ml[at, :, 1]).sum(0)[:, None]
+                want, size = (w * acc[at]).sum(0) / den, (w * acc[at].abs()).sum(0) / den
+                assert bool(((out[b] - want).abs() <= 2.0 ** -8 * want.abs() + 2.0 ** -18 * size).all()), (rows, b)
+    finally:
+        cache.close()
