@@ -149,6 +149,7 @@ struct SharedArgs {
     const int32_t *items;
     int n_items;      // own items: slots [0, n_items); the prefixes' partials have [n_items, n_slots)
     int own_blocks;   // the first workgroups, a wavefront for each (own item, kv head)
+    int blocks;
     tkv_prefix p;
     int n_kv_heads;
     int log2_r;
@@ -747,10 +748,10 @@ template <bool THROUGH> __device__ __forceinline__ void store_row(float *row, in
     }
 }
 // The own tokens of a sequence: a wavefront for each (item, kv head), whose rows are the query heads of the kv head.
-template <bool KC, bool THROUGH, class L> __device__ __forceinline__ void own_item(const SharedArgs &a, L &lds, int wave, int lane)
+template <bool KC, bool THROUGH, class L> __device__ __forceinline__ void own_item(const SharedArgs &a, L &lds, int block, int wave, int lane)
 {
     const int r16 = lane & 15, q4 = lane >> 4, R = 1 << a.log2_r, n_q_heads = a.n_kv_heads << a.log2_r;
-    const int64_t unit = (int64_t)blockIdx.x * kWaves + wave;
+    const int64_t unit = (int64_t)block * kWaves + wave;
     if (unit >= (int64_t)a.n_items * a.n_kv_heads) return;
     const int item = (int)(unit / a.n_kv_heads), kvh = (int)(unit % a.n_kv_heads);
     const ConstWords words = (ConstWords)(a.items + 4 * (size_t)item);
@@ -795,11 +796,11 @@ template <bool KC, bool THROUGH, class L> __device__ __forceinline__ void own_it
 }
 
 // A prefix's pages [item_pb, item_pe) for rows_of(MODE) query rows of its members.
-template <int MODE, bool KC> __device__ __forceinline__ void prefix_item(const SharedArgs &a, Shared<MODE> &lds, int wave, int lane)
+template <int MODE, bool KC> __device__ __forceinline__ void prefix_item(const SharedArgs &a, Shared<MODE> &lds, int block, int wave, int lane)
 {
     constexpr int NT = tiles_of(MODE), ROWS = rows_of(MODE), SETS = Shared<MODE>::kSets;
     const int r16 = lane & 15, q4 = lane >> 4, R = 1 << a.log2_r, n_q_heads = a.n_kv_heads << a.log2_r;
-    const int block = blockIdx.x - a.own_blocks, item = block / a.n_kv_heads, kvh = block - item * a.n_kv_heads;
+    const int item = block / a.n_kv_heads, kvh = block - item * a.n_kv_heads;
     const ConstWords words = (ConstWords)(a.p.items + 5 * (size_t)item);
     const int group = words[0], item_pb = words[1], item_pe = words[2], part = words[3], row0 = words[4];
     if (group < 0 || group >= a.p.n_groups || part < 0 || row0 < 0) {
@@ -907,8 +908,10 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2, 
 {
     __shared__ Shared<MODE> lds;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    if ((int)blockIdx.x < a.own_blocks) own_item<KC, MODE != 0>(a, lds, wave, lane);
-    else prefix_item<MODE, KC>(a, lds, wave, lane);
+    const uint32_t block = blockIdx.x + blockIdx.y * gridDim.x;
+    if (block >= (uint32_t)a.blocks) return;
+    if ((int)block < a.own_blocks) own_item<KC, MODE != 0>(a, lds, (int)block, wave, lane);
+    else prefix_item<MODE, KC>(a, lds, (int)block - a.own_blocks, wave, lane);
 }
 
 // out = sum_i 2^(m_i - M) acc_i / sum_i 2^(m_i - M) l_i over a sequence's own items and its prefixes'.  One workgroup per (sequence,
@@ -999,9 +1002,12 @@ __global__ __launch_bounds__(64 * kMergeWaves) void tkv_merge_shared_kernel(Merg
     reinterpret_cast<uint32_t *>(a.out + ((size_t)b * a.n_q_heads + h) * kHeadDim)[lane] = __builtin_bit_cast(uint32_t, v);
 }
 
-template <int MODE> void launch_shared(bool kc, unsigned blocks, hipStream_t s, const SharedArgs &a)
+template <int MODE> void launch_shared(bool kc, hipStream_t s, const SharedArgs &a)
 {
-    hipLaunchKernelGGL((kc ? tkv_shared_kernel<MODE, true> : tkv_shared_kernel<MODE, false>), dim3(blocks), dim3(64 * kWaves), 0, s, a);
+    constexpr unsigned kMaxX = 1 << 22;   // a grid has less than 2^32 threads in a dimension
+    const unsigned blocks = (unsigned)a.blocks;
+    hipLaunchKernelGGL((kc ? tkv_shared_kernel<MODE, true> : tkv_shared_kernel<MODE, false>), dim3(blocks < kMaxX ? blocks : kMaxX, (blocks + kMaxX - 1) / kMaxX),
+                       dim3(64 * kWaves), 0, s, a);
 }
 
 } // namespace
@@ -1046,9 +1052,10 @@ int tkv_launch_shared(const tkv_desc *desc, const void *pool, const uint8_t *bit
     if (blocks > INT32_MAX) return TKV_ERR_INVALID_ARG;
     if (blocks > 0) {
         const bool kc = desc->int2_key_axis == TKV_KEYS_PER_CHANNEL;
-        if (per == 16) launch_shared<0>(kc, (unsigned)blocks, (hipStream_t)stream, a);
-        else if (per == 64) launch_shared<1>(kc, (unsigned)blocks, (hipStream_t)stream, a);
-        else launch_shared<2>(kc, (unsigned)blocks, (hipStream_t)stream, a);
+        a.blocks = (int)blocks;
+        if (per == 16) launch_shared<0>(kc, (hipStream_t)stream, a);
+        else if (per == 64) launch_shared<1>(kc, (hipStream_t)stream, a);
+        else launch_shared<2>(kc, (hipStream_t)stream, a);
         if (hipGetLastError() != hipSuccess) return TKV_ERR_HIP;
     }
     MergeArgs m = {};

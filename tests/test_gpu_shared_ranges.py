@@ -157,3 +157,36 @@ def test_partials_are_rows_of_512_bytes_behind_one_another(kv_heads, r, own):
                 assert bool(((out[b] - want).abs() <= 2.0 ** -8 * want.abs() + 2.0 ** -18 * size).all()), (rows, b)
     finally:
         cache.close()
+
+
+@pytest.mark.parametrize("rows", [16, 64])
+def test_more_workgroups_than_a_dimension_of_the_grid(rows):
+    """2^23 + 5 parts, all but the last few of them empty: the same bits as the plan's parts by themselves in their slots."""
+    cache, _, _ = build(97, [190], [70, 0], 1)
+    try:
+        q = harness.bf16_tensor(wl.make_q(np.random.SeedSequence([97, 5]), 2, 2), DEV)
+        plan = cache.plan_shared([[1]], 2, 1, 1)
+        cut_rows(cache, rows, [2])
+        want = attend(cache, q, gc.SM)
+        n, _, prefix, d_items, d_indptr = cache._shared
+        old, n_own = prefix.tensors[7], d_items.shape[0]
+        n_old, n_items = old.shape[0], (1 << 23) + 5
+        items = torch.zeros((n_items, 5), dtype=torch.int32, device=DEV)      # (pages [0, 0) of group 0)
+        items[:, 3] = torch.arange(n_items, dtype=torch.int32, device=DEV)
+        items[-n_old:, [0, 1, 2, 4]] = old[:, [0, 1, 2, 4]]
+        slots = torch.full((1,), n_own, dtype=torch.int32, device=DEV)
+        indptr = d_indptr.clone()
+        indptr[3:] = torch.tensor([n_own, n_own, n_own + n_items], dtype=torch.int32, device=DEV)
+        many = tkv.tkv_prefix(1, 1, rows, n_items, *[t.data_ptr() for t in prefix.tensors[:6]], slots.data_ptr(), items.data_ptr())
+        n_slots = n_own + n_items
+        ws = torch.empty(tkv.tkv_decode_workspace_bytes(cache.desc, n_slots, 2), dtype=torch.uint8, device=DEV)
+        out = torch.empty_like(want)
+        tkv.tkv_decode_attention_shared(cache.desc, cache.pool, cache.bit_map, q, cache.d_page_indptr[n:], cache.d_page_ids, cache.d_n_tok2[n:],
+                                        cache.d_n_tok4[n:], d_items, many, indptr, n_slots, gc.SM, out, ws, cache.status)
+        torch.cuda.synchronize()
+        assert int(cache.status.item()) == 0 and torch.isfinite(out.float()).all()
+        assert torch.equal(out[0], want[0])
+        # (the merge adds the same partials in another order: 32-bit sums, then half a step of bf16 on either side)
+        assert bool(((out[1] - want[1]).float().abs() <= 2.0 ** -7 * want[1].float().abs() + 2.0 ** -16).all())
+    finally:
+        cache.close()
