@@ -618,7 +618,8 @@ int tkv_table_append(const tkv_desc *desc, const tkv_table *table, const int32_t
  *
  * tkv_rope_table (host): one word per pair of channels, table_out[i] = the
  * turns per position of pair i, inv_freq[i] / 2 pi, modulo 1, in units of
- * 2^-64, its lowest two bits replaced by the pair's axis.
+ * 2^-64, rounded to a multiple of four units (2^-63 turns), which leaves its
+ * lowest two bits for the pair's axis.
  *   rotary_dim  channels 0 .. rotary_dim-1 of a head turn, a multiple of 16,
  *               0 .. 128; the others keep their place
  *   sections    host i32[n_axes], pairs of each axis, summing to rotary_dim/2;
@@ -648,7 +649,8 @@ int tkv_rope_table(int32_t rotary_dim, int32_t n_axes, const int32_t *sections, 
  * channels, x * rsqrt(mean(x^2) + eps) * weight, where a weight is given, then
  * the rotation of its pairs: (a, b) becomes (a cos - b sin, a sin + b cos) *
  * scale with angle positions[axis][t] * frequency.  Values v, if given, are
- * copied.  All in 32 bits (angles: 2^-32 turns at any position), rounded once.
+ * copied.  All in 32 bits (angles: what the table holds to 2^-33 turns at any
+ * position), rounded once.
  *   q, k, v      device bf16, 16-byte aligned; token t, head h, channel c at
  *                t * stride + h * 128 + c with the tensor's own stride in
  *                elements (a multiple of 8): parts of a packed projection, or

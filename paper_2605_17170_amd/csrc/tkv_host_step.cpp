@@ -98,7 +98,7 @@ int tkv_rope_table(int32_t rotary_dim, int32_t n_axes, const int32_t *sections, 
         const long double f = inv_freq ? (long double)inv_freq[i] : std::pow((long double)theta, -2.0L * i / rotary_dim);
         long double turns = f / 6.283185307179586476925286766559005768L;
         turns -= std::floor(turns);
-        // the lowest two bits hold the axis: 2^-63 turns at most, times a position
+        // the nearest multiple of four units, off by two at most, 2^-63 turns: the lowest two bits hold the axis
         const long double units = turns * 18446744073709551616.0L;
         const uint64_t word = units >= 18446744073709551614.0L ? 0 : ((uint64_t)units + 2) & ~(uint64_t)3;
         table_out[i] = word | (uint64_t)axis;

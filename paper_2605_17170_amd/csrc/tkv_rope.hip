@@ -13,8 +13,9 @@
 // angles computed by each lane for its own pairs, and walks over many rows to make up for it, 48 heads of 2501 tokens took
 // 20.9 us, and 80 of 16384 136; two and four rows a lane, all asked for at first, are no faster.)
 //
-// Angles: f_i / 2 pi is held as a fraction of a turn in 64 bits (tkv_rope_table), position times fraction modulo 2^64 is
-// exact but for the table's rounding (position * 2^-64 turns), and its top 32 bits are the angle to 2^-32 turns at any position.
+// Angles: f_i / 2 pi is held as a fraction of a turn in 64 bits (tkv_rope_table), of which the lowest two hold the axis and
+// count as zero here.  Position times fraction modulo 2^64 is exact but for the table's rounding (2^-63 turns a position), and rounded
+// to 32 bits (2^-33 turns): the angle to 1.5 * 2^-32 turns at any position, and one of zero where the frequency is.
 // Sine and cosine of the remainder in [-pi/4, pi/4] are Taylor polynomials of degree 9 and 8 (off by 2e-9 and 3e-8).
 // Everything is 32 bits until the one rounding to bf16.
 //
@@ -139,7 +140,7 @@ __global__ __launch_bounds__(256) void tkv_norm_rope_kernel(RopeArgs a)
             if (turns) {
                 const int axis = (int)turn & 3;
                 const int32_t p = (axis & 2) ? ((axis & 1) ? pos[3] : pos[2]) : ((axis & 1) ? pos[1] : pos[0]);
-                cos_sin((uint32_t)((uint64_t)(int64_t)p * turn >> 32), c, s);
+                cos_sin((uint32_t)((uint64_t)(int64_t)p * (turn & ~(uint64_t)3) + 0x80000000u >> 32), c, s);
                 c *= a.scale;
                 s *= a.scale;
             }
