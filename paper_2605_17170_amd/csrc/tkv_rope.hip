@@ -88,7 +88,9 @@ __global__ __launch_bounds__(256) void tkv_norm_rope_kernel(RopeArgs a)
     extern __shared__ Trig trig[];   // of the workgroup's tokens
     const int l = threadIdx.x & 7;
     const int rows = a.heads[0] + a.heads[1] + a.heads[2], half = a.rotary_dim >> 1;
-    const int first = blockIdx.x * kRopeRows, end = a.n_rows - first < kRopeRows ? a.n_rows : first + kRopeRows;
+    const int first = (int)((blockIdx.x + blockIdx.y * gridDim.x) * kRopeRows);
+    if (first >= a.n_rows) return;
+    const int end = a.n_rows - first < kRopeRows ? a.n_rows : first + kRopeRows;
     const int token0 = first / rows, head0 = first - token0 * rows;
 
     // angles: thread i has frequency i % 64 of every fourth token
@@ -221,7 +223,9 @@ int tkv_launch_norm_rope(const tkv_rope *rope, const void *q, int64_t q_stride, 
     a.scale = rope->scale;
     a.eps = eps;
     const int most = (kRopeRows + rows - 2) / rows + 1;   // tokens that a workgroup's rows can touch
-    const dim3 grid((unsigned)((a.n_rows + (int64_t)kRopeRows - 1) / kRopeRows));
+    constexpr unsigned kMaxX = 1 << 23;   // a grid has less than 2^32 threads in a dimension
+    const unsigned blocks = (unsigned)((a.n_rows + (int64_t)kRopeRows - 1) / kRopeRows);
+    const dim3 grid(blocks < kMaxX ? blocks : kMaxX, (blocks + kMaxX - 1) / kMaxX);
     hipLaunchKernelGGL(rope->adjacent ? tkv_norm_rope_kernel<true> : tkv_norm_rope_kernel<false>, grid, dim3(256), (size_t)most * sizeof(Trig),
                        (hipStream_t)stream, a);
     return hipGetLastError() == hipSuccess ? TKV_OK : TKV_ERR_HIP;

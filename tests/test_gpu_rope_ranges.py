@@ -58,3 +58,32 @@ def test_sines_of_angles_near_whole_turns(sections, interleaved):
         # (the host's division and remainder in 64 bits: half a unit of 2^-64 a position besides)
         tol += 2 * math.pi * abs(pos[k]) * 2.0 ** -64
         assert abs(s[k, k] - want) <= tol, (k, pos[k], s[k, k], want, tol)
+
+
+def test_more_rows_than_a_dimension_of_the_grid():
+    """2^29 + 192 rows, in place; the first and last tokens and those around 2^28 and 2^29 rows, against calls of their own."""
+    heads, tokens = 64, (1 << 23) + 3
+    if torch.cuda.mem_get_info()[0] + torch.cuda.memory_reserved() - torch.cuda.memory_allocated() < tokens * heads * 256 + (8 << 30):
+        pytest.skip("needs 146 GB of device memory")
+    x = torch.empty((tokens, heads, 128), dtype=torch.bfloat16, device=DEV)
+    x.fill_(0.5)
+    at = [0, 1, (1 << 22) - 1, 1 << 22, (1 << 23) - 2, (1 << 23) - 1, 1 << 23, tokens - 1]
+    g = torch.Generator(device=DEV)
+    g.manual_seed(3)
+    rows = torch.randn((len(at), heads, 128), device=DEV, generator=g).to(torch.bfloat16)
+    for i, t in enumerate(at):
+        x[t] = rows[i]
+    weight = (1.0 + 0.3 * torch.randn((128,), device=DEV, generator=g)).to(torch.bfloat16)
+    pos = torch.arange(tokens, dtype=torch.int32, device=DEV)[None]
+    rope = tkv.tkv_rope_make(128, 1e6, device=DEV)
+    want = torch.empty_like(rows)
+    tkv.tkv_norm_rope(rope, rows, None, None, pos[:, at].contiguous(), weight, None, 1e-6, want, None)
+    tkv.tkv_norm_rope(rope, x, None, None, pos, weight, None, 1e-6, x, None)
+    torch.cuda.synchronize()
+    for i, t in enumerate(at):
+        assert torch.equal(x[t], want[i]), t
+    # every token was normed: no row still holds what it did
+    left = sum(int((x[t:t + (1 << 18)] == 0.5).all(-1).any(-1).sum()) for t in range(0, tokens, 1 << 18))
+    del x
+    torch.cuda.empty_cache()
+    assert left == 0
