@@ -665,7 +665,8 @@ int tkv_rope_table(int32_t rotary_dim, int32_t n_axes, const int32_t *sections, 
  *                and overlaps no other buffer of the call
  * The sum of a row's squares must be finite in 32 bits (a row beyond that gives
  * zeros, one that holds NaN or infinities NaN; other rows are left alone), and
- * with eps = 0 a row of zeros gives NaN.  At most 2^31 - 4096 rows of heads in
+ * with eps = 0 a row whose mean square is below 2^-126, the smallest normal
+ * number, gives NaN or infinities.  At most 2^31 - 4096 rows of heads in
  * all.  n_tokens = 0 is a no-op.  One launch on `stream`.
  */
 int tkv_norm_rope(const tkv_rope *rope, const void *q, int64_t q_stride, const void *k, int64_t k_stride,
