@@ -594,12 +594,17 @@ size_t tkv_table_workspace_bytes(int32_t n_seqs, int32_t n_tokens);
  *   status        device i32, may be NULL
  * All or nothing: where lengths are negative or sum to more than n_tokens, a
  * width is neither 2 nor 4, counts of per-channel INT2 keys are no multiples of
- * 32 (arriving or kept) or the table contradicts itself
- * (TKV_STATUS_TABLE_REFUSED), a pool has too few pages
+ * 32 (arriving or kept) or a count of the table cannot be (tokens below zero or
+ * beyond max_pages, free pages below zero or, with those given back, more than
+ * the pool has: TKV_STATUS_TABLE_REFUSED), a pool has too few pages
  * (TKV_STATUS_POOL_EXHAUSTED), or max_pages or max_work does not suffice
  * (TKV_STATUS_CAPACITY), the table stays as it is, n_work and token_indptr are
  * 0, no slot is named, and slot_ids and positions are -1.
- * One launch for up to 1024 sequences and 6144 tokens, else up to four.
+ * Page ids are not compared with their pools: what a row or a free list holds is
+ * handed on as it is, and tkv_quantize_append and attention leave out a page
+ * that is none or not of its width, with their own status bits.
+ * One launch for up to 1024 sequences, 6144 tokens and max_work of 1024, else up
+ * to four.
  */
 int tkv_table_append(const tkv_desc *desc, const tkv_table *table, const int32_t *keep_int2, const int32_t *keep_int4,
                      const int32_t *n_new, const uint8_t *tag_bits, int32_t n_tokens,
