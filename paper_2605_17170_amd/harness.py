@@ -179,7 +179,7 @@ class PagedCache:
         plan = tkv.tkv_plan_decode_shared(self.desc, batch, n_q_heads, self.n_tok2[:n], self.n_tok4[:n], indptr, members, target_cus, items, sip)
         d = lambda a: torch.from_numpy(np.ascontiguousarray(a)).to(self.device)  # noqa: E731
         prefix = tkv.tkv_prefix.make(self.d_page_indptr[:n + 1], self.d_page_ids, self.d_n_tok2[:n], self.d_n_tok4[:n], d(indptr), d(members),
-                                     d(plan.member_slots), d(plan.prefix_items), plan.max_members)
+                                     d(plan.member_slots), d(plan.prefix_items), tile_rows=plan.tile_rows)
         self._shared = (n, plan, prefix, d(plan.items), d(plan.seq_item_indptr))
         return plan
 

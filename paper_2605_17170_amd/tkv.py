@@ -88,17 +88,19 @@ class tkv_prefix(C.Structure):
                 ("member_indptr", C.c_void_p), ("member_seqs", C.c_void_p), ("member_slots", C.c_void_p), ("items", C.c_void_p)]
 
     @classmethod
-    def make(cls, page_indptr, page_ids, n_tok_int2, n_tok_int4, member_indptr, member_seqs, member_slots, items, max_members):
+    def make(cls, page_indptr, page_ids, n_tok_int2, n_tok_int4, member_indptr, member_seqs, member_slots, items, max_members=None, *, tile_rows=None):
         """i32 device tensors: page_indptr, member_indptr [n_groups+1]; page_ids; n_tok_int2/4 [n_groups]; member_seqs,
-        member_slots [n_members]; items [n_items, 5] (the last two and max_members from tkv_plan_decode_shared, whose
-        max_members also names the rows of an item)."""
+        member_slots [n_members]; items [n_items, 5].  The last two and tile_rows as tkv_plan_decode_shared gives them;
+        SharedPlan.max_members in place of tile_rows names the rows too, a plain number there does not."""
         tensors = (page_indptr, page_ids, n_tok_int2, n_tok_int4, member_indptr, member_seqs, member_slots, items)
         n = n_tok_int2.numel()
         assert all(_i32(t) for t in tensors) and n_tok_int4.numel() == n and page_indptr.numel() == member_indptr.numel() == n + 1
         assert member_seqs.numel() == member_slots.numel() and items.numel() % 5 == 0
-        if not hasattr(max_members, "tile_rows"):
-            raise ValueError("max_members: as tkv_plan_decode_shared gives it, with the rows of the items")
-        prefix = cls(n, member_seqs.numel(), max_members.tile_rows, items.numel() // 5, *(_dev(t) for t in tensors))
+        if tile_rows is None:
+            tile_rows = getattr(max_members, "tile_rows", None)
+        if tile_rows not in (16, 64, 128):
+            raise ValueError("tile_rows: the rows of the plan's items, SharedPlan.tile_rows")
+        prefix = cls(n, member_seqs.numel(), int(tile_rows), items.numel() // 5, *(_dev(t) for t in tensors))
         prefix.tensors = tensors
         return prefix
 
@@ -572,14 +574,15 @@ class MaxMembers(int):
     """Members of the largest group, with the rows of the plan's items (`tile_rows`)."""
 
 
-SharedPlan = collections.namedtuple("SharedPlan", "items seq_item_indptr n_slots prefix_items member_slots max_members")
+SharedPlan = collections.namedtuple("SharedPlan", "items seq_item_indptr n_slots prefix_items member_slots max_members tile_rows")
 
 
 def tkv_plan_decode_shared(desc, batch: int, n_q_heads: int, n_tok_int2, n_tok_int4, member_indptr, member_seqs, target_cus: int, items,
                            seq_item_indptr) -> SharedPlan:
     """Plan over the groups' prefixes (host arrays, per group) beside the plan (items, seq_item_indptr) of the sequences' own
     tokens from tkv_plan_decode.  SharedPlan: items i32[n_items, 4] and seq_item_indptr i32[2*(batch+1)] of the sequences,
-    n_slots, prefix_items i32[n, 5], member_slots i32[n_members], max_members."""
+    n_slots, prefix_items i32[n, 5], member_slots i32[n_members], max_members, tile_rows (the rows that the items are cut
+    for, which tkv_prefix.make takes)."""
     n2, p2 = _np(n_tok_int2, np.int32)
     n4, p4 = _np(n_tok_int4, np.int32)
     ip, pip = _np(member_indptr, np.int32)
@@ -596,7 +599,8 @@ def tkv_plan_decode_shared(desc, batch: int, n_q_heads: int, n_tok_int2, n_tok_i
                                             C.c_void_p(indptr.ctypes.data), C.byref(tile_rows)), "tkv_plan_decode_shared")
     members = MaxMembers(np.diff(ip).max() if n2.size else 0)
     members.tile_rows = tile_rows.value
-    return SharedPlan(np.asarray(items, np.int32).reshape(-1, 4), np.concatenate([sip, indptr]), int(indptr[-1]), prefix_items[:n].copy(), slots, members)
+    return SharedPlan(np.asarray(items, np.int32).reshape(-1, 4), np.concatenate([sip, indptr]), int(indptr[-1]), prefix_items[:n].copy(), slots, members,
+                      tile_rows.value)
 
 
 def tkv_decode_attention_shared(desc, pool, bit_map, q, page_indptr, page_ids, n_tok_int2, n_tok_int4, items, prefix: tkv_prefix, slot_indptr,
