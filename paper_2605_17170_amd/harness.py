@@ -5,6 +5,7 @@ to the GPU with torch, and launches the library's kernels; it computes
 nothing itself."""
 from __future__ import annotations
 
+import contextlib
 import math
 
 import numpy as np
@@ -48,6 +49,14 @@ def device_q(batch: int, n_q_heads: int, seed: int, device):
     g = torch.Generator(device=device)
     g.manual_seed((int(seed) * 7919 + 13) & 0x7FFFFFFF)
     return torch.randn((batch, n_q_heads, tkv.HEAD_DIM), dtype=torch.float32, device=device, generator=g).to(torch.bfloat16)
+
+
+def _allocating_on(stream):
+    """Where buffers of a call on `stream` come from: memory of that stream, which the work of another one does not hold and
+    does not get while the call runs."""
+    if stream is None:
+        return contextlib.nullcontext()
+    return torch.cuda.stream(stream if isinstance(stream, torch.cuda.Stream) else torch.cuda.ExternalStream(stream))
 
 
 class PagedCache:
@@ -139,10 +148,11 @@ class PagedCache:
         assert not prepare or (out is not None and workspace is not None)
         d_items, d_sip, items, _ = self._plan
         B, Hq = int(q.shape[0]), int(q.shape[1])
-        if out is None:
-            out = torch.empty((B, Hq, tkv.HEAD_DIM), dtype=torch.float32, device=self.device)
-        if workspace is None:
-            workspace = self.workspace(Hq)
+        with _allocating_on(stream):
+            if out is None:
+                out = torch.empty((B, Hq, tkv.HEAD_DIM), dtype=torch.float32, device=self.device)
+            if workspace is None:
+                workspace = self.workspace(Hq)
         sm_scale = np.float32(1.0 / math.sqrt(tkv.HEAD_DIM))
         call = tkv.tkv_decode_attention(self.desc, self.pool if pool is None else pool, self.bit_map, q,
                                         self.d_page_indptr, self.d_page_ids, self.d_n_tok2, self.d_n_tok4, d_items, d_sip,
@@ -185,11 +195,13 @@ class PagedCache:
 
     def decode_shared(self, q: torch.Tensor, out: torch.Tensor | None = None, workspace=None, pool=None, stream=None, prepare=False):
         """Attention of the batch of plan_shared over prefixes and own tokens, bf16; arguments as for decode."""
+        assert not prepare or (out is not None and workspace is not None)
         n, plan, prefix, d_items, d_indptr = self._shared
-        if out is None:
-            out = torch.empty(q.shape, dtype=torch.bfloat16, device=self.device)
-        if workspace is None:
-            workspace = torch.empty(max(16, tkv.tkv_decode_workspace_bytes(self.desc, plan.n_slots, int(q.shape[1]))), dtype=torch.uint8, device=self.device)
+        with _allocating_on(stream):
+            if out is None:
+                out = torch.empty(q.shape, dtype=torch.bfloat16, device=self.device)
+            if workspace is None:
+                workspace = torch.empty(max(16, tkv.tkv_decode_workspace_bytes(self.desc, plan.n_slots, int(q.shape[1]))), dtype=torch.uint8, device=self.device)
         sm_scale = np.float32(1.0 / math.sqrt(tkv.HEAD_DIM))
         call = tkv.tkv_decode_attention_shared(self.desc, self.pool if pool is None else pool, self.bit_map, q, self.d_page_indptr[n:], self.d_page_ids,
                                                self.d_n_tok2[n:], self.d_n_tok4[n:], d_items, prefix, d_indptr, plan.n_slots, float(sm_scale), out, workspace,
