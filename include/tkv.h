@@ -545,7 +545,11 @@ int tkv_decode_attention_shared(const tkv_desc *desc, const void *pool, const ui
  * n_free[1]) those of the INT4 pool; behind them anything.
  * A decode plan (tkv_plan_decode) made for more INT4 pages than a sequence has
  * yet stays valid while it grows into them: what an item names beyond the
- * sequence's pages is not read.
+ * sequence's pages is not read.  Pages beyond the plan's are not read either, and
+ * no status bit says so: the plan is made, by the host, for the pages that the
+ * sequences can have when the next one replaces it.  (A sequence of n tokens of
+ * a width has at most (n + 63) / 64 pages of it, and the host knows how many
+ * tokens it has handed in, if not how many were cut off.)
  */
 typedef struct tkv_table {
     int32_t n_seqs;
