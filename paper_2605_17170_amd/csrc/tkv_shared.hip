@@ -16,13 +16,13 @@
 //   QK^T  D[token, row] = sum_c K[token, c] q[row, c] (v_mfma_f32_16x16x32_f16), q in fp16, each row scaled by a power of two
 //         of its own that its softmax factor takes back: bf16 has 8 bits, so q is exact down to 2^-26 of the row's largest.
 //   PV    D[row, channel] = sum_token W[row, token] V[token, channel]: the results of QK^T lie where PV wants its operand.
-//         W = 2^(logit - m + 8) in fp16, m a reference that follows the row's maximum lazily (within 2^4), so that W stays
+//         W = 2^(logit - m + 8) in fp16, m a reference that follows the row's own maximum lazily (within 2^4), so that W stays
 //         below 2^12 and weights down to 2^-22 of the largest are exact to half a step.  The denominators are one more MFMA
 //         against ones: of the rounded weights, as the numerators.
 // All sums are 32 bits.  V, W and the expanded K carry 11 bits where the split kernel carries what its fp32 results need; the output is
 // bf16, which has 8.
 //
-// Workgroups of eight wavefronts, one a compute unit (196 to 256 registers), do one of three things:
+// Workgroups of eight wavefronts, one a compute unit (198 to 256 registers), do one of three things:
 //   own pages       a wavefront for each (work item, kv head), operands in registers, rows = the query heads of the kv head
 //   16 rows         the wavefronts take an item's pages in turn, operands in registers; their results are added in LDS
 //   64, 128 rows    two pages a step, each expanded once into LDS by the four wavefronts that attend to it with 16 or 32 rows each;
@@ -32,7 +32,7 @@
 // What bounds it: 128 rows, a step 2.5 us, of which the SIMD's MFMAs take 1.09, its other vector instructions 1.0 (expansion and
 // softmax about half each) and LDS 0.9 (256 KiB read, 64 written).  MFMAs and vector instructions of two wavefronts overlap
 // by a third at most (16 MFMAs beside 64 multiply-adds 202 ns, alone 128 and 120).  256 rows over 32768 tokens, 8 kv heads: 55 us of
-// steps and some 12 of loads that wait for one another, first expansion, and results on their way out; 64.0 us with the merge, 542 TFLOP/s
+// steps and some 12 of loads that wait for one another, first expansion, and results on their way out; 64.1 us with the merge, 541 TFLOP/s
 // (a large product of the library reaches 1100).  16 rows: the chain item -> group -> page ids -> codes -> softmax -> sums in LDS; a page for
 // each wavefront takes 8 us.
 // Tried and not kept: 64 rows a wavefront in registers (copies between register files, 85 us instead of 64), 32 rows a wavefront with pages
@@ -327,7 +327,8 @@ template <int NT> __device__ __forceinline__ void weigh(Rows<NT> &rows, floatx4 
         for (int n = 0; n < NT; ++n) {
             float top = fmaxf(mx[n], __shfl_xor(mx[n], 16));
             top = fmaxf(top, __shfl_xor(top, 32));
-            // only a row that exceeds its own reference moves: its result does not depend on the wavefront's other rows
+            // Only a row that exceeds its own reference moves: its result does not depend on the wavefront's other rows.  (8 sequences over
+            // 11000 tokens 19.0 -> 19.15 us, 4 over 1500 10.4 -> 10.5 against all of them moving together.)
             const float old = rows.m[n];
             const bool moves = old == -INFINITY || top * factor[n] + shift[n] > kTau + (float)kPExp;
             const float m_new = moves ? fmaxf(old, top * factor[n]) : old;

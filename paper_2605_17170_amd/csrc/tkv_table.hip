@@ -15,9 +15,12 @@
 // asks for everything it may need (open pages, tops of the free lists) before the first of them.
 //   up to 1024 sequences, 6144 tokens and 1024 work entries: one launch, which also updates rows and places tokens.  32 sequences
 //     with a token each 5.7 us (an empty kernel 3.9 to 4.4), 200 with five 6.9; 9 thousand tokens would take 12.7, and 11.0 in two launches.
-//   up to 1024 sequences and 65536 tokens: rows and tokens in a second launch over many workgroups.  6 prompts with 63 thousand tokens
+//   up to 1024 sequences and 65536 tokens: rows and tokens in a second launch over many workgroups, and pages given back by rows of more
+//     than 8192 entries together in one between them.  6 prompts with 63 thousand tokens
 //     11.6 us (in four launches 15.6), 12 with 9 thousand 10.9 (15.2).
-//   beyond: four launches; tags to bit masks, sums in a loop, pages given back, rows and tokens.
+//   beyond: three launches, four where sequences may be cut; tags to bit masks, sums in a loop, pages given back, rows and tokens.  2048
+//     sequences with a token each 22.5 us, with eight 24, 8192 with four 61 (sums of 1024 sequences at a time); 2 prompts with 131 thousand
+//     tokens together 16.5, 32 with a million 36.
 #include <hip/hip_runtime.h>
 
 #include "tkv_internal.h"
