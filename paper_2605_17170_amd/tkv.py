@@ -71,14 +71,25 @@ class tkv_desc(C.Structure):
         return cls(n_kv_heads, head_dim, group_size, page_tokens, n_pages_int2, n_pages_int4, int2_key_axis)
 
 
+_KINDS = {"torch.int32": "i32", "torch.uint32": "i32", "torch.bfloat16": "bf16", "torch.int16": "bf16", "torch.uint16": "bf16"}
+_kinds = {}   # of the types met so far: looking a name up takes 0.3 us, and a call has up to eleven tensors
+
+
+def _kind(t) -> str:
+    """What a tensor can hold: "i32" whole numbers of 32 bits, "bf16" values (of that type, or raw 16-bit patterns; fp16 numbers
+    would be read as others), or "other"."""
+    kind = _kinds.get(t.dtype)
+    if kind is None:
+        kind = _kinds[t.dtype] = _KINDS.get(str(t.dtype), "other")
+    return kind
+
+
 def _i32(t) -> bool:
-    """Whether a tensor can hold the 32-bit whole numbers that are read from it."""
-    return t.element_size() == 4 and not t.is_floating_point()
+    return _kind(t) == "i32"
 
 
 def _bf16(t) -> bool:
-    """Whether a tensor can hold bf16 values: of that type, or raw 16-bit patterns; fp16 numbers would be read as others."""
-    return t.element_size() == 2 and str(t.dtype) != "torch.float16"
+    return _kind(t) == "bf16"
 
 
 class tkv_prefix(C.Structure):
