@@ -71,25 +71,17 @@ class tkv_desc(C.Structure):
         return cls(n_kv_heads, head_dim, group_size, page_tokens, n_pages_int2, n_pages_int4, int2_key_axis)
 
 
-_KINDS = {"torch.int32": "i32", "torch.uint32": "i32", "torch.bfloat16": "bf16", "torch.int16": "bf16", "torch.uint16": "bf16"}
-_kinds = {}   # of the types met so far: looking a name up takes 0.3 us, and a call has up to eleven tensors
+class _Holds(dict):
+    """By a tensor's type what it can hold: "i32" whole numbers of 32 bits, "bf16" values (of that type, or raw 16-bit patterns;
+    fp16 numbers would be read as others), or "other"."""
+    _NAMES = {"torch.int32": "i32", "torch.uint32": "i32", "torch.bfloat16": "bf16", "torch.int16": "bf16", "torch.uint16": "bf16"}
+
+    def __missing__(self, dtype):
+        self[dtype] = kind = self._NAMES.get(str(dtype), "other")
+        return kind
 
 
-def _kind(t) -> str:
-    """What a tensor can hold: "i32" whole numbers of 32 bits, "bf16" values (of that type, or raw 16-bit patterns; fp16 numbers
-    would be read as others), or "other"."""
-    kind = _kinds.get(t.dtype)
-    if kind is None:
-        kind = _kinds[t.dtype] = _KINDS.get(str(t.dtype), "other")
-    return kind
-
-
-def _i32(t) -> bool:
-    return _kind(t) == "i32"
-
-
-def _bf16(t) -> bool:
-    return _kind(t) == "bf16"
+_holds = _Holds()
 
 
 class tkv_prefix(C.Structure):
@@ -105,7 +97,7 @@ class tkv_prefix(C.Structure):
         SharedPlan.max_members in place of tile_rows names the rows too, a plain number there does not."""
         tensors = (page_indptr, page_ids, n_tok_int2, n_tok_int4, member_indptr, member_seqs, member_slots, items)
         n = n_tok_int2.numel()
-        assert all(_i32(t) for t in tensors) and n_tok_int4.numel() == n and page_indptr.numel() == member_indptr.numel() == n + 1
+        assert all(_holds[t.dtype] == "i32" for t in tensors) and n_tok_int4.numel() == n and page_indptr.numel() == member_indptr.numel() == n + 1
         assert member_seqs.numel() == member_slots.numel() and items.numel() % 5 == 0
         if tile_rows is None:
             tile_rows = getattr(max_members, "tile_rows", None)
@@ -126,7 +118,7 @@ class tkv_table(C.Structure):
         """i32 device tensors: page_ids [n_seqs, max_pages], n_tok_int2/4 [n_seqs], free_pages [pages of both pools], n_free [2]."""
         tensors = (page_ids, n_tok_int2, n_tok_int4, free_pages, n_free)
         n, m = int(page_ids.shape[0]), int(page_ids.shape[1])
-        assert all(_i32(t) for t in tensors) and n_tok_int2.numel() == n_tok_int4.numel() == n and n_free.numel() == 2
+        assert all(_holds[t.dtype] == "i32" for t in tensors) and n_tok_int2.numel() == n_tok_int4.numel() == n and n_free.numel() == 2
         table = cls(n, m, *(_dev(t) for t in tensors))
         table.tensors = tensors
         return table
@@ -621,12 +613,12 @@ def tkv_decode_attention_shared(desc, pool, bit_map, q, page_indptr, page_ids, n
     batch, n_q_heads = int(q.shape[0]), int(q.shape[1])
     n_items = int(items.shape[0]) if items is not None else 0
     ws_bytes = int(workspace.numel() * workspace.element_size()) if workspace is not None else 0
-    assert _bf16(q) and int(q.shape[2]) == desc.head_dim
-    assert out.numel() == q.numel() and _bf16(out)
-    assert slot_indptr.numel() == 2 * (batch + 1) and _i32(slot_indptr)
+    assert _holds[q.dtype] == "bf16" and int(q.shape[2]) == desc.head_dim
+    assert out.numel() == q.numel() and _holds[out.dtype] == "bf16"
+    assert slot_indptr.numel() == 2 * (batch + 1) and _holds[slot_indptr.dtype] == "i32"
     if n_items:
         assert items.numel() == 4 * n_items and page_indptr.numel() == batch + 1 and n_tok_int2.numel() == batch and n_tok_int4.numel() == batch
-        assert all(_i32(t) for t in (items, page_indptr, page_ids, n_tok_int2, n_tok_int4))
+        assert all(_holds[t.dtype] == "i32" for t in (items, page_indptr, page_ids, n_tok_int2, n_tok_int4))
     if n_items or prefix.n_items:
         assert pool.numel() * pool.element_size() >= tkv_pool_bytes(desc) and bit_map.numel() >= desc.n_pages_int2 + desc.n_pages_int4
     return _run(lib().tkv_decode_attention_shared,
@@ -660,9 +652,9 @@ def tkv_table_append(desc, table: tkv_table, keep_int2, keep_int4, n_new, tag_bi
     n, n_tokens = table.n_seqs, int(tag_bits.numel()) if tag_bits is not None else 0
     max_work = int(work_pages.numel()) if work_pages is not None else 0
     for t, count in ((keep_int2, n), (keep_int4, n), (n_new, n), (token_indptr, n + 1), (positions, n_tokens), (slot_ids, n_tokens), (n_work, 1)):
-        assert t is None or (t.numel() == count and _i32(t))
+        assert t is None or (t.numel() == count and _holds[t.dtype] == "i32")
     assert tag_bits is None or tag_bits.element_size() == 1
-    assert max_work == 0 or (work_src.numel() == max_work * PAGE_TOKENS and _i32(work_src) and _i32(work_pages))
+    assert max_work == 0 or (work_src.numel() == max_work * PAGE_TOKENS and _holds[work_src.dtype] == "i32" and _holds[work_pages.dtype] == "i32")
     assert table.tensors[3].numel() >= desc.n_pages_int2 + desc.n_pages_int4
     ws_bytes = int(workspace.numel() * workspace.element_size()) if workspace is not None else 0
     return _run(lib().tkv_table_append,
@@ -703,7 +695,7 @@ def _rows(t, heads: str):
     """(device pointer, token stride in elements, heads) of a bf16 tensor [T, heads, 128] whose heads lie densely."""
     if t is None:
         return None, 0, 0
-    assert t.dim() == 3 and int(t.shape[2]) == HEAD_DIM and _bf16(t), heads + " is bf16 [tokens, heads, 128]"
+    assert t.dim() == 3 and int(t.shape[2]) == HEAD_DIM and _holds[t.dtype] == "bf16", heads + " is bf16 [tokens, heads, 128]"
     assert t.stride(2) == 1 and (t.shape[1] <= 1 or t.stride(1) == HEAD_DIM), "the heads of a token lie one behind the other"
     return t.data_ptr(), t.stride(0) if t.shape[0] > 1 else int(t.shape[1]) * HEAD_DIM, int(t.shape[1])
 
@@ -714,11 +706,11 @@ def tkv_norm_rope(rope: tkv_rope, q, k, v, positions, q_weight, k_weight, eps: f
     (pq, sq, hq), (pk, sk, hk), (pv, sv, hv) = _rows(q, "q"), _rows(k, "k"), _rows(v, "v")
     n = int((q if q is not None else k).shape[0]) if q is not None or k is not None else 0
     for t, o in ((q, q_out), (k, k_out), (v, v_out)):
-        assert t is None or (o is not None and tuple(o.shape) == tuple(t.shape) and _bf16(o) and int(t.shape[0]) == n)
+        assert t is None or (o is not None and tuple(o.shape) == tuple(t.shape) and _holds[o.dtype] == "bf16" and int(t.shape[0]) == n)
     assert v is None or (k is not None and hv == hk)
-    assert rope.rotary_dim == 0 or positions.numel() == rope.n_axes * n and _i32(positions)
+    assert rope.rotary_dim == 0 or positions.numel() == rope.n_axes * n and _holds[positions.dtype] == "i32"
     for w in (q_weight, k_weight):
-        assert w is None or (w.numel() == HEAD_DIM and _bf16(w))
+        assert w is None or (w.numel() == HEAD_DIM and _holds[w.dtype] == "bf16")
     return _run(lib().tkv_norm_rope,
                 (C.byref(rope), pq, sq, pk, sk, pv, sv, n, hq, hk, _dev(positions), _dev(q_weight), _dev(k_weight), float(eps),
                  _dev(q_out if q is not None else None), _dev(k_out if k is not None else None), _dev(v_out if v is not None else None), _stream(stream)),
