@@ -190,3 +190,23 @@ def test_more_workgroups_than_a_dimension_of_the_grid(rows):
         assert bool(((out[1] - want[1]).float().abs() <= 2.0 ** -7 * want[1].float().abs() + 2.0 ** -16).all())
     finally:
         cache.close()
+
+
+@pytest.mark.parametrize("key_axis", [0, 1])
+def test_queries_that_are_subnormal_numbers(key_axis):
+    """Multiples of 2^-133, the smallest bf16 number, up to fifteen of them, as the same multiples of 1/4."""
+    cache, _, _ = build(103, [700], [30, 0, 130], 2, key_axis)
+    try:
+        f = np.clip(np.round(4 * wl.bf16_bits_to_f32(wl.make_q(np.random.SeedSequence([103, 5]), 3, 16))), -15, 15).astype(np.float32) / 4
+        f[1] = np.clip(f[1], -0.25, 0.25)        # (all of these heads' values are subnormal then)
+        q = (f.view(np.uint32) >> 16).astype(np.uint16)
+        small = np.where(f < 0, 0x8000, 0).astype(np.uint16) | (4 * np.abs(f)).astype(np.uint16)     # (the bits of a subnormal number are its multiple)
+        cache.plan_shared([[0, 1, 2]], 16, 8, 8)
+        scale = np.float32(gc.SM) / np.float32(16)
+        for rows in (16, 64, 128):
+            cut_rows(cache, rows, [3 * 8])
+            want = attend(cache, times(q, 1.0), scale)
+            got = attend(cache, harness.bf16_tensor(small, DEV), scale * np.float32(2.0 ** 127) * np.float32(2.0 ** 4))
+            assert torch.isfinite(want.float()).all() and torch.equal(got, want), rows
+    finally:
+        cache.close()
