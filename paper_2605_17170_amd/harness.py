@@ -148,7 +148,7 @@ class PagedCache:
         assert not prepare or (out is not None and workspace is not None)
         d_items, d_sip, items, _ = self._plan
         B, Hq = int(q.shape[0]), int(q.shape[1])
-        with _allocating_on(stream):
+        with _allocating_on(stream if out is None or workspace is None else None):
             if out is None:
                 out = torch.empty((B, Hq, tkv.HEAD_DIM), dtype=torch.float32, device=self.device)
             if workspace is None:
@@ -197,7 +197,7 @@ class PagedCache:
         """Attention of the batch of plan_shared over prefixes and own tokens, bf16; arguments as for decode."""
         assert not prepare or (out is not None and workspace is not None)
         n, plan, prefix, d_items, d_indptr = self._shared
-        with _allocating_on(stream):
+        with _allocating_on(stream if out is None or workspace is None else None):
             if out is None:
                 out = torch.empty(q.shape, dtype=torch.bfloat16, device=self.device)
             if workspace is None:
