@@ -45,15 +45,18 @@ enum {
 
 /* Bits the kernels may OR into the optional device status word. */
 enum {
-    TKV_STATUS_TAG_MISMATCH = 1,     /* append: tag_bits[token] differs from its page's pool width (token skipped) */
+    TKV_STATUS_TAG_MISMATCH = 1,     /* append: tag_bits[token] differs from its page's pool width (token skipped);
+                                        tkv_quantize_rows: it is none of 0, 2 and 4 (token skipped) */
     TKV_STATUS_BITMAP_MISMATCH = 2,  /* decode: bit_map[page] differs from the width its position implies (page skipped) */
     TKV_STATUS_PAGE_RANGE = 4,       /* a page id read on the device lies outside the pool (page skipped) */
     TKV_STATUS_DST_RANGE = 8,        /* tkv_gather_dequant: an output row index >= n_tokens (slot skipped) */
-    TKV_STATUS_BLOCK_PARTIAL = 16,   /* append, per-channel INT2 keys: a 32-token block arrived incomplete (block skipped) */
+    TKV_STATUS_BLOCK_PARTIAL = 16,   /* append, per-channel INT2 keys: a 32-token block arrived incomplete (block skipped);
+                                        tkv_quantize_rows: a block names a token outside the call or not at INT2 (block skipped) */
     TKV_STATUS_SCALE_SATURATED = 32, /* decode: a stored V scale above 255, or a per-channel INT2 key scale above 1023, was
                                         clamped: the output is finite but not the attention over the stored values */
     TKV_STATUS_BAD_ITEM = 64,        /* decode: a work item names a sequence outside the batch (it contributes nothing)
-                                        or a partial slot outside the workspace (its partial is not stored) */
+                                        or a partial slot outside the workspace (its partial is not stored); prefill: an
+                                        item names tokens, rows or slots that the call does not have (it is skipped) */
     TKV_STATUS_TABLE_REFUSED = 128,  /* tkv_table_append: lengths, widths or a table that cannot be (nothing was changed) */
     TKV_STATUS_POOL_EXHAUSTED = 256, /* tkv_table_append: too few free pages (nothing was changed) */
     TKV_STATUS_CAPACITY = 512        /* tkv_table_append: max_pages or max_work is too small (nothing was changed) */
@@ -682,6 +685,132 @@ int tkv_norm_rope(const tkv_rope *rope, const void *q, int64_t q_stride, const v
                   const void *v, int64_t v_stride, int32_t n_tokens, int32_t n_q_heads, int32_t n_kv_heads,
                   const int32_t *positions, const void *q_weight, const void *k_weight, float eps,
                   void *q_out, void *k_out, void *v_out, void *stream /* hipStream_t */);
+
+/* ------------------------------------------------------------------ */
+/* P2: attention of prompts over a gathered prefix (host plan, device). */
+/* ------------------------------------------------------------------ */
+/* Types of rows where an entry point takes more than one. */
+enum { TKV_BF16 = 0, TKV_FP16 = 1, TKV_FP32 = 2 };
+/*
+ * Plan of tkv_prefill_attention: which query rows meet which keys in which
+ * workgroup.  All host memory.  Row r of a sequence and kv head is query head
+ * r mod R of new token r / R, R = n_q_heads / n_kv_heads.  An item is a tile of
+ * tile_rows such rows (the same tile of every kv head) and a range of tiles of
+ * 64 keys, those of the prefix first; where there are too few tiles of rows to
+ * fill target_cus compute units, long ranges are cut into equal parts, whose
+ * partial results lie in a workspace and are joined.  Items come by falling
+ * length.  The plan depends on the lengths alone: layers, and replays of the
+ * same requests, share it.
+ *   desc             n_kv_heads and geometry; the pools may be empty
+ *   seq_indptr       host i32[batch+1], from 0: the sequences' new tokens
+ *   prefix_indptr    host i32[batch+1], from 0, or NULL: their prefix rows
+ *   target_cus       compute units to fill (>= 1)
+ *   items_out        host i32[10*capacity]: {first new token, new tokens, first
+ *                    prefix row, prefix rows, first row, first key tile, end,
+ *                    partial slot or -1, part, parts}
+ *   tile_rows_out    host i32
+ *   n_slots_out      host i32: partial slots, 0 if no range is cut
+ * Returns the number of items (>= 0) or a negative status.  A sequence without
+ * new tokens has none.  At most 2^30 rows (tokens * R) a sequence.
+ * tkv_plan_prefill_capacity: an upper bound of the items for n_tokens new tokens.
+ */
+int32_t tkv_plan_prefill_capacity(const tkv_desc *desc, int32_t batch, int32_t n_tokens, int32_t n_q_heads, int32_t target_cus);
+int32_t tkv_plan_prefill(const tkv_desc *desc, int32_t batch, int32_t n_q_heads, const int32_t *seq_indptr, const int32_t *prefix_indptr,
+                         int32_t target_cus, int32_t *items_out, int32_t capacity, int32_t *tile_rows_out, int32_t *n_slots_out);
+typedef struct tkv_prefill {
+    int32_t tile_rows, n_items, n_slots;   /* as tkv_plan_prefill gives them */
+    const int32_t *items;                  /* device, 4-byte aligned */
+} tkv_prefill;
+/* Bytes of workspace that n_slots partial slots take; 0 on a bad argument or if there are none. */
+size_t tkv_prefill_workspace_bytes(const tkv_desc *desc, int32_t n_slots, int32_t tile_rows);
+/*
+ * Causal attention of packed sequences (Sec. 3.2.3, "Prefill"): for new token i
+ * of a sequence and query head h, which reads kv head h / R,
+ *   out[i, h] = softmax_j(sm_scale * q[i, h] . k_j) v_j
+ * over the sequence's prefix rows (fp16, as tkv_gather_dequant writes them) and
+ * its new tokens' rows 0 .. i: a prompt, a chunk of one, or a single token.
+ *   q            device bf16 or fp16 (q_type), K, V bf16 or fp16 (kv_type):
+ *                bf16 queries go with either, fp16 ones with fp16.  16-byte
+ *                aligned; token t, head h, channel c at t * stride + h * 128 +
+ *                c with the tensor's own stride in elements (a multiple of 8,
+ *                below 2^23): parts of a packed projection, or tensors of their own
+ *   K_prefix,    device fp16 [n_prefix, n_kv_heads, 128], contiguous, 16-byte
+ *   V_prefix     aligned; may be NULL if n_prefix = 0
+ *   prefill      host struct, above; its items are for these lengths
+ *   out          device bf16 or fp16 (out_type) [n_tokens, n_q_heads, 128],
+ *                contiguous, 16-byte aligned, overlaps no input; rows that no
+ *                item covers (behind the last sequence) stay as they were
+ *   workspace    device, >= tkv_prefill_workspace_bytes(...), 16-byte aligned,
+ *                needs no initialisation; calls that overlap in time need one each
+ *   status       device i32, may be NULL: TKV_STATUS_BAD_ITEM
+ * Products are exact and summed in 32 bits; weights are rounded to the values'
+ * type, their sum is that of the rounded ones; bf16 queries meet fp16 keys as
+ * fp16 numbers with a power of two of their row (what lies 2^-24 below the
+ * row's largest, or below 2^-144, rounds to the grid of the subnormals).
+ * q . k and sm_scale * q . k (times log2 e, and for bf16 queries over fp16 keys
+ * sm_scale times the row's largest |q|) must be finite in 32 bits.  A row of q
+ * that holds NaN or infinities gives NaN and leaves the others alone; what
+ * stands in keys and values that a token does not see does not reach it.
+ * sm_scale > 0.  n_q_heads must be a multiple of n_kv_heads.  One launch on
+ * `stream`, a second one if n_slots > 0.
+ */
+int tkv_prefill_attention(const tkv_desc *desc, int32_t n_q_heads, const void *q, int64_t q_stride, int32_t q_type,
+                          const void *K, int64_t k_stride, const void *V, int64_t v_stride, int32_t kv_type, int32_t n_tokens,
+                          const void *K_prefix, const void *V_prefix, int32_t n_prefix, const tkv_prefill *prefill, float sm_scale,
+                          void *out, int32_t out_type, void *workspace, size_t workspace_bytes, int32_t *status,
+                          void *stream /* hipStream_t */);
+
+/* ------------------------------------------------------------------ */
+/* C1: what calibration replays (host plan, device).                    */
+/* ------------------------------------------------------------------ */
+/*
+ * The tokens at INT2 of every sequence, 32 a block in order of arrival, for
+ * per-channel keys: blocks_out host i32[32*capacity], token numbers over the
+ * whole of tag_bits (host, u8[seq_indptr[batch]]; other widths are passed over).
+ * A sequence whose INT2 tokens are no multiple of 32 is TKV_ERR_INVALID_ARG
+ * (tkv_route_residual first).  Returns the number of blocks or a negative status.
+ */
+int32_t tkv_plan_row_blocks(const uint8_t *tag_bits, const int32_t *seq_indptr, int32_t batch, int32_t *blocks_out, int32_t capacity);
+/*
+ * Keys and values as the cache would give them back: fp16 rows of what
+ * tkv_quantize_append stores and tkv_gather_dequant reads, for the tokens that
+ * tag_bits puts at INT2 or INT4; other tokens (width 0) are rounded to fp16.
+ * (Calibration replays attention with the tokens of one tag at one width,
+ * Sec. 3.1.3.)
+ *   desc         n_kv_heads and int2_key_axis; the pools may be empty
+ *   K, V         device bf16, 16-byte aligned, with a token stride each (in
+ *                elements, a multiple of 8): [n_tokens, n_kv_heads, 128]
+ *   tag_bits     device u8[n_tokens]: 0, 2 or 4; a token with another width is
+ *                skipped (TKV_STATUS_TAG_MISMATCH)
+ *   blocks       device i32[32*n_blocks] (tkv_plan_row_blocks), may be NULL if
+ *                n_blocks = 0.  With TKV_KEYS_PER_CHANNEL the keys of INT2
+ *                tokens are those of their block, and a key that no block names
+ *                stays as it was; with TKV_KEYS_PER_TOKEN n_blocks must be 0.
+ *                A block that names a token outside the call or not at INT2 is
+ *                skipped (TKV_STATUS_BLOCK_PARTIAL); no token in two blocks
+ *   K_out, V_out device fp16 [n_tokens, n_kv_heads, 128], contiguous, 16-byte
+ *                aligned, overlapping no input
+ *   status       device i32, may be NULL
+ * Inputs at width 2 or 4 finite and at most 65504.  One launch.
+ */
+int tkv_quantize_rows(const tkv_desc *desc, const void *K, int64_t k_stride, const void *V, int64_t v_stride, const uint8_t *tag_bits,
+                      int32_t n_tokens, const int32_t *blocks, int32_t n_blocks, void *K_out, void *V_out, int32_t *status,
+                      void *stream /* hipStream_t */);
+/*
+ * out[b, h] = mean over the tokens of sequence b and the 128 channels of
+ * (x - y)^2, in 64 bits, added up in the same order every time; 0 for a sequence
+ * without tokens: the distortion of a replay (Sec. 3.1.3).
+ *   x, y         device [n_tokens, n_heads, 128] of `type` (TKV_BF16, TKV_FP16 or
+ *                TKV_FP32), contiguous, 16-byte aligned
+ *   seq_indptr   device i32[batch+1], not falling, within [0, n_tokens]; a
+ *                sequence of which that does not hold gives NaN
+ *   out          device f64 [batch, n_heads]
+ *   workspace    device, >= tkv_distortion_workspace_bytes(...), 16-byte aligned
+ * Two launches.
+ */
+size_t tkv_distortion_workspace_bytes(int32_t batch, int32_t n_tokens, int32_t n_heads);
+int tkv_head_distortion(const void *x, const void *y, int32_t type, const int32_t *seq_indptr, int32_t batch, int32_t n_tokens,
+                        int32_t n_heads, double *out, void *workspace, size_t workspace_bytes, void *stream /* hipStream_t */);
 
 /* ------------------------------------------------------------------ */
 /* Measurement aid (device).                                            */

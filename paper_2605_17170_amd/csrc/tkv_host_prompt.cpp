@@ -1,0 +1,192 @@
+// Host side of prompts and calibration: the plan of prompt attention, the blocks of per-channel keys, and argument validation in
+// front of the launchers of tkv_prefill.hip and tkv_rows.hip.  Nothing here touches the GPU.
+#include "tkv.h"
+#include "tkv_internal.h"
+
+#include <algorithm>
+#include <cmath>
+#include <new>
+#include <vector>
+
+namespace {
+constexpr int kHeadDim = 128, kGroup = 32;
+constexpr int32_t kTileRows = 128;
+constexpr int64_t kMaxStride = 1 << 23;
+
+int group_of(const tkv_desc *desc, int32_t n_q_heads, int32_t &group)
+{
+    if (int st = tkv_desc_status(desc)) return st;
+    if (n_q_heads <= 0) return TKV_ERR_INVALID_ARG;
+    if (n_q_heads % desc->n_kv_heads) return TKV_ERR_BAD_SHAPE;
+    group = n_q_heads / desc->n_kv_heads;
+    return TKV_OK;
+}
+bool rows_ok(const void *p, int64_t stride, int64_t heads, int32_t n_tokens)
+{
+    return p && !((uintptr_t)p & 15) && stride >= 0 && stride % 8 == 0 && stride < kMaxStride && (stride >= heads * kHeadDim || n_tokens == 1);
+}
+int64_t up(int64_t a, int64_t b) { return (a + b - 1) / b; }
+// Parts that a plan cuts beyond one of each tile: for one kv head at most eight for a compute unit.
+constexpr int64_t kPartsPerCu = 8;
+} // namespace
+
+extern "C" {
+
+/* ---------------------------------------------------------------- P2: attention of prompts */
+
+int32_t tkv_plan_prefill_capacity(const tkv_desc *desc, int32_t batch, int32_t n_tokens, int32_t n_q_heads, int32_t target_cus)
+{
+    int32_t group = 0;
+    if (int st = group_of(desc, n_q_heads, group)) return st;
+    if (batch < 0 || n_tokens < 0 || target_cus < 1) return TKV_ERR_INVALID_ARG;
+    const int64_t n = (int64_t)n_tokens * group / kTileRows + batch + kPartsPerCu * target_cus;
+    return n > INT32_MAX ? (int32_t)TKV_ERR_INVALID_ARG : (int32_t)n;
+}
+
+int32_t tkv_plan_prefill(const tkv_desc *desc, int32_t batch, int32_t n_q_heads, const int32_t *seq_indptr, const int32_t *prefix_indptr,
+                         int32_t target_cus, int32_t *items_out, int32_t capacity, int32_t *tile_rows_out, int32_t *n_slots_out)
+{
+    int32_t group = 0;
+    if (int st = group_of(desc, n_q_heads, group)) return st;
+    if (batch < 0 || target_cus < 1 || capacity < 0 || !seq_indptr || !tile_rows_out || !n_slots_out || (capacity > 0 && !items_out)) return TKV_ERR_INVALID_ARG;
+    if (seq_indptr[0] != 0 || (prefix_indptr && prefix_indptr[0] != 0)) return TKV_ERR_INVALID_ARG;
+    for (int32_t b = 0; b < batch; ++b) {
+        if (seq_indptr[b + 1] < seq_indptr[b] || (prefix_indptr && prefix_indptr[b + 1] < prefix_indptr[b])) return TKV_ERR_INVALID_ARG;
+        if (((int64_t)seq_indptr[b + 1] - seq_indptr[b]) * group > 1 << 30) return TKV_ERR_INVALID_ARG;
+    }
+    try {
+        struct Tile { int32_t seq, row, keys, parts; };   // keys: tiles of 64
+        std::vector<Tile> tiles;
+        int64_t all = 0;
+        for (int32_t b = 0; b < batch; ++b) {
+            const int32_t n = seq_indptr[b + 1] - seq_indptr[b], pre = prefix_indptr ? prefix_indptr[b + 1] - prefix_indptr[b] : 0;
+            const int64_t rows = (int64_t)n * group;
+            for (int64_t r = 0; r < rows; r += kTileRows) {
+                const int64_t see = (std::min(r + kTileRows, rows) - 1) / group + 1;
+                const int64_t keys = up(pre, kPrefillKeys) + up(see, kPrefillKeys);
+                tiles.push_back({b, (int32_t)r, (int32_t)keys, 1});
+                all += keys;
+            }
+        }
+        // two workgroups to a compute unit; a part costs a partial of its rows, written and read
+        const int64_t slots = std::max<int64_t>(1, 2 * (int64_t)target_cus / desc->n_kv_heads), share = std::max<int64_t>(4, up(all, slots));
+        int64_t n_slots = 0, n_items = 0;
+        for (Tile &t : tiles) {
+            if (t.keys > share + share / 4) t.parts = (int32_t)std::min<int64_t>(up(t.keys, share), kPartsPerCu * target_cus / 2);
+            n_items += t.parts;
+            if (t.parts > 1) n_slots += t.parts;
+        }
+        if (n_items > capacity) return TKV_ERR_CAPACITY;
+        if (n_items * desc->n_kv_heads > INT32_MAX || n_slots > INT32_MAX) return TKV_ERR_INVALID_ARG;
+        std::stable_sort(tiles.begin(), tiles.end(), [](const Tile &x, const Tile &y) { return (int64_t)x.keys * y.parts > (int64_t)y.keys * x.parts; });
+        int32_t slot = 0, *it = items_out;
+        for (const Tile &t : tiles)
+            for (int32_t k = 0; k < t.parts; ++k, it += kPrefillItemWords) {
+                const int32_t b = t.seq;
+                it[0] = seq_indptr[b];
+                it[1] = seq_indptr[b + 1] - seq_indptr[b];
+                it[2] = prefix_indptr ? prefix_indptr[b] : 0;
+                it[3] = prefix_indptr ? prefix_indptr[b + 1] - prefix_indptr[b] : 0;
+                it[4] = t.row;
+                it[5] = (int32_t)((int64_t)t.keys * k / t.parts);
+                it[6] = (int32_t)((int64_t)t.keys * (k + 1) / t.parts);
+                it[7] = t.parts > 1 ? slot++ : -1;
+                it[8] = k;
+                it[9] = t.parts;
+            }
+        *tile_rows_out = kTileRows;
+        *n_slots_out = slot;
+        return (int32_t)n_items;
+    } catch (const std::bad_alloc &) {
+        return TKV_ERR_INVALID_ARG;
+    }
+}
+
+size_t tkv_prefill_workspace_bytes(const tkv_desc *desc, int32_t n_slots, int32_t tile_rows)
+{
+    if (tkv_desc_status(desc) || n_slots < 0 || tile_rows != kTileRows) return 0;
+    return (size_t)n_slots * desc->n_kv_heads * tile_rows * (kHeadDim + 2) * sizeof(float);
+}
+
+int tkv_prefill_attention(const tkv_desc *desc, int32_t n_q_heads, const void *q, int64_t q_stride, int32_t q_type, const void *K, int64_t k_stride,
+                          const void *V, int64_t v_stride, int32_t kv_type, int32_t n_tokens, const void *K_prefix, const void *V_prefix, int32_t n_prefix,
+                          const tkv_prefill *prefill, float sm_scale, void *out, int32_t out_type, void *workspace, size_t workspace_bytes, int32_t *status,
+                          void *stream)
+{
+    int32_t group = 0;
+    if (int st = group_of(desc, n_q_heads, group)) return st;
+    if (!prefill || n_tokens < 0 || n_prefix < 0 || prefill->n_items < 0 || prefill->n_slots < 0) return TKV_ERR_INVALID_ARG;
+    if ((q_type != TKV_BF16 && q_type != TKV_FP16) || (kv_type != TKV_BF16 && kv_type != TKV_FP16) || (out_type != TKV_BF16 && out_type != TKV_FP16) ||
+        (q_type == TKV_FP16 && kv_type == TKV_BF16))
+        return TKV_ERR_INVALID_ARG;
+    if (!(sm_scale > 0.0f) || !(sm_scale < 2.0e38f)) return TKV_ERR_INVALID_ARG;
+    if (prefill->n_items == 0 || n_tokens == 0) return TKV_OK;
+    if (prefill->tile_rows != kTileRows || !prefill->items || ((uintptr_t)prefill->items & 3)) return TKV_ERR_INVALID_ARG;
+    if (!rows_ok(q, q_stride, n_q_heads, n_tokens) || !rows_ok(K, k_stride, desc->n_kv_heads, n_tokens) || !rows_ok(V, v_stride, desc->n_kv_heads, n_tokens)) return TKV_ERR_INVALID_ARG;
+    if (n_prefix > 0 && (!rows_ok(K_prefix, 0, 0, n_prefix) || !rows_ok(V_prefix, 0, 0, n_prefix))) return TKV_ERR_INVALID_ARG;
+    if ((int64_t)desc->n_kv_heads * kHeadDim >= kMaxStride) return TKV_ERR_BAD_SHAPE;
+    if (!out || ((uintptr_t)out & 15) || ((uintptr_t)workspace & 15) || ((uintptr_t)status & 3)) return TKV_ERR_INVALID_ARG;
+    if ((int64_t)prefill->n_items * desc->n_kv_heads > INT32_MAX / 64 || (int64_t)n_tokens * group > INT32_MAX) return TKV_ERR_INVALID_ARG;
+    if (prefill->n_slots > 0) {
+        if (!workspace) return TKV_ERR_INVALID_ARG;
+        if (workspace_bytes < tkv_prefill_workspace_bytes(desc, prefill->n_slots, prefill->tile_rows)) return TKV_ERR_WORKSPACE_TOO_SMALL;
+    }
+    return tkv_launch_prefill(n_q_heads, desc->n_kv_heads, q, q_stride, q_type, K, k_stride, V, v_stride, kv_type, n_tokens, K_prefix, V_prefix, n_prefix, prefill,
+                              sm_scale, out, out_type, workspace, status, stream);
+}
+
+/* ---------------------------------------------------------------- C1: rows as the cache gives them back, distortion */
+
+int32_t tkv_plan_row_blocks(const uint8_t *tag_bits, const int32_t *seq_indptr, int32_t batch, int32_t *blocks_out, int32_t capacity)
+{
+    if (!seq_indptr || batch < 0 || capacity < 0 || (capacity > 0 && !blocks_out) || seq_indptr[0] != 0) return TKV_ERR_INVALID_ARG;
+    int64_t n = 0;
+    for (int32_t b = 0; b < batch; ++b) {
+        if (seq_indptr[b + 1] < seq_indptr[b]) return TKV_ERR_INVALID_ARG;
+        if (seq_indptr[b + 1] > seq_indptr[b] && !tag_bits) return TKV_ERR_INVALID_ARG;
+        int64_t mine = 0;
+        for (int32_t t = seq_indptr[b]; t < seq_indptr[b + 1]; ++t) mine += tag_bits[t] == 2;
+        if (mine % kGroup) return TKV_ERR_INVALID_ARG;
+        n += mine;
+    }
+    if (n > kGroup * (int64_t)capacity) return TKV_ERR_CAPACITY;
+    int32_t *to = blocks_out;
+    for (int32_t t = 0; t < seq_indptr[batch]; ++t)
+        if (tag_bits[t] == 2) *to++ = t;
+    return (int32_t)(n / kGroup);
+}
+
+int tkv_quantize_rows(const tkv_desc *desc, const void *K, int64_t k_stride, const void *V, int64_t v_stride, const uint8_t *tag_bits, int32_t n_tokens,
+                      const int32_t *blocks, int32_t n_blocks, void *K_out, void *V_out, int32_t *status, void *stream)
+{
+    if (int st = tkv_desc_status(desc)) return st;
+    if (n_tokens < 0 || n_blocks < 0 || n_blocks > n_tokens / kGroup) return TKV_ERR_INVALID_ARG;
+    if (n_tokens == 0) return TKV_OK;
+    if (n_blocks > 0 && (!blocks || ((uintptr_t)blocks & 3) || desc->int2_key_axis != TKV_KEYS_PER_CHANNEL)) return TKV_ERR_INVALID_ARG;
+    if (!rows_ok(K, k_stride, desc->n_kv_heads, n_tokens) || !rows_ok(V, v_stride, desc->n_kv_heads, n_tokens)) return TKV_ERR_INVALID_ARG;
+    if (!tag_bits || !K_out || !V_out || ((uintptr_t)K_out & 15) || ((uintptr_t)V_out & 15) || ((uintptr_t)status & 3)) return TKV_ERR_INVALID_ARG;
+    if ((int64_t)n_tokens * desc->n_kv_heads > INT32_MAX) return TKV_ERR_INVALID_ARG;
+    return tkv_launch_quantize_rows(desc, K, k_stride, V, v_stride, tag_bits, n_tokens, blocks, n_blocks, K_out, V_out, status, stream);
+}
+
+size_t tkv_distortion_workspace_bytes(int32_t batch, int32_t n_tokens, int32_t n_heads)
+{
+    if (batch < 0 || n_tokens < 0 || n_heads < 0) return 0;
+    return ((size_t)(n_tokens / kDistortionChunk) + (size_t)batch) * (size_t)n_heads * sizeof(double);
+}
+
+int tkv_head_distortion(const void *x, const void *y, int32_t type, const int32_t *seq_indptr, int32_t batch, int32_t n_tokens, int32_t n_heads, double *out,
+                        void *workspace, size_t workspace_bytes, void *stream)
+{
+    if (type != TKV_BF16 && type != TKV_FP16 && type != TKV_FP32) return TKV_ERR_INVALID_ARG;
+    if (batch < 0 || n_tokens < 0 || n_heads < 0) return TKV_ERR_INVALID_ARG;
+    if (batch == 0 || n_heads == 0) return TKV_OK;
+    if (!seq_indptr || ((uintptr_t)seq_indptr & 3) || !out || ((uintptr_t)out & 7)) return TKV_ERR_INVALID_ARG;
+    if (n_tokens > 0 && (!x || !y || (((uintptr_t)x | (uintptr_t)y) & 15))) return TKV_ERR_INVALID_ARG;
+    if (!workspace || ((uintptr_t)workspace & 15)) return TKV_ERR_INVALID_ARG;
+    if ((int64_t)batch * n_heads > INT32_MAX || (int64_t)n_tokens * n_heads > INT32_MAX) return TKV_ERR_INVALID_ARG;
+    if (workspace_bytes < tkv_distortion_workspace_bytes(batch, n_tokens, n_heads)) return TKV_ERR_WORKSPACE_TOO_SMALL;
+    return tkv_launch_distortion(x, y, type, seq_indptr, batch, n_tokens, n_heads, out, workspace, stream);
+}
+
+} // extern "C"

@@ -1,6 +1,6 @@
 // Internal interface between the host-side validation (tkv_host.cpp) and the
 // kernel launchers (tkv_append.hip, tkv_gather.hip, tkv_decode.hip,
-// tkv_shared.hip, tkv_table.hip, tkv_rope.hip, tkv_probe.hip).  Arguments are already
+// tkv_shared.hip, tkv_table.hip, tkv_rope.hip, tkv_prefill.hip, tkv_rows.hip, tkv_probe.hip).  Arguments are already
 // validated; the launchers return TKV_OK or TKV_ERR_HIP.
 #ifndef TKV_INTERNAL_H
 #define TKV_INTERNAL_H
@@ -43,6 +43,21 @@ int tkv_launch_table_reset(const tkv_desc *desc, const tkv_table *table, void *s
 int tkv_launch_table_append(const tkv_desc *desc, const tkv_table *table, const int32_t *keep_int2, const int32_t *keep_int4, const int32_t *n_new,
                             const uint8_t *tag_bits, int32_t n_tokens, int32_t *token_indptr, int32_t *positions, int32_t *slot_ids,
                             int32_t *work_pages, int32_t *work_src, int32_t max_work, int32_t *n_work, void *workspace, int32_t *status, void *stream);
+
+constexpr int kPrefillKeys = 64;         // keys of a tile of tkv_prefill_attention
+constexpr int kPrefillItemWords = 10;    // of an item of its plan
+constexpr int kDistortionChunk = 16;     // tokens of a partial sum of tkv_head_distortion
+
+int tkv_launch_prefill(int32_t n_q_heads, int32_t n_kv_heads, const void *q, int64_t q_stride, int32_t q_type, const void *K, int64_t k_stride,
+                       const void *V, int64_t v_stride, int32_t kv_type, int32_t n_tokens, const void *K_prefix, const void *V_prefix,
+                       int32_t n_prefix, const tkv_prefill *prefill, float sm_scale, void *out, int32_t out_type, void *workspace,
+                       int32_t *status, void *stream);
+
+int tkv_launch_quantize_rows(const tkv_desc *desc, const void *K, int64_t k_stride, const void *V, int64_t v_stride, const uint8_t *tag_bits,
+                             int32_t n_tokens, const int32_t *blocks, int32_t n_blocks, void *K_out, void *V_out, int32_t *status, void *stream);
+
+int tkv_launch_distortion(const void *a, const void *b, int32_t type, const int32_t *seq_indptr, int32_t batch, int32_t n_tokens, int32_t n_heads,
+                          double *out, void *workspace, void *stream);
 
 // Argument checks shared by the entry points (tkv_host.cpp); TKV_OK or a negative status.
 int tkv_desc_status(const tkv_desc *desc);

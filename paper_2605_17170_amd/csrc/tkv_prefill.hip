@@ -1,0 +1,469 @@
+// tkv_prefill_attention: causal attention of packed sequences' new tokens over the rows of a cached prefix (fp16, as
+// tkv_gather_dequant writes them) and over the new tokens themselves (Sec. 3.2.3, "Prefill").
+//
+//   out[i, h] = sum_j p_j v_j / sum_j p_j,   p_j = 2^(c q[i, h] . k_j - m),   c = sm_scale log2 e
+//
+// over the sequence's prefix rows and its new rows 0 .. i.  A workgroup takes a tile of query rows of one kv head -- row r is
+// query head r mod R of token r / R, so that all heads that share a key fill one tile -- and walks over tiles of 64 keys:
+// S^T = K Q^T and O^T += V^T P^T on v_mfma_f32_32x32x16, a wavefront 32 rows.  Transposed, a lane holds one query row: the running
+// maximum, the sum and the mask's limit are one register each, and the weights leave the first product's accumulators in the
+// order in which the second one takes its operand, if V's rows are read in that order too (ds_read_b64_tr_b16).
+#include <hip/hip_runtime.h>
+
+#include <type_traits>
+
+#include "tkv_internal.h"
+#include "tkv_layout.h"
+
+namespace {
+
+using namespace tkv;
+
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
+typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+
+constexpr int kKeys = kPrefillKeys;   // of a tile
+constexpr int kRow = kHeadDim * 2;        // bytes
+constexpr int kTile = kKeys * kRow;       // bytes of a tile of K or of V
+constexpr int kItem = kPrefillItemWords;
+constexpr float kNone = -3.4028235e38f;   // reference of a row that has seen no key
+constexpr float kSlack = 8.0f;            // weights grow to 2^8 before the reference follows the maximum
+
+struct PrefillArgs {
+    const uint16_t *q, *k[2], *v[2];      // keys and values: prefix, new tokens
+    int64_t q_stride, k_stride[2], v_stride[2];
+    const int32_t *items;
+    uint16_t *out;
+    float *partial;
+    int32_t *status;
+    int32_t n_items, n_slots, n_tokens, n_prefix, group, n_kv_heads, q_bf16, out_bf16;
+    float c;
+};
+
+__device__ __forceinline__ float lo_f32(uint32_t v) { return __uint_as_float(v << 16); }
+__device__ __forceinline__ float hi_f32(uint32_t v) { return __uint_as_float(v & 0xffff0000u); }
+template <bool BF16> __device__ __forceinline__ uint32_t pack(float a, float b)   // nearest even
+{
+    if constexpr (BF16) {
+        const bf16x2 v = {(__bf16)a, (__bf16)b};
+        return __builtin_bit_cast(uint32_t, v);
+    } else {
+        const f16x2 v = {(_Float16)a, (_Float16)b};
+        return __builtin_bit_cast(uint32_t, v);
+    }
+}
+template <bool BF16> __device__ __forceinline__ f32x16 mfma(u32x4 a, u32x4 b, f32x16 c)
+{
+    if constexpr (BF16) return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
+    else return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
+}
+template <bool BF16> __device__ __forceinline__ float add_pair(uint32_t p, float sum)
+{
+    if constexpr (BF16) {
+        const bf16x2 one = {(__bf16)1.0f, (__bf16)1.0f};
+        return __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, p), one, sum, false);
+    } else {
+        const f16x2 one = {(_Float16)1.0f, (_Float16)1.0f};
+        return __builtin_amdgcn_fdot2(__builtin_bit_cast(f16x2, p), one, sum, false);
+    }
+}
+// The other half's value of the same query row.
+__device__ __forceinline__ float both_max(float x)
+{
+    const auto s = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    return fmaxf(__uint_as_float(s[0]), __uint_as_float(s[1]));
+}
+__device__ __forceinline__ float both_sum(float x)
+{
+    const auto s = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    return __uint_as_float(s[0]) + __uint_as_float(s[1]);
+}
+
+// Sixteen bytes a lane from global memory to LDS (lane l: `lds` + 16 l), zeros from beyond the buffer.  Written out, with the waits
+// beside it: the compiler waits for every such load before any read of LDS.
+__device__ __forceinline__ void load_lds(uint32_t lds, u32x4 buffer, uint32_t offset, uint32_t base)
+{
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, %3 offen lds" :: "s"(lds), "v"(offset), "s"(buffer), "s"(base) : "memory");
+}
+__device__ __forceinline__ void wait_barrier() { asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
+
+__device__ __forceinline__ u32x4 buffer_of(const void *p, uint32_t bytes)
+{
+    const uint64_t a = (uint64_t)(uintptr_t)p;
+    u32x4 r;
+    r.x = __builtin_amdgcn_readfirstlane((uint32_t)a);
+    r.y = __builtin_amdgcn_readfirstlane((uint32_t)(a >> 32) & 0xffffu);
+    r.z = __builtin_amdgcn_readfirstlane(bytes);
+    r.w = 0x00020000u;
+    return r;
+}
+
+struct Item {
+    int32_t token0, n_new, prefix0, n_prefix, row0, begin, end, slot, part, n_parts;
+};
+__device__ __forceinline__ Item item_of(const int32_t *items, int k)
+{
+    const int32_t *p = items + (int64_t)kItem * k;
+    return {p[0], p[1], p[2], p[3], p[4], p[5], p[6], p[7], p[8], p[9]};
+}
+// Whether everything that the item names lies inside what the call has.
+__device__ __forceinline__ bool item_ok(const Item &it, const PrefillArgs &a)
+{
+    return it.token0 >= 0 && it.n_new > 0 && (int64_t)it.token0 + it.n_new <= a.n_tokens && it.prefix0 >= 0 && it.n_prefix >= 0 &&
+           (int64_t)it.prefix0 + it.n_prefix <= a.n_prefix && it.row0 >= 0 && it.row0 < (int64_t)it.n_new * a.group && it.begin >= 0 && it.begin <= it.end &&
+           it.slot >= -1 && it.slot < a.n_slots && it.n_parts >= 1 && it.part >= 0 && it.part < it.n_parts && (int64_t)it.slot - it.part + it.n_parts <= a.n_slots &&
+           (it.slot < 0 ? it.n_parts == 1 : it.slot >= it.part);
+}
+
+// What a wavefront knows of its 32 rows: lane l has row l % 32.
+struct Rows {
+    u32x4 q[8];        // channels 16 s + 8 (l / 32) .. of the row
+    f32x16 o[4];       // channel 32 t + 8 (i / 4) + 4 (l / 32) + i % 4 of the row
+    float m;           // reference of the exponents
+    float sum;         // of this half's weights
+    float c;           // logits to exponents of 2
+};
+
+// Queries of the rows, as fp16 (times a power of two for each row, if they are bf16: exact but for what lies 2^-24 below the largest)
+// or as they are.
+template <bool BF16> __device__ __forceinline__ void load_q(Rows &w, const uint16_t *row, bool live, const PrefillArgs &a)
+{
+    const int half = (threadIdx.x >> 5) & 1;
+#pragma unroll
+    for (int s = 0; s < 8; ++s) w.q[s] = live ? reinterpret_cast<const u32x4 *>(row)[2 * s + half] : u32x4{};
+    w.c = a.c;
+    if constexpr (!BF16) {
+        if (a.q_bf16) {
+            uint32_t big = 0;
+#pragma unroll
+            for (int s = 0; s < 8; ++s)
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    const uint32_t hi = w.q[s][k] >> 16 & 0x7fff, lo = w.q[s][k] & 0x7fff;
+                    big = hi < 0x7f80 && hi > big ? hi : big;      // NaN and infinities stay what they are
+                    big = lo < 0x7f80 && lo > big ? lo : big;
+                }
+            const auto o = __builtin_amdgcn_permlane32_swap(big, big, false, false);
+            big = o[0] > o[1] ? o[0] : o[1];
+            int e = 14 - ((int)(big >> 7) - 127);                   // the largest becomes 2^14 .. 2^15
+            e = e > 120 ? 120 : e;
+            const float by = __uint_as_float((uint32_t)(e + 127) << 23);
+            w.c = a.c * __uint_as_float((uint32_t)(127 - e) << 23);
+#pragma unroll
+            for (int s = 0; s < 8; ++s)
+#pragma unroll
+                for (int k = 0; k < 4; ++k) w.q[s][k] = pack<false>(lo_f32(w.q[s][k]) * by, hi_f32(w.q[s][k]) * by);
+        }
+    }
+    // the loads have come back here: a wait for them inside the loop over the tiles would wait for the next tile too
+#pragma unroll
+    for (int s = 0; s < 8; ++s) asm volatile("" : "+v"(w.q[s]));
+}
+
+// Values of V that are finite; infinities and NaN as zero.
+template <bool BF16> __device__ __forceinline__ uint32_t finite_only(uint32_t v)
+{
+    constexpr uint32_t top = BF16 ? 0x7f80u : 0x7c00u;
+    const uint32_t low = (v & top) == top ? 0u : 0xffffu, high = (v >> 16 & top) == top ? 0u : 0xffff0000u;
+    return v & (low | high);
+}
+
+template <int WAVES> struct Tiles {
+    uint32_t lds;               // byte address of [2 buffers][K, V][64 keys][256 bytes]
+    uint32_t k_lane, v_lane;    // byte offsets of this lane's piece of the wavefront's first rows in global memory
+    uint32_t k_at, v_at;        // and the places that it reads from: see below
+};
+
+// V's operand of channels 32 t .. and keys 16 s ..: two transposed reads of four keys each.
+template <int WAVES> __device__ __forceinline__ u32x4 v_operand(const Tiles<WAVES> &t, uint32_t tile, int d, int s)
+{
+    u32x4 r;
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+        const uint32_t at = (t.v_at ^ (uint32_t)(d << 6)) + tile + s * 16 * kRow + u * 8 * kRow;
+        const s16x4 x = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4 *)(uintptr_t)at);
+        const u32x2 y = __builtin_bit_cast(u32x2, x);
+        r[2 * u] = y.x;
+        r[2 * u + 1] = y.y;
+    }
+    return r;
+}
+
+// Rows of a tile in LDS: 16 pieces of 16 bytes.  Piece p of key r lies at place p ^ (r & 15) in K, whose operand is read 32 keys at a
+// time, and at p ^ 4 (r & 3) in V, of which a transposed read takes four keys' 64 bytes.
+template <bool BF16, int WAVES>
+__device__ __forceinline__ void attend(Rows &w, const Tiles<WAVES> &t, const uint16_t *k, int64_t k_stride, const uint16_t *v, int64_t v_stride, int begin, int end,
+                                       int n_keys, int limit, int least, int most)
+{
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, half = lane >> 5;
+    constexpr int kLoads = kKeys / 4 / WAVES;   // of a wavefront, of K and of V each
+    const int64_t k_bytes = 2 * k_stride, v_bytes = 2 * v_stride;
+    const uint32_t k_offset = (uint32_t)(4 * wave + (lane >> 4)) * (uint32_t)k_bytes + t.k_lane, v_offset = (uint32_t)(4 * wave + (lane >> 4)) * (uint32_t)v_bytes + t.v_lane;
+    auto fetch = [&](int i) {
+        const int left = n_keys - i * kKeys, rows = left < kKeys ? left : kKeys;
+        const u32x4 kb = buffer_of(reinterpret_cast<const uint8_t *>(k) + (int64_t)i * kKeys * k_bytes, (uint32_t)rows * (uint32_t)k_bytes);
+        const u32x4 vb = buffer_of(reinterpret_cast<const uint8_t *>(v) + (int64_t)i * kKeys * v_bytes, (uint32_t)rows * (uint32_t)v_bytes);
+        const uint32_t to = __builtin_amdgcn_readfirstlane(t.lds + (uint32_t)(i & 1) * 2 * kTile + wave * 4 * kRow);
+#pragma unroll
+        for (int j = 0; j < kLoads; ++j)
+            load_lds(to + j * WAVES * 4 * kRow, kb, k_offset, __builtin_amdgcn_readfirstlane((uint32_t)(j * WAVES * 4) * (uint32_t)k_bytes));
+#pragma unroll
+        for (int j = 0; j < kLoads; ++j)
+            load_lds(to + kTile + j * WAVES * 4 * kRow, vb, v_offset, __builtin_amdgcn_readfirstlane((uint32_t)(j * WAVES * 4) * (uint32_t)v_bytes));
+    };
+    uint32_t strange = 0;   // a masked tile has values that are not finite
+    auto step = [&](int i, auto masked) {
+        const int first = i * kKeys;
+        const uint32_t tile = t.lds + (uint32_t)(i & 1) * 2 * kTile;
+        f32x16 s[2];
+#pragma unroll
+        for (int b = 0; b < 2; ++b) {
+            s[b] = f32x16{};
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const uint32_t at = (t.k_at ^ (uint32_t)(j << 5)) + tile + b * 32 * kRow;
+                const u32x4 x = *(__attribute__((address_space(3))) const u32x4 *)(uintptr_t)at;
+                s[b] = mfma<BF16>(x, w.q[j], s[b]);
+            }
+        }
+        if constexpr (masked) {
+#pragma unroll
+            for (int b = 0; b < 2; ++b)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) s[b][r] = first + 32 * b + 8 * (r >> 2) + 4 * half + (r & 3) > limit ? -INFINITY : s[b][r];
+        }
+        float top = s[0][0];
+#pragma unroll
+        for (int b = 0; b < 2; ++b)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) top = fmaxf(top, s[b][r]);
+        top = both_max(top) * w.c;
+        const bool grows = top > w.m + kSlack;
+        if (__any(grows)) {   // row by row: what a row gives does not depend on the others of its wavefront
+            const float m = grows ? top : w.m, by = __builtin_amdgcn_exp2f(w.m - m);
+            w.m = m;
+            w.sum *= by;
+#pragma unroll
+            for (int d = 0; d < 4; ++d)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) w.o[d][r] *= by;
+        }
+        uint32_t p[16];
+#pragma unroll
+        for (int b = 0; b < 2; ++b)
+#pragma unroll
+            for (int r = 0; r < 16; r += 2) {
+                const float x = __builtin_amdgcn_exp2f(fmaf(s[b][r], w.c, -w.m)), y = __builtin_amdgcn_exp2f(fmaf(s[b][r + 1], w.c, -w.m));
+                p[8 * b + r / 2] = pack<BF16>(x, y);
+                w.sum = add_pair<BF16>(p[8 * b + r / 2], w.sum);
+            }
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+#pragma unroll
+            for (int d = 0; d < 4; ++d) {
+                u32x4 x = v_operand(t, tile + kTile, d, j);
+                if constexpr (masked) {   // a weight of zero must not meet infinities and NaN of keys that its row does not see
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const uint32_t y = finite_only<BF16>(x[e]);
+                        strange |= x[e] ^ y;
+                        x[e] = y;
+                    }
+                }
+                w.o[d] = mfma<BF16>(x, u32x4{p[4 * j], p[4 * j + 1], p[4 * j + 2], p[4 * j + 3]}, w.o[d]);
+            }
+    };
+    // the tiles that all rows of the wavefront see, then those that need a mask
+    const int seen = (least + 1) / kKeys, plain = seen < begin ? begin : seen < end ? seen : end;
+    if (begin < end) fetch(begin);
+    int i = begin;
+    for (; i < plain; ++i) {
+        wait_barrier();   // this tile has arrived, and nobody reads the one before it
+        if (i + 1 < end) fetch(i + 1);
+        step(i, std::false_type{});
+    }
+    for (; i < end; ++i) {
+        wait_barrier();
+        if (i + 1 < end) fetch(i + 1);
+        if (i * kKeys <= most) step(i, std::true_type{});
+    }
+    if (__any(strange != 0)) {   // what was left out above, for the rows that see it
+        const int from = (least + 1) / kKeys, last = end * kKeys < most + 1 ? end * kKeys : most + 1;
+#pragma unroll 1
+        for (int key = (from > begin ? from : begin) * kKeys; key < last; ++key) {
+            const u32x2 *row = reinterpret_cast<const u32x2 *>(v + (int64_t)key * v_stride) + half;
+#pragma unroll
+            for (int d = 0; d < 4; ++d)
+#pragma unroll
+                for (int r = 0; r < 16; r += 4) {
+                    const u32x2 x = row[8 * d + r / 2];
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const uint32_t bits = e & 1 ? x[e >> 1] >> 16 : x[e >> 1] & 0xffffu;
+                        const float value = BF16 ? __uint_as_float(bits << 16) : (float)__builtin_bit_cast(_Float16, (uint16_t)bits);
+                        w.o[d][r + e] += key <= limit && !(fabsf(value) < INFINITY) ? value : 0.0f;
+                    }
+                }
+        }
+    }
+    wait_barrier();   // nobody reads the last tile: its place may be filled again
+}
+
+// BF16: the new tokens' keys, values and queries are bf16; else keys and values are fp16.
+template <bool BF16, int WAVES>
+__global__ __launch_bounds__(64 * WAVES) __attribute__((amdgpu_waves_per_eu(2, 2))) void tkv_prefill_kernel(PrefillArgs a)
+{
+    extern __shared__ __attribute__((aligned(1024))) uint8_t smem[];
+    const uint32_t block = blockIdx.x + blockIdx.y * gridDim.x;
+    const int kv_head = (int)(block % (uint32_t)a.n_kv_heads), number = (int)(block / (uint32_t)a.n_kv_heads);
+    if (number >= a.n_items) return;
+    const Item it = item_of(a.items, number);
+    if (!item_ok(it, a)) {
+        if (a.status && threadIdx.x == 0) atomicOr(a.status, TKV_STATUS_BAD_ITEM);
+        return;
+    }
+    constexpr int kTileRows = 32 * WAVES;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, half = lane >> 5;
+    const uint32_t n_rows = (uint32_t)it.n_new * (uint32_t)a.group, row = (uint32_t)it.row0 + 32 * wave + (lane & 31);
+    const bool live = row < n_rows;
+    const uint32_t use = live ? row : n_rows - 1;
+    const int token = (int)(use / (uint32_t)a.group), head = kv_head * a.group + (int)(use - (uint32_t)token * (uint32_t)a.group);
+    const uint32_t last = (uint32_t)it.row0 + kTileRows < n_rows ? (uint32_t)it.row0 + kTileRows : n_rows;
+    const int n_see = (int)((last - 1) / (uint32_t)a.group) + 1;   // new keys that any row of the workgroup sees
+    const int tiles0 = (it.n_prefix + kKeys - 1) / kKeys, tiles1 = (n_see + kKeys - 1) / kKeys;
+    const int begin = it.begin, end = it.end < tiles0 + tiles1 ? it.end : tiles0 + tiles1;
+    const bool idle = (uint32_t)it.row0 + 32 * wave >= n_rows;     // no row of this wavefront exists
+
+    Tiles<WAVES> t;
+    t.lds = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t *)smem;
+    const int r16 = 4 * (wave & 3) + (lane >> 4);   // key of this lane's piece, modulo 16
+    t.k_lane = (uint32_t)(((lane & 15) ^ r16) * 16);
+    t.v_lane = (uint32_t)(((lane & 15) ^ ((lane >> 4) << 2)) * 16);
+    t.k_at = (uint32_t)((lane & 31) * kRow + ((half ^ (lane & 15)) << 4));
+    const int v_key = 4 * half + ((lane & 15) >> 2);
+    t.v_at = (uint32_t)(v_key * kRow + (((v_key & 3) << 2 ^ (2 * ((lane >> 4) & 1) + ((lane >> 1) & 1))) << 4) + (lane & 1) * 8);
+
+    Rows w;
+#pragma unroll
+    for (int d = 0; d < 4; ++d) w.o[d] = f32x16{};
+    w.m = kNone;
+    w.sum = 0.0f;
+    const uint16_t *q = a.q + (int64_t)(it.token0 + token) * a.q_stride + (int64_t)head * kHeadDim;
+    if (begin < tiles0) {
+        load_q<false>(w, q, live, a);
+        const int see = idle ? -1 : it.n_prefix - 1;
+        attend<false, WAVES>(w, t, a.k[0] + (int64_t)it.prefix0 * a.k_stride[0] + (int64_t)kv_head * kHeadDim, a.k_stride[0],
+                             a.v[0] + (int64_t)it.prefix0 * a.v_stride[0] + (int64_t)kv_head * kHeadDim, a.v_stride[0], begin, end < tiles0 ? end : tiles0, it.n_prefix, it.n_prefix - 1,
+                             see, see);
+    }
+    if (end > tiles0) {
+        load_q<BF16>(w, q, live, a);
+        const int least = idle ? -1 : __builtin_amdgcn_readlane(token, 0), most = idle ? -1 : __builtin_amdgcn_readlane(token, 31);
+        attend<BF16, WAVES>(w, t, a.k[1] + (int64_t)it.token0 * a.k_stride[1] + (int64_t)kv_head * kHeadDim, a.k_stride[1],
+                            a.v[1] + (int64_t)it.token0 * a.v_stride[1] + (int64_t)kv_head * kHeadDim, a.v_stride[1], begin > tiles0 ? begin - tiles0 : 0, end - tiles0, n_see, token,
+                            least, most);
+    }
+    const float sum = both_sum(w.sum);
+    if (it.slot < 0) {
+        const float by = 1.0f / sum;
+        uint16_t *to = a.out + ((int64_t)(it.token0 + token) * (a.n_kv_heads * a.group) + head) * kHeadDim;
+#pragma unroll
+        for (int d = 0; d < 4; ++d)
+#pragma unroll
+            for (int r = 0; r < 16; r += 8) {
+                uint32_t x[4];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const float u = w.o[d][r + 2 * e] * by, v = w.o[d][r + 2 * e + 1] * by;
+                    x[e] = a.out_bf16 ? pack<true>(u, v) : pack<false>(u, v);
+                }
+                // channels 4 half .. and 8 + 4 half .. of 16: each half takes eight in a row
+                const auto y = __builtin_amdgcn_permlane32_swap(x[0], x[2], false, false), z = __builtin_amdgcn_permlane32_swap(x[1], x[3], false, false);
+                if (live) *reinterpret_cast<u32x4 *>(to + 32 * d + 2 * r + 8 * half) = u32x4{y[0], z[0], y[1], z[1]};
+            }
+    } else {
+        const int64_t at = ((int64_t)it.slot * a.n_kv_heads + kv_head) * kTileRows + 32 * wave + (lane & 31);
+        float *to = a.partial + at * kHeadDim;
+        if (live) {
+#pragma unroll
+            for (int d = 0; d < 4; ++d)
+#pragma unroll
+                for (int r = 0; r < 16; r += 4)
+                    *reinterpret_cast<float4 *>(to + 32 * d + 2 * r + 4 * half) = make_float4(w.o[d][r], w.o[d][r + 1], w.o[d][r + 2], w.o[d][r + 3]);
+            if (half == 0) reinterpret_cast<float2 *>(a.partial + (int64_t)a.n_slots * a.n_kv_heads * kTileRows * kHeadDim)[at] = make_float2(w.m, sum);
+        }
+    }
+}
+
+// Joins the parts of a tile's rows: a wavefront takes a row, two channels a lane.
+__global__ __launch_bounds__(256) void tkv_prefill_merge_kernel(PrefillArgs a, int32_t tile_rows)
+{
+    const uint32_t chunks = (uint32_t)tile_rows / 4, block = blockIdx.x + blockIdx.y * gridDim.x;
+    const uint32_t of = block / chunks;
+    const int kv_head = (int)(of % (uint32_t)a.n_kv_heads), number = (int)(of / (uint32_t)a.n_kv_heads);
+    if (number >= a.n_items) return;
+    const Item it = item_of(a.items, number);
+    if (it.slot < 0 || it.part != 0 || !item_ok(it, a)) return;
+    const int lane = threadIdx.x & 63, in_tile = (int)(block % chunks) * 4 + (int)(threadIdx.x >> 6);
+    const uint32_t row = (uint32_t)it.row0 + in_tile, n_rows = (uint32_t)it.n_new * (uint32_t)a.group;
+    if (row >= n_rows) return;
+    const float2 *ml = reinterpret_cast<const float2 *>(a.partial + (int64_t)a.n_slots * a.n_kv_heads * tile_rows * kHeadDim);
+    auto at = [&](int p) { return ((int64_t)(it.slot + p) * a.n_kv_heads + kv_head) * tile_rows + in_tile; };
+    float m = kNone;
+    for (int p = 0; p < it.n_parts; ++p) m = fmaxf(m, ml[at(p)].x);
+    float sum = 0.0f, x = 0.0f, y = 0.0f;
+    for (int p = 0; p < it.n_parts; ++p) {
+        const float2 s = ml[at(p)];
+        const float by = __builtin_amdgcn_exp2f(s.x - m);
+        const float2 o = reinterpret_cast<const float2 *>(a.partial + at(p) * kHeadDim)[lane];
+        sum = fmaf(s.y, by, sum);
+        x = fmaf(o.x, by, x);
+        y = fmaf(o.y, by, y);
+    }
+    const float by = 1.0f / sum;
+    const uint32_t token = row / (uint32_t)a.group, head = kv_head * a.group + (row - token * a.group);
+    uint32_t *to = reinterpret_cast<uint32_t *>(a.out + ((int64_t)(it.token0 + (int)token) * (a.n_kv_heads * a.group) + head) * kHeadDim);
+    to[lane] = a.out_bf16 ? pack<true>(x * by, y * by) : pack<false>(x * by, y * by);
+}
+
+} // namespace
+
+int tkv_launch_prefill(int32_t n_q_heads, int32_t n_kv_heads, const void *q, int64_t q_stride, int32_t q_type, const void *K, int64_t k_stride, const void *V,
+                       int64_t v_stride, int32_t kv_type, int32_t n_tokens, const void *K_prefix, const void *V_prefix, int32_t n_prefix, const tkv_prefill *prefill,
+                       float sm_scale, void *out, int32_t out_type, void *workspace, int32_t *status, void *stream)
+{
+    PrefillArgs a = {};
+    a.q = (const uint16_t *)q;
+    a.k[0] = (const uint16_t *)K_prefix; a.k[1] = (const uint16_t *)K;
+    a.v[0] = (const uint16_t *)V_prefix; a.v[1] = (const uint16_t *)V;
+    // (the stride of a single token is any number)
+    a.q_stride = q_stride;
+    if (n_tokens == 1) k_stride = v_stride = (int64_t)n_kv_heads * kHeadDim;
+    a.k_stride[0] = a.v_stride[0] = (int64_t)n_kv_heads * kHeadDim;
+    a.k_stride[1] = k_stride; a.v_stride[1] = v_stride;
+    a.items = prefill->items;
+    a.out = (uint16_t *)out;
+    a.partial = (float *)workspace;
+    a.status = status;
+    a.n_items = prefill->n_items; a.n_slots = prefill->n_slots; a.n_tokens = n_tokens; a.n_prefix = n_prefix;
+    a.group = n_q_heads / n_kv_heads; a.n_kv_heads = n_kv_heads;
+    a.q_bf16 = q_type == TKV_BF16; a.out_bf16 = out_type == TKV_BF16;
+    a.c = sm_scale * 1.44269504088896340736f;
+    constexpr int64_t kMaxX = 1 << 22;   // a grid has less than 2^32 threads in a dimension
+    auto grid = [&](int64_t blocks) { return dim3((unsigned)(blocks < kMaxX ? blocks : kMaxX), (unsigned)((blocks + kMaxX - 1) / kMaxX)); };
+    const int64_t blocks = (int64_t)prefill->n_items * n_kv_heads;
+    auto *kernel = kv_type == TKV_BF16 ? tkv_prefill_kernel<true, 4> : tkv_prefill_kernel<false, 4>;
+    hipLaunchKernelGGL(kernel, grid(blocks), dim3(256), 4 * kTile, (hipStream_t)stream, a);
+    if (hipGetLastError() != hipSuccess) return TKV_ERR_HIP;
+    if (prefill->n_slots > 0) {
+        hipLaunchKernelGGL(tkv_prefill_merge_kernel, grid(blocks * (prefill->tile_rows / 4)), dim3(256), 0, (hipStream_t)stream, a, prefill->tile_rows);
+        if (hipGetLastError() != hipSuccess) return TKV_ERR_HIP;
+    }
+    return TKV_OK;
+}

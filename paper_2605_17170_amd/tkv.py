@@ -35,6 +35,9 @@ TKV_STATUS_POOL_EXHAUSTED = 256
 TKV_STATUS_CAPACITY = 512
 TKV_KEYS_PER_TOKEN = 0
 TKV_KEYS_PER_CHANNEL = 1
+TKV_BF16 = 0
+TKV_FP16 = 1
+TKV_FP32 = 2
 
 PAGE_TOKENS = 64
 HEAD_DIM = 128
@@ -49,7 +52,9 @@ EXPORTS = [
     "tkv_decode_split", "tkv_decode_reduce", "tkv_decode_attention_static", "tkv_allocate_bits_greedy", "tkv_allocate_bits_exhaustive",
     "tkv_tag_tokens", "tkv_tags_to_bits", "tkv_tag_counts", "tkv_plan_shared_capacity",
     "tkv_plan_decode_shared", "tkv_decode_attention_shared", "tkv_table_reset", "tkv_table_max_work",
-    "tkv_table_workspace_bytes", "tkv_table_append", "tkv_rope_table", "tkv_norm_rope", "tkv_probe_stream_read",
+    "tkv_table_workspace_bytes", "tkv_table_append", "tkv_rope_table", "tkv_norm_rope", "tkv_plan_prefill_capacity", "tkv_plan_prefill",
+    "tkv_prefill_workspace_bytes", "tkv_prefill_attention", "tkv_plan_row_blocks", "tkv_quantize_rows", "tkv_distortion_workspace_bytes",
+    "tkv_head_distortion", "tkv_probe_stream_read",
     "tkv_probe_decode_reads", "tkv_probe_stream_mix",
 ]
 
@@ -131,6 +136,20 @@ class tkv_rope(C.Structure):
                 ("table", C.c_void_p)]
 
 
+class tkv_prefill(C.Structure):
+    """The plan of prompt attention on the device; `make` keeps the tensor alive."""
+    _fields_ = [("tile_rows", C.c_int32), ("n_items", C.c_int32), ("n_slots", C.c_int32), ("items", C.c_void_p)]
+
+    @classmethod
+    def make(cls, plan, device="cuda"):
+        """`plan`: a PrefillPlan."""
+        import torch
+        items = torch.from_numpy(np.ascontiguousarray(plan.items, np.int32)).to(device)
+        prefill = cls(int(plan.tile_rows), items.numel() // PREFILL_ITEM_WORDS, int(plan.n_slots), _dev(items))
+        prefill.tensors = (items,)
+        return prefill
+
+
 _lib = None
 
 
@@ -206,6 +225,20 @@ def lib():
         L.tkv_rope_table.argtypes = [i32, i32, vp, i32, C.c_double, vp, vp]
         L.tkv_norm_rope.argtypes = [C.POINTER(tkv_rope), vp, C.c_int64, vp, C.c_int64, vp, C.c_int64, i32, i32, i32, vp, vp, vp, C.c_float,
                                     vp, vp, vp, vp]
+        L.tkv_plan_prefill_capacity.restype = i32
+        L.tkv_plan_prefill_capacity.argtypes = [dp, i32, i32, i32, i32]
+        L.tkv_plan_prefill.restype = i32
+        L.tkv_plan_prefill.argtypes = [dp, i32, i32, vp, vp, i32, vp, i32, C.POINTER(i32), C.POINTER(i32)]
+        L.tkv_prefill_workspace_bytes.restype = sz
+        L.tkv_prefill_workspace_bytes.argtypes = [dp, i32, i32]
+        L.tkv_prefill_attention.argtypes = [dp, i32, vp, C.c_int64, i32, vp, C.c_int64, vp, C.c_int64, i32, i32, vp, vp, i32, C.POINTER(tkv_prefill),
+                                            C.c_float, vp, i32, vp, sz, vp, vp]
+        L.tkv_plan_row_blocks.restype = i32
+        L.tkv_plan_row_blocks.argtypes = [vp, vp, i32, vp, i32]
+        L.tkv_quantize_rows.argtypes = [dp, vp, C.c_int64, vp, C.c_int64, vp, i32, vp, i32, vp, vp, vp, vp]
+        L.tkv_distortion_workspace_bytes.restype = sz
+        L.tkv_distortion_workspace_bytes.argtypes = [i32, i32, i32]
+        L.tkv_head_distortion.argtypes = [vp, vp, i32, vp, i32, i32, i32, vp, vp, sz, vp]
         L.tkv_probe_stream_read.argtypes = [vp, sz, vp, vp]
         L.tkv_probe_decode_reads.argtypes = [dp, vp, vp, vp, vp, vp, vp, i32, i32, i32, vp, vp]
         L.tkv_probe_stream_mix.argtypes = [vp, vp, sz, i32, i32, vp]
@@ -715,6 +748,115 @@ def tkv_norm_rope(rope: tkv_rope, q, k, v, positions, q_weight, k_weight, eps: f
                 (C.byref(rope), pq, sq, pk, sk, pv, sv, n, hq, hk, _dev(positions), _dev(q_weight), _dev(k_weight), float(eps),
                  _dev(q_out if q is not None else None), _dev(k_out if k is not None else None), _dev(v_out if v is not None else None), _stream(stream)),
                 "tkv_norm_rope", (rope, q, k, v, positions, q_weight, k_weight, q_out, k_out, v_out, stream), prepare)
+
+
+# ---------------------------------------------------------------- P2 (host plan, device)
+PREFILL_ITEM_WORDS = 10
+PrefillPlan = collections.namedtuple("PrefillPlan", "items n_slots tile_rows")
+_TYPES = {"torch.bfloat16": TKV_BF16, "torch.float16": TKV_FP16, "torch.float32": TKV_FP32}
+
+
+def _type(t, allowed, what):
+    kind = _TYPES.get(str(t.dtype))
+    assert kind in allowed, what + " has the type " + str(t.dtype)
+    return kind
+
+
+def tkv_plan_prefill(desc, n_q_heads: int, seq_indptr, prefix_indptr=None, target_cus: int = 256) -> PrefillPlan:
+    """Plan for sequences of seq_indptr's new tokens behind prefix_indptr's cached ones (host arrays [batch+1]).
+    PrefillPlan: items i32[n_items, 10], n_slots, tile_rows."""
+    ip, pip = _np(seq_indptr, np.int32)
+    batch = ip.size - 1
+    pp = None
+    if prefix_indptr is not None:
+        pre, pp = _np(prefix_indptr, np.int32)
+        if pre.size != ip.size:
+            raise ValueError("prefix_indptr has one entry per sequence and one more, as seq_indptr")
+    cap = _check(lib().tkv_plan_prefill_capacity(C.byref(desc), batch, int(ip[-1]) if ip.size else 0, n_q_heads, target_cus), "tkv_plan_prefill_capacity")
+    items = np.empty((cap, PREFILL_ITEM_WORDS), np.int32)
+    rows, slots = C.c_int32(0), C.c_int32(0)
+    n = _check(lib().tkv_plan_prefill(C.byref(desc), batch, n_q_heads, pip, pp, target_cus, C.c_void_p(items.ctypes.data), cap, C.byref(rows),
+                                      C.byref(slots)), "tkv_plan_prefill")
+    return PrefillPlan(items[:n].copy(), slots.value, rows.value)
+
+
+def tkv_prefill_workspace_bytes(desc, n_slots: int, tile_rows: int) -> int:
+    return int(lib().tkv_prefill_workspace_bytes(C.byref(desc), n_slots, tile_rows))
+
+
+def _typed_rows(t, heads, n, allowed, what):
+    """(device pointer, token stride in elements, type) of a tensor [n, heads, 128] whose heads lie densely."""
+    assert t.dim() == 3 and tuple(t.shape) == (n, heads, HEAD_DIM), "%s is [%d, %d, 128]" % (what, n, heads)
+    assert t.stride(2) == 1 and (heads <= 1 or t.stride(1) == HEAD_DIM), "the heads of a token lie one behind the other"
+    return t.data_ptr(), t.stride(0) if n > 1 else heads * HEAD_DIM, _type(t, allowed, what)
+
+
+def tkv_prefill_attention(desc, q, K, V, K_prefix, V_prefix, prefill: tkv_prefill, sm_scale: float, out, workspace=None, status=None, stream=None,
+                          prepare=False):
+    """Device tensors: q [T,Hq,128], K and V [T,Hkv,128], each with a token stride of its own, bf16 or fp16 (fp16 queries with fp16 keys
+    and values only); K_prefix, V_prefix fp16 [P,Hkv,128] or None; out bf16 or fp16 [T,Hq,128]; workspace u8 or None if the plan has no slots."""
+    n, hq, hk = int(q.shape[0]), int(q.shape[1]), desc.n_kv_heads
+    pq, sq, tq = _typed_rows(q, hq, n, (TKV_BF16, TKV_FP16), "q")
+    pk, sk, tk = _typed_rows(K, hk, n, (TKV_BF16, TKV_FP16), "K")
+    pv, sv, tv = _typed_rows(V, hk, n, (TKV_BF16, TKV_FP16), "V")
+    assert tk == tv, "K and V have one type"
+    assert (K_prefix is None) == (V_prefix is None)
+    n_prefix = int(K_prefix.shape[0]) if K_prefix is not None else 0
+    for t in (K_prefix, V_prefix):
+        assert t is None or (tuple(t.shape) == (n_prefix, hk, HEAD_DIM) and _type(t, (TKV_FP16,), "the prefix") == TKV_FP16)
+    assert tuple(out.shape) == (n, hq, HEAD_DIM)
+    ws_bytes = int(workspace.numel() * workspace.element_size()) if workspace is not None else 0
+    return _run(lib().tkv_prefill_attention,
+                (C.byref(desc), hq, pq, sq, tq, pk, sk, pv, sv, tk, n, _dev(K_prefix), _dev(V_prefix), n_prefix, C.byref(prefill), float(sm_scale),
+                 _dev(out), _type(out, (TKV_BF16, TKV_FP16), "out"), _dev(workspace), ws_bytes, _dev(status), _stream(stream)),
+                "tkv_prefill_attention", (desc, q, K, V, K_prefix, V_prefix, prefill, out, workspace, status, stream), prepare)
+
+
+# ---------------------------------------------------------------- C1 (host plan, device)
+def tkv_plan_row_blocks(tag_bits, seq_indptr) -> np.ndarray:
+    """Blocks of 32 INT2 tokens of each sequence i32[n, 32] (host arrays: u8 per token, offsets of the sequences)."""
+    bits, pb = _np(tag_bits, np.uint8)
+    ip, pip = _np(seq_indptr, np.int32)
+    if ip.size < 1 or (ip.size > 1 and ip[-1] != bits.size):
+        raise ValueError("seq_indptr ends at the number of tokens")
+    blocks = np.empty((bits.size // GROUP_SIZE, GROUP_SIZE), np.int32)
+    n = _check(lib().tkv_plan_row_blocks(pb, pip, ip.size - 1, C.c_void_p(blocks.ctypes.data if blocks.size else None), blocks.shape[0]),
+               "tkv_plan_row_blocks")
+    return blocks[:n].copy()
+
+
+def tkv_quantize_rows(desc, K, V, tag_bits, blocks, K_out, V_out, status=None, stream=None, prepare=False):
+    """Device tensors: K, V bf16 [T,Hkv,128] with a token stride each; tag_bits u8[T]; blocks i32[n, 32] or None;
+    K_out, V_out fp16 [T,Hkv,128]."""
+    n, hk = int(K.shape[0]), desc.n_kv_heads
+    pk, sk, _ = _typed_rows(K, hk, n, (TKV_BF16,), "K")
+    pv, sv, _ = _typed_rows(V, hk, n, (TKV_BF16,), "V")
+    for t in (K_out, V_out):
+        assert tuple(t.shape) == (n, hk, HEAD_DIM) and _type(t, (TKV_FP16,), "the output") == TKV_FP16
+    assert tag_bits.numel() == n and tag_bits.element_size() == 1
+    n_blocks = 0
+    if blocks is not None:
+        assert _holds[blocks.dtype] == "i32" and blocks.numel() % GROUP_SIZE == 0
+        n_blocks = blocks.numel() // GROUP_SIZE
+    return _run(lib().tkv_quantize_rows,
+                (C.byref(desc), pk, sk, pv, sv, _dev(tag_bits), n, _dev(blocks), n_blocks, _dev(K_out), _dev(V_out), _dev(status), _stream(stream)),
+                "tkv_quantize_rows", (desc, K, V, tag_bits, blocks, K_out, V_out, status, stream), prepare)
+
+
+def tkv_distortion_workspace_bytes(batch: int, n_tokens: int, n_heads: int) -> int:
+    return int(lib().tkv_distortion_workspace_bytes(batch, n_tokens, n_heads))
+
+
+def tkv_head_distortion(x, y, seq_indptr, out, workspace, stream=None, prepare=False):
+    """Device tensors: x, y [T,H,128] of one type (bf16, fp16 or fp32); seq_indptr i32[B+1]; out f64 [B,H]; workspace u8."""
+    assert x.dim() == 3 and tuple(x.shape) == tuple(y.shape) and int(x.shape[2]) == HEAD_DIM and x.dtype == y.dtype
+    n, heads, batch = int(x.shape[0]), int(x.shape[1]), int(seq_indptr.numel()) - 1
+    assert _holds[seq_indptr.dtype] == "i32" and tuple(out.shape) == (batch, heads) and str(out.dtype) == "torch.float64"
+    ws_bytes = int(workspace.numel() * workspace.element_size()) if workspace is not None else 0
+    return _run(lib().tkv_head_distortion,
+                (_dev(x), _dev(y), _type(x, (TKV_BF16, TKV_FP16, TKV_FP32), "x"), _dev(seq_indptr), batch, n, heads, _dev(out), _dev(workspace), ws_bytes,
+                 _stream(stream)),
+                "tkv_head_distortion", (x, y, seq_indptr, out, workspace, stream), prepare)
 
 
 # ---------------------------------------------------------------- measurement aid (device)

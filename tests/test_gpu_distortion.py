@@ -1,0 +1,97 @@
+"""tkv_head_distortion against sums in 64 bits by another order.
+
+Tolerance: differences of bf16 and fp16 numbers, and of fp32 numbers in 64 bits, lose nothing or 2^-53; n squares of one sign added in any order are
+off by at most n 2^-53 of their sum, on either side."""
+import numpy as np
+import pytest
+import torch
+
+from paper_2605_17170_amd import tkv
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+
+
+def make(lens, heads, kind, seed, spare=0):
+    g = torch.Generator(device=DEV)
+    g.manual_seed(seed)
+    shape = (sum(lens) + spare, heads, 128)
+    x = torch.randn(shape, device=DEV, generator=g)
+    y = x + torch.randn(shape, device=DEV, generator=g) * 0.05
+    return x.to(kind), y.to(kind), torch.from_numpy(np.concatenate([[0], np.cumsum(lens)]).astype(np.int32)).to(DEV)
+
+
+def call(x, y, ip, **kw):
+    out = torch.full((ip.numel() - 1, x.shape[1]), -1.0, dtype=torch.float64, device=DEV)
+    ws = torch.full((max(16, tkv.tkv_distortion_workspace_bytes(ip.numel() - 1, x.shape[0], x.shape[1])),), 255, dtype=torch.uint8, device=DEV)
+    tkv.tkv_head_distortion(x, y, ip, out, ws, **kw)
+    return out
+
+
+def check(got, x, y, lens):
+    a = 0
+    for b, n in enumerate(lens):
+        ref = (x[a:a + n].double() - y[a:a + n].double()).square().sum((0, 2)) / max(1, n * 128)
+        assert ((got[b] - ref).abs() <= (n * 128 + 4) * 2.0 ** -52 * ref).all(), "sequence %d of %d tokens" % (b, n)
+        a += n
+
+
+@pytest.mark.parametrize("kind", [torch.bfloat16, torch.float16, torch.float32])
+@pytest.mark.parametrize("lens,heads", [([1], 1), ([0], 3), ([15, 16, 17], 2), ([0, 1, 0, 0, 33, 0], 5), ([1000, 3, 500], 20), ([63] * 300, 1), ([2] * 1000, 3), ([5000], 64)])
+def test_lengths_and_heads(kind, lens, heads):
+    x, y, ip = make(lens, heads, kind, heads, spare=5)
+    got = call(x, y, ip)
+    torch.cuda.synchronize()
+    check(got, x, y, lens)
+    assert torch.equal(got, call(x, y, ip))
+
+
+def test_what_is_not_finite_stays_in_its_sequence_and_head():
+    lens = [40, 50, 3]
+    x, y, ip = make(lens, 4, torch.bfloat16, 1, spare=2)
+    clean = call(x, y, ip)
+    x[45, 2, 7], y[91, 0, 0] = float("nan"), float("inf")
+    x[93:] = float("nan")
+    got = call(x, y, ip)
+    torch.cuda.synchronize()
+    assert torch.isnan(got[1, 2]) and got[2, 0] == float("inf")
+    got[1, 2], got[2, 0] = clean[1, 2], clean[2, 0]
+    assert torch.equal(got, clean)
+
+
+@pytest.mark.parametrize("offsets", [[0, 10, 5, 20], [0, 10, 21, 21], [-1, 5, 10, 20], [0, 30, 10, 20], [20, 10, 5, 0]])
+def test_offsets_that_cannot_be_give_nan_for_their_sequences(offsets):
+    x, y, _ = make([20], 2, torch.float16, 2)
+    got = call(x, y, torch.tensor(offsets, dtype=torch.int32, device=DEV))
+    torch.cuda.synchronize()
+    for b in range(3):
+        lo, hi = offsets[b], offsets[b + 1]
+        assert torch.isnan(got[b]).all() == (not 0 <= lo <= hi <= 20)
+
+
+def test_no_tokens_at_all():
+    got = call(torch.zeros((0, 3, 128), device=DEV), torch.zeros((0, 3, 128), device=DEV), torch.zeros(3, dtype=torch.int32, device=DEV))
+    torch.cuda.synchronize()
+    assert (got == 0).all()
+
+
+def test_on_another_stream_and_captured():
+    lens = [100, 300]
+    x, y, ip = make(lens, 8, torch.bfloat16, 3)
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    out = torch.zeros((2, 8), dtype=torch.float64, device=DEV)
+    ws = torch.zeros(tkv.tkv_distortion_workspace_bytes(2, 400, 8), dtype=torch.uint8, device=DEV)
+    s.wait_stream(torch.cuda.current_stream())
+    tkv.tkv_head_distortion(x, y, ip, out, ws, stream=s)
+    s.synchronize()
+    check(out, x, y, lens)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        tkv.tkv_head_distortion(x, y, ip, out, ws)
+    for k in range(3):
+        x.mul_(1.5)
+        out.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        check(out, x, y, lens)
