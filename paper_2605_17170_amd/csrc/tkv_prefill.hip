@@ -175,20 +175,21 @@ template <bool BF16> __device__ __forceinline__ uint32_t finite_only(uint32_t v)
 }
 
 template <int WAVES> struct Tiles {
-    uint32_t lds;               // byte address of [2 buffers][K, V][64 keys][256 bytes]
-    uint32_t k_lane, v_lane;    // byte offsets of this lane's piece of the wavefront's first rows in global memory
-    uint32_t k_at, v_at;        // and the places that it reads from: see below
+    uint32_t lds;               // byte address of two buffers for tiles of K, two for tiles of V
+    uint32_t k_lane, v_lane;    // this lane's piece of its row in global memory, in bytes
+    uint32_t k_at[8], v_at[4];  // where it reads its operands in a buffer: channels 16 j .. of K, 32 d .. of V
 };
+typedef __attribute__((address_space(3))) const u32x4 lds_u32x4;
+typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
 
-// V's operand of channels 32 t .. and keys 16 s ..: two transposed reads of four keys each.
-template <int WAVES> __device__ __forceinline__ u32x4 v_operand(const Tiles<WAVES> &t, uint32_t tile, int d, int s)
+__device__ __forceinline__ u32x4 k_operand(uint32_t at, int b) { return *(lds_u32x4 *)(uintptr_t)(at + b * 32 * kRow); }
+// V's operand of keys 16 s ..: two transposed reads of four keys each.
+__device__ __forceinline__ u32x4 v_operand(uint32_t at, int s)
 {
     u32x4 r;
 #pragma unroll
     for (int u = 0; u < 2; ++u) {
-        const uint32_t at = (t.v_at ^ (uint32_t)(d << 6)) + tile + s * 16 * kRow + u * 8 * kRow;
-        const s16x4 x = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4 *)(uintptr_t)at);
-        const u32x2 y = __builtin_bit_cast(u32x2, x);
+        const u32x2 y = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(uintptr_t)(at + s * 16 * kRow + u * 8 * kRow)));
         r[2 * u] = y.x;
         r[2 * u + 1] = y.y;
     }
@@ -197,53 +198,41 @@ template <int WAVES> __device__ __forceinline__ u32x4 v_operand(const Tiles<WAVE
 
 // Rows of a tile in LDS: 16 pieces of 16 bytes.  Piece p of key r lies at place p ^ (r & 15) in K, whose operand is read 32 keys at a
 // time, and at p ^ 4 (r & 3) in V, of which a transposed read takes four keys' 64 bytes.
+//
+// A step takes the weights of tile i from its logits while the matrix cores make those of tile i + 1, then adds tile i's values while the
+// maximum of tile i + 1 is found.  K is a tile ahead of V; there are two buffers of each, and one barrier a step.
 template <bool BF16, int WAVES>
 __device__ __forceinline__ void attend(Rows &w, const Tiles<WAVES> &t, const uint16_t *k, int64_t k_stride, const uint16_t *v, int64_t v_stride, int begin, int end,
                                        int n_keys, int limit, int least, int most)
 {
+    if (begin >= end) return;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, half = lane >> 5;
     constexpr int kLoads = kKeys / 4 / WAVES;   // of a wavefront, of K and of V each
-    const int64_t k_bytes = 2 * k_stride, v_bytes = 2 * v_stride;
-    const uint32_t k_offset = (uint32_t)(4 * wave + (lane >> 4)) * (uint32_t)k_bytes + t.k_lane, v_offset = (uint32_t)(4 * wave + (lane >> 4)) * (uint32_t)v_bytes + t.v_lane;
-    auto fetch = [&](int i) {
+    const uint32_t k_bytes = 2 * (uint32_t)k_stride, v_bytes = 2 * (uint32_t)v_stride;
+    const uint32_t k_offset = (uint32_t)(4 * wave + (lane >> 4)) * k_bytes + t.k_lane, v_offset = (uint32_t)(4 * wave + (lane >> 4)) * v_bytes + t.v_lane;
+    auto fetch = [&](const uint16_t *of, uint32_t bytes, uint32_t offset, int i, uint32_t to) {
         const int left = n_keys - i * kKeys, rows = left < kKeys ? left : kKeys;
-        const u32x4 kb = buffer_of(reinterpret_cast<const uint8_t *>(k) + (int64_t)i * kKeys * k_bytes, (uint32_t)rows * (uint32_t)k_bytes);
-        const u32x4 vb = buffer_of(reinterpret_cast<const uint8_t *>(v) + (int64_t)i * kKeys * v_bytes, (uint32_t)rows * (uint32_t)v_bytes);
-        const uint32_t to = __builtin_amdgcn_readfirstlane(t.lds + (uint32_t)(i & 1) * 2 * kTile + wave * 4 * kRow);
+        const u32x4 buffer = buffer_of(reinterpret_cast<const uint8_t *>(of) + (int64_t)i * kKeys * bytes, (uint32_t)rows * bytes);
+        to = __builtin_amdgcn_readfirstlane(to + wave * 4 * kRow);
 #pragma unroll
-        for (int j = 0; j < kLoads; ++j)
-            load_lds(to + j * WAVES * 4 * kRow, kb, k_offset, __builtin_amdgcn_readfirstlane((uint32_t)(j * WAVES * 4) * (uint32_t)k_bytes));
-#pragma unroll
-        for (int j = 0; j < kLoads; ++j)
-            load_lds(to + kTile + j * WAVES * 4 * kRow, vb, v_offset, __builtin_amdgcn_readfirstlane((uint32_t)(j * WAVES * 4) * (uint32_t)v_bytes));
+        for (int j = 0; j < kLoads; ++j) load_lds(to + j * WAVES * 4 * kRow, buffer, offset, __builtin_amdgcn_readfirstlane((uint32_t)(j * WAVES * 4) * bytes));
     };
-    uint32_t strange = 0;   // a masked tile has values that are not finite
-    auto step = [&](int i, auto masked) {
-        const int first = i * kKeys;
-        const uint32_t tile = t.lds + (uint32_t)(i & 1) * 2 * kTile;
-        f32x16 s[2];
-#pragma unroll
-        for (int b = 0; b < 2; ++b) {
-            s[b] = f32x16{};
-#pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                const uint32_t at = (t.k_at ^ (uint32_t)(j << 5)) + tile + b * 32 * kRow;
-                const u32x4 x = *(__attribute__((address_space(3))) const u32x4 *)(uintptr_t)at;
-                s[b] = mfma<BF16>(x, w.q[j], s[b]);
-            }
-        }
-        if constexpr (masked) {
-#pragma unroll
-            for (int b = 0; b < 2; ++b)
-#pragma unroll
-                for (int r = 0; r < 16; ++r) s[b][r] = first + 32 * b + 8 * (r >> 2) + 4 * half + (r & 3) > limit ? -INFINITY : s[b][r];
-        }
-        float top = s[0][0];
+    auto fetch_k = [&](int i) { fetch(k, k_bytes, k_offset, i, t.lds + (uint32_t)((i - begin) & 1) * kTile); };
+    auto fetch_v = [&](int i) { fetch(v, v_bytes, v_offset, i, t.lds + (uint32_t)(2 + ((i - begin) & 1)) * kTile); };
+    auto hide = [&](f32x16 (&s)[2], int i) {
+        const int sees = limit - i * kKeys - 4 * half;
 #pragma unroll
         for (int b = 0; b < 2; ++b)
 #pragma unroll
-            for (int r = 0; r < 16; ++r) top = fmaxf(top, s[b][r]);
-        top = both_max(top) * w.c;
+            for (int r = 0; r < 16; ++r) s[b][r] = 32 * b + 8 * (r >> 2) + (r & 3) > sees ? -INFINITY : s[b][r];
+    };
+    auto top_of = [&](const f32x16 (&s)[2]) {
+        float top = fmaxf(s[0][0], s[1][0]);
+#pragma unroll
+        for (int r = 1; r < 16; ++r) top = fmaxf(fmaxf(top, s[0][r]), s[1][r]);
+        return both_max(top) * w.c;
+    };
+    auto follow = [&](float top) {
         const bool grows = top > w.m + kSlack;
         if (__any(grows)) {   // row by row: what a row gives does not depend on the others of its wavefront
             const float m = grows ? top : w.m, by = __builtin_amdgcn_exp2f(w.m - m);
@@ -254,7 +243,14 @@ __device__ __forceinline__ void attend(Rows &w, const Tiles<WAVES> &t, const uin
 #pragma unroll
                 for (int r = 0; r < 16; ++r) w.o[d][r] *= by;
         }
-        uint32_t p[16];
+    };
+    auto logits = [&](f32x16 (&s)[2], uint32_t buffer) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+#pragma unroll
+            for (int b = 0; b < 2; ++b) s[b] = mfma<BF16>(k_operand(t.k_at[j] + buffer, b), w.q[j], j ? s[b] : f32x16{});
+    };
+    auto weights = [&](uint32_t (&p)[16], const f32x16 (&s)[2]) {
 #pragma unroll
         for (int b = 0; b < 2; ++b)
 #pragma unroll
@@ -263,40 +259,92 @@ __device__ __forceinline__ void attend(Rows &w, const Tiles<WAVES> &t, const uin
                 p[8 * b + r / 2] = pack<BF16>(x, y);
                 w.sum = add_pair<BF16>(p[8 * b + r / 2], w.sum);
             }
+    };
+    auto values = [&](const uint32_t (&p)[16], uint32_t buffer, auto cleaned) {
 #pragma unroll
         for (int j = 0; j < 4; ++j)
 #pragma unroll
             for (int d = 0; d < 4; ++d) {
-                u32x4 x = v_operand(t, tile + kTile, d, j);
-                if constexpr (masked) {   // a weight of zero must not meet infinities and NaN of keys that its row does not see
+                u32x4 x = v_operand(t.v_at[d] + buffer, j);
+                if constexpr (cleaned) {
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        const uint32_t y = finite_only<BF16>(x[e]);
-                        strange |= x[e] ^ y;
-                        x[e] = y;
-                    }
+                    for (int e = 0; e < 4; ++e) x[e] = finite_only<BF16>(x[e]);
+                    __builtin_amdgcn_sched_barrier(0);
                 }
                 w.o[d] = mfma<BF16>(x, u32x4{p[4 * j], p[4 * j + 1], p[4 * j + 2], p[4 * j + 3]}, w.o[d]);
             }
     };
+    // Whether a tile of V holds infinities or NaN.  Where not all rows see all of its keys, a weight of zero must not meet them.
+    auto strange = [&](uint32_t buffer) {
+        typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
+        u16x2 most = {0, 0};
+#pragma unroll
+        for (int j = 0; j < kTile / 1024; ++j) {
+            const u32x4 x = *(lds_u32x4 *)(uintptr_t)(t.lds + buffer + 1024 * j + 16 * lane);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) most = __builtin_elementwise_max(most, __builtin_bit_cast(u16x2, x[e] & 0x7fff7fffu));
+        }
+        constexpr uint32_t inf = BF16 ? 0x7f80u : 0x7c00u;
+        return __any(most.x >= inf || most.y >= inf);
+    };
     // the tiles that all rows of the wavefront see, then those that need a mask
     const int seen = (least + 1) / kKeys, plain = seen < begin ? begin : seen < end ? seen : end;
-    if (begin < end) fetch(begin);
+    fetch_k(begin);
+    fetch_v(begin);
+    if (begin + 1 < end) {
+        fetch_k(begin + 1);
+        asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" :: "n"(2 * kLoads) : "memory");
+    } else
+        asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" :: "n"(kLoads) : "memory");
+    f32x16 s[2];
+    logits(s, 0);
+    if (begin >= plain) hide(s, begin);
+    follow(top_of(s));
     int i = begin;
-    for (; i < plain; ++i) {
-        wait_barrier();   // this tile has arrived, and nobody reads the one before it
-        if (i + 1 < end) fetch(i + 1);
-        step(i, std::false_type{});
+    auto step = [&](auto odd) {
+        wait_barrier();   // K of tile i + 1 and V of tile i have arrived, and nobody reads the tiles before them
+        if (i + 2 < end) fetch_k(i + 2);
+        fetch_v(i + 1);
+        f32x16 next[2];
+        uint32_t p[16];
+        logits(next, odd ? 0 : kTile);
+        weights(p, s);
+        values(p, (odd ? 3 : 2) * kTile, std::false_type{});
+        const float top = top_of(next);
+        follow(top);
+        s[0] = next[0];
+        s[1] = next[1];
+        ++i;
+    };
+    while (i + 2 < plain) {
+        step(std::false_type{});
+        step(std::true_type{});
     }
+    const int from = i;
+    bool left_out = false;
     for (; i < end; ++i) {
         wait_barrier();
-        if (i + 1 < end) fetch(i + 1);
-        if (i * kKeys <= most) step(i, std::true_type{});
+        if (i + 2 < end) fetch_k(i + 2);
+        if (i + 1 < end) fetch_v(i + 1);
+        if (i * kKeys > most) continue;   // no row of this wavefront sees the tile
+        const uint32_t odd = (uint32_t)((i - begin) & 1) * kTile;
+        uint32_t p[16];
+        weights(p, s);
+        if (!strange(2 * kTile + odd)) values(p, 2 * kTile + odd, std::false_type{});
+        else {
+            values(p, 2 * kTile + odd, std::true_type{});
+            left_out = true;
+        }
+        if (i + 1 < end) {
+            logits(s, kTile - odd);
+            hide(s, i + 1);
+            follow(top_of(s));
+        }
     }
-    if (__any(strange != 0)) {   // what was left out above, for the rows that see it
-        const int from = (least + 1) / kKeys, last = end * kKeys < most + 1 ? end * kKeys : most + 1;
+    if (left_out) {   // what is not finite, for the rows that see it
+        const int last = end * kKeys < most + 1 ? end * kKeys : most + 1;
 #pragma unroll 1
-        for (int key = (from > begin ? from : begin) * kKeys; key < last; ++key) {
+        for (int key = from * kKeys; key < last; ++key) {
             const u32x2 *row = reinterpret_cast<const u32x2 *>(v + (int64_t)key * v_stride) + half;
 #pragma unroll
             for (int d = 0; d < 4; ++d)
@@ -345,9 +393,12 @@ __global__ __launch_bounds__(64 * WAVES) __attribute__((amdgpu_waves_per_eu(2, 2
     const int r16 = 4 * (wave & 3) + (lane >> 4);   // key of this lane's piece, modulo 16
     t.k_lane = (uint32_t)(((lane & 15) ^ r16) * 16);
     t.v_lane = (uint32_t)(((lane & 15) ^ ((lane >> 4) << 2)) * 16);
-    t.k_at = (uint32_t)((lane & 31) * kRow + ((half ^ (lane & 15)) << 4));
     const int v_key = 4 * half + ((lane & 15) >> 2);
-    t.v_at = (uint32_t)(v_key * kRow + (((v_key & 3) << 2 ^ (2 * ((lane >> 4) & 1) + ((lane >> 1) & 1))) << 4) + (lane & 1) * 8);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) t.k_at[j] = t.lds + (uint32_t)((lane & 31) * kRow + ((2 * j + half) ^ (lane & 15)) * 16);
+#pragma unroll
+    for (int d = 0; d < 4; ++d)
+        t.v_at[d] = t.lds + (uint32_t)(v_key * kRow + ((4 * d + 2 * ((lane >> 4) & 1) + ((lane >> 1) & 1)) ^ (v_key & 3) << 2) * 16 + (lane & 1) * 8);
 
     Rows w;
 #pragma unroll
