@@ -696,29 +696,33 @@ enum { TKV_BF16 = 0, TKV_FP16 = 1, TKV_FP32 = 2 };
  * workgroup.  All host memory.  Row r of a sequence and kv head is query head
  * r mod R of new token r / R, R = n_q_heads / n_kv_heads.  An item is a tile of
  * tile_rows such rows (the same tile of every kv head) and a range of tiles of
- * 64 keys, those of the prefix first; where there are too few tiles of rows to
- * fill target_cus compute units, long ranges are cut into equal parts, whose
- * partial results lie in a workspace and are joined.  Items come by falling
- * length.  The plan depends on the lengths alone: layers, and replays of the
- * same requests, share it.
+ * keys (32 with 32 rows, 64 with 128 and 256), those of the prefix first; where
+ * there are too few tiles of rows to fill target_cus compute units, long ranges
+ * are cut into equal parts, whose partial results lie in a workspace and are
+ * joined.  The number of rows is the one that is expected to take least time.
+ * Items come by falling length.  The plan depends on the lengths alone: layers,
+ * and replays of the same requests, share it.
  *   desc             n_kv_heads and geometry; the pools may be empty
  *   seq_indptr       host i32[batch+1], from 0: the sequences' new tokens
  *   prefix_indptr    host i32[batch+1], from 0, or NULL: their prefix rows
  *   target_cus       compute units to fill (>= 1)
- *   items_out        host i32[10*capacity]: {first new token, new tokens, first
+ *   items_out        host i32[11*capacity]: {first new token, new tokens, first
  *                    prefix row, prefix rows, first row, first key tile, end,
- *                    partial slot or -1, part, parts}
- *   tile_rows_out    host i32
+ *                    partial slot or -1, part, parts, and in the k-th item the
+ *                    number of the first part of the k-th tile that is cut}
+ *   tile_rows_out    host i32: 32, 128 or 256
  *   n_slots_out      host i32: partial slots, 0 if no range is cut
+ *   n_cut_out        host i32: tiles whose ranges are cut
  * Returns the number of items (>= 0) or a negative status.  A sequence without
  * new tokens has none.  At most 2^30 rows (tokens * R) a sequence.
  * tkv_plan_prefill_capacity: an upper bound of the items for n_tokens new tokens.
  */
 int32_t tkv_plan_prefill_capacity(const tkv_desc *desc, int32_t batch, int32_t n_tokens, int32_t n_q_heads, int32_t target_cus);
 int32_t tkv_plan_prefill(const tkv_desc *desc, int32_t batch, int32_t n_q_heads, const int32_t *seq_indptr, const int32_t *prefix_indptr,
-                         int32_t target_cus, int32_t *items_out, int32_t capacity, int32_t *tile_rows_out, int32_t *n_slots_out);
+                         int32_t target_cus, int32_t *items_out, int32_t capacity, int32_t *tile_rows_out, int32_t *n_slots_out,
+                         int32_t *n_cut_out);
 typedef struct tkv_prefill {
-    int32_t tile_rows, n_items, n_slots;   /* as tkv_plan_prefill gives them */
+    int32_t tile_rows, n_items, n_slots, n_cut;   /* as tkv_plan_prefill gives them */
     const int32_t *items;                  /* device, 4-byte aligned */
 } tkv_prefill;
 /* Bytes of workspace that n_slots partial slots take; 0 on a bad argument or if there are none. */

@@ -10,7 +10,6 @@
 
 namespace {
 constexpr int kHeadDim = 128, kGroup = 32;
-constexpr int32_t kTileRows = 128;
 constexpr int64_t kMaxStride = 1 << 23;
 
 int group_of(const tkv_desc *desc, int32_t n_q_heads, int32_t &group)
@@ -26,8 +25,20 @@ bool rows_ok(const void *p, int64_t stride, int64_t heads, int32_t n_tokens)
     return p && !((uintptr_t)p & 15) && stride >= 0 && stride % 8 == 0 && stride < kMaxStride && (stride >= heads * kHeadDim || n_tokens == 1);
 }
 int64_t up(int64_t a, int64_t b) { return (a + b - 1) / b; }
-// Parts that a plan cuts beyond one of each tile: for one kv head at most eight for a compute unit.
-constexpr int64_t kPartsPerCu = 8;
+// Workgroups of tkv_prefill_attention.  Times in us.
+struct Kind {
+    int32_t rows, keys, resident;   // rows, keys of a tile, workgroups that a compute unit holds at once
+    double begin, again;            // what a workgroup takes beside its steps: the first one of a place, those behind it
+    double alone, step;             // a step (a tile of keys) of a workgroup by itself; steps of a full compute unit, one behind the other
+};
+constexpr Kind kKinds[3] = {{32, 32, 4, 5.0, 1.2, 0.72, 0.192}, {128, 64, 2, 6.0, 2.5, 1.2, 0.96}, {256, 64, 1, 6.5, 5.0, 1.83, 1.83}};
+constexpr double kMergeUs = 3.0, kBytesPerUs = 4.6e6;
+bool kind_of(int32_t rows)
+{
+    for (const Kind &k : kKinds)
+        if (k.rows == rows) return true;
+    return false;
+}
 } // namespace
 
 extern "C" {
@@ -39,50 +50,98 @@ int32_t tkv_plan_prefill_capacity(const tkv_desc *desc, int32_t batch, int32_t n
     int32_t group = 0;
     if (int st = group_of(desc, n_q_heads, group)) return st;
     if (batch < 0 || n_tokens < 0 || target_cus < 1) return TKV_ERR_INVALID_ARG;
-    const int64_t n = (int64_t)n_tokens * group / kTileRows + batch + kPartsPerCu * target_cus;
+    // a tile of each sequence and kind of workgroup, and as many parts again as are resident at once
+    const int64_t n = (int64_t)n_tokens * group / kKinds[0].rows + batch + 4 * (int64_t)target_cus;
     return n > INT32_MAX ? (int32_t)TKV_ERR_INVALID_ARG : (int32_t)n;
 }
 
 int32_t tkv_plan_prefill(const tkv_desc *desc, int32_t batch, int32_t n_q_heads, const int32_t *seq_indptr, const int32_t *prefix_indptr,
-                         int32_t target_cus, int32_t *items_out, int32_t capacity, int32_t *tile_rows_out, int32_t *n_slots_out)
+                         int32_t target_cus, int32_t *items_out, int32_t capacity, int32_t *tile_rows_out, int32_t *n_slots_out, int32_t *n_cut_out)
 {
     int32_t group = 0;
     if (int st = group_of(desc, n_q_heads, group)) return st;
-    if (batch < 0 || target_cus < 1 || capacity < 0 || !seq_indptr || !tile_rows_out || !n_slots_out || (capacity > 0 && !items_out)) return TKV_ERR_INVALID_ARG;
+    if (batch < 0 || target_cus < 1 || capacity < 0 || !seq_indptr || !tile_rows_out || !n_slots_out || !n_cut_out || (capacity > 0 && !items_out)) return TKV_ERR_INVALID_ARG;
     if (seq_indptr[0] != 0 || (prefix_indptr && prefix_indptr[0] != 0)) return TKV_ERR_INVALID_ARG;
     for (int32_t b = 0; b < batch; ++b) {
         if (seq_indptr[b + 1] < seq_indptr[b] || (prefix_indptr && prefix_indptr[b + 1] < prefix_indptr[b])) return TKV_ERR_INVALID_ARG;
         if (((int64_t)seq_indptr[b + 1] - seq_indptr[b]) * group > 1 << 30) return TKV_ERR_INVALID_ARG;
     }
     try {
-        struct Tile { int32_t seq, row, keys, parts; };   // keys: tiles of 64
-        std::vector<Tile> tiles;
-        int64_t all = 0;
-        for (int32_t b = 0; b < batch; ++b) {
-            const int32_t n = seq_indptr[b + 1] - seq_indptr[b], pre = prefix_indptr ? prefix_indptr[b + 1] - prefix_indptr[b] : 0;
-            const int64_t rows = (int64_t)n * group;
-            for (int64_t r = 0; r < rows; r += kTileRows) {
-                const int64_t see = (std::min(r + kTileRows, rows) - 1) / group + 1;
-                const int64_t keys = up(pre, kPrefillKeys) + up(see, kPrefillKeys);
-                tiles.push_back({b, (int32_t)r, (int32_t)keys, 1});
-                all += keys;
+        struct Tile { int32_t seq, row, keys, parts; };   // keys: tiles of keys that its rows see
+        const Kind *best = nullptr;
+        std::vector<Tile> tiles, mine;
+        double least = 0.0;
+        for (const Kind &kind : kKinds) {
+            mine.clear();
+            int64_t all = 0, longest = 0;
+            double bytes = 0.0;
+            for (int32_t b = 0; b < batch; ++b) {
+                const int32_t n = seq_indptr[b + 1] - seq_indptr[b], pre = prefix_indptr ? prefix_indptr[b + 1] - prefix_indptr[b] : 0;
+                const int64_t rows = (int64_t)n * group;
+                for (int64_t r = 0; r < rows; r += kind.rows) {
+                    const int64_t see = (std::min(r + kind.rows, rows) - 1) / group + 1, keys = up(pre, kind.keys) + up(see, kind.keys);
+                    mine.push_back({b, (int32_t)r, (int32_t)keys, 1});
+                    all += keys;
+                    longest = std::max(longest, keys);
+                }
+                // the first tile's keys and values come from memory, the others' partly from the L2
+                if (rows > 0) bytes += ((double)pre + n) * 4.0 * kHeadDim * (1.0 + 0.35 * std::min<double>(3.0, (double)(up(rows, kind.rows) - 1)));
+            }
+            if (mine.empty()) break;
+            const double heads = desc->n_kv_heads, slots = std::max(1.0, kind.resident * (double)target_cus / heads);
+            // What a call is expected to take with ranges of at most `most` tiles.
+            auto expect = [&](int64_t most) {
+                int64_t n = 0;
+                double partial = 0.0;
+                for (const Tile &t : mine) {
+                    const int64_t k = up(t.keys, most);
+                    n += k;
+                    if (k > 1) partial += (double)k * (double)std::min<int64_t>(kind.rows, ((int64_t)seq_indptr[t.seq + 1] - seq_indptr[t.seq]) * group - t.row);
+                }
+                const double work = std::max((double)all * heads / target_cus * kind.step, bytes * heads / kBytesPerUs), line = (double)std::min(most, longest) * kind.alone;
+                const double rounds = std::max(1.0, (double)n * heads / (kind.resident * (double)target_cus));
+                return kind.begin + (rounds - 1.0) * kind.again + std::max(work, line) + 0.15 * std::min(work, line) / rounds +
+                       (partial > 0.0 ? kMergeUs + partial * heads * 8.0 * (kHeadDim + 2) / kBytesPerUs : 0.0);
+            };
+            auto parts = [&](int64_t most) { int64_t n = 0; for (const Tile &t : mine) n += up(t.keys, most); return n; };
+            // whole ranges, or as short ones as give no more workgroups than are resident at once, or half or a quarter as many
+            int64_t most = longest;
+            double time = expect(longest);
+            for (double share = 1.0; share > 0.2; share *= 0.5) {
+                if ((double)mine.size() > slots * share) break;
+                int64_t lo = 1, hi = longest;
+                while (lo < hi) {
+                    const int64_t mid = lo + (hi - lo) / 2;
+                    if ((double)parts(mid) <= slots * share) hi = mid;
+                    else lo = mid + 1;
+                }
+                const double t = lo < longest ? expect(lo) : time;
+                if (t < time) {
+                    most = lo;
+                    time = t;
+                }
+            }
+            if (!best || time < least) {
+                best = &kind;
+                least = time;
+                for (Tile &t : mine) t.parts = (int32_t)up(t.keys, most);
+                tiles.swap(mine);
             }
         }
-        // two workgroups to a compute unit; a part costs a partial of its rows, written and read
-        const int64_t slots = std::max<int64_t>(1, 2 * (int64_t)target_cus / desc->n_kv_heads), share = std::max<int64_t>(4, up(all, slots));
         int64_t n_slots = 0, n_items = 0;
-        for (Tile &t : tiles) {
-            if (t.keys > share + share / 4) t.parts = (int32_t)std::min<int64_t>(up(t.keys, share), kPartsPerCu * target_cus / 2);
+        for (const Tile &t : tiles) {
             n_items += t.parts;
             if (t.parts > 1) n_slots += t.parts;
         }
         if (n_items > capacity) return TKV_ERR_CAPACITY;
         if (n_items * desc->n_kv_heads > INT32_MAX || n_slots > INT32_MAX) return TKV_ERR_INVALID_ARG;
         std::stable_sort(tiles.begin(), tiles.end(), [](const Tile &x, const Tile &y) { return (int64_t)x.keys * y.parts > (int64_t)y.keys * x.parts; });
-        int32_t slot = 0, *it = items_out;
-        for (const Tile &t : tiles)
-            for (int32_t k = 0; k < t.parts; ++k, it += kPrefillItemWords) {
+        int32_t slot = 0, cut = 0, number = 0;
+        for (const Tile &t : tiles) {
+            if (t.parts > 1) items_out[kPrefillItemWords * (int64_t)cut++ + 10] = number;
+            for (int32_t k = 0; k < t.parts; ++k, ++number) {
                 const int32_t b = t.seq;
+                int32_t *it = items_out + kPrefillItemWords * (int64_t)number;
                 it[0] = seq_indptr[b];
                 it[1] = seq_indptr[b + 1] - seq_indptr[b];
                 it[2] = prefix_indptr ? prefix_indptr[b] : 0;
@@ -94,9 +153,12 @@ int32_t tkv_plan_prefill(const tkv_desc *desc, int32_t batch, int32_t n_q_heads,
                 it[8] = k;
                 it[9] = t.parts;
             }
-        *tile_rows_out = kTileRows;
+        }
+        for (int32_t k = cut; k < number; ++k) items_out[kPrefillItemWords * (int64_t)k + 10] = -1;
+        *tile_rows_out = best ? best->rows : kKinds[0].rows;
         *n_slots_out = slot;
-        return (int32_t)n_items;
+        *n_cut_out = cut;
+        return number;
     } catch (const std::bad_alloc &) {
         return TKV_ERR_INVALID_ARG;
     }
@@ -104,7 +166,7 @@ int32_t tkv_plan_prefill(const tkv_desc *desc, int32_t batch, int32_t n_q_heads,
 
 size_t tkv_prefill_workspace_bytes(const tkv_desc *desc, int32_t n_slots, int32_t tile_rows)
 {
-    if (tkv_desc_status(desc) || n_slots < 0 || tile_rows != kTileRows) return 0;
+    if (tkv_desc_status(desc) || n_slots < 0 || !kind_of(tile_rows)) return 0;
     return (size_t)n_slots * desc->n_kv_heads * tile_rows * (kHeadDim + 2) * sizeof(float);
 }
 
@@ -115,13 +177,13 @@ int tkv_prefill_attention(const tkv_desc *desc, int32_t n_q_heads, const void *q
 {
     int32_t group = 0;
     if (int st = group_of(desc, n_q_heads, group)) return st;
-    if (!prefill || n_tokens < 0 || n_prefix < 0 || prefill->n_items < 0 || prefill->n_slots < 0) return TKV_ERR_INVALID_ARG;
+    if (!prefill || n_tokens < 0 || n_prefix < 0 || prefill->n_items < 0 || prefill->n_slots < 0 || prefill->n_cut < 0 || prefill->n_cut > prefill->n_slots) return TKV_ERR_INVALID_ARG;
     if ((q_type != TKV_BF16 && q_type != TKV_FP16) || (kv_type != TKV_BF16 && kv_type != TKV_FP16) || (out_type != TKV_BF16 && out_type != TKV_FP16) ||
         (q_type == TKV_FP16 && kv_type == TKV_BF16))
         return TKV_ERR_INVALID_ARG;
     if (!(sm_scale > 0.0f) || !(sm_scale < 2.0e38f)) return TKV_ERR_INVALID_ARG;
     if (prefill->n_items == 0 || n_tokens == 0) return TKV_OK;
-    if (prefill->tile_rows != kTileRows || !prefill->items || ((uintptr_t)prefill->items & 3)) return TKV_ERR_INVALID_ARG;
+    if (!kind_of(prefill->tile_rows) || !prefill->items || ((uintptr_t)prefill->items & 3)) return TKV_ERR_INVALID_ARG;
     if (!rows_ok(q, q_stride, n_q_heads, n_tokens) || !rows_ok(K, k_stride, desc->n_kv_heads, n_tokens) || !rows_ok(V, v_stride, desc->n_kv_heads, n_tokens)) return TKV_ERR_INVALID_ARG;
     if (n_prefix > 0 && (!rows_ok(K_prefix, 0, 0, n_prefix) || !rows_ok(V_prefix, 0, 0, n_prefix))) return TKV_ERR_INVALID_ARG;
     if ((int64_t)desc->n_kv_heads * kHeadDim >= kMaxStride) return TKV_ERR_BAD_SHAPE;

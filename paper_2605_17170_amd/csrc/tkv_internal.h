@@ -44,8 +44,7 @@ int tkv_launch_table_append(const tkv_desc *desc, const tkv_table *table, const 
                             const uint8_t *tag_bits, int32_t n_tokens, int32_t *token_indptr, int32_t *positions, int32_t *slot_ids,
                             int32_t *work_pages, int32_t *work_src, int32_t max_work, int32_t *n_work, void *workspace, int32_t *status, void *stream);
 
-constexpr int kPrefillKeys = 64;         // keys of a tile of tkv_prefill_attention
-constexpr int kPrefillItemWords = 10;    // of an item of its plan
+constexpr int kPrefillItemWords = 11;    // of an item of its plan
 constexpr int kDistortionChunk = 16;     // tokens of a partial sum of tkv_head_distortion
 
 int tkv_launch_prefill(int32_t n_q_heads, int32_t n_kv_heads, const void *q, int64_t q_stride, int32_t q_type, const void *K, int64_t k_stride,

@@ -28,9 +28,7 @@ typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef short s16x4 __attribute__((ext_vector_type(4)));
 
-constexpr int kKeys = kPrefillKeys;   // of a tile
 constexpr int kRow = kHeadDim * 2;        // bytes
-constexpr int kTile = kKeys * kRow;       // bytes of a tile of K or of V
 constexpr int kItem = kPrefillItemWords;
 constexpr float kNone = -3.4028235e38f;   // reference of a row that has seen no key
 constexpr float kSlack = 8.0f;            // weights grow to 2^8 before the reference follows the maximum
@@ -42,7 +40,7 @@ struct PrefillArgs {
     uint16_t *out;
     float *partial;
     int32_t *status;
-    int32_t n_items, n_slots, n_tokens, n_prefix, group, n_kv_heads, q_bf16, out_bf16;
+    int32_t n_items, n_slots, n_cut, n_tokens, n_prefix, group, n_kv_heads, q_bf16, out_bf16;
     float c;
 };
 
@@ -174,9 +172,8 @@ template <bool BF16> __device__ __forceinline__ uint32_t finite_only(uint32_t v)
     return v & (low | high);
 }
 
-template <int WAVES> struct Tiles {
+struct Tiles {
     uint32_t lds;               // byte address of two buffers for tiles of K, two for tiles of V
-    uint32_t k_lane, v_lane;    // this lane's piece of its row in global memory, in bytes
     uint32_t k_at[8], v_at[4];  // where it reads its operands in a buffer: channels 16 j .. of K, 32 d .. of V
 };
 typedef __attribute__((address_space(3))) const u32x4 lds_u32x4;
@@ -201,35 +198,52 @@ __device__ __forceinline__ u32x4 v_operand(uint32_t at, int s)
 //
 // A step takes the weights of tile i from its logits while the matrix cores make those of tile i + 1, then adds tile i's values while the
 // maximum of tile i + 1 is found.  K is a tile ahead of V; there are two buffers of each, and one barrier a step.
-template <bool BF16, int WAVES>
-__device__ __forceinline__ void attend(Rows &w, const Tiles<WAVES> &t, const uint16_t *k, int64_t k_stride, const uint16_t *v, int64_t v_stride, int begin, int end,
-                                       int n_keys, int limit, int least, int most)
+// WAVES wavefronts share a tile of 32 KB keys.
+template <bool BF16, int WAVES, int KB>
+__device__ __forceinline__ void attend(Rows &w, const Tiles &t, const uint16_t *q, bool live, const PrefillArgs &a, const uint16_t *k, int64_t k_stride, const uint16_t *v,
+                                       int64_t v_stride, int begin, int end, int n_keys, int limit, int least, int most)
 {
     if (begin >= end) return;
+    constexpr int kKeys = 32 * KB, kTile = kKeys * kRow;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, half = lane >> 5;
     constexpr int kLoads = kKeys / 4 / WAVES;   // of a wavefront, of K and of V each
     const uint32_t k_bytes = 2 * (uint32_t)k_stride, v_bytes = 2 * (uint32_t)v_stride;
-    const uint32_t k_offset = (uint32_t)(4 * wave + (lane >> 4)) * k_bytes + t.k_lane, v_offset = (uint32_t)(4 * wave + (lane >> 4)) * v_bytes + t.v_lane;
-    auto fetch = [&](const uint16_t *of, uint32_t bytes, uint32_t offset, int i, uint32_t to) {
+    // key r of the lane's piece in load j is 4 (WAVES j + wave) + lane / 16
+    const uint32_t first_row = (uint32_t)(4 * wave + (lane >> 4)), piece = (uint32_t)(lane & 15);
+    const uint32_t v_offset = first_row * v_bytes + (piece ^ (uint32_t)(lane >> 4) << 2) * 16;
+    auto buffer_at = [&](const uint16_t *of, uint32_t bytes, int i) {
         const int left = n_keys - i * kKeys, rows = left < kKeys ? left : kKeys;
-        const u32x4 buffer = buffer_of(reinterpret_cast<const uint8_t *>(of) + (int64_t)i * kKeys * bytes, (uint32_t)rows * bytes);
-        to = __builtin_amdgcn_readfirstlane(to + wave * 4 * kRow);
-#pragma unroll
-        for (int j = 0; j < kLoads; ++j) load_lds(to + j * WAVES * 4 * kRow, buffer, offset, __builtin_amdgcn_readfirstlane((uint32_t)(j * WAVES * 4) * bytes));
+        return buffer_of(reinterpret_cast<const uint8_t *>(of) + (int64_t)i * kKeys * bytes, (uint32_t)rows * bytes);
     };
-    auto fetch_k = [&](int i) { fetch(k, k_bytes, k_offset, i, t.lds + (uint32_t)((i - begin) & 1) * kTile); };
-    auto fetch_v = [&](int i) { fetch(v, v_bytes, v_offset, i, t.lds + (uint32_t)(2 + ((i - begin) & 1)) * kTile); };
-    auto hide = [&](f32x16 (&s)[2], int i) {
+    auto fetch_k = [&](int i) {
+        const u32x4 buffer = buffer_at(k, k_bytes, i);
+        const uint32_t to = __builtin_amdgcn_readfirstlane(t.lds + (uint32_t)((i - begin) & 1) * kTile + wave * 4 * kRow);
+#pragma unroll
+        for (int j = 0; j < kLoads; ++j) {
+            // (with four wavefronts or more the piece is the same in every load)
+            const uint32_t r16 = (WAVES >= 4 ? first_row : first_row + 4 * WAVES * j) & 15;
+            load_lds(to + j * WAVES * 4 * kRow, buffer, first_row * k_bytes + (piece ^ r16) * 16, __builtin_amdgcn_readfirstlane((uint32_t)(j * WAVES * 4) * k_bytes));
+        }
+    };
+    auto fetch_v = [&](int i) {
+        const u32x4 buffer = buffer_at(v, v_bytes, i);
+        const uint32_t to = __builtin_amdgcn_readfirstlane(t.lds + (uint32_t)(2 + ((i - begin) & 1)) * kTile + wave * 4 * kRow);
+#pragma unroll
+        for (int j = 0; j < kLoads; ++j) load_lds(to + j * WAVES * 4 * kRow, buffer, v_offset, __builtin_amdgcn_readfirstlane((uint32_t)(j * WAVES * 4) * v_bytes));
+    };
+    auto hide = [&](f32x16 (&s)[KB], int i) {
         const int sees = limit - i * kKeys - 4 * half;
 #pragma unroll
-        for (int b = 0; b < 2; ++b)
+        for (int b = 0; b < KB; ++b)
 #pragma unroll
             for (int r = 0; r < 16; ++r) s[b][r] = 32 * b + 8 * (r >> 2) + (r & 3) > sees ? -INFINITY : s[b][r];
     };
-    auto top_of = [&](const f32x16 (&s)[2]) {
-        float top = fmaxf(s[0][0], s[1][0]);
+    auto top_of = [&](const f32x16 (&s)[KB]) {
+        float top = s[0][0];
 #pragma unroll
-        for (int r = 1; r < 16; ++r) top = fmaxf(fmaxf(top, s[0][r]), s[1][r]);
+        for (int r = 0; r < 16; ++r)
+#pragma unroll
+            for (int b = 0; b < KB; ++b) top = fmaxf(top, s[b][r]);
         return both_max(top) * w.c;
     };
     auto follow = [&](float top) {
@@ -244,15 +258,15 @@ __device__ __forceinline__ void attend(Rows &w, const Tiles<WAVES> &t, const uin
                 for (int r = 0; r < 16; ++r) w.o[d][r] *= by;
         }
     };
-    auto logits = [&](f32x16 (&s)[2], uint32_t buffer) {
+    auto logits = [&](f32x16 (&s)[KB], uint32_t buffer) {
 #pragma unroll
         for (int j = 0; j < 8; ++j)
 #pragma unroll
-            for (int b = 0; b < 2; ++b) s[b] = mfma<BF16>(k_operand(t.k_at[j] + buffer, b), w.q[j], j ? s[b] : f32x16{});
+            for (int b = 0; b < KB; ++b) s[b] = mfma<BF16>(k_operand(t.k_at[j] + buffer, b), w.q[j], j ? s[b] : f32x16{});
     };
-    auto weights = [&](uint32_t (&p)[16], const f32x16 (&s)[2]) {
+    auto weights = [&](uint32_t (&p)[8 * KB], const f32x16 (&s)[KB]) {
 #pragma unroll
-        for (int b = 0; b < 2; ++b)
+        for (int b = 0; b < KB; ++b)
 #pragma unroll
             for (int r = 0; r < 16; r += 2) {
                 const float x = __builtin_amdgcn_exp2f(fmaf(s[b][r], w.c, -w.m)), y = __builtin_amdgcn_exp2f(fmaf(s[b][r + 1], w.c, -w.m));
@@ -260,9 +274,9 @@ __device__ __forceinline__ void attend(Rows &w, const Tiles<WAVES> &t, const uin
                 w.sum = add_pair<BF16>(p[8 * b + r / 2], w.sum);
             }
     };
-    auto values = [&](const uint32_t (&p)[16], uint32_t buffer, auto cleaned) {
+    auto values = [&](const uint32_t (&p)[8 * KB], uint32_t buffer, auto cleaned) {
 #pragma unroll
-        for (int j = 0; j < 4; ++j)
+        for (int j = 0; j < 2 * KB; ++j)
 #pragma unroll
             for (int d = 0; d < 4; ++d) {
                 u32x4 x = v_operand(t.v_at[d] + buffer, j);
@@ -289,14 +303,16 @@ __device__ __forceinline__ void attend(Rows &w, const Tiles<WAVES> &t, const uin
     };
     // the tiles that all rows of the wavefront see, then those that need a mask
     const int seen = (least + 1) / kKeys, plain = seen < begin ? begin : seen < end ? seen : end;
+    // the first keys and the queries at once; what the first logits do not need waits until these are there
     fetch_k(begin);
+    load_q<BF16>(w, q, live, a);
     fetch_v(begin);
     if (begin + 1 < end) {
         fetch_k(begin + 1);
         asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" :: "n"(2 * kLoads) : "memory");
     } else
         asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" :: "n"(kLoads) : "memory");
-    f32x16 s[2];
+    f32x16 s[KB];
     logits(s, 0);
     if (begin >= plain) hide(s, begin);
     follow(top_of(s));
@@ -305,15 +321,15 @@ __device__ __forceinline__ void attend(Rows &w, const Tiles<WAVES> &t, const uin
         wait_barrier();   // K of tile i + 1 and V of tile i have arrived, and nobody reads the tiles before them
         if (i + 2 < end) fetch_k(i + 2);
         fetch_v(i + 1);
-        f32x16 next[2];
-        uint32_t p[16];
+        f32x16 next[KB];
+        uint32_t p[8 * KB];
         logits(next, odd ? 0 : kTile);
         weights(p, s);
         values(p, (odd ? 3 : 2) * kTile, std::false_type{});
         const float top = top_of(next);
         follow(top);
-        s[0] = next[0];
-        s[1] = next[1];
+#pragma unroll
+        for (int b = 0; b < KB; ++b) s[b] = next[b];
         ++i;
     };
     while (i + 2 < plain) {
@@ -328,7 +344,7 @@ __device__ __forceinline__ void attend(Rows &w, const Tiles<WAVES> &t, const uin
         if (i + 1 < end) fetch_v(i + 1);
         if (i * kKeys > most) continue;   // no row of this wavefront sees the tile
         const uint32_t odd = (uint32_t)((i - begin) & 1) * kTile;
-        uint32_t p[16];
+        uint32_t p[8 * KB];
         weights(p, s);
         if (!strange(2 * kTile + odd)) values(p, 2 * kTile + odd, std::false_type{});
         else {
@@ -364,7 +380,7 @@ __device__ __forceinline__ void attend(Rows &w, const Tiles<WAVES> &t, const uin
 }
 
 // BF16: the new tokens' keys, values and queries are bf16; else keys and values are fp16.
-template <bool BF16, int WAVES>
+template <bool BF16, int WAVES, int KB>
 __global__ __launch_bounds__(64 * WAVES) __attribute__((amdgpu_waves_per_eu(2, 2))) void tkv_prefill_kernel(PrefillArgs a)
 {
     extern __shared__ __attribute__((aligned(1024))) uint8_t smem[];
@@ -376,7 +392,7 @@ __global__ __launch_bounds__(64 * WAVES) __attribute__((amdgpu_waves_per_eu(2, 2
         if (a.status && threadIdx.x == 0) atomicOr(a.status, TKV_STATUS_BAD_ITEM);
         return;
     }
-    constexpr int kTileRows = 32 * WAVES;
+    constexpr int kTileRows = 32 * WAVES, kKeys = 32 * KB;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, half = lane >> 5;
     const uint32_t n_rows = (uint32_t)it.n_new * (uint32_t)a.group, row = (uint32_t)it.row0 + 32 * wave + (lane & 31);
     const bool live = row < n_rows;
@@ -388,11 +404,8 @@ __global__ __launch_bounds__(64 * WAVES) __attribute__((amdgpu_waves_per_eu(2, 2
     const int begin = it.begin, end = it.end < tiles0 + tiles1 ? it.end : tiles0 + tiles1;
     const bool idle = (uint32_t)it.row0 + 32 * wave >= n_rows;     // no row of this wavefront exists
 
-    Tiles<WAVES> t;
+    Tiles t;
     t.lds = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t *)smem;
-    const int r16 = 4 * (wave & 3) + (lane >> 4);   // key of this lane's piece, modulo 16
-    t.k_lane = (uint32_t)(((lane & 15) ^ r16) * 16);
-    t.v_lane = (uint32_t)(((lane & 15) ^ ((lane >> 4) << 2)) * 16);
     const int v_key = 4 * half + ((lane & 15) >> 2);
 #pragma unroll
     for (int j = 0; j < 8; ++j) t.k_at[j] = t.lds + (uint32_t)((lane & 31) * kRow + ((2 * j + half) ^ (lane & 15)) * 16);
@@ -407,18 +420,16 @@ __global__ __launch_bounds__(64 * WAVES) __attribute__((amdgpu_waves_per_eu(2, 2
     w.sum = 0.0f;
     const uint16_t *q = a.q + (int64_t)(it.token0 + token) * a.q_stride + (int64_t)head * kHeadDim;
     if (begin < tiles0) {
-        load_q<false>(w, q, live, a);
         const int see = idle ? -1 : it.n_prefix - 1;
-        attend<false, WAVES>(w, t, a.k[0] + (int64_t)it.prefix0 * a.k_stride[0] + (int64_t)kv_head * kHeadDim, a.k_stride[0],
-                             a.v[0] + (int64_t)it.prefix0 * a.v_stride[0] + (int64_t)kv_head * kHeadDim, a.v_stride[0], begin, end < tiles0 ? end : tiles0, it.n_prefix, it.n_prefix - 1,
-                             see, see);
+        attend<false, WAVES, KB>(w, t, q, live, a, a.k[0] + (int64_t)it.prefix0 * a.k_stride[0] + (int64_t)kv_head * kHeadDim, a.k_stride[0],
+                                 a.v[0] + (int64_t)it.prefix0 * a.v_stride[0] + (int64_t)kv_head * kHeadDim, a.v_stride[0], begin, end < tiles0 ? end : tiles0, it.n_prefix,
+                                 it.n_prefix - 1, see, see);
     }
     if (end > tiles0) {
-        load_q<BF16>(w, q, live, a);
         const int least = idle ? -1 : __builtin_amdgcn_readlane(token, 0), most = idle ? -1 : __builtin_amdgcn_readlane(token, 31);
-        attend<BF16, WAVES>(w, t, a.k[1] + (int64_t)it.token0 * a.k_stride[1] + (int64_t)kv_head * kHeadDim, a.k_stride[1],
-                            a.v[1] + (int64_t)it.token0 * a.v_stride[1] + (int64_t)kv_head * kHeadDim, a.v_stride[1], begin > tiles0 ? begin - tiles0 : 0, end - tiles0, n_see, token,
-                            least, most);
+        attend<BF16, WAVES, KB>(w, t, q, live, a, a.k[1] + (int64_t)it.token0 * a.k_stride[1] + (int64_t)kv_head * kHeadDim, a.k_stride[1],
+                                a.v[1] + (int64_t)it.token0 * a.v_stride[1] + (int64_t)kv_head * kHeadDim, a.v_stride[1], begin > tiles0 ? begin - tiles0 : 0, end - tiles0,
+                                n_see, token, least, most);
     }
     const float sum = both_sum(w.sum);
     if (it.slot < 0) {
@@ -452,35 +463,61 @@ __global__ __launch_bounds__(64 * WAVES) __attribute__((amdgpu_waves_per_eu(2, 2
     }
 }
 
-// Joins the parts of a tile's rows: a wavefront takes a row, two channels a lane.
+// Joins the parts of a tile's rows: 32 lanes take a row, four channels each.
 __global__ __launch_bounds__(256) void tkv_prefill_merge_kernel(PrefillArgs a, int32_t tile_rows)
 {
-    const uint32_t chunks = (uint32_t)tile_rows / 4, block = blockIdx.x + blockIdx.y * gridDim.x;
+    const uint32_t chunks = (uint32_t)tile_rows / 8, block = blockIdx.x + blockIdx.y * gridDim.x;
     const uint32_t of = block / chunks;
-    const int kv_head = (int)(of % (uint32_t)a.n_kv_heads), number = (int)(of / (uint32_t)a.n_kv_heads);
-    if (number >= a.n_items) return;
+    const int kv_head = (int)(of % (uint32_t)a.n_kv_heads), cut = (int)(of / (uint32_t)a.n_kv_heads);
+    if (cut >= a.n_cut) return;
+    const int number = a.items[(int64_t)kItem * cut + 10];
+    if (number < 0 || number >= a.n_items) return;
     const Item it = item_of(a.items, number);
     if (it.slot < 0 || it.part != 0 || !item_ok(it, a)) return;
-    const int lane = threadIdx.x & 63, in_tile = (int)(block % chunks) * 4 + (int)(threadIdx.x >> 6);
+    const int lane = threadIdx.x & 31, in_tile = (int)(block % chunks) * 8 + (int)(threadIdx.x >> 5);
     const uint32_t row = (uint32_t)it.row0 + in_tile, n_rows = (uint32_t)it.n_new * (uint32_t)a.group;
     if (row >= n_rows) return;
     const float2 *ml = reinterpret_cast<const float2 *>(a.partial + (int64_t)a.n_slots * a.n_kv_heads * tile_rows * kHeadDim);
     auto at = [&](int p) { return ((int64_t)(it.slot + p) * a.n_kv_heads + kv_head) * tile_rows + in_tile; };
-    float m = kNone;
-    for (int p = 0; p < it.n_parts; ++p) m = fmaxf(m, ml[at(p)].x);
-    float sum = 0.0f, x = 0.0f, y = 0.0f;
-    for (int p = 0; p < it.n_parts; ++p) {
-        const float2 s = ml[at(p)];
-        const float by = __builtin_amdgcn_exp2f(s.x - m);
-        const float2 o = reinterpret_cast<const float2 *>(a.partial + at(p) * kHeadDim)[lane];
-        sum = fmaf(s.y, by, sum);
-        x = fmaf(o.x, by, x);
-        y = fmaf(o.y, by, y);
+    // (m, sum) of up to 32 parts at once, a lane each
+    float m = kNone, sum = 0.0f;
+    float4 x = {0.0f, 0.0f, 0.0f, 0.0f};
+    for (int first = 0; first < it.n_parts; first += 32) {
+        const int n = it.n_parts - first < 32 ? it.n_parts - first : 32;
+        const float2 mine = lane < n ? ml[at(first + lane)] : make_float2(kNone, 0.0f);
+        float top = mine.x;
+#pragma unroll
+        for (int k = 16; k > 0; k >>= 1) top = fmaxf(top, __shfl_xor(top, k));
+        top = fmaxf(top, m);
+        const float before = __builtin_amdgcn_exp2f(m - top), by = __builtin_amdgcn_exp2f(mine.x - top);
+        m = top;
+        sum *= before;
+        x.x *= before; x.y *= before; x.z *= before; x.w *= before;
+        float add = mine.y * by;
+#pragma unroll
+        for (int k = 16; k > 0; k >>= 1) add += __shfl_xor(add, k);
+        sum += add;
+        for (int p = 0; p < n; p += 8) {
+            float4 o[8];
+#pragma unroll
+            for (int k = 0; k < 8; ++k) o[k] = p + k < n ? reinterpret_cast<const float4 *>(a.partial + at(first + p + k) * kHeadDim)[lane] : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+                const float f = __shfl(by, (p + k) & 31, 32);
+                x.x = fmaf(o[k].x, f, x.x); x.y = fmaf(o[k].y, f, x.y); x.z = fmaf(o[k].z, f, x.z); x.w = fmaf(o[k].w, f, x.w);
+            }
+        }
     }
     const float by = 1.0f / sum;
     const uint32_t token = row / (uint32_t)a.group, head = kv_head * a.group + (row - token * a.group);
-    uint32_t *to = reinterpret_cast<uint32_t *>(a.out + ((int64_t)(it.token0 + (int)token) * (a.n_kv_heads * a.group) + head) * kHeadDim);
-    to[lane] = a.out_bf16 ? pack<true>(x * by, y * by) : pack<false>(x * by, y * by);
+    u32x2 *to = reinterpret_cast<u32x2 *>(a.out + ((int64_t)(it.token0 + (int)token) * (a.n_kv_heads * a.group) + head) * kHeadDim);
+    to[lane] = a.out_bf16 ? u32x2{pack<true>(x.x * by, x.y * by), pack<true>(x.z * by, x.w * by)} : u32x2{pack<false>(x.x * by, x.y * by), pack<false>(x.z * by, x.w * by)};
+}
+
+template <int WAVES, int KB> hipError_t launch(const PrefillArgs &a, bool bf16, dim3 grid, hipStream_t stream)
+{
+    hipLaunchKernelGGL((bf16 ? tkv_prefill_kernel<true, WAVES, KB> : tkv_prefill_kernel<false, WAVES, KB>), grid, dim3(64 * WAVES), 4 * 32 * KB * kRow, stream, a);   // two buffers of K, two of V
+    return hipGetLastError();
 }
 
 } // namespace
@@ -502,18 +539,20 @@ int tkv_launch_prefill(int32_t n_q_heads, int32_t n_kv_heads, const void *q, int
     a.out = (uint16_t *)out;
     a.partial = (float *)workspace;
     a.status = status;
-    a.n_items = prefill->n_items; a.n_slots = prefill->n_slots; a.n_tokens = n_tokens; a.n_prefix = n_prefix;
+    a.n_items = prefill->n_items; a.n_slots = prefill->n_slots; a.n_cut = prefill->n_cut; a.n_tokens = n_tokens; a.n_prefix = n_prefix;
     a.group = n_q_heads / n_kv_heads; a.n_kv_heads = n_kv_heads;
     a.q_bf16 = q_type == TKV_BF16; a.out_bf16 = out_type == TKV_BF16;
     a.c = sm_scale * 1.44269504088896340736f;
     constexpr int64_t kMaxX = 1 << 22;   // a grid has less than 2^32 threads in a dimension
     auto grid = [&](int64_t blocks) { return dim3((unsigned)(blocks < kMaxX ? blocks : kMaxX), (unsigned)((blocks + kMaxX - 1) / kMaxX)); };
     const int64_t blocks = (int64_t)prefill->n_items * n_kv_heads;
-    auto *kernel = kv_type == TKV_BF16 ? tkv_prefill_kernel<true, 4> : tkv_prefill_kernel<false, 4>;
-    hipLaunchKernelGGL(kernel, grid(blocks), dim3(256), 4 * kTile, (hipStream_t)stream, a);
-    if (hipGetLastError() != hipSuccess) return TKV_ERR_HIP;
-    if (prefill->n_slots > 0) {
-        hipLaunchKernelGGL(tkv_prefill_merge_kernel, grid(blocks * (prefill->tile_rows / 4)), dim3(256), 0, (hipStream_t)stream, a, prefill->tile_rows);
+    const dim3 groups = grid(blocks);
+    const bool bf16 = kv_type == TKV_BF16;
+    const hipError_t e = prefill->tile_rows == 32 ? launch<1, 1>(a, bf16, groups, (hipStream_t)stream)
+                         : prefill->tile_rows == 128 ? launch<4, 2>(a, bf16, groups, (hipStream_t)stream) : launch<8, 2>(a, bf16, groups, (hipStream_t)stream);
+    if (e != hipSuccess) return TKV_ERR_HIP;
+    if (prefill->n_cut > 0) {
+        hipLaunchKernelGGL(tkv_prefill_merge_kernel, grid((int64_t)prefill->n_cut * n_kv_heads * (prefill->tile_rows / 8)), dim3(256), 0, (hipStream_t)stream, a, prefill->tile_rows);
         if (hipGetLastError() != hipSuccess) return TKV_ERR_HIP;
     }
     return TKV_OK;

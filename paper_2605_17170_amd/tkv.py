@@ -138,14 +138,14 @@ class tkv_rope(C.Structure):
 
 class tkv_prefill(C.Structure):
     """The plan of prompt attention on the device; `make` keeps the tensor alive."""
-    _fields_ = [("tile_rows", C.c_int32), ("n_items", C.c_int32), ("n_slots", C.c_int32), ("items", C.c_void_p)]
+    _fields_ = [("tile_rows", C.c_int32), ("n_items", C.c_int32), ("n_slots", C.c_int32), ("n_cut", C.c_int32), ("items", C.c_void_p)]
 
     @classmethod
     def make(cls, plan, device="cuda"):
         """`plan`: a PrefillPlan."""
         import torch
         items = torch.from_numpy(np.ascontiguousarray(plan.items, np.int32)).to(device)
-        prefill = cls(int(plan.tile_rows), items.numel() // PREFILL_ITEM_WORDS, int(plan.n_slots), _dev(items))
+        prefill = cls(int(plan.tile_rows), items.numel() // PREFILL_ITEM_WORDS, int(plan.n_slots), int(plan.n_cut), _dev(items))
         prefill.tensors = (items,)
         return prefill
 
@@ -228,7 +228,7 @@ def lib():
         L.tkv_plan_prefill_capacity.restype = i32
         L.tkv_plan_prefill_capacity.argtypes = [dp, i32, i32, i32, i32]
         L.tkv_plan_prefill.restype = i32
-        L.tkv_plan_prefill.argtypes = [dp, i32, i32, vp, vp, i32, vp, i32, C.POINTER(i32), C.POINTER(i32)]
+        L.tkv_plan_prefill.argtypes = [dp, i32, i32, vp, vp, i32, vp, i32, C.POINTER(i32), C.POINTER(i32), C.POINTER(i32)]
         L.tkv_prefill_workspace_bytes.restype = sz
         L.tkv_prefill_workspace_bytes.argtypes = [dp, i32, i32]
         L.tkv_prefill_attention.argtypes = [dp, i32, vp, C.c_int64, i32, vp, C.c_int64, vp, C.c_int64, i32, i32, vp, vp, i32, C.POINTER(tkv_prefill),
@@ -751,8 +751,8 @@ def tkv_norm_rope(rope: tkv_rope, q, k, v, positions, q_weight, k_weight, eps: f
 
 
 # ---------------------------------------------------------------- P2 (host plan, device)
-PREFILL_ITEM_WORDS = 10
-PrefillPlan = collections.namedtuple("PrefillPlan", "items n_slots tile_rows")
+PREFILL_ITEM_WORDS = 11
+PrefillPlan = collections.namedtuple("PrefillPlan", "items n_slots tile_rows n_cut")
 _TYPES = {"torch.bfloat16": TKV_BF16, "torch.float16": TKV_FP16, "torch.float32": TKV_FP32}
 
 
@@ -764,7 +764,7 @@ def _type(t, allowed, what):
 
 def tkv_plan_prefill(desc, n_q_heads: int, seq_indptr, prefix_indptr=None, target_cus: int = 256) -> PrefillPlan:
     """Plan for sequences of seq_indptr's new tokens behind prefix_indptr's cached ones (host arrays [batch+1]).
-    PrefillPlan: items i32[n_items, 10], n_slots, tile_rows."""
+    PrefillPlan: items i32[n_items, 11], n_slots, tile_rows, n_cut."""
     ip, pip = _np(seq_indptr, np.int32)
     batch = ip.size - 1
     pp = None
@@ -774,10 +774,10 @@ def tkv_plan_prefill(desc, n_q_heads: int, seq_indptr, prefix_indptr=None, targe
             raise ValueError("prefix_indptr has one entry per sequence and one more, as seq_indptr")
     cap = _check(lib().tkv_plan_prefill_capacity(C.byref(desc), batch, int(ip[-1]) if ip.size else 0, n_q_heads, target_cus), "tkv_plan_prefill_capacity")
     items = np.empty((cap, PREFILL_ITEM_WORDS), np.int32)
-    rows, slots = C.c_int32(0), C.c_int32(0)
+    rows, slots, cut = C.c_int32(0), C.c_int32(0), C.c_int32(0)
     n = _check(lib().tkv_plan_prefill(C.byref(desc), batch, n_q_heads, pip, pp, target_cus, C.c_void_p(items.ctypes.data), cap, C.byref(rows),
-                                      C.byref(slots)), "tkv_plan_prefill")
-    return PrefillPlan(items[:n].copy(), slots.value, rows.value)
+                                      C.byref(slots), C.byref(cut)), "tkv_plan_prefill")
+    return PrefillPlan(items[:n].copy(), slots.value, rows.value, cut.value)
 
 
 def tkv_prefill_workspace_bytes(desc, n_slots: int, tile_rows: int) -> int:

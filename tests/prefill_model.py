@@ -37,3 +37,28 @@ def attention(q, k, v, before, lens, cached, sm_scale, out_type, prefix_type=tor
                 tol[a:a + n, h] += 2.0 ** -25 * (c + n) * V.abs().amax()
         a, p = a + n, p + c
     return out, tol
+
+
+KEYS = {32: 32, 128: 64, 256: 64}     # keys of a tile, by rows
+
+
+def plan_of(rows, most, lens, cached, group):
+    """A plan with tiles of `rows` rows and ranges of at most `most` tiles of keys."""
+    import numpy as np
+
+    from paper_2605_17170_amd import tkv
+    items, cuts, slot, a, p = [], [], 0, 0, 0
+    for n, c in zip(lens, cached):
+        for row in range(0, n * group, rows):
+            see = (min(row + rows, n * group) - 1) // group + 1
+            keys = -(-c // KEYS[rows]) + -(-see // KEYS[rows])
+            parts = -(-keys // most)
+            if parts > 1:
+                cuts.append(len(items))
+            for k in range(parts):
+                items.append([a, n, p, c, row, keys * k // parts, keys * (k + 1) // parts, slot if parts > 1 else -1, k, parts, -1])
+                slot += parts > 1
+        a, p = a + n, p + c
+    for k, number in enumerate(cuts):
+        items[k][10] = number
+    return tkv.PrefillPlan(np.array(items, np.int32).reshape(-1, 11), slot, rows, len(cuts))

@@ -6,7 +6,7 @@ import pytest
 import torch
 
 from paper_2605_17170_amd import tkv
-from tests.prefill_model import attention
+from tests.prefill_model import attention, plan_of
 
 pytestmark = pytest.mark.gpu
 DEV = "cuda:0"
@@ -19,7 +19,7 @@ def indptr(lens):
 
 
 class Case:
-    def __init__(self, lens, cached, hq, hk, q=BF, kv=BF, out=BF, packed=False, pad=0, spare=0, seed=0, target=256, sm=SM, size=1.0):
+    def __init__(self, lens, cached, hq, hk, q=BF, kv=BF, out=BF, packed=False, pad=0, spare=0, seed=0, target=256, sm=SM, size=1.0, kind=None, most=1 << 20):
         g = torch.Generator(device=DEV)
         g.manual_seed(seed)
         self.lens, self.cached, self.hq, self.hk, self.sm = list(lens), list(cached), hq, hk, sm
@@ -37,7 +37,7 @@ class Case:
         m = sum(cached)
         self.before = [(torch.randn((m, hk, 128), device=DEV, generator=g) * 2.0).to(FP) if m else None for _ in range(2)]
         self.desc = tkv.tkv_desc.make(hk, 0, 0)
-        self.plan = tkv.tkv_plan_prefill(self.desc, hq, indptr(lens), indptr(cached), target)
+        self.plan = tkv.tkv_plan_prefill(self.desc, hq, indptr(lens), indptr(cached), target) if kind is None else plan_of(kind, most, lens, cached, hq // hk)
         self.prefill = tkv.tkv_prefill.make(self.plan, DEV)
         self.out = torch.full((n, hq, 128), 7.0, dtype=out, device=DEV)
         self.workspace = torch.full((max(16, tkv.tkv_prefill_workspace_bytes(self.desc, self.plan.n_slots, self.plan.tile_rows)),), 255, dtype=torch.uint8, device=DEV)
@@ -83,12 +83,38 @@ def test_parts_of_a_packed_projection(kind, pad):
     c.check("packed, pad %d" % pad)
 
 
-@pytest.mark.parametrize("target", [1, 3, 16, 256, 1024])
-def test_ranges_of_keys_cut_into_parts(target):
-    c = Case([5, 90, 1], [3000, 700, 1500], 8, 2, target=target, seed=target)
-    assert (c.plan.n_slots > 0) == (target > 1)
+@pytest.mark.parametrize("rows", [32, 128, 256])
+@pytest.mark.parametrize("most", [1, 2, 3, 7, 1 << 20])
+@pytest.mark.parametrize("kv", [BF, FP])
+def test_workgroups_of_every_kind_and_ranges_of_every_length(rows, most, kv):
+    c = Case([5, 90, 1, 300], [1500, 70, 129, 0], 8, 2, BF, kv, BF, kind=rows, most=most, seed=rows + most % 100)
+    assert (c.plan.n_slots > 0) == (most < 1000)
     c.call()
-    c.check("target %d" % target)
+    c.check("%d rows, ranges of %d" % (rows, most))
+
+
+@pytest.mark.parametrize("rows", [32, 128, 256])
+@pytest.mark.parametrize("n", [1, 31, 32, 33, 63, 64, 65, 96, 127, 128, 129, 255, 256, 257, 383])
+def test_one_head_at_the_borders_of_tiles(rows, n):
+    for cached, most in ((0, 1 << 20), (n, 2)):
+        c = Case([n], [cached], 1, 1, kind=rows, most=most, seed=n)
+        c.call()
+        c.check("%d rows, %d behind %d" % (rows, n, cached))
+
+
+@pytest.mark.parametrize("parts", [31, 32, 33, 64, 70])
+def test_many_parts(parts):
+    c = Case([3], [32 * parts - 3], 4, 1, kind=32, most=1, seed=parts)
+    assert c.plan.n_slots == parts + 0 + (1 if (32 * parts - 3) % 32 else 0)
+    c.call()
+    c.check("%d parts" % parts)
+
+
+@pytest.mark.parametrize("target", [1, 3, 16, 256, 1024])
+def test_plans_for_fewer_and_more_compute_units(target):
+    c = Case([5, 90, 1], [3000, 700, 1500], 8, 2, target=target, seed=target)
+    c.call()
+    c.check("target %d, %d rows" % (target, c.plan.tile_rows))
 
 
 def test_the_same_call_gives_the_same_bits():
@@ -102,10 +128,12 @@ def test_the_same_call_gives_the_same_bits():
         assert torch.equal(c.out, first)
 
 
-def test_a_sequence_does_not_depend_on_the_batch():
-    c = Case([64, 100], [130, 0], 4, 2, seed=6, target=1)
+@pytest.mark.parametrize("rows", [32, 128, 256])
+def test_a_sequence_does_not_depend_on_the_batch(rows):
+    """With workgroups of one kind and whole ranges (which the plan chooses by the batch)."""
+    c = Case([64, 100], [130, 0], 4, 2, seed=6, kind=rows)
     c.call()
-    d = Case([100], [0], 4, 2, seed=7, target=1)
+    d = Case([100], [0], 4, 2, seed=7, kind=rows)
     d.q, d.k, d.v = c.q[64:].contiguous(), c.k[64:].contiguous(), c.v[64:].contiguous()
     d.call()
     assert torch.equal(c.out[64:], d.out)
@@ -128,12 +156,12 @@ def test_logits_far_apart_follow_the_maximum():
 
 @pytest.mark.parametrize("kind", [BF, FP])
 @pytest.mark.parametrize("bad", [math.inf, -math.inf, math.nan])
-@pytest.mark.parametrize("target", [1, 256])
-def test_what_a_token_does_not_see_does_not_reach_it(kind, bad, target):
+@pytest.mark.parametrize("rows,most", [(32, 3), (32, 1 << 20), (128, 2), (128, 1 << 20), (256, 1 << 20)])
+def test_what_a_token_does_not_see_does_not_reach_it(kind, bad, rows, most):
     """NaN and infinities in keys and values of later tokens, of other sequences, of rows behind the last one."""
     lens, cached = [90, 70, 3], [70, 0, 1100]
-    c = Case(lens, cached, 2, 1, kind, kind, kind, spare=4, seed=10, target=target)
-    clean = Case(lens, cached, 2, 1, kind, kind, kind, spare=4, seed=10, target=target)
+    c = Case(lens, cached, 2, 1, kind, kind, kind, spare=4, seed=10, kind=rows, most=most)
+    clean = Case(lens, cached, 2, 1, kind, kind, kind, spare=4, seed=10, kind=rows, most=most)
     clean.call()
     hit = [40, 90 + 69, 160 + 1]      # a token of each sequence
     for t in hit:
@@ -149,9 +177,10 @@ def test_what_a_token_does_not_see_does_not_reach_it(kind, bad, target):
 
 @pytest.mark.parametrize("kind", [BF, FP])
 @pytest.mark.parametrize("at", [0, 63, 100, 149])
-def test_values_that_are_not_finite_reach_the_tokens_that_see_them(kind, at):
-    c = Case([150], [0], 2, 1, kind, kind, kind, seed=11)
-    clean = Case([150], [0], 2, 1, kind, kind, kind, seed=11)
+@pytest.mark.parametrize("rows", [32, 128, 256])
+def test_values_that_are_not_finite_reach_the_tokens_that_see_them(kind, at, rows):
+    c = Case([150], [0], 2, 1, kind, kind, kind, seed=11, kind=rows)
+    clean = Case([150], [0], 2, 1, kind, kind, kind, seed=11, kind=rows)
     clean.call()
     c.v[at, 0, 3], c.v[at, 0, 40], c.v[at, 0, 127] = math.inf, -math.inf, math.nan
     c.call()
@@ -196,7 +225,7 @@ def test_on_another_stream_than_the_current_one():
 
 
 def test_two_calls_at_once_with_workspaces_of_their_own():
-    a, b = Case([7], [5000], 8, 2, seed=15), Case([9], [4000], 8, 2, seed=16)
+    a, b = Case([7], [5000], 8, 2, seed=15, kind=32, most=9), Case([9], [4000], 8, 2, seed=16, kind=128, most=9)
     assert a.plan.n_slots and b.plan.n_slots
     streams = [torch.cuda.Stream(), torch.cuda.Stream()]
     for s in streams:
@@ -211,14 +240,14 @@ def test_two_calls_at_once_with_workspaces_of_their_own():
 
 
 def test_captured_and_replayed_with_other_inputs():
-    c = Case([60, 1], [2000, 700], 8, 2, seed=17)
+    c = Case([60, 1], [2000, 700], 8, 2, seed=17, kind=128, most=9)
     c.call()
     torch.cuda.synchronize()
     graph = torch.cuda.CUDAGraph()
     with torch.cuda.graph(graph):
         c.call()
     for k in range(4):
-        d = Case([60, 1], [2000, 700], 8, 2, seed=18 + k)
+        d = Case([60, 1], [2000, 700], 8, 2, seed=18 + k, kind=128, most=9)
         for x, y in zip([c.q, c.k, c.v] + c.before, [d.q, d.k, d.v] + d.before):
             x.copy_(y)
         c.out.fill_(7.0)
@@ -231,9 +260,9 @@ def test_captured_and_replayed_with_other_inputs():
 
 
 @pytest.mark.parametrize("word,value", [(0, -1), (0, 1000), (1, 0), (1, 1 << 30), (2, -1), (2, 1 << 30), (3, -1), (3, 1 << 20), (4, -128), (4, 1 << 30), (5, -1), (5, 99),
-                                        (7, 1000), (7, -2), (8, -1), (8, 9), (9, 0), (9, 1 << 30)])
+                                        (7, 1000), (7, -2), (8, -1), (8, 99), (9, 0), (9, 1 << 30)])
 def test_items_that_name_what_is_not_there_are_skipped(word, value):
-    c = Case([30, 20], [700, 3000], 4, 2, seed=19)
+    c = Case([30, 20], [700, 3000], 4, 2, seed=19, kind=128, most=9)
     plan = c.plan._replace(items=c.plan.items.copy())
     first = int(np.flatnonzero(plan.items[:, 0] == 30)[0])
     plan.items[first, word] = value
@@ -246,7 +275,7 @@ def test_items_that_name_what_is_not_there_are_skipped(word, value):
 
 def test_a_plan_without_items_and_a_call_without_tokens():
     c = Case([0, 0], [5, 0], 4, 2, spare=2)
-    assert c.plan.items.shape == (0, 10) and c.plan.n_slots == 0
+    assert c.plan.items.shape == (0, 11) and c.plan.n_slots == 0
     c.call()
     torch.cuda.synchronize()
     assert (c.out == 7.0).all()
