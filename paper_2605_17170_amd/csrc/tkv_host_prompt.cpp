@@ -234,7 +234,7 @@ int tkv_quantize_rows(const tkv_desc *desc, const void *K, int64_t k_stride, con
 size_t tkv_distortion_workspace_bytes(int32_t batch, int32_t n_tokens, int32_t n_heads)
 {
     if (batch < 0 || n_tokens < 0 || n_heads < 0) return 0;
-    return ((size_t)(n_tokens / kDistortionChunk) + (size_t)batch) * (size_t)n_heads * sizeof(double);
+    return ((size_t)(n_tokens / tkv_distortion_chunk(n_tokens, n_heads)) + (size_t)batch) * (size_t)n_heads * sizeof(double);
 }
 
 int tkv_head_distortion(const void *x, const void *y, int32_t type, const int32_t *seq_indptr, int32_t batch, int32_t n_tokens, int32_t n_heads, double *out,

@@ -26,81 +26,120 @@ struct RowsArgs {
     const int32_t *blocks;
     int32_t *status;
     int32_t n_tokens, n_heads, n_blocks, channel_keys;
-    uint32_t row_groups;       // workgroups of the rows of K and of V each; the blocks' follow
+    uint32_t block_groups;     // workgroups of the blocks, which take longest; the rows' follow
 };
 
-constexpr int kRowsWg = 16;    // rows (a token of a head) of a workgroup
+typedef _Float16 half2_t __attribute__((ext_vector_type(2)));
 
 template <int CTRL> __device__ __forceinline__ float dpp(float v)
 {
     return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v), CTRL, 0xf, 0xf, true));
 }
+__device__ __forceinline__ float lo_f32(uint32_t v) { return __uint_as_float(v << 16); }
+__device__ __forceinline__ float hi_f32(uint32_t v) { return __uint_as_float(v & 0xffff0000u); }
 struct Grid {
     float zero, inv, levels;
-    _Float16 scale_h, zero_h;
+    half2_t scale, shift;   // scale and zero-point, twice
 };
-__device__ __forceinline__ Grid grid_of(float mn, float mx, float levels)
+__device__ __forceinline__ Grid grid_of(float mn, float mx, bool wide)
 {
     if (mn == 0.0f) mn = 0.0f;   // -0 -> +0
     Grid g;
-    g.scale_h = (_Float16)__fdiv_rn(__fsub_rn(mx, mn), levels);
-    g.zero_h = (_Float16)mn;
-    const float s = (float)g.scale_h;
-    g.zero = (float)g.zero_h;
-    g.inv = s == 0.0f ? 0.0f : __fdiv_rn(1.0f, s);
-    g.levels = levels;
+    g.levels = wide ? 15.0f : 3.0f;
+    // Quotient by the levels and reciprocal of the scale, both correctly rounded: a product with the rounded reciprocal (the hardware's,
+    // one unit off at most) and one step of Newton, whose residual the fused multiply-add gives exactly.  (Where a quotient is too small for
+    // that it rounds to an fp16 zero either way.)  The plain divisions are ten instructions each.
+    const float r = __fsub_rn(mx, mn), y = wide ? 1.0f / 15.0f : 1.0f / 3.0f, q = __fmul_rn(r, y);
+    const _Float16 sh = (_Float16)__builtin_fmaf(__builtin_fmaf(-q, g.levels, r), y, q), zh = (_Float16)mn;
+    const float s = (float)sh, i = __builtin_amdgcn_rcpf(s);
+    g.zero = (float)zh;
+    g.inv = s == 0.0f ? 0.0f : __builtin_fmaf(__builtin_fmaf(-s, i, 1.0f), i, i);
+    g.scale = half2_t{sh, sh};
+    g.shift = half2_t{zh, zh};
     return g;
 }
-__device__ __forceinline__ uint32_t back(const Grid &g, float x)   // bits of the fp16 value
+// Bits of two fp16 values that the codes of x and y stand for.
+__device__ __forceinline__ uint32_t back(const Grid &g, float x, float y)
 {
-    const float t = __builtin_amdgcn_fmed3f(__fmul_rn(__fsub_rn(x, g.zero), g.inv), 0.0f, g.levels);
-    const _Float16 code = (_Float16)__builtin_rintf(t);
-    return __builtin_bit_cast(uint16_t, (_Float16)__builtin_fmaf16(code, g.scale_h, g.zero_h));
+    const float t = __builtin_rintf(__builtin_amdgcn_fmed3f(__fmul_rn(__fsub_rn(x, g.zero), g.inv), 0.0f, g.levels));
+    const float u = __builtin_rintf(__builtin_amdgcn_fmed3f(__fmul_rn(__fsub_rn(y, g.zero), g.inv), 0.0f, g.levels));
+    const half2_t code = {(_Float16)t, (_Float16)u};
+    return __builtin_bit_cast(uint32_t, __builtin_elementwise_fma(code, g.scale, g.shift));   // one rounding
 }
-__device__ __forceinline__ uint32_t half_bits(float x) { return __builtin_bit_cast(uint16_t, (_Float16)x); }
+__device__ __forceinline__ uint32_t halves(uint32_t v)   // two bf16 numbers as fp16
+{
+    const half2_t h = {(_Float16)lo_f32(v), (_Float16)hi_f32(v)};
+    return __builtin_bit_cast(uint32_t, h);
+}
 
+// Eight channels of a row, whose group the four lanes of a quad hold.
+__device__ __forceinline__ uint4 row_piece(uint4 x, uint32_t bits)
+{
+    const float f[8] = {lo_f32(x.x), hi_f32(x.x), lo_f32(x.y), hi_f32(x.y), lo_f32(x.z), hi_f32(x.z), lo_f32(x.w), hi_f32(x.w)};
+    float mn = f[0], mx = f[0];
+#pragma unroll
+    for (int i = 1; i < 8; ++i) {
+        mn = fminf(mn, f[i]);
+        mx = fmaxf(mx, f[i]);
+    }
+    mn = fminf(mn, dpp<0xB1>(mn)); mx = fmaxf(mx, dpp<0xB1>(mx));
+    mn = fminf(mn, dpp<0x4E>(mn)); mx = fmaxf(mx, dpp<0x4E>(mx));
+    const Grid g = grid_of(mn, mx, bits == 4);
+    return make_uint4(back(g, f[0], f[1]), back(g, f[2], f[3]), back(g, f[4], f[5]), back(g, f[6], f[7]));
+}
+
+// PER: rows of K and of V that a thread has a piece of; ONCE: past the caches.
+template <int PER, bool ONCE>
 __global__ __launch_bounds__(256) void tkv_rows_kernel(RowsArgs a)
 {
-    const uint32_t block = blockIdx.x + blockIdx.y * gridDim.x;
-    if (block < 2 * a.row_groups) {
-        const int which = block >= a.row_groups, part = threadIdx.x & 15;
-        const int64_t row = (int64_t)(block - which * a.row_groups) * kRowsWg + (threadIdx.x >> 4);
-        if (row >= (int64_t)a.n_tokens * a.n_heads) return;
-        const int token = (int)(row / a.n_heads), head = (int)(row - (int64_t)token * a.n_heads);
-        const uint32_t bits = a.tag_bits[token];
-        if (bits != 0 && bits != 2 && bits != 4) {
-            if (a.status && part == 0 && head == 0) atomicOr(a.status, TKV_STATUS_TAG_MISMATCH);
-            return;
-        }
-        if (which == 0 && bits == 2 && a.channel_keys) return;   // a block's
-        const uint4 x = reinterpret_cast<const uint4 *>(a.in[which] + token * a.stride[which] + (int64_t)head * kHeadDim)[part];
-        const uint32_t u[4] = {x.x, x.y, x.z, x.w};
-        float f[8];
+    uint32_t block = blockIdx.x + blockIdx.y * gridDim.x;
+    if (block >= a.block_groups) {
+        block -= a.block_groups;
+        constexpr int kRows = 16 * PER;   // of a workgroup
+        const int part = threadIdx.x & 15;
+        const uint32_t first = block * kRows, heads = (uint32_t)a.n_heads, n_rows = (uint32_t)a.n_tokens * heads;
+        const int token0 = (int)(first / heads), head0 = (int)(first - (uint32_t)token0 * heads);
+        int token[PER], head[PER];
+        uint32_t bits[PER];
+        bool live[PER];
+        uint4 x[PER][2];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            f[2 * i] = __uint_as_float(u[i] << 16);
-            f[2 * i + 1] = __uint_as_float(u[i] & 0xffff0000u);
-        }
-        float mn = f[0], mx = f[0];
+        for (int k = 0; k < PER; ++k) {
+            const int local = 16 * k + (int)(threadIdx.x >> 4), at = head0 + local;
+            // (below 32 heads the quotient is 1 / 64 from the next integer at least, and off by 2^-17)
+            const int of = heads >= 32 ? (at >= (int)heads ? 1 : 0) : (int)(((float)at + 0.5f) * __builtin_amdgcn_rcpf((float)heads));
+            live[k] = (uint64_t)first + local < n_rows;
+            token[k] = live[k] ? token0 + of : 0;
+            head[k] = live[k] ? at - of * (int)heads : 0;
+            bits[k] = a.tag_bits[token[k]];
 #pragma unroll
-        for (int i = 1; i < 8; ++i) {
-            mn = fminf(mn, f[i]);
-            mx = fmaxf(mx, f[i]);
+            for (int w = 0; w < 2; ++w) {
+                const uint4 *src = reinterpret_cast<const uint4 *>(a.in[w] + token[k] * a.stride[w] + (int64_t)head[k] * kHeadDim) + part;
+                x[k][w] = ONCE ? load_once(src) : *src;
+            }
         }
-        mn = fminf(mn, dpp<0xB1>(mn)); mx = fmaxf(mx, dpp<0xB1>(mx));   // the four lanes of a group
-        mn = fminf(mn, dpp<0x4E>(mn)); mx = fmaxf(mx, dpp<0x4E>(mx));
-        const Grid g = grid_of(mn, mx, bits == 4 ? 15.0f : 3.0f);
-        uint32_t o[4];
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
-            o[i] = bits ? back(g, f[2 * i]) | back(g, f[2 * i + 1]) << 16 : half_bits(f[2 * i]) | half_bits(f[2 * i + 1]) << 16;
-        store_once(reinterpret_cast<uint4 *>(a.out[which] + row * kHeadDim) + part, make_uint4(o[0], o[1], o[2], o[3]));
+        for (int k = 0; k < PER; ++k) {
+            if (!live[k]) continue;
+            const uint32_t b = bits[k];
+            const int64_t row = (int64_t)token[k] * heads + head[k];
+            if (b != 0 && b != 2 && b != 4) {
+                if (a.status && part == 0 && head[k] == 0) atomicOr(a.status, TKV_STATUS_TAG_MISMATCH);
+                continue;
+            }
+#pragma unroll
+            for (int w = 0; w < 2; ++w) {
+                if (w == 0 && b == 2 && a.channel_keys) continue;   // a block's
+                const uint4 y = b ? row_piece(x[k][w], b) : make_uint4(halves(x[k][w].x), halves(x[k][w].y), halves(x[k][w].z), halves(x[k][w].w));
+                store_once(reinterpret_cast<uint4 *>(a.out[w] + row * kHeadDim) + part, y);
+            }
+        }
         return;
     }
     // keys per channel: a wavefront takes a block of 32 tokens of a head, lane (i, part) its tokens i, 4 + i, .. and channels 8 part ..
-    const int64_t unit = (int64_t)(block - 2 * a.row_groups) * 4 + (threadIdx.x >> 6);
+    const int64_t unit = (int64_t)block * 4 + (threadIdx.x >> 6);
     if (unit >= (int64_t)a.n_blocks * a.n_heads) return;
-    const int number = (int)(unit / a.n_heads), head = (int)(unit - (int64_t)number * a.n_heads);
+    const int number = (int)((uint32_t)unit / (uint32_t)a.n_heads), head = (int)(unit - (int64_t)number * a.n_heads);
     const int lane = threadIdx.x & 63, part = lane & 15, i0 = lane >> 4;
     int token[8];
     bool ok = true;
@@ -108,40 +147,58 @@ __global__ __launch_bounds__(256) void tkv_rows_kernel(RowsArgs a)
     for (int k = 0; k < 8; ++k) {
         token[k] = a.blocks[(int64_t)number * kGroup + 4 * k + i0];
         const bool in = token[k] >= 0 && token[k] < a.n_tokens;
+        ok = ok && in;
         if (!in) token[k] = 0;
-        ok = ok && in && a.tag_bits[token[k]] == 2;
     }
+    uint4 x[8];
+    uint32_t bits[8];
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+        bits[k] = a.tag_bits[token[k]];
+        x[k] = reinterpret_cast<const uint4 *>(a.in[0] + token[k] * a.stride[0] + (int64_t)head * kHeadDim)[part];
+    }
+#pragma unroll
+    for (int k = 0; k < 8; ++k) ok = ok && bits[k] == 2;
     if (!__all(ok)) {
         if (a.status && lane == 0) atomicOr(a.status, TKV_STATUS_BLOCK_PARTIAL);
         return;
     }
-    uint4 x[8];
+    uint32_t o[8][4];
 #pragma unroll
-    for (int k = 0; k < 8; ++k) x[k] = reinterpret_cast<const uint4 *>(a.in[0] + token[k] * a.stride[0] + (int64_t)head * kHeadDim)[part];
-    Grid g[8];
+    for (int c = 0; c < 4; ++c) {
+        float f[2][8], mn[2], mx[2];
+        Grid g[2];
 #pragma unroll
-    for (int c = 0; c < 8; ++c) {
-        float mn = INFINITY, mx = -INFINITY;
+        for (int h = 0; h < 2; ++h) {
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+                const uint32_t u = c == 0 ? x[k].x : c == 1 ? x[k].y : c == 2 ? x[k].z : x[k].w;
+                f[h][k] = h ? hi_f32(u) : lo_f32(u);
+            }
+            mn[h] = mx[h] = f[h][0];
+#pragma unroll
+            for (int k = 1; k < 8; ++k) {
+                mn[h] = fminf(mn[h], f[h][k]);
+                mx[h] = fmaxf(mx[h], f[h][k]);
+            }
+            mn[h] = fminf(mn[h], __shfl_xor(mn[h], 16)); mx[h] = fmaxf(mx[h], __shfl_xor(mx[h], 16));
+            mn[h] = fminf(mn[h], __shfl_xor(mn[h], 32)); mx[h] = fmaxf(mx[h], __shfl_xor(mx[h], 32));
+            g[h] = grid_of(mn[h], mx[h], false);
+        }
+        Grid both = g[0];
+        both.scale.y = g[1].scale.x;
+        both.shift.y = g[1].shift.x;
 #pragma unroll
         for (int k = 0; k < 8; ++k) {
-            const uint32_t u = c < 2 ? x[k].x : c < 4 ? x[k].y : c < 6 ? x[k].z : x[k].w;
-            const float f = __uint_as_float(c & 1 ? u & 0xffff0000u : u << 16);
-            mn = fminf(mn, f);
-            mx = fmaxf(mx, f);
+            const float t = __builtin_rintf(__builtin_amdgcn_fmed3f(__fmul_rn(__fsub_rn(f[0][k], g[0].zero), g[0].inv), 0.0f, 3.0f));
+            const float u = __builtin_rintf(__builtin_amdgcn_fmed3f(__fmul_rn(__fsub_rn(f[1][k], g[1].zero), g[1].inv), 0.0f, 3.0f));
+            const half2_t code = {(_Float16)t, (_Float16)u};
+            o[k][c] = __builtin_bit_cast(uint32_t, __builtin_elementwise_fma(code, both.scale, both.shift));
         }
-        mn = fminf(mn, __shfl_xor(mn, 16)); mx = fmaxf(mx, __shfl_xor(mx, 16));
-        mn = fminf(mn, __shfl_xor(mn, 32)); mx = fmaxf(mx, __shfl_xor(mx, 32));
-        g[c] = grid_of(mn, mx, 3.0f);
     }
 #pragma unroll
-    for (int k = 0; k < 8; ++k) {
-        const uint32_t u[4] = {x[k].x, x[k].y, x[k].z, x[k].w};
-        uint32_t o[4];
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-            o[i] = back(g[2 * i], __uint_as_float(u[i] << 16)) | back(g[2 * i + 1], __uint_as_float(u[i] & 0xffff0000u)) << 16;
-        store_once(reinterpret_cast<uint4 *>(a.out[0] + ((int64_t)token[k] * a.n_heads + head) * kHeadDim) + part, make_uint4(o[0], o[1], o[2], o[3]));
-    }
+    for (int k = 0; k < 8; ++k)
+        store_once(reinterpret_cast<uint4 *>(a.out[0] + ((int64_t)token[k] * a.n_heads + head) * kHeadDim) + part, make_uint4(o[k][0], o[k][1], o[k][2], o[k][3]));
 }
 
 // ------------------------------------------------------------------ distortion
@@ -149,77 +206,114 @@ struct DistortionArgs {
     const void *a, *b;
     const int32_t *seq_indptr;
     double *out, *partial;
-    int32_t batch, n_tokens, n_heads;
+    int32_t batch, n_tokens, n_heads, chunk;   // chunk: tokens whose squares a workgroup adds up
 };
-constexpr int kChunk = kDistortionChunk;   // tokens whose squares a workgroup adds up
-
-// The sequence's slots among the partial sums begin at first / kChunk + b: chunks of a sequence begin at its first token, and
-// ceil(n / kChunk) of them end before the next one's begin.
-__device__ __forceinline__ int first_slot(int first, int b) { return first / kChunk + b; }
+// The sequence's slots among the partial sums begin at first / chunk + b: chunks of a sequence begin at its first token, and
+// ceil(n / chunk) of them end before the next one's begin.
+__device__ __forceinline__ int first_slot(int first, int b, int chunk) { return (int)((uint32_t)first / (uint32_t)chunk) + b; }
 
 __device__ __forceinline__ float f32_of(uint32_t bits, int type) { return type == TKV_BF16 ? __uint_as_float(bits << 16) : (float)__builtin_bit_cast(_Float16, (uint16_t)bits); }
 
-template <int TYPE>
+// A workgroup takes a chunk of one sequence's tokens: sixteen (fp32: eight) rows at a time, all heads of a token or several tokens'.
+template <int TYPE, bool ONCE>
 __global__ __launch_bounds__(256) void tkv_distortion_kernel(DistortionArgs a)
 {
-    __shared__ int whose;
+    __shared__ double sums[16];
     const uint32_t slot = blockIdx.x + blockIdx.y * gridDim.x;
-    // the last sequence whose slots begin at or before this one
-    if (threadIdx.x == 0) whose = -1;
-    __syncthreads();
-    for (int b = threadIdx.x; b < a.batch; b += 256) {
-        const int lo = a.seq_indptr[b], hi = a.seq_indptr[b + 1];
-        if (lo >= 0 && hi >= lo && hi <= a.n_tokens && (uint32_t)first_slot(lo, b) <= slot && slot < (uint32_t)first_slot(lo, b) + (uint32_t)((hi - lo + kChunk - 1) / kChunk)) whose = b;
+    // the sequence that the slot belongs to: every wavefront looks through all of them
+    int begin = 0, end = 0;
+    for (int b0 = 0; b0 < a.batch; b0 += 64) {
+        const int b = b0 + (int)(threadIdx.x & 63), at = b < a.batch ? b : a.batch - 1;
+        const int lo = a.seq_indptr[at], hi = a.seq_indptr[at + 1];
+        const bool ok = b < a.batch && lo >= 0 && hi > lo && hi <= a.n_tokens;
+        const int first = ok ? first_slot(lo, b, a.chunk) : 0;
+        const uint64_t mine = __ballot(ok && (uint32_t)first <= slot && slot - (uint32_t)first < (uint32_t)((hi - lo + a.chunk - 1) / a.chunk));
+        if (mine) {
+            const int lane = __builtin_ctzll(mine), l = __builtin_amdgcn_readlane(lo, lane), h = __builtin_amdgcn_readlane(hi, lane), f = __builtin_amdgcn_readlane(first, lane);
+            begin = l + (int)(slot - (uint32_t)f) * a.chunk;
+            end = begin + a.chunk < h ? begin + a.chunk : h;
+            break;
+        }
     }
-    __syncthreads();
-    const int b = whose;
-    if (b < 0) return;
-    const int lo = a.seq_indptr[b], hi = a.seq_indptr[b + 1];
-    const int begin = lo + (int)(slot - first_slot(lo, b)) * kChunk, end = begin + kChunk < hi ? begin + kChunk : hi;
-    constexpr int kPer = TYPE == TKV_FP32 ? 4 : 8, kLanes = kHeadDim / kPer;   // values of a 16-byte piece; lanes of a row
-    const int part = threadIdx.x % kLanes;
-    for (int head = threadIdx.x / kLanes; head < a.n_heads; head += 256 / kLanes) {
+    if (begin >= end) return;
+    constexpr int kPer = TYPE == TKV_FP32 ? 4 : 8, kLanes = kHeadDim / kPer, kGroups = 256 / kLanes;   // values of a 16-byte piece; lanes of a row; rows at once
+    const int part = threadIdx.x % kLanes, group = threadIdx.x / kLanes;
+    const int width = a.n_heads < kGroups ? a.n_heads : kGroups, tokens = kGroups / width;             // heads and tokens at once
+    const int sub = group / width;
+    for (int head0 = 0; head0 < a.n_heads; head0 += width) {
+        const int head = head0 + group - sub * width;
         double sum = 0.0;
-        for (int t = begin; t < end; ++t) {
-            const int64_t at = ((int64_t)t * a.n_heads + head) * kLanes + part;
-            const uint4 x = reinterpret_cast<const uint4 *>(a.a)[at], y = reinterpret_cast<const uint4 *>(a.b)[at];
-            const uint32_t u[4] = {x.x, x.y, x.z, x.w}, v[4] = {y.x, y.y, y.z, y.w};
+        if (sub < tokens && head < a.n_heads) {
+            const int64_t step = (int64_t)a.n_heads * kLanes;
+            const uint4 *x = reinterpret_cast<const uint4 *>(a.a) + ((int64_t)head * kLanes + part), *y = reinterpret_cast<const uint4 *>(a.b) + ((int64_t)head * kLanes + part);
+            for (int t = begin + sub; t < end; t += 4 * tokens) {
+                uint4 u[4], v[4];
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                if constexpr (TYPE == TKV_FP32) {
-                    const double d = (double)__uint_as_float(u[i]) - (double)__uint_as_float(v[i]);
-                    sum = __builtin_fma(d, d, sum);
-                } else {
+                for (int k = 0; k < 4; ++k) {
+                    const int64_t at = (t + k * tokens < end ? t + k * tokens : t) * step;
+                    u[k] = ONCE ? load_once(x + at) : x[at];
+                    v[k] = ONCE ? load_once(y + at) : y[at];
+                }
 #pragma unroll
-                    for (int k = 0; k < 32; k += 16) {
-                        const double d = (double)f32_of(u[i] >> k & 0xffffu, TYPE) - (double)f32_of(v[i] >> k & 0xffffu, TYPE);
-                        sum = __builtin_fma(d, d, sum);
+                for (int k = 0; k < 4; ++k) {
+                    if (t + k * tokens >= end) break;
+                    const uint32_t p[4] = {u[k].x, u[k].y, u[k].z, u[k].w}, q[4] = {v[k].x, v[k].y, v[k].z, v[k].w};
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        if constexpr (TYPE == TKV_FP32) {
+                            const double d = (double)__uint_as_float(p[i]) - (double)__uint_as_float(q[i]);
+                            sum = __builtin_fma(d, d, sum);
+                        } else {
+#pragma unroll
+                            for (int h = 0; h < 32; h += 16) {
+                                const double d = (double)f32_of(p[i] >> h & 0xffffu, TYPE) - (double)f32_of(q[i] >> h & 0xffffu, TYPE);
+                                sum = __builtin_fma(d, d, sum);
+                            }
+                        }
                     }
                 }
             }
         }
 #pragma unroll
         for (int k = kLanes / 2; k > 0; k >>= 1) sum += __shfl_xor(sum, k);
-        if (part == 0) a.partial[(int64_t)slot * a.n_heads + head] = sum;
+        if (tokens > 1) {
+            if (part == 0) sums[group] = sum;
+            __syncthreads();
+            for (int k = 1; k < tokens; ++k)
+                if (sub == 0 && part == 0) sum += sums[group + k * width];
+            __syncthreads();
+        }
+        if (sub == 0 && part == 0 && head < a.n_heads) a.partial[(int64_t)slot * a.n_heads + head] = sum;
     }
 }
-// A wavefront adds up the slots of a sequence's head.
-__global__ __launch_bounds__(256) void tkv_distortion_join_kernel(DistortionArgs a)
+// Adds up the slots of a sequence: `width` lanes (a power of two) take a head each, 256 / width rows of them every so many slots.
+__global__ __launch_bounds__(256) void tkv_distortion_join_kernel(DistortionArgs a, int32_t width)
 {
-    const int64_t unit = ((int64_t)blockIdx.x + (int64_t)blockIdx.y * gridDim.x) * 4 + (threadIdx.x >> 6);
-    if (unit >= (int64_t)a.batch * a.n_heads) return;
-    const int b = (int)(unit / a.n_heads), head = (int)(unit - (int64_t)b * a.n_heads), lane = threadIdx.x & 63;
+    __shared__ double sums[256];
+    const uint32_t block = blockIdx.x + blockIdx.y * gridDim.x, passes = (uint32_t)((a.n_heads + width - 1) / width);
+    const int b = (int)(block / passes), head = (int)(block % passes) * width + (int)(threadIdx.x % width), row = (int)(threadIdx.x / width), rows = 256 / width;
+    if (b >= a.batch) return;
     const int lo = a.seq_indptr[b], hi = a.seq_indptr[b + 1];
-    if (!(lo >= 0 && hi >= lo && hi <= a.n_tokens)) {
-        if (lane == 0) a.out[unit] = __builtin_nan("");
-        return;
-    }
-    const int n = (hi - lo + kChunk - 1) / kChunk;
+    const bool ok = lo >= 0 && hi >= lo && hi <= a.n_tokens;
+    const int n = ok ? (hi - lo + a.chunk - 1) / a.chunk : 0;
     double sum = 0.0;
-    for (int k = lane; k < n; k += 64) sum += a.partial[(int64_t)(first_slot(lo, b) + k) * a.n_heads + head];
+    if (head < a.n_heads) {
+        const double *from = a.partial + (int64_t)(ok ? first_slot(lo, b, a.chunk) : 0) * a.n_heads + head;
+        for (int k = row; k < n; k += 8 * rows) {
+            double x[8];
 #pragma unroll
-    for (int k = 32; k > 0; k >>= 1) sum += __shfl_xor(sum, k);
-    if (lane == 0) a.out[unit] = hi > lo ? sum / ((double)(hi - lo) * kHeadDim) : 0.0;
+            for (int j = 0; j < 8; ++j) x[j] = k + j * rows < n ? from[(int64_t)(k + j * rows) * a.n_heads] : 0.0;
+            sum += ((x[0] + x[1]) + (x[2] + x[3])) + ((x[4] + x[5]) + (x[6] + x[7]));
+        }
+    }
+    sums[threadIdx.x] = sum;
+    __syncthreads();
+    for (int k = 128; k >= width; k >>= 1) {
+        if ((int)threadIdx.x < k) sums[threadIdx.x] += sums[threadIdx.x + k];
+        __syncthreads();
+    }
+    if ((int)threadIdx.x < width && head < a.n_heads)
+        a.out[(int64_t)b * a.n_heads + head] = !ok ? __builtin_nan("") : hi > lo ? sums[threadIdx.x] / ((double)(hi - lo) * kHeadDim) : 0.0;
 }
 
 constexpr int64_t kMaxX = 1 << 22;   // a grid has less than 2^32 threads in a dimension
@@ -237,20 +331,31 @@ int tkv_launch_quantize_rows(const tkv_desc *desc, const void *K, int64_t k_stri
     a.tag_bits = tag_bits; a.blocks = blocks; a.status = status;
     a.n_tokens = n_tokens; a.n_heads = desc->n_kv_heads; a.n_blocks = n_blocks;
     a.channel_keys = desc->int2_key_axis == TKV_KEYS_PER_CHANNEL;
-    a.row_groups = (uint32_t)(((int64_t)n_tokens * a.n_heads + kRowsWg - 1) / kRowsWg);
-    const int64_t groups = 2 * (int64_t)a.row_groups + ((int64_t)n_blocks * a.n_heads + 3) / 4;
-    hipLaunchKernelGGL(tkv_rows_kernel, grid(groups), dim3(256), 0, (hipStream_t)stream, a);
+    // Two rows of K and of V a thread keep more on the way; beyond what the Infinity Cache holds, one row, read past the caches.  us, 8 heads, rows not
+    // read for two calls or more, one / two / one past the caches: 4000 tokens 7.2 / 6.7 / 8.0, 32 000 42.4 / 39.8 / 44.0, 64 000 86.0 / 90.5 / 83.9, 128 000 170 / 181 / 163;
+    // per-channel keys 8000 12.9 / 12.8 / 14.3, 64 000 98.0 / 93.9 / 97.0: two.
+    const bool far = n_blocks == 0 && (int64_t)n_tokens * a.n_heads > (int64_t)192 << 11;   // 512 bytes a token of a head
+    const int per = far ? 1 : 2;
+    a.block_groups = (uint32_t)(((int64_t)n_blocks * a.n_heads + 3) / 4);
+    const int64_t groups = (int64_t)a.block_groups + ((int64_t)n_tokens * a.n_heads + 16 * per - 1) / (16 * per);
+    if (far) hipLaunchKernelGGL((tkv_rows_kernel<1, true>), grid(groups), dim3(256), 0, (hipStream_t)stream, a);
+    else hipLaunchKernelGGL((tkv_rows_kernel<2, false>), grid(groups), dim3(256), 0, (hipStream_t)stream, a);
     return hipGetLastError() == hipSuccess ? TKV_OK : TKV_ERR_HIP;
 }
 
 int tkv_launch_distortion(const void *a_rows, const void *b_rows, int32_t type, const int32_t *seq_indptr, int32_t batch, int32_t n_tokens, int32_t n_heads,
                           double *out, void *workspace, void *stream)
 {
-    DistortionArgs a = {a_rows, b_rows, seq_indptr, out, (double *)workspace, batch, n_tokens, n_heads};
-    const int64_t slots = n_tokens / kChunk + (int64_t)batch;
-    auto *kernel = type == TKV_BF16 ? tkv_distortion_kernel<TKV_BF16> : type == TKV_FP16 ? tkv_distortion_kernel<TKV_FP16> : tkv_distortion_kernel<TKV_FP32>;
+    DistortionArgs a = {a_rows, b_rows, seq_indptr, out, (double *)workspace, batch, n_tokens, n_heads, tkv_distortion_chunk(n_tokens, n_heads)};
+    const int64_t slots = n_tokens / a.chunk + (int64_t)batch;
+    const bool far = (int64_t)n_tokens * n_heads * kHeadDim * (type == TKV_FP32 ? 8 : 4) > (int64_t)256 << 20;
+    auto *kernel = type == TKV_BF16   ? (far ? tkv_distortion_kernel<TKV_BF16, true> : tkv_distortion_kernel<TKV_BF16, false>)
+                   : type == TKV_FP16 ? (far ? tkv_distortion_kernel<TKV_FP16, true> : tkv_distortion_kernel<TKV_FP16, false>)
+                                      : (far ? tkv_distortion_kernel<TKV_FP32, true> : tkv_distortion_kernel<TKV_FP32, false>);
     hipLaunchKernelGGL(kernel, grid(slots), dim3(256), 0, (hipStream_t)stream, a);
     if (hipGetLastError() != hipSuccess) return TKV_ERR_HIP;
-    hipLaunchKernelGGL(tkv_distortion_join_kernel, grid(((int64_t)batch * n_heads + 3) / 4), dim3(256), 0, (hipStream_t)stream, a);
+    int32_t width = 1;
+    while (width < n_heads && width < 16) width *= 2;
+    hipLaunchKernelGGL(tkv_distortion_join_kernel, grid((int64_t)batch * ((n_heads + width - 1) / width)), dim3(256), 0, (hipStream_t)stream, a, width);
     return hipGetLastError() == hipSuccess ? TKV_OK : TKV_ERR_HIP;
 }

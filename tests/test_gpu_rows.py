@@ -182,3 +182,19 @@ def test_on_another_stream_and_captured():
         graph.replay()
         torch.cuda.synchronize()
         assert all(np.array_equal(o.view(torch.int16).cpu().numpy().view(np.uint16), r) for o, r in zip(out, ref))
+
+
+def test_every_scale_that_bf16_numbers_give():
+    """Groups from zero to every positive bf16 number that fp16 holds: all quotients by 3 and 15 and all reciprocals that occur."""
+    most = np.arange(1, 0x4780, dtype=np.uint16)       # up to 65280
+    most = np.concatenate([most, most[:-most.size % 4 or None][:(-most.size) % 4]])
+    rng = np.random.default_rng(5)
+    part = rng.random((most.size, 32))
+    part[:, 0], part[:, 1], part[:, 2:8] = 0.0, 1.0, np.arange(1, 7) / 6.0      # the middles between codes of 2 bits among them
+    x = torch.from_numpy(orc.bf16_to_f32(most).astype(np.float64)[:, None] * part).to(torch.float32).to(torch.bfloat16)
+    x[:, 1] = torch.from_numpy(most.view(np.int16)).view(torch.bfloat16)
+    K = x.view(torch.int16).numpy().view(np.uint16).reshape(-1, 1, 128)
+    for b in (2, 4):
+        bits = np.full(K.shape[0], b, np.uint8)
+        for got, ref in zip(call(K, K, bits, None, False), want(K, K, bits, np.zeros((0, 32)), False)):
+            assert np.array_equal(got, ref)
