@@ -50,7 +50,9 @@ __device__ __forceinline__ Grid grid_of(float mn, float mx, bool wide)
     // one unit off at most) and one step of Newton, whose residual the fused multiply-add gives exactly.  (Where a quotient is too small for
     // that it rounds to an fp16 zero either way.)  The plain divisions are ten instructions each.
     const float r = __fsub_rn(mx, mn), y = wide ? 1.0f / 15.0f : 1.0f / 3.0f, q = __fmul_rn(r, y);
-    const _Float16 sh = (_Float16)__builtin_fmaf(__builtin_fmaf(-q, g.levels, r), y, q), zh = (_Float16)mn;
+    float quotient = __builtin_fmaf(__builtin_fmaf(-q, g.levels, r), y, q);
+    asm("" : "+v"(quotient));   // rounded to 32 bits before it is rounded to 16: the compiler would do both at once, and miss ties
+    const _Float16 sh = (_Float16)quotient, zh = (_Float16)mn;
     const float s = (float)sh, i = __builtin_amdgcn_rcpf(s);
     g.zero = (float)zh;
     g.inv = s == 0.0f ? 0.0f : __builtin_fmaf(__builtin_fmaf(-s, i, 1.0f), i, i);
