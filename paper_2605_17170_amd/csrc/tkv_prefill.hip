@@ -211,26 +211,42 @@ __device__ __forceinline__ void attend(Rows &w, const Tiles &t, const uint16_t *
     // key r of the lane's piece in load j is 4 (WAVES j + wave) + lane / 16
     const uint32_t first_row = (uint32_t)(4 * wave + (lane >> 4)), piece = (uint32_t)(lane & 15);
     const uint32_t v_offset = first_row * v_bytes + (piece ^ (uint32_t)(lane >> 4) << 2) * 16;
-    auto buffer_at = [&](const uint16_t *of, uint32_t bytes, int i) {
-        const int left = n_keys - i * kKeys, rows = left < kKeys ? left : kKeys;
-        return buffer_of(reinterpret_cast<const uint8_t *>(of) + (int64_t)i * kKeys * bytes, (uint32_t)rows * bytes);
+    // Buffers of the next tile to fetch; keys behind the last one read as zeros.
+    struct Next {
+        const uint8_t *at;
+        int left;
+        uint32_t bytes, to;   // of a row; where in LDS
+        __device__ __forceinline__ u32x4 take(int step)
+        {
+            const u32x4 buffer = buffer_of(at, (uint32_t)(left < step ? left : step) * bytes);
+            at += (uint64_t)step * bytes;
+            left -= step;
+            return buffer;
+        }
     };
-    auto fetch_k = [&](int i) {
-        const u32x4 buffer = buffer_at(k, k_bytes, i);
-        const uint32_t to = __builtin_amdgcn_readfirstlane(t.lds + (uint32_t)((i - begin) & 1) * kTile + wave * 4 * kRow);
+    const uint32_t own = __builtin_amdgcn_readfirstlane(t.lds + wave * 4 * kRow);
+    Next next_k = {reinterpret_cast<const uint8_t *>(k) + (int64_t)begin * kKeys * k_bytes, n_keys - begin * kKeys, k_bytes, own};
+    Next next_v = {reinterpret_cast<const uint8_t *>(v) + (int64_t)begin * kKeys * v_bytes, n_keys - begin * kKeys, v_bytes, own + 2 * kTile};
+    auto fetch_k = [&] {
+        const u32x4 buffer = next_k.take(kKeys);
 #pragma unroll
         for (int j = 0; j < kLoads; ++j) {
             // (with four wavefronts or more the piece is the same in every load)
             const uint32_t r16 = (WAVES >= 4 ? first_row : first_row + 4 * WAVES * j) & 15;
-            load_lds(to + j * WAVES * 4 * kRow, buffer, first_row * k_bytes + (piece ^ r16) * 16, __builtin_amdgcn_readfirstlane((uint32_t)(j * WAVES * 4) * k_bytes));
+            load_lds(next_k.to + j * WAVES * 4 * kRow, buffer, first_row * k_bytes + (piece ^ r16) * 16, (uint32_t)(j * WAVES * 4) * k_bytes);
         }
+        next_k.to = 2 * own + kTile - next_k.to;   // the other one of two places
     };
-    auto fetch_v = [&](int i) {
-        const u32x4 buffer = buffer_at(v, v_bytes, i);
-        const uint32_t to = __builtin_amdgcn_readfirstlane(t.lds + (uint32_t)(2 + ((i - begin) & 1)) * kTile + wave * 4 * kRow);
+    auto fetch_v = [&] {
+        const u32x4 buffer = next_v.take(kKeys);
 #pragma unroll
-        for (int j = 0; j < kLoads; ++j) load_lds(to + j * WAVES * 4 * kRow, buffer, v_offset, __builtin_amdgcn_readfirstlane((uint32_t)(j * WAVES * 4) * v_bytes));
+        for (int j = 0; j < kLoads; ++j) load_lds(next_v.to + j * WAVES * 4 * kRow, buffer, v_offset, (uint32_t)(j * WAVES * 4) * v_bytes);
+        next_v.to = 2 * (own + 2 * kTile) + kTile - next_v.to;
     };
+    constexpr std::integral_constant<int, 0> c0{};
+    constexpr std::integral_constant<int, 2> c2{};
+    constexpr std::integral_constant<int, 4> c4{};
+    constexpr std::integral_constant<int, 8> c8{};
     auto hide = [&](f32x16 (&s)[KB], int i) {
         const int sees = limit - i * kKeys - 4 * half;
 #pragma unroll
@@ -258,9 +274,9 @@ __device__ __forceinline__ void attend(Rows &w, const Tiles &t, const uint16_t *
                 for (int r = 0; r < 16; ++r) w.o[d][r] *= by;
         }
     };
-    auto logits = [&](f32x16 (&s)[KB], uint32_t buffer) {
+    auto logits = [&](f32x16 (&s)[KB], uint32_t buffer, auto from, auto to) {
 #pragma unroll
-        for (int j = 0; j < 8; ++j)
+        for (int j = from; j < to; ++j)
 #pragma unroll
             for (int b = 0; b < KB; ++b) s[b] = mfma<BF16>(k_operand(t.k_at[j] + buffer, b), w.q[j], j ? s[b] : f32x16{});
     };
@@ -304,26 +320,29 @@ __device__ __forceinline__ void attend(Rows &w, const Tiles &t, const uint16_t *
     // the tiles that all rows of the wavefront see, then those that need a mask
     const int seen = (least + 1) / kKeys, plain = seen < begin ? begin : seen < end ? seen : end;
     // the first keys and the queries at once; what the first logits do not need waits until these are there
-    fetch_k(begin);
+    fetch_k();
     load_q<BF16>(w, q, live, a);
-    fetch_v(begin);
+    fetch_v();
     if (begin + 1 < end) {
-        fetch_k(begin + 1);
+        fetch_k();
         asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" :: "n"(2 * kLoads) : "memory");
     } else
         asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" :: "n"(kLoads) : "memory");
     f32x16 s[KB];
-    logits(s, 0);
+    logits(s, 0, c0, c8);
     if (begin >= plain) hide(s, begin);
     follow(top_of(s));
     int i = begin;
     auto step = [&](auto odd) {
         wait_barrier();   // K of tile i + 1 and V of tile i have arrived, and nobody reads the tiles before them
-        if (i + 2 < end) fetch_k(i + 2);
-        fetch_v(i + 1);
         f32x16 next[KB];
         uint32_t p[8 * KB];
-        logits(next, odd ? 0 : kTile);
+        // (the scalar work of the fetches beside the first products)
+        logits(next, odd ? 0 : kTile, c0, c2);
+        if (i + 2 < end) fetch_k();
+        logits(next, odd ? 0 : kTile, c2, c4);
+        fetch_v();
+        logits(next, odd ? 0 : kTile, c4, c8);
         weights(p, s);
         values(p, (odd ? 3 : 2) * kTile, std::false_type{});
         const float top = top_of(next);
@@ -340,8 +359,8 @@ __device__ __forceinline__ void attend(Rows &w, const Tiles &t, const uint16_t *
     bool left_out = false;
     for (; i < end; ++i) {
         wait_barrier();
-        if (i + 2 < end) fetch_k(i + 2);
-        if (i + 1 < end) fetch_v(i + 1);
+        if (i + 2 < end) fetch_k();
+        if (i + 1 < end) fetch_v();
         if (i * kKeys > most) continue;   // no row of this wavefront sees the tile
         const uint32_t odd = (uint32_t)((i - begin) & 1) * kTile;
         uint32_t p[8 * KB];
@@ -352,7 +371,7 @@ __device__ __forceinline__ void attend(Rows &w, const Tiles &t, const uint16_t *
             left_out = true;
         }
         if (i + 1 < end) {
-            logits(s, kTile - odd);
+            logits(s, kTile - odd, c0, c8);
             hide(s, i + 1);
             follow(top_of(s));
         }
