@@ -707,10 +707,11 @@ enum { TKV_BF16 = 0, TKV_FP16 = 1, TKV_FP32 = 2 };
  *   seq_indptr       host i32[batch+1], from 0: the sequences' new tokens
  *   prefix_indptr    host i32[batch+1], from 0, or NULL: their prefix rows
  *   target_cus       compute units to fill (>= 1)
- *   items_out        host i32[11*capacity]: {first new token, new tokens, first
+ *   items_out        host i32[16*capacity]: {first new token, new tokens, first
  *                    prefix row, prefix rows, first row, first key tile, end,
- *                    partial slot or -1, part, parts, and in the k-th item the
- *                    number of the first part of the k-th tile that is cut}
+ *                    partial slot or -1, part, parts; and in the k-th item, of
+ *                    the k-th tile that is cut, first new token, new tokens,
+ *                    first row, first slot, parts; 0}
  *   tile_rows_out    host i32: 32, 128 or 256
  *   n_slots_out      host i32: partial slots, 0 if no range is cut
  *   n_cut_out        host i32: tiles whose ranges are cut

@@ -32,7 +32,7 @@ struct Kind {
     double alone, step;             // a step (a tile of keys) of a workgroup by itself; steps of a full compute unit, one behind the other
 };
 constexpr Kind kKinds[3] = {{32, 32, 4, 5.0, 1.2, 0.72, 0.192}, {128, 64, 2, 6.0, 2.5, 1.2, 0.96}, {256, 64, 1, 6.5, 5.0, 1.83, 1.83}};
-constexpr double kMergeUs = 3.0, kBytesPerUs = 4.6e6;
+constexpr double kMergeUs = 3.0, kBytesPerUs = 5.1e6;
 bool kind_of(int32_t rows)
 {
     for (const Kind &k : kKinds)
@@ -143,7 +143,14 @@ int32_t tkv_plan_prefill(const tkv_desc *desc, int32_t batch, int32_t n_q_heads,
         if (best && best->resident == 2 && n_slots == 0 && tiles.size() > units) std::reverse(tiles.begin(), tiles.begin() + (int64_t)units);
         int32_t slot = 0, cut = 0, number = 0;
         for (const Tile &t : tiles) {
-            if (t.parts > 1) items_out[kPrefillItemWords * (int64_t)cut++ + 10] = number;
+            if (t.parts > 1) {
+                int32_t *of = items_out + kPrefillItemWords * (int64_t)cut++ + 10;
+                of[0] = seq_indptr[t.seq];
+                of[1] = seq_indptr[t.seq + 1] - seq_indptr[t.seq];
+                of[2] = t.row;
+                of[3] = slot;
+                of[4] = t.parts;
+            }
             for (int32_t k = 0; k < t.parts; ++k, ++number) {
                 const int32_t b = t.seq;
                 int32_t *it = items_out + kPrefillItemWords * (int64_t)number;
@@ -159,7 +166,10 @@ int32_t tkv_plan_prefill(const tkv_desc *desc, int32_t batch, int32_t n_q_heads,
                 it[9] = t.parts;
             }
         }
-        for (int32_t k = cut; k < number; ++k) items_out[kPrefillItemWords * (int64_t)k + 10] = -1;
+        for (int32_t k = 0; k < number; ++k) {
+            int32_t *of = items_out + kPrefillItemWords * (int64_t)k;
+            for (int32_t j = k < cut ? 15 : 10; j < 16; ++j) of[j] = 0;
+        }
         *tile_rows_out = best ? best->rows : kKinds[0].rows;
         *n_slots_out = slot;
         *n_cut_out = cut;

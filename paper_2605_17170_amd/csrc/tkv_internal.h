@@ -44,7 +44,7 @@ int tkv_launch_table_append(const tkv_desc *desc, const tkv_table *table, const 
                             const uint8_t *tag_bits, int32_t n_tokens, int32_t *token_indptr, int32_t *positions, int32_t *slot_ids,
                             int32_t *work_pages, int32_t *work_src, int32_t max_work, int32_t *n_work, void *workspace, int32_t *status, void *stream);
 
-constexpr int kPrefillItemWords = 11;    // of an item of its plan
+constexpr int kPrefillItemWords = 16;    // of an item of the plan of tkv_prefill_attention
 // Tokens of a partial sum of tkv_head_distortion: a workgroup takes sixteen rows at a time.  701 tokens of 16 heads, 44 workgroups of 16 tokens
 // 7.2 us, 176 of 4 4.3; from 8192 tokens on there are enough of them.
 inline int tkv_distortion_chunk(int32_t n_tokens, int32_t n_heads) { return n_tokens >= 8192 || n_heads < 4 ? 16 : 4; }

@@ -83,12 +83,41 @@ __device__ __forceinline__ float both_sum(float x)
     return __uint_as_float(s[0]) + __uint_as_float(s[1]);
 }
 
-// Sixteen bytes a lane from global memory to LDS (lane l: `lds` + 16 l), zeros from beyond the buffer.  Written out, with the waits
-// beside it: the compiler waits for every such load before any read of LDS.
-__device__ __forceinline__ void load_lds(uint32_t lds, u32x4 buffer, uint32_t offset, uint32_t base)
+// LOADS times sixteen bytes a lane from global memory to LDS, zeros from beyond the buffer: load j takes offset[j % 4] (all the same, unless MIXED) + j
+// `step` bytes to `lds` + j `stride` + 16 times the lane.  Written out, with the waits beside it: the compiler waits for every such load
+// before any read of LDS.  In one block: scalars that a vector instruction wrote, as reloads of spilled ones do, need five wait states before the
+// first load; M0 one.
+//
+// ONCE: non-temporal, where no other workgroup has a use for the lines.  16 single tokens behind 1500 to 5000 cached ones 41.6 -> 38.0 us, 64 of them
+// 96.8 -> 86.2; but four prompts of 2000 tokens 290 -> 317 (2048 tokens behind 30000 1888 -> 1830), 1000 tokens by workgroups of 32 rows 36.8 -> 40.4.
+#define TKV_LOAD_FIRST(NT) "s_mov_b32 m0, %1\n\ts_mov_b32 %0, 0\n\ts_nop 2\n\tbuffer_load_dwordx4 %6, %2, %0 offen" NT " lds\n\t"
+#define TKV_LOAD_NEXT(NT, V) "s_add_u32 m0, m0, %4\n\ts_add_u32 %0, %0, %3\n\tbuffer_load_dwordx4 " V ", %2, %0 offen" NT " lds\n\t"
+#define TKV_LOADS(TEXT) \
+    asm volatile(TEXT : "=&s"(at) : "s"(lds), "s"(buffer), "s"(step), "n"(STRIDE), "n"(0), "v"(offset[0]), "v"(offset[1]), "v"(offset[2]), "v"(offset[3]) : "memory", "scc")
+template <int LOADS, int STRIDE, bool MIXED, bool ONCE> __device__ __forceinline__ void load_lds(uint32_t lds, u32x4 buffer, const uint32_t (&offset)[4], uint32_t step)
 {
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, %3 offen lds" :: "s"(lds), "v"(offset), "s"(buffer), "s"(base) : "memory");
+    static_assert(LOADS == 2 || LOADS == 4 || LOADS == 8);
+    uint32_t at;
+    if constexpr (LOADS == 2 && ONCE) TKV_LOADS(TKV_LOAD_FIRST(" nt") TKV_LOAD_NEXT(" nt", "%6"));
+    else if constexpr (LOADS == 2) TKV_LOADS(TKV_LOAD_FIRST("") TKV_LOAD_NEXT("", "%6"));
+    else if constexpr (LOADS == 4 && ONCE) TKV_LOADS(TKV_LOAD_FIRST(" nt") TKV_LOAD_NEXT(" nt", "%6") TKV_LOAD_NEXT(" nt", "%6") TKV_LOAD_NEXT(" nt", "%6"));
+    else if constexpr (LOADS == 4) TKV_LOADS(TKV_LOAD_FIRST("") TKV_LOAD_NEXT("", "%6") TKV_LOAD_NEXT("", "%6") TKV_LOAD_NEXT("", "%6"));
+    else if constexpr (MIXED && ONCE)
+        TKV_LOADS(TKV_LOAD_FIRST(" nt") TKV_LOAD_NEXT(" nt", "%7") TKV_LOAD_NEXT(" nt", "%8") TKV_LOAD_NEXT(" nt", "%9") TKV_LOAD_NEXT(" nt", "%6") TKV_LOAD_NEXT(" nt", "%7")
+                      TKV_LOAD_NEXT(" nt", "%8") TKV_LOAD_NEXT(" nt", "%9"));
+    else if constexpr (MIXED)
+        TKV_LOADS(TKV_LOAD_FIRST("") TKV_LOAD_NEXT("", "%7") TKV_LOAD_NEXT("", "%8") TKV_LOAD_NEXT("", "%9") TKV_LOAD_NEXT("", "%6") TKV_LOAD_NEXT("", "%7")
+                      TKV_LOAD_NEXT("", "%8") TKV_LOAD_NEXT("", "%9"));
+    else if constexpr (ONCE)
+        TKV_LOADS(TKV_LOAD_FIRST(" nt") TKV_LOAD_NEXT(" nt", "%6") TKV_LOAD_NEXT(" nt", "%6") TKV_LOAD_NEXT(" nt", "%6") TKV_LOAD_NEXT(" nt", "%6") TKV_LOAD_NEXT(" nt", "%6")
+                      TKV_LOAD_NEXT(" nt", "%6") TKV_LOAD_NEXT(" nt", "%6"));
+    else
+        TKV_LOADS(TKV_LOAD_FIRST("") TKV_LOAD_NEXT("", "%6") TKV_LOAD_NEXT("", "%6") TKV_LOAD_NEXT("", "%6") TKV_LOAD_NEXT("", "%6") TKV_LOAD_NEXT("", "%6")
+                      TKV_LOAD_NEXT("", "%6") TKV_LOAD_NEXT("", "%6"));
 }
+#undef TKV_LOADS
+#undef TKV_LOAD_NEXT
+#undef TKV_LOAD_FIRST
 __device__ __forceinline__ void wait_barrier() { asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
 
 __device__ __forceinline__ u32x4 buffer_of(const void *p, uint32_t bytes)
@@ -150,7 +179,10 @@ template <bool BF16> __device__ __forceinline__ void load_q(Rows &w, const uint1
             const auto o = __builtin_amdgcn_permlane32_swap(big, big, false, false);
             big = o[0] > o[1] ? o[0] : o[1];
             int e = 14 - ((int)(big >> 7) - 127);                   // the largest becomes 2^14 .. 2^15
+            const int most = (int)(__float_as_uint(a.c) >> 23) - 27;   // with which the factor of the logits stays above 2^-101
             e = e > 120 ? 120 : e;
+            e = e > most ? most : e;
+            e = e < -113 ? -113 : e;
             const float by = __uint_as_float((uint32_t)(e + 127) << 23);
             w.c = a.c * __uint_as_float((uint32_t)(127 - e) << 23);
 #pragma unroll
@@ -201,7 +233,7 @@ __device__ __forceinline__ u32x4 v_operand(uint32_t at, int s)
 // WAVES wavefronts share a tile of 32 KB keys.
 template <bool BF16, int WAVES, int KB>
 __device__ __forceinline__ void attend(Rows &w, const Tiles &t, const uint16_t *q, bool live, const PrefillArgs &a, const uint16_t *k, int64_t k_stride, const uint16_t *v,
-                                       int64_t v_stride, int begin, int end, int n_keys, int limit, int least, int most)
+                                       int64_t v_stride, int begin, int end, int n_keys, int limit, int least, int most, bool once)
 {
     if (begin >= end) return;
     constexpr int kKeys = 32 * KB, kTile = kKeys * kRow;
@@ -210,7 +242,6 @@ __device__ __forceinline__ void attend(Rows &w, const Tiles &t, const uint16_t *
     const uint32_t k_bytes = 2 * (uint32_t)k_stride, v_bytes = 2 * (uint32_t)v_stride;
     // key r of the lane's piece in load j is 4 (WAVES j + wave) + lane / 16
     const uint32_t first_row = (uint32_t)(4 * wave + (lane >> 4)), piece = (uint32_t)(lane & 15);
-    const uint32_t v_offset = first_row * v_bytes + (piece ^ (uint32_t)(lane >> 4) << 2) * 16;
     // Buffers of the next tile to fetch; keys behind the last one read as zeros.
     struct Next {
         const uint8_t *at;
@@ -227,20 +258,25 @@ __device__ __forceinline__ void attend(Rows &w, const Tiles &t, const uint16_t *
     const uint32_t own = __builtin_amdgcn_readfirstlane(t.lds + wave * 4 * kRow);
     Next next_k = {reinterpret_cast<const uint8_t *>(k) + (int64_t)begin * kKeys * k_bytes, n_keys - begin * kKeys, k_bytes, own};
     Next next_v = {reinterpret_cast<const uint8_t *>(v) + (int64_t)begin * kKeys * v_bytes, n_keys - begin * kKeys, v_bytes, own + 2 * kTile};
-    auto fetch_k = [&] {
-        const u32x4 buffer = next_k.take(kKeys);
+    auto fetch = [&](Next &next, const uint32_t (&offset)[4], auto mixed) {
+        const u32x4 buffer = next.take(kKeys);
+        const uint32_t step = (uint32_t)(WAVES * 4) * next.bytes;
+        if (WAVES == 1 && once) load_lds<kLoads, WAVES * 4 * kRow, mixed, true>(next.to, buffer, offset, step);
+        else load_lds<kLoads, WAVES * 4 * kRow, mixed, false>(next.to, buffer, offset, step);
+    };
+    // (with four wavefronts or more a lane's piece of K is the same in every load)
+    uint32_t k_offset[4], v_offset[4];
 #pragma unroll
-        for (int j = 0; j < kLoads; ++j) {
-            // (with four wavefronts or more the piece is the same in every load)
-            const uint32_t r16 = (WAVES >= 4 ? first_row : first_row + 4 * WAVES * j) & 15;
-            load_lds(next_k.to + j * WAVES * 4 * kRow, buffer, first_row * k_bytes + (piece ^ r16) * 16, (uint32_t)(j * WAVES * 4) * k_bytes);
-        }
+    for (int j = 0; j < 4; ++j) {
+        k_offset[j] = first_row * k_bytes + (piece ^ ((WAVES >= 4 ? first_row : first_row + 4 * WAVES * j) & 15)) * 16;
+        v_offset[j] = first_row * v_bytes + (piece ^ (uint32_t)(lane >> 4) << 2) * 16;
+    }
+    auto fetch_k = [&] {
+        fetch(next_k, k_offset, std::bool_constant<(WAVES < 4)>{});
         next_k.to = 2 * own + kTile - next_k.to;   // the other one of two places
     };
     auto fetch_v = [&] {
-        const u32x4 buffer = next_v.take(kKeys);
-#pragma unroll
-        for (int j = 0; j < kLoads; ++j) load_lds(next_v.to + j * WAVES * 4 * kRow, buffer, v_offset, (uint32_t)(j * WAVES * 4) * v_bytes);
+        fetch(next_v, v_offset, std::false_type{});
         next_v.to = 2 * (own + 2 * kTile) + kTile - next_v.to;
     };
     constexpr std::integral_constant<int, 0> c0{};
@@ -437,18 +473,19 @@ __global__ __launch_bounds__(64 * WAVES) __attribute__((amdgpu_waves_per_eu(2, 2
     for (int d = 0; d < 4; ++d) w.o[d] = f32x16{};
     w.m = kNone;
     w.sum = 0.0f;
+    const bool once = n_rows <= kTileRows;   // one workgroup of a kv head reads all keys
     const uint16_t *q = a.q + (int64_t)(it.token0 + token) * a.q_stride + (int64_t)head * kHeadDim;
     if (begin < tiles0) {
         const int see = idle ? -1 : it.n_prefix - 1;
         attend<false, WAVES, KB>(w, t, q, live, a, a.k[0] + (int64_t)it.prefix0 * a.k_stride[0] + (int64_t)kv_head * kHeadDim, a.k_stride[0],
                                  a.v[0] + (int64_t)it.prefix0 * a.v_stride[0] + (int64_t)kv_head * kHeadDim, a.v_stride[0], begin, end < tiles0 ? end : tiles0, it.n_prefix,
-                                 it.n_prefix - 1, see, see);
+                                 it.n_prefix - 1, see, see, once);
     }
     if (end > tiles0) {
         const int least = idle ? -1 : __builtin_amdgcn_readlane(token, 0), most = idle ? -1 : __builtin_amdgcn_readlane(token, 31);
         attend<BF16, WAVES, KB>(w, t, q, live, a, a.k[1] + (int64_t)it.token0 * a.k_stride[1] + (int64_t)kv_head * kHeadDim, a.k_stride[1],
                                 a.v[1] + (int64_t)it.token0 * a.v_stride[1] + (int64_t)kv_head * kHeadDim, a.v_stride[1], begin > tiles0 ? begin - tiles0 : 0, end - tiles0,
-                                n_see, token, least, most);
+                                n_see, token, least, most, once);
     }
     const float sum = both_sum(w.sum);
     if (it.slot < 0) {
@@ -489,21 +526,28 @@ __global__ __launch_bounds__(256) void tkv_prefill_merge_kernel(PrefillArgs a, i
     const uint32_t of = block / chunks;
     const int kv_head = (int)(of % (uint32_t)a.n_kv_heads), cut = (int)(of / (uint32_t)a.n_kv_heads);
     if (cut >= a.n_cut) return;
-    const int number = a.items[(int64_t)kItem * cut + 10];
-    if (number < 0 || number >= a.n_items) return;
-    const Item it = item_of(a.items, number);
-    if (it.slot < 0 || it.part != 0 || !item_ok(it, a)) return;
+    const int32_t *what = a.items + (int64_t)kItem * cut + 10;
+    const int token0 = what[0], n_new = what[1], row0 = what[2], slot = what[3], n_parts = what[4];
+    if (token0 < 0 || n_new <= 0 || (int64_t)token0 + n_new > a.n_tokens || row0 < 0 || slot < 0 || n_parts < 1 || (int64_t)slot + n_parts > a.n_slots) {
+        if (a.status && threadIdx.x == 0) atomicOr(a.status, TKV_STATUS_BAD_ITEM);
+        return;
+    }
     const int lane = threadIdx.x & 31, in_tile = (int)(block % chunks) * 8 + (int)(threadIdx.x >> 5);
-    const uint32_t row = (uint32_t)it.row0 + in_tile, n_rows = (uint32_t)it.n_new * (uint32_t)a.group;
+    const uint32_t row = (uint32_t)row0 + in_tile, n_rows = (uint32_t)n_new * (uint32_t)a.group;
     if (row >= n_rows) return;
-    const float2 *ml = reinterpret_cast<const float2 *>(a.partial + (int64_t)a.n_slots * a.n_kv_heads * tile_rows * kHeadDim);
-    auto at = [&](int p) { return ((int64_t)(it.slot + p) * a.n_kv_heads + kv_head) * tile_rows + in_tile; };
-    // (m, sum) of up to 32 parts at once, a lane each
+    const int64_t step = (int64_t)a.n_kv_heads * tile_rows, at = ((int64_t)slot * a.n_kv_heads + kv_head) * tile_rows + in_tile;   // from part to part; of the first one
+    const float2 *ml = reinterpret_cast<const float2 *>(a.partial + (int64_t)a.n_slots * step * kHeadDim) + at;
+    const float4 *rows = reinterpret_cast<const float4 *>(a.partial + at * kHeadDim) + lane;
+    auto fetch = [&](float4 (&o)[8], int p) {
+#pragma unroll
+        for (int k = 0; k < 8; ++k) o[k] = p + k < n_parts ? rows[(p + k) * step * (kHeadDim / 4)] : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+    };
+    // (m, sum) of up to 32 parts at once, a lane each, and the first rows beside them
     float m = kNone, sum = 0.0f;
-    float4 x = {0.0f, 0.0f, 0.0f, 0.0f};
-    for (int first = 0; first < it.n_parts; first += 32) {
-        const int n = it.n_parts - first < 32 ? it.n_parts - first : 32;
-        const float2 mine = lane < n ? ml[at(first + lane)] : make_float2(kNone, 0.0f);
+    float4 x = {0.0f, 0.0f, 0.0f, 0.0f}, o[8];
+    for (int first = 0; first < n_parts; first += 32) {
+        const float2 mine = first + lane < n_parts ? ml[(first + lane) * step] : make_float2(kNone, 0.0f);
+        fetch(o, first);
         float top = mine.x;
 #pragma unroll
         for (int k = 16; k > 0; k >>= 1) top = fmaxf(top, __shfl_xor(top, k));
@@ -516,20 +560,18 @@ __global__ __launch_bounds__(256) void tkv_prefill_merge_kernel(PrefillArgs a, i
 #pragma unroll
         for (int k = 16; k > 0; k >>= 1) add += __shfl_xor(add, k);
         sum += add;
-        for (int p = 0; p < n; p += 8) {
-            float4 o[8];
-#pragma unroll
-            for (int k = 0; k < 8; ++k) o[k] = p + k < n ? reinterpret_cast<const float4 *>(a.partial + at(first + p + k) * kHeadDim)[lane] : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+        for (int p = 0; p < 32 && first + p < n_parts; p += 8) {
+            if (p > 0) fetch(o, first + p);
 #pragma unroll
             for (int k = 0; k < 8; ++k) {
-                const float f = __shfl(by, (p + k) & 31, 32);
+                const float f = __shfl(by, p + k, 32);
                 x.x = fmaf(o[k].x, f, x.x); x.y = fmaf(o[k].y, f, x.y); x.z = fmaf(o[k].z, f, x.z); x.w = fmaf(o[k].w, f, x.w);
             }
         }
     }
     const float by = 1.0f / sum;
     const uint32_t token = row / (uint32_t)a.group, head = kv_head * a.group + (row - token * a.group);
-    u32x2 *to = reinterpret_cast<u32x2 *>(a.out + ((int64_t)(it.token0 + (int)token) * (a.n_kv_heads * a.group) + head) * kHeadDim);
+    u32x2 *to = reinterpret_cast<u32x2 *>(a.out + ((int64_t)(token0 + (int)token) * (a.n_kv_heads * a.group) + head) * kHeadDim);
     to[lane] = a.out_bf16 ? u32x2{pack<true>(x.x * by, x.y * by), pack<true>(x.z * by, x.w * by)} : u32x2{pack<false>(x.x * by, x.y * by), pack<false>(x.z * by, x.w * by)};
 }
 

@@ -751,7 +751,7 @@ def tkv_norm_rope(rope: tkv_rope, q, k, v, positions, q_weight, k_weight, eps: f
 
 
 # ---------------------------------------------------------------- P2 (host plan, device)
-PREFILL_ITEM_WORDS = 11
+PREFILL_ITEM_WORDS = 16
 PrefillPlan = collections.namedtuple("PrefillPlan", "items n_slots tile_rows n_cut")
 _TYPES = {"torch.bfloat16": TKV_BF16, "torch.float16": TKV_FP16, "torch.float32": TKV_FP32}
 
@@ -764,7 +764,7 @@ def _type(t, allowed, what):
 
 def tkv_plan_prefill(desc, n_q_heads: int, seq_indptr, prefix_indptr=None, target_cus: int = 256) -> PrefillPlan:
     """Plan for sequences of seq_indptr's new tokens behind prefix_indptr's cached ones (host arrays [batch+1]).
-    PrefillPlan: items i32[n_items, 11], n_slots, tile_rows, n_cut."""
+    PrefillPlan: items i32[n_items, 16], n_slots, tile_rows, n_cut."""
     ip, pip = _np(seq_indptr, np.int32)
     batch = ip.size - 1
     pp = None

@@ -32,16 +32,16 @@ int main()
         }
         const int32_t cap = tkv_plan_prefill_capacity(&d, batch, ip.back(), hk * group, cus);
         CHECK(cap >= 0);
-        std::vector<int32_t> items((size_t)cap * 11);
+        std::vector<int32_t> items((size_t)cap * 16);
         int32_t rows = -1, slots = -1, cut = -1;
         const int32_t n = tkv_plan_prefill(&d, batch, hk * group, ip.data(), round % 2 ? pp.data() : nullptr, cus, items.data(), cap, &rows, &slots, &cut);
         CHECK(n >= 0 && n <= cap && (rows == 32 || rows == 128 || rows == 256) && slots >= 0 && cut >= 0 && 2 * cut <= slots);
         std::vector<char> used((size_t)slots, 0);
         for (int32_t k = 0; k < n; ++k) {
-            const int32_t *it = &items[(size_t)k * 11];
+            const int32_t *it = &items[(size_t)k * 16];
             CHECK(it[5] < it[6] && it[8] >= 0 && it[8] < it[9] && (it[9] == 1) == (it[7] < 0));
             if (it[7] >= 0) CHECK(it[7] < slots && !used[(size_t)it[7]]++);
-            CHECK(k < cut ? it[10] >= 0 && it[10] < n : it[10] == -1);
+            CHECK(k < cut ? it[14] > 1 && it[13] >= 0 && it[13] + it[14] <= slots : it[14] == 0);
         }
         if (n > 0) CHECK(tkv_plan_prefill(&d, batch, hk * group, ip.data(), round % 2 ? pp.data() : nullptr, cus, items.data(), n - 1, &rows, &slots, &cut) == TKV_ERR_CAPACITY);
         // blocks

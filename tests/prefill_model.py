@@ -54,11 +54,11 @@ def plan_of(rows, most, lens, cached, group):
             keys = -(-c // KEYS[rows]) + -(-see // KEYS[rows])
             parts = -(-keys // most)
             if parts > 1:
-                cuts.append(len(items))
+                cuts.append([a, n, row, slot, parts])
             for k in range(parts):
-                items.append([a, n, p, c, row, keys * k // parts, keys * (k + 1) // parts, slot if parts > 1 else -1, k, parts, -1])
+                items.append([a, n, p, c, row, keys * k // parts, keys * (k + 1) // parts, slot if parts > 1 else -1, k, parts] + 6 * [0])
                 slot += parts > 1
         a, p = a + n, p + c
-    for k, number in enumerate(cuts):
-        items[k][10] = number
-    return tkv.PrefillPlan(np.array(items, np.int32).reshape(-1, 11), slot, rows, len(cuts))
+    for k, cut in enumerate(cuts):
+        items[k][10:15] = cut
+    return tkv.PrefillPlan(np.array(items, np.int32).reshape(-1, 16), slot, rows, len(cuts))

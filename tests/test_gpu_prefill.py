@@ -139,7 +139,8 @@ def test_a_sequence_does_not_depend_on_the_batch(rows):
     assert torch.equal(c.out[64:], d.out)
 
 
-@pytest.mark.parametrize("size,sm", [(40.0, SM), (1e-3, SM), (2.0 ** -110, SM * 2.0 ** 110), (2.0 ** 60, SM * 2.0 ** -60), (2.0 ** -122, 2.0 ** 118)])
+@pytest.mark.parametrize("size,sm", [(40.0, SM), (1e-3, SM), (2.0 ** -110, SM * 2.0 ** 110), (2.0 ** 60, SM * 2.0 ** -60), (2.0 ** -122, 2.0 ** 118), (0.0, SM),
+                                     (0.0, 2.0 ** -90), (1.0, 2.0 ** -100), (2.0 ** -120, 2.0 ** -20), (2.0 ** 120, 2.0 ** -126), (2.0 ** 100, 2.0 ** -120)])
 @pytest.mark.parametrize("kv", [BF, FP])
 def test_sizes_of_queries(size, sm, kv):
     c = Case([40], [100], 2, 1, BF, kv, BF, seed=8, sm=sm, size=size)
@@ -273,9 +274,22 @@ def test_items_that_name_what_is_not_there_are_skipped(word, value):
     assert torch.isfinite(c.out[:30].float()).all()
 
 
+@pytest.mark.parametrize("word,value", [(10, -1), (10, 40), (11, 0), (11, 60), (12, -8), (13, -1), (13, 1000), (14, 0), (14, 1000), (14, -3)])
+def test_cut_tiles_that_name_what_is_not_there_are_skipped(word, value):
+    c = Case([30, 20], [700, 3000], 4, 2, seed=19, kind=128, most=9)
+    plan = c.plan._replace(items=c.plan.items.copy())
+    assert plan.n_cut == 2 and plan.items[1, 10] == 30
+    plan.items[1, word] = value
+    c.prefill = tkv.tkv_prefill.make(plan, DEV)
+    c.call()
+    torch.cuda.synchronize()
+    assert int(c.status.item()) == tkv.TKV_STATUS_BAD_ITEM
+    assert torch.isfinite(c.out[:30].float()).all() and (c.out[30:] == 7.0).all()
+
+
 def test_a_plan_without_items_and_a_call_without_tokens():
     c = Case([0, 0], [5, 0], 4, 2, spare=2)
-    assert c.plan.items.shape == (0, 11) and c.plan.n_slots == 0
+    assert c.plan.items.shape == (0, 16) and c.plan.n_slots == 0
     c.call()
     torch.cuda.synchronize()
     assert (c.out == 7.0).all()

@@ -34,8 +34,8 @@ def test_every_row_meets_every_key_that_it_sees_once(lens, cached, hq, hk, targe
             want[(b, r)] = -(-c // keys) + -(-see // keys)
     seen, slots, cuts = {}, [], []
     owner = {(int(starts[b]), int(lens[b])): b for b in range(len(lens)) if lens[b]}
-    for number, it in enumerate(p.items.tolist()):
-        token0, n, prefix0, c, row, begin, end, slot, part, parts, _ = it
+    for it in p.items.tolist():
+        token0, n, prefix0, c, row, begin, end, slot, part, parts = it[:10]
         b = owner[(token0, n)]
         assert c == cached[b] and (c == 0 or prefix0 == pres[b]) and begin < end
         ranges = seen.setdefault((b, row), [])
@@ -44,7 +44,7 @@ def test_every_row_meets_every_key_that_it_sees_once(lens, cached, hq, hk, targe
         if parts > 1:
             slots.append(slot)
             if part == 0:
-                cuts.append(number)
+                cuts.append([token0, n, row, slot, parts])
         else:
             assert slot == -1
     assert seen.keys() == want.keys()
@@ -53,7 +53,7 @@ def test_every_row_meets_every_key_that_it_sees_once(lens, cached, hq, hk, targe
         if len(ranges) > 1:
             assert [r[3] for r in ranges] == list(range(ranges[0][3], ranges[0][3] + len(ranges)))
     assert sorted(slots) == list(range(p.n_slots)) and p.n_cut == len(cuts)
-    assert p.items[:, 10].tolist() == cuts + [-1] * (len(p.items) - len(cuts))
+    assert p.items[:len(cuts), 10:15].tolist() == cuts and not p.items[len(cuts):, 10:15].any() and not p.items[:, 15].any()
     assert len(p.items) <= tkv.lib().tkv_plan_prefill_capacity(C.byref(tkv.tkv_desc.make(hk, 0, 0)), len(lens), sum(lens), hq, target)
     lengths = [r[-1][1] / len(r) for r in ([(x[0], x[1]) for x in v] for v in seen.values())]
     if p.tile_rows == 128 and not p.n_slots:      # the longest ones of a first round last
@@ -70,7 +70,7 @@ def test_longer_batches_never_make_more_workgroups_than_twice_the_places_when_cu
 
 
 def raw_plan(desc, batch, hq, ip, pp, target=4, cap=100):
-    items = np.zeros((max(cap, 1), 11), np.int32)
+    items = np.zeros((max(cap, 1), 16), np.int32)
     out = [C.c_int32(-7) for _ in range(3)]
     keep = [None if a is None else np.ascontiguousarray(a, np.int32) for a in (ip, pp)]
     return tkv.lib().tkv_plan_prefill(C.byref(desc) if desc is not None else None, batch, hq, *(None if a is None else C.c_void_p(a.ctypes.data) for a in keep), target,
