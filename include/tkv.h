@@ -809,10 +809,12 @@ int tkv_quantize_rows(const tkv_desc *desc, const void *K, int64_t k_stride, con
  *   x, y         device [n_tokens, n_heads, 128] of `type` (TKV_BF16, TKV_FP16 or
  *                TKV_FP32), contiguous, 16-byte aligned
  *   seq_indptr   device i32[batch+1], not falling, within [0, n_tokens]; a
- *                sequence of which that does not hold gives NaN
+ *                sequence of which that does not hold gives NaN, and what the
+ *                others then give is not defined
  *   out          device f64 [batch, n_heads]
- *   workspace    device, >= tkv_distortion_workspace_bytes(...), 16-byte aligned
- * Two launches.
+ *   workspace    device, >= tkv_distortion_workspace_bytes(...), 16-byte aligned,
+ *                needs no initialisation; calls that overlap in time need one each
+ * NaN and infinities stay in their sequence and head.  One launch, or two.
  */
 size_t tkv_distortion_workspace_bytes(int32_t batch, int32_t n_tokens, int32_t n_heads);
 int tkv_head_distortion(const void *x, const void *y, int32_t type, const int32_t *seq_indptr, int32_t batch, int32_t n_tokens,

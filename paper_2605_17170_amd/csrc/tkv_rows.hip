@@ -216,12 +216,47 @@ __device__ __forceinline__ int first_slot(int first, int b, int chunk) { return 
 
 __device__ __forceinline__ float f32_of(uint32_t bits, int type) { return type == TKV_BF16 ? __uint_as_float(bits << 16) : (float)__builtin_bit_cast(_Float16, (uint16_t)bits); }
 
-// A workgroup takes a chunk of one sequence's tokens: sixteen (fp32: eight) rows at a time, all heads of a token or several tokens'.
+// Adds to `sum` the squares of a lane's piece of rows t, t + tokens, .. of four, those before `end`.
+template <int TYPE, bool ONCE>
+__device__ __forceinline__ double squares(const uint4 *x, const uint4 *y, int t, int end, int tokens, int64_t step, double sum)
+{
+    uint4 u[4], v[4];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        const int64_t at = (t + k * tokens < end ? t + k * tokens : t) * step;
+        u[k] = ONCE ? load_once(x + at) : x[at];
+        v[k] = ONCE ? load_once(y + at) : y[at];
+    }
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        if (t + k * tokens >= end) break;
+        const uint32_t p[4] = {u[k].x, u[k].y, u[k].z, u[k].w}, q[4] = {v[k].x, v[k].y, v[k].z, v[k].w};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            if constexpr (TYPE == TKV_FP32) {
+                const double d = (double)__uint_as_float(p[i]) - (double)__uint_as_float(q[i]);
+                sum = __builtin_fma(d, d, sum);
+            } else {
+#pragma unroll
+                for (int h = 0; h < 32; h += 16) {
+                    const double d = (double)f32_of(p[i] >> h & 0xffffu, TYPE) - (double)f32_of(q[i] >> h & 0xffffu, TYPE);
+                    sum = __builtin_fma(d, d, sum);
+                }
+            }
+        }
+    }
+    return sum;
+}
+
+// A workgroup takes a chunk of one sequence's tokens and sixteen (fp32: eight) heads, or all heads of several tokens at a time.  Bound by
+// HBM: eight loads of 16 bytes a lane are on the way, 975 MB of bf16 rows in 148 us, 6.6 TB/s (all heads of the tokens by one workgroup, sixteen behind sixteen, 164 us).
 template <int TYPE, bool ONCE>
 __global__ __launch_bounds__(256) void tkv_distortion_kernel(DistortionArgs a)
 {
     __shared__ double sums[16];
-    const uint32_t slot = blockIdx.x + blockIdx.y * gridDim.x;
+    constexpr int kPer = TYPE == TKV_FP32 ? 4 : 8, kLanes = kHeadDim / kPer, kGroups = 256 / kLanes;   // values of a 16-byte piece; lanes of a row; rows at once
+    const int width = a.n_heads < kGroups ? a.n_heads : kGroups, tokens = kGroups / width;             // heads and tokens at once
+    const uint32_t block = blockIdx.x + blockIdx.y * gridDim.x, passes = (uint32_t)((a.n_heads + width - 1) / width), slot = block / passes;
     // the sequence that the slot belongs to: every wavefront looks through all of them
     int begin = 0, end = 0;
     for (int b0 = 0; b0 < a.batch; b0 += 64) {
@@ -238,55 +273,23 @@ __global__ __launch_bounds__(256) void tkv_distortion_kernel(DistortionArgs a)
         }
     }
     if (begin >= end) return;
-    constexpr int kPer = TYPE == TKV_FP32 ? 4 : 8, kLanes = kHeadDim / kPer, kGroups = 256 / kLanes;   // values of a 16-byte piece; lanes of a row; rows at once
-    const int part = threadIdx.x % kLanes, group = threadIdx.x / kLanes;
-    const int width = a.n_heads < kGroups ? a.n_heads : kGroups, tokens = kGroups / width;             // heads and tokens at once
-    const int sub = group / width;
-    for (int head0 = 0; head0 < a.n_heads; head0 += width) {
-        const int head = head0 + group - sub * width;
-        double sum = 0.0;
-        if (sub < tokens && head < a.n_heads) {
-            const int64_t step = (int64_t)a.n_heads * kLanes;
-            const uint4 *x = reinterpret_cast<const uint4 *>(a.a) + ((int64_t)head * kLanes + part), *y = reinterpret_cast<const uint4 *>(a.b) + ((int64_t)head * kLanes + part);
-            for (int t = begin + sub; t < end; t += 4 * tokens) {
-                uint4 u[4], v[4];
-#pragma unroll
-                for (int k = 0; k < 4; ++k) {
-                    const int64_t at = (t + k * tokens < end ? t + k * tokens : t) * step;
-                    u[k] = ONCE ? load_once(x + at) : x[at];
-                    v[k] = ONCE ? load_once(y + at) : y[at];
-                }
-#pragma unroll
-                for (int k = 0; k < 4; ++k) {
-                    if (t + k * tokens >= end) break;
-                    const uint32_t p[4] = {u[k].x, u[k].y, u[k].z, u[k].w}, q[4] = {v[k].x, v[k].y, v[k].z, v[k].w};
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        if constexpr (TYPE == TKV_FP32) {
-                            const double d = (double)__uint_as_float(p[i]) - (double)__uint_as_float(q[i]);
-                            sum = __builtin_fma(d, d, sum);
-                        } else {
-#pragma unroll
-                            for (int h = 0; h < 32; h += 16) {
-                                const double d = (double)f32_of(p[i] >> h & 0xffffu, TYPE) - (double)f32_of(q[i] >> h & 0xffffu, TYPE);
-                                sum = __builtin_fma(d, d, sum);
-                            }
-                        }
-                    }
-                }
-            }
-        }
-#pragma unroll
-        for (int k = kLanes / 2; k > 0; k >>= 1) sum += __shfl_xor(sum, k);
-        if (tokens > 1) {
-            if (part == 0) sums[group] = sum;
-            __syncthreads();
-            for (int k = 1; k < tokens; ++k)
-                if (sub == 0 && part == 0) sum += sums[group + k * width];
-            __syncthreads();
-        }
-        if (sub == 0 && part == 0 && head < a.n_heads) a.partial[(int64_t)slot * a.n_heads + head] = sum;
+    const int part = threadIdx.x % kLanes, group = threadIdx.x / kLanes, sub = group / width;
+    const int head = (int)(block - slot * passes) * width + group - sub * width;
+    double sum = 0.0;
+    if (sub < tokens && head < a.n_heads) {
+        const int64_t step = (int64_t)a.n_heads * kLanes;
+        const uint4 *x = reinterpret_cast<const uint4 *>(a.a) + ((int64_t)head * kLanes + part), *y = reinterpret_cast<const uint4 *>(a.b) + ((int64_t)head * kLanes + part);
+        for (int t = begin + sub; t < end; t += 4 * tokens) sum = squares<TYPE, ONCE>(x, y, t, end, tokens, step, sum);
     }
+#pragma unroll
+    for (int k = kLanes / 2; k > 0; k >>= 1) sum += __shfl_xor(sum, k);
+    if (tokens > 1) {
+        if (part == 0) sums[group] = sum;
+        __syncthreads();
+        for (int k = 1; k < tokens; ++k)
+            if (sub == 0 && part == 0) sum += sums[group + k * width];
+    }
+    if (sub == 0 && part == 0 && head < a.n_heads) a.partial[(int64_t)slot * a.n_heads + head] = sum;
 }
 // Adds up the slots of a sequence: `width` lanes (a power of two) take a head each, 256 / width rows of them every so many slots.
 __global__ __launch_bounds__(256) void tkv_distortion_join_kernel(DistortionArgs a, int32_t width)
@@ -318,7 +321,35 @@ __global__ __launch_bounds__(256) void tkv_distortion_join_kernel(DistortionArgs
         a.out[(int64_t)b * a.n_heads + head] = !ok ? __builtin_nan("") : hi > lo ? sums[threadIdx.x] / ((double)(hi - lo) * kHeadDim) : 0.0;
 }
 
-constexpr int64_t kMaxX = 1 << 22;   // a grid has less than 2^32 threads in a dimension
+// Few tokens: a workgroup takes all of a sequence and head, and there is nothing to join.  One compute unit reads 100 GB/s of rows that lie
+// apart: bf16, 16 heads, one sequence, this / chunks and a join, us: 16 tokens 3.4 / 5.6, 256 4.5 / 6.1, 512 6.5 / 6.4, 701 7.8 / 6.9; 64 heads 3.4 / 9.2, 4.8 / 11.9.
+template <int TYPE>
+__global__ __launch_bounds__(1024) void tkv_distortion_short_kernel(DistortionArgs a)
+{
+    __shared__ double sums[16];
+    const uint32_t block = blockIdx.x + blockIdx.y * gridDim.x;
+    const int b = (int)(block / (uint32_t)a.n_heads), head = (int)(block % (uint32_t)a.n_heads);
+    if (b >= a.batch) return;
+    const int lo = a.seq_indptr[b], hi = a.seq_indptr[b + 1];
+    const bool ok = lo >= 0 && hi >= lo && hi <= a.n_tokens;
+    constexpr int kPer = TYPE == TKV_FP32 ? 4 : 8, kLanes = kHeadDim / kPer, kRows = 1024 / kLanes;
+    const int part = threadIdx.x % kLanes;
+    const int64_t step = (int64_t)a.n_heads * kLanes;
+    const uint4 *x = reinterpret_cast<const uint4 *>(a.a) + ((int64_t)head * kLanes + part), *y = reinterpret_cast<const uint4 *>(a.b) + ((int64_t)head * kLanes + part);
+    double sum = 0.0;
+    if (ok)
+        for (int t = lo + (int)(threadIdx.x / kLanes); t < hi; t += 4 * kRows) sum = squares<TYPE, false>(x, y, t, hi, kRows, step, sum);
+#pragma unroll
+    for (int k = 32; k > 0; k >>= 1) sum += __shfl_xor(sum, k);
+    if ((threadIdx.x & 63) == 0) sums[threadIdx.x >> 6] = sum;
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        for (int k = 1; k < 16; ++k) sum += sums[k];
+        a.out[(int64_t)b * a.n_heads + head] = !ok ? __builtin_nan("") : hi > lo ? sum / ((double)(hi - lo) * kHeadDim) : 0.0;
+    }
+}
+
+constexpr int64_t kMaxX = 1 << 21;   // a grid has less than 2^32 threads in a dimension
 dim3 grid(int64_t blocks) { return dim3((unsigned)(blocks < kMaxX ? blocks : kMaxX), (unsigned)((blocks + kMaxX - 1) / kMaxX)); }
 
 } // namespace
@@ -349,15 +380,25 @@ int tkv_launch_distortion(const void *a_rows, const void *b_rows, int32_t type, 
                           double *out, void *workspace, void *stream)
 {
     DistortionArgs a = {a_rows, b_rows, seq_indptr, out, (double *)workspace, batch, n_tokens, n_heads, tkv_distortion_chunk(n_tokens, n_heads)};
+    if (n_tokens <= 256) {
+        auto *whole = type == TKV_BF16 ? tkv_distortion_short_kernel<TKV_BF16> : type == TKV_FP16 ? tkv_distortion_short_kernel<TKV_FP16> : tkv_distortion_short_kernel<TKV_FP32>;
+        hipLaunchKernelGGL(whole, grid((int64_t)batch * n_heads), dim3(1024), 0, (hipStream_t)stream, a);
+        return hipGetLastError() == hipSuccess ? TKV_OK : TKV_ERR_HIP;
+    }
     const int64_t slots = n_tokens / a.chunk + (int64_t)batch;
+    const int32_t groups = 256 / (type == TKV_FP32 ? 32 : 16);
+    // past the caches what does not fit the Infinity Cache: bf16, 8 heads, rows not read for seven calls, 256 MiB 54.6 us, past them 50.2, 512 MiB 103.2 / 93.7; but of the
+    // rows of the last two calls 128 MiB 25.4 / 25.9, 192 MiB 35.5 / 36.8
     const bool far = (int64_t)n_tokens * n_heads * kHeadDim * (type == TKV_FP32 ? 8 : 4) > (int64_t)256 << 20;
     auto *kernel = type == TKV_BF16   ? (far ? tkv_distortion_kernel<TKV_BF16, true> : tkv_distortion_kernel<TKV_BF16, false>)
                    : type == TKV_FP16 ? (far ? tkv_distortion_kernel<TKV_FP16, true> : tkv_distortion_kernel<TKV_FP16, false>)
                                       : (far ? tkv_distortion_kernel<TKV_FP32, true> : tkv_distortion_kernel<TKV_FP32, false>);
-    hipLaunchKernelGGL(kernel, grid(slots), dim3(256), 0, (hipStream_t)stream, a);
+    hipLaunchKernelGGL(kernel, grid(slots * (n_heads <= groups ? 1 : (n_heads + groups - 1) / groups)), dim3(256), 0, (hipStream_t)stream, a);
     if (hipGetLastError() != hipSuccess) return TKV_ERR_HIP;
     int32_t width = 1;
     while (width < n_heads && width < 16) width *= 2;
+    // few sequences: more workgroups of fewer heads (one sequence of 16 heads, 4096 tokens 14.2 us, so 11.6; 32 768 59.8, 52.9)
+    while (width > 2 && (int64_t)batch * ((n_heads + width - 1) / width) < 64) width /= 2;
     hipLaunchKernelGGL(tkv_distortion_join_kernel, grid((int64_t)batch * ((n_heads + width - 1) / width)), dim3(256), 0, (hipStream_t)stream, a, width);
     return hipGetLastError() == hipSuccess ? TKV_OK : TKV_ERR_HIP;
 }

@@ -69,6 +69,39 @@ def test_offsets_that_cannot_be_give_nan_for_their_sequences(offsets):
         assert torch.isnan(got[b]).all() == (not 0 <= lo <= hi <= 20)
 
 
+@pytest.mark.parametrize("kind", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("lens,heads", [([256], 6), ([257], 6), ([255, 2], 17), ([0, 250, 6], 33), ([300, 0, 1, 0], 9), ([4095, 1], 16), ([100] * 90, 16), ([8191], 8), ([8192], 8), ([20000], 2)])
+def test_around_the_sizes_at_which_the_split_changes(kind, lens, heads):
+    x, y, ip = make(lens, heads, kind, heads, spare=0)
+    got = call(x, y, ip)
+    torch.cuda.synchronize()
+    check(got, x, y, lens)
+    assert torch.equal(got, call(x, y, ip))
+
+
+def test_what_is_not_finite_stays_in_its_sequence_and_head_of_many_tokens():
+    lens = [400, 500, 3]
+    x, y, ip = make(lens, 20, torch.float16, 1, spare=2)
+    clean = call(x, y, ip)
+    x[450, 2, 7], y[901, 17, 0] = float("nan"), float("inf")
+    x[903:] = float("nan")
+    got = call(x, y, ip)
+    torch.cuda.synchronize()
+    assert torch.isnan(got[1, 2]) and got[2, 17] == float("inf")
+    got[1, 2], got[2, 17] = clean[1, 2], clean[2, 17]
+    assert torch.equal(got, clean)
+
+
+@pytest.mark.parametrize("offsets", [[0, 100, 50, 2000], [0, 100, 2001, 2001], [-1, 500, 1000, 2000], [0, 3000, 10, 2000], [2000, 10, 5, 0]])
+def test_offsets_that_cannot_be_of_many_tokens(offsets):
+    x, y, _ = make([2000], 2, torch.float16, 2)
+    got = call(x, y, torch.tensor(offsets, dtype=torch.int32, device=DEV))
+    torch.cuda.synchronize()
+    for b in range(3):
+        lo, hi = offsets[b], offsets[b + 1]
+        assert torch.isnan(got[b]).all() if not 0 <= lo <= hi <= 2000 else True
+
+
 def test_no_tokens_at_all():
     got = call(torch.zeros((0, 3, 128), device=DEV), torch.zeros((0, 3, 128), device=DEV), torch.zeros(3, dtype=torch.int32, device=DEV))
     torch.cuda.synchronize()
