@@ -753,12 +753,16 @@ size_t tkv_prefill_workspace_bytes(const tkv_desc *desc, int32_t n_slots, int32_
  * type, their sum is that of the rounded ones; bf16 queries meet fp16 keys as
  * fp16 numbers with a power of two of their row (what lies 2^-24 below the
  * row's largest, or below 2^-144, rounds to the grid of the subnormals).
- * q . k and sm_scale * q . k (times log2 e, and for bf16 queries over fp16 keys
- * sm_scale times the row's largest |q|) must be finite in 32 bits.  A row of q
- * that holds NaN or infinities gives NaN and leaves the others alone; what
- * stands in keys and values that a token does not see does not reach it.
- * sm_scale > 0.  n_q_heads must be a multiple of n_kv_heads.  One launch on
- * `stream`, a second one if n_slots > 0.
+ * q . k (for bf16 queries over fp16 keys also sm_scale times the row's largest
+ * |q|) must be finite in 32 bits, and sm_scale * q . k * log2 e below 2^26 in
+ * magnitude, where the rounding of a row's reference still leaves its weights
+ * in the range of fp16; a row that goes beyond is NaN or off.  A row of q that
+ * holds NaN or infinities gives NaN and leaves the others alone; what
+ * stands in keys and values that a token does not see does not reach it, an
+ * infinite or NaN value that it sees makes that channel infinite or NaN.
+ * A prefill with other lengths or heads than the call's gives what its items
+ * say, or BAD_ITEM.  sm_scale > 0.  n_q_heads must be a multiple of n_kv_heads.
+ * One launch on `stream`, a second one if n_cut > 0.
  */
 int tkv_prefill_attention(const tkv_desc *desc, int32_t n_q_heads, const void *q, int64_t q_stride, int32_t q_type,
                           const void *K, int64_t k_stride, const void *V, int64_t v_stride, int32_t kv_type, int32_t n_tokens,

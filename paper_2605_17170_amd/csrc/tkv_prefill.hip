@@ -4,10 +4,17 @@
 //   out[i, h] = sum_j p_j v_j / sum_j p_j,   p_j = 2^(c q[i, h] . k_j - m),   c = sm_scale log2 e
 //
 // over the sequence's prefix rows and its new rows 0 .. i.  A workgroup takes a tile of query rows of one kv head -- row r is
-// query head r mod R of token r / R, so that all heads that share a key fill one tile -- and walks over tiles of 64 keys:
+// query head r mod R of token r / R, so that all heads that share a key fill one tile -- and walks over tiles of 32 or 64 keys:
 // S^T = K Q^T and O^T += V^T P^T on v_mfma_f32_32x32x16, a wavefront 32 rows.  Transposed, a lane holds one query row: the running
 // maximum, the sum and the mask's limit are one register each, and the weights leave the first product's accumulators in the
 // order in which the second one takes its operand, if V's rows are read in that order too (ds_read_b64_tr_b16).
+//
+// Workgroups of 32 rows (one wavefront, four of them on a compute unit: loads of many workgroups on the way), 128 (four wavefronts, two
+// workgroups: one takes the matrix cores while the other takes exponentials) and 256 (eight, one workgroup: keys and values are
+// read half as often).  One MI355X, us: 2048 tokens of 64 heads behind 30 000 with 128 rows 1954, with 256 1888, now 1857 (1121 TFLOP/s, MFMAs busy 62 % of the
+// cycles at the 1.4 to 1.7 GHz that power leaves; the library's bf16 product of 8192^3 runs at 1414); 8192 tokens 1000 (1100 TFLOP/s); 16
+// single tokens of 64 heads behind 1500 to 5000 with 128 rows 63, with 32 41, now 38 (171 MB; 5.2 TB/s within the kernel).  In between, where there are
+// few workgroups, a step's chain bounds the call: logits 870 cycles, weights 600, values 900, fetches 350, maximum and reference 300.
 #include <hip/hip_runtime.h>
 
 #include <type_traits>
@@ -31,7 +38,7 @@ typedef short s16x4 __attribute__((ext_vector_type(4)));
 constexpr int kRow = kHeadDim * 2;        // bytes
 constexpr int kItem = kPrefillItemWords;
 constexpr float kNone = -3.4028235e38f;   // reference of a row that has seen no key
-constexpr float kSlack = 8.0f;            // weights grow to 2^8 before the reference follows the maximum
+constexpr float kSlack = 8.0f;            // weights grow to 2^8 before the reference follows the maximum (8192 tokens of 64 heads 954 us, by every new maximum 1016; six ragged prompts 65.9, 68.8)
 
 struct PrefillArgs {
     const uint16_t *q, *k[2], *v[2];      // keys and values: prefix, new tokens
@@ -519,7 +526,8 @@ __global__ __launch_bounds__(64 * WAVES) __attribute__((amdgpu_waves_per_eu(2, 2
     }
 }
 
-// Joins the parts of a tile's rows: 32 lanes take a row, four channels each; or, of many parts, eight times 32 lanes every eighth part of a row.
+// Joins the parts of a tile's rows: out = sum_p 2^(m_p - m) o_p / sum_p 2^(m_p - m) l_p.  Bound by the
+// loads' latency.  32 lanes take a row, four channels each, eight parts on the way; or, of many parts, eight times 32 lanes every eighth part of it.
 template <bool MANY>
 __global__ __launch_bounds__(256) void tkv_prefill_merge_kernel(PrefillArgs a, int32_t tile_rows)
 {
