@@ -260,6 +260,43 @@ def test_captured_and_replayed_with_other_inputs():
         c.check("replay %d" % k)
 
 
+def test_two_captured_graphs_share_a_workspace():
+    cases = [Case([60, 1], [2000, 700], 8, 2, seed=23, kind=128, most=9), Case([3], [6000], 8, 2, FP, FP, FP, seed=24, kind=32, most=5)]
+    shared = max((c.workspace for c in cases), key=lambda w: w.numel())
+    graphs = []
+    for c in cases:
+        assert c.plan.n_slots > 0
+        c.workspace = shared
+        c.call()
+        torch.cuda.synchronize()
+        graphs.append(torch.cuda.CUDAGraph())
+        with torch.cuda.graph(graphs[-1]):
+            c.call()
+    for k in (0, 1, 1, 0, 1, 0):
+        cases[k].out.fill_(7.0)
+        graphs[k].replay()
+        cases[1 - k].call()
+        graphs[k].replay()
+        torch.cuda.synchronize()
+        cases[0].check("replay")
+        cases[1].check("replay")
+
+
+@pytest.mark.parametrize("lens,cached,hq,hk", [([9, 2], [100, 0], 64, 1), ([3], [130], 300, 1), ([20, 70], [0, 65], 21, 3), ([40], [33], 32, 32), ([2, 5], [1, 900], 77, 7)])
+@pytest.mark.parametrize("rows,most", [(32, 1 << 20), (128, 3), (256, 1 << 20)])
+def test_groups_beyond_a_tile_and_of_odd_sizes(lens, cached, hq, hk, rows, most):
+    c = Case(lens, cached, hq, hk, kind=rows, most=most, spare=2, seed=hq)
+    c.call()
+    c.check("%d on %d heads, %d rows" % (hq, hk, rows))
+
+
+def test_two_hundred_short_sequences():
+    lens = [(7 * k) % 5 for k in range(200)]
+    c = Case(lens, [(31 * k) % 190 for k in range(200)], 8, 2, seed=25, spare=4)
+    c.call()
+    c.check("200 sequences")
+
+
 @pytest.mark.parametrize("word,value", [(0, -1), (0, 1000), (1, 0), (1, 1 << 30), (2, -1), (2, 1 << 30), (3, -1), (3, 1 << 20), (4, -128), (4, 1 << 30), (5, -1), (5, 99),
                                         (7, 1000), (7, -2), (8, -1), (8, 99), (9, 0), (9, 1 << 30)])
 def test_items_that_name_what_is_not_there_are_skipped(word, value):
