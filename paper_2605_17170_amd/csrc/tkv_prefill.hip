@@ -333,9 +333,10 @@ __device__ __forceinline__ void attend(Rows &w, const Tiles &t, const uint16_t *
                 w.sum = add_pair<BF16>(p[8 * b + r / 2], w.sum);
             }
     };
-    auto values = [&](const uint32_t (&p)[8 * KB], uint32_t buffer, auto cleaned) {
+    // `beside`: what is done beside the products of 16 keys.
+    auto values = [&](const uint32_t (&p)[8 * KB], uint32_t buffer, auto cleaned, auto beside) {
 #pragma unroll
-        for (int j = 0; j < 2 * KB; ++j)
+        for (int j = 0; j < 2 * KB; ++j) {
 #pragma unroll
             for (int d = 0; d < 4; ++d) {
                 u32x4 x = v_operand(t.v_at[d] + buffer, j);
@@ -346,6 +347,8 @@ __device__ __forceinline__ void attend(Rows &w, const Tiles &t, const uint16_t *
                 }
                 w.o[d] = mfma<BF16>(x, u32x4{p[4 * j], p[4 * j + 1], p[4 * j + 2], p[4 * j + 3]}, w.o[d]);
             }
+            beside(j);
+        }
     };
     // Whether a tile of V holds infinities or NaN.  Where not all rows see all of its keys, a weight of zero must not meet them.
     auto strange = [&](uint32_t buffer) {
@@ -387,9 +390,13 @@ __device__ __forceinline__ void attend(Rows &w, const Tiles &t, const uint16_t *
         fetch_v();
         logits(next, odd ? 0 : kTile, c4, c8);
         weights(p, s);
-        values(p, (odd ? 3 : 2) * kTile, std::false_type{});
-        const float top = top_of(next);
-        follow(top);
+        // (the maximum a piece beside each four products: 8192 tokens 973 -> 957 us, 4 replays 49.8 -> 49.5)
+        float top = -INFINITY;
+        values(p, (odd ? 3 : 2) * kTile, std::false_type{}, [&](int j) {
+#pragma unroll
+            for (int r = 0; r < 8; ++r) top = fmaxf(top, next[j / 2][8 * (j & 1) + r]);
+        });
+        follow(both_max(top) * w.c);
 #pragma unroll
         for (int b = 0; b < KB; ++b) s[b] = next[b];
         ++i;
@@ -408,9 +415,9 @@ __device__ __forceinline__ void attend(Rows &w, const Tiles &t, const uint16_t *
         const uint32_t odd = (uint32_t)((i - begin) & 1) * kTile;
         uint32_t p[8 * KB];
         weights(p, s);
-        if (!strange(2 * kTile + odd)) values(p, 2 * kTile + odd, std::false_type{});
+        if (!strange(2 * kTile + odd)) values(p, 2 * kTile + odd, std::false_type{}, [](int) {});
         else {
-            values(p, 2 * kTile + odd, std::true_type{});
+            values(p, 2 * kTile + odd, std::true_type{}, [](int) {});
             left_out = true;
         }
         if (i + 1 < end) {
