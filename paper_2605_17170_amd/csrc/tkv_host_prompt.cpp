@@ -25,8 +25,8 @@ bool rows_ok(const void *p, int64_t stride, int64_t heads, int32_t n_tokens)
     return p && !((uintptr_t)p & 15) && stride >= 0 && stride % 8 == 0 && stride < kMaxStride && (stride >= heads * kHeadDim || n_tokens == 1);
 }
 int64_t up(int64_t a, int64_t b) { return (a + b - 1) / b; }
-// Workgroups of tkv_prefill_attention.  Times in us, fitted to 792 measured plans of 94 calls (1 to 64 sequences of 1 to 16384 tokens behind 0 to 100000,
-// 1 to 8 key heads, groups of 1 to 8): the plan chosen is 1.3 % behind the best of a call's in the mean, 20 % at most.
+// Workgroups of tkv_prefill_attention.  Times in us, fitted to 792 measured plans of 94 calls on rows that are not in the caches (1 to 64 sequences of 1 to 16384 tokens behind 0 to 100000,
+// 1 to 8 key heads, groups of 1 to 8): the plan chosen is 1.1 % behind the best of a call's in the mean, 20 % at most.
 struct Kind {
     int32_t rows, keys, resident;   // rows, keys of a tile, workgroups that a compute unit holds at once
     double begin, again;            // what a workgroup takes beside its steps: the first one of a place, those behind it
@@ -85,7 +85,9 @@ int32_t tkv_plan_prefill(const tkv_desc *desc, int32_t batch, int32_t n_q_heads,
                     all += keys;
                     longest = std::max(longest, keys);
                 }
-                if (rows > 0) bytes += ((double)pre + n) * 4.0 * kHeadDim;   // once: tiles of a sequence find them in the caches
+                // the first tile's keys and values come from memory, most of the next three tiles' from the caches (4 chunks of 16 tokens of 64 heads
+                // behind 2000 to 6000 38.6 us with 32 rows, which the plan took without this, 33.8 with 128)
+                if (rows > 0) bytes += ((double)pre + n) * 4.0 * kHeadDim * (1.0 + 0.15 * std::min<double>(3.0, (double)(up(rows, kind.rows) - 1)));
             }
             if (mine.empty()) break;
             const double heads = desc->n_kv_heads, slots = std::max(1.0, kind.resident * (double)target_cus / heads);
