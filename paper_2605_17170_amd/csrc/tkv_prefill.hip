@@ -11,8 +11,8 @@
 //
 // Workgroups of 32 rows (one wavefront, four of them on a compute unit: loads of many workgroups on the way), 128 (four wavefronts, two
 // workgroups: one takes the matrix cores while the other takes exponentials) and 256 (eight, one workgroup: keys and values are
-// read half as often).  One MI355X, us: 2048 tokens of 64 heads behind 30 000 with 128 rows 1954, with 256 1888, now 1857 (1121 TFLOP/s, MFMAs busy 62 % of the
-// cycles at the 1.4 to 1.7 GHz that power leaves; the library's bf16 product of 8192^3 runs at 1414); 8192 tokens 1000 (1100 TFLOP/s); 16
+// read half as often).  One MI355X, us: 2048 tokens of 64 heads behind 30 000 with 128 rows 1954, with 256 1888, now 1813 (1149 TFLOP/s, MFMAs busy 62 % of the
+// cycles at the 1.4 to 1.7 GHz that power leaves; the library's bf16 product of 8192^3 runs at 1414); 8192 tokens 949 (1159 TFLOP/s); 16
 // single tokens of 64 heads behind 1500 to 5000 with 128 rows 63, with 32 41, now 38 (171 MB; 5.2 TB/s within the kernel).  In between, where there are
 // few workgroups, a step's chain bounds the call: logits 870 cycles, weights 600, values 900, fetches 350, maximum and reference 300.
 #include <hip/hip_runtime.h>
