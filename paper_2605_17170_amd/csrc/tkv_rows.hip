@@ -324,8 +324,9 @@ __global__ __launch_bounds__(256) void tkv_distortion_join_kernel(DistortionArgs
         a.out[(int64_t)b * a.n_heads + head] = !ok ? __builtin_nan("") : hi > lo ? sums[threadIdx.x] / ((double)(hi - lo) * kHeadDim) : 0.0;
 }
 
-// Few tokens: a workgroup takes all of a sequence and head, and there is nothing to join.  One compute unit reads 100 GB/s of rows that lie
-// apart: bf16, 16 heads, one sequence, this / chunks and a join, us: 16 tokens 3.4 / 5.6, 256 4.5 / 6.1, 512 6.5 / 6.4, 701 7.8 / 6.9; 64 heads 3.4 / 9.2, 4.8 / 11.9.
+// Few tokens: a workgroup takes all of a sequence and head, and there is nothing to join.  Its sums in 64 bits take 9 us a thousand rows (more loads on the way
+// change nothing).  bf16, 16 heads, one sequence, this / chunks and a join, us: 16 tokens 3.4 / 5.6, 256 4.6 / 6.1, 384 5.4 / 6.6, 512 6.4 / 6.7, 701 7.7 / 6.7; 64 heads
+// 3.5 / 9.2, 4.9 / 11.9, 6.2 / 8.3, 7.8 / 8.5, 9.6 / 9.2; fp32, 64 heads, 384 8.9 / 9.2, 512 11.2 / 10.6.
 template <int TYPE>
 __global__ __launch_bounds__(1024) void tkv_distortion_short_kernel(DistortionArgs a)
 {
@@ -383,7 +384,7 @@ int tkv_launch_distortion(const void *a_rows, const void *b_rows, int32_t type, 
                           double *out, void *workspace, void *stream)
 {
     DistortionArgs a = {a_rows, b_rows, seq_indptr, out, (double *)workspace, batch, n_tokens, n_heads, tkv_distortion_chunk(n_tokens, n_heads)};
-    if (n_tokens <= 256) {
+    if (n_tokens <= 384) {
         auto *whole = type == TKV_BF16 ? tkv_distortion_short_kernel<TKV_BF16> : type == TKV_FP16 ? tkv_distortion_short_kernel<TKV_FP16> : tkv_distortion_short_kernel<TKV_FP32>;
         hipLaunchKernelGGL(whole, grid((int64_t)batch * n_heads), dim3(1024), 0, (hipStream_t)stream, a);
         return hipGetLastError() == hipSuccess ? TKV_OK : TKV_ERR_HIP;

@@ -70,7 +70,7 @@ def test_offsets_that_cannot_be_give_nan_for_their_sequences(offsets):
 
 
 @pytest.mark.parametrize("kind", [torch.bfloat16, torch.float32])
-@pytest.mark.parametrize("lens,heads", [([256], 6), ([257], 6), ([255, 2], 17), ([0, 250, 6], 33), ([300, 0, 1, 0], 9), ([4095, 1], 16), ([100] * 90, 16), ([8191], 8), ([8192], 8), ([20000], 2)])
+@pytest.mark.parametrize("lens,heads", [([256], 6), ([257], 6), ([384], 3), ([385], 3), ([0, 200, 185], 12), ([255, 2], 17), ([0, 250, 6], 33), ([300, 0, 1, 0], 9), ([4095, 1], 16), ([100] * 90, 16), ([8191], 8), ([8192], 8), ([20000], 2)])
 def test_around_the_sizes_at_which_the_split_changes(kind, lens, heads):
     x, y, ip = make(lens, heads, kind, heads, spare=0)
     got = call(x, y, ip)
