@@ -26,14 +26,15 @@ bool rows_ok(const void *p, int64_t stride, int64_t heads, int32_t n_tokens)
 }
 int64_t up(int64_t a, int64_t b) { return (a + b - 1) / b; }
 // Workgroups of tkv_prefill_attention.  Times in us, fitted to 792 measured plans of 94 calls on rows that are not in the caches (1 to 64 sequences of 1 to 16384 tokens behind 0 to 100000,
-// 1 to 8 key heads, groups of 1 to 8): the plan chosen is 1.1 % behind the best of a call's in the mean, 20 % at most.
+// 1 to 8 key heads, groups of 1 to 8): the plan chosen is 0.6 % behind the best of a call's in the mean, 22 % at most.
 struct Kind {
     int32_t rows, keys, resident;   // rows, keys of a tile, workgroups that a compute unit holds at once
     double begin, again;            // what a workgroup takes beside its steps: the first one of a place, those behind it
     double alone, step;             // a step (a tile of keys) of a workgroup by itself; steps of a full compute unit, one behind the other
 };
-constexpr Kind kKinds[3] = {{32, 32, 4, 5.0, 9.4, 0.74, 0.177}, {128, 64, 2, 6.0, 8.4, 1.14, 0.98}, {256, 64, 1, 7.0, 12.0, 1.5, 1.82}};
-constexpr double kMergeUs = 3.0, kBytesPerUs = 5.5e6, kPartialBytesPerUs = 4.2e6;   // a second launch; keys and values; partial results
+constexpr Kind kKinds[3] = {{32, 32, 4, 4.5, 10.8, 0.70, 0.173}, {128, 64, 2, 6.0, 6.4, 0.96, 0.98}, {256, 64, 1, 6.0, 8.1, 1.32, 1.90}};
+constexpr double kMergeUs = 3.1, kCrossUs = 2.0;   // a second launch; going on from a prefix to the new tokens
+constexpr double kBytesPerUs = 6.1e6, kPartialBytesPerUs = 3.4e6;   // keys and values; partial results
 bool kind_of(int32_t rows)
 {
     for (const Kind &k : kKinds)
@@ -76,9 +77,11 @@ int32_t tkv_plan_prefill(const tkv_desc *desc, int32_t batch, int32_t n_q_heads,
             mine.clear();
             int64_t all = 0, longest = 0;
             double bytes = 0.0;
+            bool crosses = false;
             for (int32_t b = 0; b < batch; ++b) {
                 const int32_t n = seq_indptr[b + 1] - seq_indptr[b], pre = prefix_indptr ? prefix_indptr[b + 1] - prefix_indptr[b] : 0;
                 const int64_t rows = (int64_t)n * group;
+                crosses = crosses || (n > 0 && pre > 0);
                 for (int64_t r = 0; r < rows; r += kind.rows) {
                     const int64_t see = (std::min(r + kind.rows, rows) - 1) / group + 1, keys = up(pre, kind.keys) + up(see, kind.keys);
                     mine.push_back({b, (int32_t)r, (int32_t)keys, 1});
@@ -87,7 +90,7 @@ int32_t tkv_plan_prefill(const tkv_desc *desc, int32_t batch, int32_t n_q_heads,
                 }
                 // the first tile's keys and values come from memory, most of the next three tiles' from the caches (4 chunks of 16 tokens of 64 heads
                 // behind 2000 to 6000 38.6 us with 32 rows, which the plan took without this, 33.8 with 128)
-                if (rows > 0) bytes += ((double)pre + n) * 4.0 * kHeadDim * (1.0 + 0.15 * std::min<double>(3.0, (double)(up(rows, kind.rows) - 1)));
+                if (rows > 0) bytes += ((double)pre + n) * 4.0 * kHeadDim * (1.0 + 0.13 * std::min<double>(3.0, (double)(up(rows, kind.rows) - 1)));
             }
             if (mine.empty()) break;
             const double heads = desc->n_kv_heads, slots = std::max(1.0, kind.resident * (double)target_cus / heads);
@@ -100,7 +103,7 @@ int32_t tkv_plan_prefill(const tkv_desc *desc, int32_t batch, int32_t n_q_heads,
                     n += k;
                     if (k > 1) partial += (double)k * (double)std::min<int64_t>(kind.rows, ((int64_t)seq_indptr[t.seq + 1] - seq_indptr[t.seq]) * group - t.row);
                 }
-                const double work = std::max((double)all * heads / target_cus * kind.step, bytes * heads / kBytesPerUs), line = (double)std::min(most, longest) * kind.alone;
+                const double work = std::max((double)all * heads / target_cus * kind.step, bytes * heads / kBytesPerUs), line = (double)std::min(most, longest) * kind.alone + (crosses && most > 1 ? kCrossUs : 0.0);
                 const double rounds = std::max(1.0, (double)n * heads / (kind.resident * (double)target_cus));
                 return kind.begin + (rounds - 1.0) * kind.again + std::max(work, line) + 0.16 * std::min(work, line) / rounds +
                        (partial > 0.0 ? kMergeUs + partial * heads * 8.0 * (kHeadDim + 2) / kPartialBytesPerUs : 0.0);
