@@ -675,8 +675,10 @@ int tkv_launch_prefill(int32_t n_q_heads, int32_t n_kv_heads, const void *q, int
                          : prefill->tile_rows == 128 ? launch<4, 2>(a, bf16, groups, (hipStream_t)stream) : launch<8, 2>(a, bf16, groups, (hipStream_t)stream);
     if (e != hipSuccess) return TKV_ERR_HIP;
     if (prefill->n_cut > 0) {
-        const bool many = prefill->n_slots > 8 * (int64_t)prefill->n_cut;   // one token of one head behind 7560 26.0 -> 11.8 us, 100000 of 64 heads 80.9 -> 72.9, 701 11.0 -> 10.0
         const int64_t rows = (int64_t)prefill->n_cut * n_kv_heads * prefill->tile_rows;
+        // Eight sets of lanes a row save half a microsecond for every eight parts behind the first, and cost two for a thousand rows: one token of one head behind 7560
+        // (237 parts) 26.0 -> 11.8 us, 100000 of 64 heads (126 parts, 256 rows) 80.9 -> 72.9, 701 11.0 -> 10.0; but 16 tokens of 64 heads (8 parts, 4096 rows) 36.9 -> 46.1
+        const bool many = prefill->n_slots > (8 + rows / 32) * prefill->n_cut;
         if (many) hipLaunchKernelGGL(tkv_prefill_merge_kernel<true>, grid(rows), dim3(256), 0, (hipStream_t)stream, a, prefill->tile_rows);
         else hipLaunchKernelGGL(tkv_prefill_merge_kernel<false>, grid(rows / 8), dim3(256), 0, (hipStream_t)stream, a, prefill->tile_rows);
         if (hipGetLastError() != hipSuccess) return TKV_ERR_HIP;

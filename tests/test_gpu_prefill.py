@@ -290,6 +290,16 @@ def test_groups_beyond_a_tile_and_of_odd_sizes(lens, cached, hq, hk, rows, most)
     c.check("%d on %d heads, %d rows" % (hq, hk, rows))
 
 
+@pytest.mark.parametrize("rows,tokens", [(32, 1), (32, 31), (128, 3), (128, 128), (256, 200), (256, 256)])
+@pytest.mark.parametrize("parts", [8, 9, 12, 17, 25, 40])
+def test_parts_of_one_tile_of_every_kind(rows, tokens, parts):
+    keys = 32 if rows == 32 else 64
+    c = Case([tokens], [keys * parts], 1, 1, kind=rows, most=1, seed=parts, spare=1)
+    assert c.plan.n_cut == 1 and c.plan.n_slots == parts + -(-tokens // keys)
+    c.call()
+    c.check("%d parts of %d rows" % (parts, rows))
+
+
 def test_two_hundred_short_sequences():
     lens = [(7 * k) % 5 for k in range(200)]
     c = Case(lens, [(31 * k) % 190 for k in range(200)], 8, 2, seed=25, spare=4)
