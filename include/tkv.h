@@ -700,8 +700,8 @@ enum { TKV_BF16 = 0, TKV_FP16 = 1, TKV_FP32 = 2 };
  * there are too few tiles of rows to fill target_cus compute units, long ranges
  * are cut into equal parts, whose partial results lie in a workspace and are
  * joined.  The number of rows is the one that is expected to take least time.
- * Items come by falling length (of 128 rows, the first target_cus workgroups
- * by rising length).  The plan depends on the lengths alone: layers,
+ * Items come by falling length (of 128 rows, if none is cut, the first target_cus
+ * workgroups by rising length).  The plan depends on the lengths alone: layers,
  * and replays of the same requests, share it.
  *   desc             n_kv_heads and geometry; the pools may be empty
  *   seq_indptr       host i32[batch+1], from 0: the sequences' new tokens
