@@ -750,7 +750,9 @@ size_t tkv_prefill_workspace_bytes(const tkv_desc *desc, int32_t n_slots, int32_
  *                needs no initialisation; calls that overlap in time need one each
  *   status       device i32, may be NULL: TKV_STATUS_BAD_ITEM
  * Products are exact and summed in 32 bits; weights are rounded to the values'
- * type, their sum is that of the rounded ones; bf16 queries meet fp16 keys as
+ * type, their sum is that of the rounded ones; those of fp16 values (all of a
+ * prefix) that lie below 2^-23 of the row's largest are rounded to multiples of
+ * 2^-33 of it or less; bf16 queries meet fp16 keys as
  * fp16 numbers with a power of two of their row (what lies 2^-24 below the
  * row's largest, or below 2^-144, rounds to the grid of the subnormals).
  * q . k (for bf16 queries over fp16 keys also sm_scale times the row's largest

@@ -38,7 +38,14 @@ typedef short s16x4 __attribute__((ext_vector_type(4)));
 constexpr int kRow = kHeadDim * 2;        // bytes
 constexpr int kItem = kPrefillItemWords;
 constexpr float kNone = -3.4028235e38f;   // reference of a row that has seen no key
-constexpr float kSlack = 8.0f;            // weights grow to 2^8 before the reference follows the maximum (8192 tokens of 64 heads 954 us, by every new maximum 1016; six ragged prompts 65.9, 68.8)
+// A row's reference is set kLift below its largest logit and follows when the largest has grown by kSlack: weights reach 2^(kLift + kSlack) at most, and
+// the row's largest is 2^kLift at least.  bf16 weights: 0 and 8 (8192 tokens of 64 heads 954 us, by every new maximum 1016; six ragged prompts 65.9, 68.8).  fp16
+// weights end at 2^16, are whole down to 2^-14 and nothing below 2^-25: 9 and 6 keep weights down to 2^-23 of the row's largest whole and drop those below 2^-34.
+// (0 and 8 dropped those below 2^-25: 60 000 keys, each e^-18 of a sink with a small value, made an output 6 % off.)  us, 0 and 8 / 7 and 8 / 9 and 6 / 11 and 4:
+// four prompts of 2000 fp16 tokens 291 / 291 / 292 / 295, 8192 1004 / 1014 / 1014 / 1026, 2048 behind 30 000 1799 / 1832 / 1824 / 1831, where weights that were zero
+// cost power now; calls that power does not bound the same to 0.5 %, with 11 and 4 to 2 %.
+template <bool BF16> constexpr float kLift = BF16 ? 0.0f : 9.0f;
+template <bool BF16> constexpr float kSlack = BF16 ? 8.0f : 6.0f;
 
 struct PrefillArgs {
     const uint16_t *q, *k[2], *v[2];      // keys and values: prefix, new tokens
@@ -305,9 +312,10 @@ __device__ __forceinline__ void attend(Rows &w, const Tiles &t, const uint16_t *
         return both_max(top) * w.c;
     };
     auto follow = [&](float top) {
-        const bool grows = top > w.m + kSlack;
+        // fp16: logits of up to 2^26 are rounded by 2, and so are the reference and the bound; 2^-22 of the logit on top keeps weights below 2^15 all the same
+        const bool grows = (BF16 ? top : fmaf(fabsf(top), 0x1p-22f, top)) > w.m + (kLift<BF16> + kSlack<BF16>);
         if (__any(grows)) {   // row by row: what a row gives does not depend on the others of its wavefront
-            const float m = grows ? top : w.m, by = __builtin_amdgcn_exp2f(w.m - m);
+            const float m = grows ? top - kLift<BF16> : w.m, by = __builtin_amdgcn_exp2f(w.m - m);
             w.m = m;
             w.sum *= by;
 #pragma unroll
@@ -382,7 +390,7 @@ __device__ __forceinline__ void attend(Rows &w, const Tiles &t, const uint16_t *
     if (begin >= plain) hide(s, begin);
     if (first) {   // nothing to rescale yet
         const float top = top_of(s);
-        w.m = top > w.m + kSlack ? top : w.m;
+        w.m = top > w.m ? top - kLift<BF16> : w.m;
     } else follow(top_of(s));
     int i = begin;
     auto step = [&](auto odd) {
