@@ -100,38 +100,44 @@ __device__ __forceinline__ float both_sum(float x)
 // LOADS times sixteen bytes a lane from global memory to LDS, zeros from beyond the buffer: load j takes offset[j % 4] (all the same, unless MIXED) + j
 // `step` bytes to `lds` + j `stride` + 16 times the lane.  Written out, with the waits beside it: the compiler waits for every such load
 // before any read of LDS.  In one block: scalars that a vector instruction wrote, as reloads of spilled ones do, need five wait states before the
-// first load; M0 one.
+// first load; M0 one.  M0 is named among the registers that change, so that the compiler keeps nothing in it across the block (its warning says that the register is
+// its own).  (Put back by the block instead: six ragged prompts 61.7 -> 62.1 us, 2048 tokens behind 30 000 1802 -> 1845.)
 //
 // ONCE: non-temporal, where no other workgroup has a use for the lines.  16 single tokens behind 1500 to 5000 cached ones 41.6 -> 38.0 us, 64 of them
 // 96.8 -> 86.2; but four prompts of 2000 tokens 290 -> 317 (2048 tokens behind 30000 1888 -> 1830), 1000 tokens by workgroups of 32 rows 36.8 -> 40.4.
-#define TKV_LOAD_FIRST(NT) "s_mov_b32 m0, %1\n\ts_mov_b32 %0, 0\n\ts_nop 2\n\tbuffer_load_dwordx4 %6, %2, %0 offen" NT " lds\n\t"
-#define TKV_LOAD_NEXT(NT, V) "s_add_u32 m0, m0, %4\n\ts_add_u32 %0, %0, %3\n\tbuffer_load_dwordx4 " V ", %2, %0 offen" NT " lds\n\t"
+#pragma clang diagnostic push
+#pragma clang diagnostic ignored "-Winline-asm"
+#define TKV_LOAD_FIRST(NT) "s_mov_b32 m0, %[lds]\n\ts_mov_b32 %[at], 0\n\ts_nop 2\n\tbuffer_load_dwordx4 %[v0], %[buffer], %[at] offen" NT " lds\n\t"
+#define TKV_LOAD_NEXT(NT, V) "s_add_u32 m0, m0, %[stride]\n\ts_add_u32 %[at], %[at], %[step]\n\tbuffer_load_dwordx4 " V ", %[buffer], %[at] offen" NT " lds\n\t"
 #define TKV_LOADS(TEXT) \
-    asm volatile(TEXT : "=&s"(at) : "s"(lds), "s"(buffer), "s"(step), "n"(STRIDE), "n"(0), "v"(offset[0]), "v"(offset[1]), "v"(offset[2]), "v"(offset[3]) : "memory", "scc")
+    asm volatile(TEXT : [at] "=&s"(at) \
+                 : [lds] "s"(lds), [buffer] "s"(buffer), [step] "s"(step), [stride] "n"(STRIDE), [v0] "v"(offset[0]), [v1] "v"(offset[1]), [v2] "v"(offset[2]), [v3] "v"(offset[3]) \
+                 : "memory", "scc", "m0")
 template <int LOADS, int STRIDE, bool MIXED, bool ONCE> __device__ __forceinline__ void load_lds(uint32_t lds, u32x4 buffer, const uint32_t (&offset)[4], uint32_t step)
 {
     static_assert(LOADS == 2 || LOADS == 4 || LOADS == 8);
     uint32_t at;
-    if constexpr (LOADS == 2 && ONCE) TKV_LOADS(TKV_LOAD_FIRST(" nt") TKV_LOAD_NEXT(" nt", "%6"));
-    else if constexpr (LOADS == 2) TKV_LOADS(TKV_LOAD_FIRST("") TKV_LOAD_NEXT("", "%6"));
-    else if constexpr (LOADS == 4 && ONCE) TKV_LOADS(TKV_LOAD_FIRST(" nt") TKV_LOAD_NEXT(" nt", "%6") TKV_LOAD_NEXT(" nt", "%6") TKV_LOAD_NEXT(" nt", "%6"));
-    else if constexpr (LOADS == 4) TKV_LOADS(TKV_LOAD_FIRST("") TKV_LOAD_NEXT("", "%6") TKV_LOAD_NEXT("", "%6") TKV_LOAD_NEXT("", "%6"));
+    if constexpr (LOADS == 2 && ONCE) TKV_LOADS(TKV_LOAD_FIRST(" nt") TKV_LOAD_NEXT(" nt", "%[v0]"));
+    else if constexpr (LOADS == 2) TKV_LOADS(TKV_LOAD_FIRST("") TKV_LOAD_NEXT("", "%[v0]"));
+    else if constexpr (LOADS == 4 && ONCE) TKV_LOADS(TKV_LOAD_FIRST(" nt") TKV_LOAD_NEXT(" nt", "%[v0]") TKV_LOAD_NEXT(" nt", "%[v0]") TKV_LOAD_NEXT(" nt", "%[v0]"));
+    else if constexpr (LOADS == 4) TKV_LOADS(TKV_LOAD_FIRST("") TKV_LOAD_NEXT("", "%[v0]") TKV_LOAD_NEXT("", "%[v0]") TKV_LOAD_NEXT("", "%[v0]"));
     else if constexpr (MIXED && ONCE)
-        TKV_LOADS(TKV_LOAD_FIRST(" nt") TKV_LOAD_NEXT(" nt", "%7") TKV_LOAD_NEXT(" nt", "%8") TKV_LOAD_NEXT(" nt", "%9") TKV_LOAD_NEXT(" nt", "%6") TKV_LOAD_NEXT(" nt", "%7")
-                      TKV_LOAD_NEXT(" nt", "%8") TKV_LOAD_NEXT(" nt", "%9"));
+        TKV_LOADS(TKV_LOAD_FIRST(" nt") TKV_LOAD_NEXT(" nt", "%[v1]") TKV_LOAD_NEXT(" nt", "%[v2]") TKV_LOAD_NEXT(" nt", "%[v3]") TKV_LOAD_NEXT(" nt", "%[v0]") TKV_LOAD_NEXT(" nt", "%[v1]")
+                      TKV_LOAD_NEXT(" nt", "%[v2]") TKV_LOAD_NEXT(" nt", "%[v3]"));
     else if constexpr (MIXED)
-        TKV_LOADS(TKV_LOAD_FIRST("") TKV_LOAD_NEXT("", "%7") TKV_LOAD_NEXT("", "%8") TKV_LOAD_NEXT("", "%9") TKV_LOAD_NEXT("", "%6") TKV_LOAD_NEXT("", "%7")
-                      TKV_LOAD_NEXT("", "%8") TKV_LOAD_NEXT("", "%9"));
+        TKV_LOADS(TKV_LOAD_FIRST("") TKV_LOAD_NEXT("", "%[v1]") TKV_LOAD_NEXT("", "%[v2]") TKV_LOAD_NEXT("", "%[v3]") TKV_LOAD_NEXT("", "%[v0]") TKV_LOAD_NEXT("", "%[v1]")
+                      TKV_LOAD_NEXT("", "%[v2]") TKV_LOAD_NEXT("", "%[v3]"));
     else if constexpr (ONCE)
-        TKV_LOADS(TKV_LOAD_FIRST(" nt") TKV_LOAD_NEXT(" nt", "%6") TKV_LOAD_NEXT(" nt", "%6") TKV_LOAD_NEXT(" nt", "%6") TKV_LOAD_NEXT(" nt", "%6") TKV_LOAD_NEXT(" nt", "%6")
-                      TKV_LOAD_NEXT(" nt", "%6") TKV_LOAD_NEXT(" nt", "%6"));
+        TKV_LOADS(TKV_LOAD_FIRST(" nt") TKV_LOAD_NEXT(" nt", "%[v0]") TKV_LOAD_NEXT(" nt", "%[v0]") TKV_LOAD_NEXT(" nt", "%[v0]") TKV_LOAD_NEXT(" nt", "%[v0]") TKV_LOAD_NEXT(" nt", "%[v0]")
+                      TKV_LOAD_NEXT(" nt", "%[v0]") TKV_LOAD_NEXT(" nt", "%[v0]"));
     else
-        TKV_LOADS(TKV_LOAD_FIRST("") TKV_LOAD_NEXT("", "%6") TKV_LOAD_NEXT("", "%6") TKV_LOAD_NEXT("", "%6") TKV_LOAD_NEXT("", "%6") TKV_LOAD_NEXT("", "%6")
-                      TKV_LOAD_NEXT("", "%6") TKV_LOAD_NEXT("", "%6"));
+        TKV_LOADS(TKV_LOAD_FIRST("") TKV_LOAD_NEXT("", "%[v0]") TKV_LOAD_NEXT("", "%[v0]") TKV_LOAD_NEXT("", "%[v0]") TKV_LOAD_NEXT("", "%[v0]") TKV_LOAD_NEXT("", "%[v0]")
+                      TKV_LOAD_NEXT("", "%[v0]") TKV_LOAD_NEXT("", "%[v0]"));
 }
 #undef TKV_LOADS
 #undef TKV_LOAD_NEXT
 #undef TKV_LOAD_FIRST
+#pragma clang diagnostic pop
 __device__ __forceinline__ void wait_barrier() { asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
 
 __device__ __forceinline__ u32x4 buffer_of(const void *p, uint32_t bytes)
