@@ -716,7 +716,10 @@ enum { TKV_BF16 = 0, TKV_FP16 = 1, TKV_FP32 = 2 };
  *   n_slots_out      host i32: partial slots, 0 if no range is cut
  *   n_cut_out        host i32: tiles whose ranges are cut
  * Returns the number of items (>= 0) or a negative status.  A sequence without
- * new tokens has none.  At most 2^30 rows (tokens * R) a sequence.
+ * new tokens has none.  At most 2^30 rows (tokens * R) a sequence, 2^31 - 1 in
+ * all, 65535 kv heads (and query heads, if there is more than one token: the
+ * token stride), 2^25 - 1 workgroups (items * kv heads) and 2^31 - 1 rows
+ * of tiles that are cut (tiles * kv heads * tile_rows); the call takes no more.
  * tkv_plan_prefill_capacity: an upper bound of the items for n_tokens new tokens.
  */
 int32_t tkv_plan_prefill_capacity(const tkv_desc *desc, int32_t batch, int32_t n_tokens, int32_t n_q_heads, int32_t target_cus);

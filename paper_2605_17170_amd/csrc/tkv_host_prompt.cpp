@@ -24,6 +24,13 @@ bool rows_ok(const void *p, int64_t stride, int64_t heads, int32_t n_tokens)
 {
     return p && !((uintptr_t)p & 15) && stride >= 0 && stride % 8 == 0 && stride < kMaxStride && (stride >= heads * kHeadDim || n_tokens == 1);
 }
+// Sizes that the plan returns and the call takes.
+bool heads_ok(const tkv_desc *desc) { return (int64_t)desc->n_kv_heads * kHeadDim < kMaxStride; }
+bool tokens_ok(int64_t n_tokens, int32_t group) { return n_tokens * group <= INT32_MAX; }
+bool items_ok(const tkv_desc *desc, int64_t n_items, int64_t n_cut, int32_t tile_rows)
+{
+    return n_items * desc->n_kv_heads <= INT32_MAX / 64 && n_cut <= n_items && n_cut * desc->n_kv_heads * tile_rows <= INT32_MAX;
+}
 int64_t up(int64_t a, int64_t b) { return (a + b - 1) / b; }
 // Workgroups of tkv_prefill_attention.  Times in us, fitted to 792 measured plans of 94 calls on rows that are not in the caches (1 to 64 sequences of 1 to 16384 tokens behind 0 to 100000,
 // 1 to 8 key heads, groups of 1 to 8): the plan chosen is 0.6 % behind the best of a call's in the mean, 22 % at most.
@@ -68,6 +75,8 @@ int32_t tkv_plan_prefill(const tkv_desc *desc, int32_t batch, int32_t n_q_heads,
         if (seq_indptr[b + 1] < seq_indptr[b] || (prefix_indptr && prefix_indptr[b + 1] < prefix_indptr[b])) return TKV_ERR_INVALID_ARG;
         if (((int64_t)seq_indptr[b + 1] - seq_indptr[b]) * group > 1 << 30) return TKV_ERR_INVALID_ARG;
     }
+    if (!heads_ok(desc) || ((int64_t)n_q_heads * kHeadDim >= kMaxStride && seq_indptr[batch] > 1)) return TKV_ERR_BAD_SHAPE;   // the token stride of more
+    if (!tokens_ok(seq_indptr[batch], group)) return TKV_ERR_INVALID_ARG;
     try {
         struct Tile { int32_t seq, row, keys, parts; };   // keys: tiles of keys that its rows see
         const Kind *best = nullptr;
@@ -133,19 +142,19 @@ int32_t tkv_plan_prefill(const tkv_desc *desc, int32_t batch, int32_t n_q_heads,
                 tiles.swap(mine);
             }
         }
-        int64_t n_slots = 0, n_items = 0;
+        int64_t n_items = 0, n_cut = 0;
         for (const Tile &t : tiles) {
             n_items += t.parts;
-            if (t.parts > 1) n_slots += t.parts;
+            n_cut += t.parts > 1;
         }
         if (n_items > capacity) return TKV_ERR_CAPACITY;
-        if (n_items * desc->n_kv_heads > INT32_MAX || n_slots > INT32_MAX) return TKV_ERR_INVALID_ARG;
+        if (best && !items_ok(desc, n_items, n_cut, best->rows)) return TKV_ERR_INVALID_ARG;
         std::stable_sort(tiles.begin(), tiles.end(), [](const Tile &x, const Tile &y) { return (int64_t)x.keys * y.parts > (int64_t)y.keys * x.parts; });
         // Two workgroups of 128 rows are dealt to each compute unit, number k and k + target_cus: the longest ranges stand beside the shortest, or
         // alone, if there are fewer than two for each unit.  (Falling from the first on, the longest share theirs with the next
         // longest: six sequences of 21 to 724 tokens behind prefixes 71.8 us, this way 68.4; 1000 tokens of 64 heads 29.7, 28.8.)
         const size_t units = (size_t)std::max(1, target_cus / desc->n_kv_heads);
-        if (best && best->resident == 2 && n_slots == 0 && tiles.size() > units) std::reverse(tiles.begin(), tiles.begin() + (int64_t)units);
+        if (best && best->resident == 2 && n_cut == 0 && tiles.size() > units) std::reverse(tiles.begin(), tiles.begin() + (int64_t)units);
         int32_t slot = 0, cut = 0, number = 0;
         for (const Tile &t : tiles) {
             if (t.parts > 1) {
@@ -206,10 +215,9 @@ int tkv_prefill_attention(const tkv_desc *desc, int32_t n_q_heads, const void *q
     if (!kind_of(prefill->tile_rows) || !prefill->items || ((uintptr_t)prefill->items & 3)) return TKV_ERR_INVALID_ARG;
     if (!rows_ok(q, q_stride, n_q_heads, n_tokens) || !rows_ok(K, k_stride, desc->n_kv_heads, n_tokens) || !rows_ok(V, v_stride, desc->n_kv_heads, n_tokens)) return TKV_ERR_INVALID_ARG;
     if (n_prefix > 0 && (!rows_ok(K_prefix, 0, 0, n_prefix) || !rows_ok(V_prefix, 0, 0, n_prefix))) return TKV_ERR_INVALID_ARG;
-    if ((int64_t)desc->n_kv_heads * kHeadDim >= kMaxStride) return TKV_ERR_BAD_SHAPE;
+    if (!heads_ok(desc)) return TKV_ERR_BAD_SHAPE;
     if (!out || ((uintptr_t)out & 15) || ((uintptr_t)workspace & 15) || ((uintptr_t)status & 3)) return TKV_ERR_INVALID_ARG;
-    if ((int64_t)prefill->n_items * desc->n_kv_heads > INT32_MAX / 64 || (int64_t)n_tokens * group > INT32_MAX) return TKV_ERR_INVALID_ARG;
-    if (prefill->n_cut > prefill->n_items || (int64_t)prefill->n_cut * desc->n_kv_heads * prefill->tile_rows > INT32_MAX) return TKV_ERR_INVALID_ARG;
+    if (!tokens_ok(n_tokens, group) || !items_ok(desc, prefill->n_items, prefill->n_cut, prefill->tile_rows)) return TKV_ERR_INVALID_ARG;
     if (prefill->n_slots > 0) {
         if (!workspace) return TKV_ERR_INVALID_ARG;
         if (workspace_bytes < tkv_prefill_workspace_bytes(desc, prefill->n_slots, prefill->tile_rows)) return TKV_ERR_WORKSPACE_TOO_SMALL;

@@ -112,8 +112,110 @@ static int workspace_of_distortions()
     return 0;
 }
 
+// A plan that is returned can be launched, and one that cannot is refused: `n` sequences of one token of `heads` kv heads and as many query heads.
+static int plan_and_call(int32_t heads, int32_t n, int want)
+{
+    tkv_desc d = {};
+    d.n_kv_heads = heads;
+    std::vector<int32_t> ip;
+    for (int32_t b = 0; b <= n; ++b) ip.push_back(b);
+    std::vector<int32_t> items((size_t)n * 16 + 4096 * 16);
+    int32_t rows = 0, slots = 0, cut = 0;
+    const int32_t got = tkv_plan_prefill(&d, n, heads, ip.data(), nullptr, 1, items.data(), n + 4096, &rows, &slots, &cut);
+    Prefill c;
+    c.d = d;
+    c.n_q_heads = heads;
+    c.n_tokens = n;
+    c.n_prefix = 0;
+    c.q_stride = c.k_stride = c.v_stride = n > 1 ? (int64_t)heads * 128 : 0;
+    c.p = {rows, got < 0 ? n : got, slots, cut, c.p.items};
+    if (got < 0) c.p.tile_rows = 32;
+    c.bytes = (size_t)1 << 40;
+    CHECK(want == TKV_OK ? got >= 0 : got == want);
+    CHECK(c.call() == want);
+    return 0;
+}
+
+// Queries of more rows in all than 32 bits count.
+static int rows_of_all_sequences()
+{
+    tkv_desc d = {};
+    d.n_kv_heads = 1;
+    const int32_t ip[] = {0, 1 << 20, 2 << 20, 3 << 20};
+    int32_t rows = 0, slots = 0, cut = 0, word = 0;
+    CHECK(tkv_plan_prefill(&d, 2, 1024, ip, nullptr, 1, &word, 0, &rows, &slots, &cut) == TKV_ERR_INVALID_ARG);
+    CHECK(prefill([](Prefill &c) { c.d.n_kv_heads = 1; c.n_q_heads = 1024; c.q_stride = 1024 * 128; c.n_tokens = 2 << 20; }) == TKV_ERR_INVALID_ARG);
+    CHECK(prefill([](Prefill &c) { c.d.n_kv_heads = 1; c.n_q_heads = 1023; c.q_stride = 1023 * 128; c.n_tokens = 2 << 20; }) == TKV_OK);
+    return 0;
+}
+
+// Query heads whose rows are as long as a token stride can be, and one more, which a single token may have.
+static int rows_as_long_as_strides()
+{
+    tkv_desc d = {};
+    d.n_kv_heads = 1;
+    const int32_t ip[] = {0, 1, 2};
+    std::vector<int32_t> items((size_t)16 * 10000);
+    int32_t rows = 0, slots = 0, cut = 0;
+    for (int32_t heads : {65535, 65536})
+        for (int32_t n : {1, 2}) {
+            const int want = heads == 65536 && n > 1 ? TKV_ERR_BAD_SHAPE : TKV_OK;
+            const int32_t got = tkv_plan_prefill(&d, n, heads, ip, nullptr, 1, items.data(), 10000, &rows, &slots, &cut);
+            CHECK(want == TKV_OK ? got > 0 : got == want);
+            if (want != TKV_OK) continue;
+            Prefill c;
+            c.d = d;
+            c.n_q_heads = heads;
+            c.n_tokens = n;
+            c.n_prefix = 0;
+            c.q_stride = n > 1 ? (int64_t)heads * 128 : 0;
+            c.p = {rows, got, slots, cut, c.p.items};
+            c.bytes = tkv_prefill_workspace_bytes(&d, slots, rows);
+            CHECK(c.call() == TKV_OK);
+        }
+    return 0;
+}
+
+// Of many heads and units: what the plan returns can be launched.
+static int plans_of_many_heads()
+{
+    int returned = 0;
+    for (int32_t heads : {1000, 65535})
+        for (int32_t n : {1, 60, 140, 250})
+            for (int32_t units : {1, 100, 400}) {
+                tkv_desc d = {};
+                d.n_kv_heads = heads;
+                std::vector<int32_t> ip, pp;
+                for (int32_t b = 0; b <= n; ++b) {
+                    ip.push_back(b * 256);
+                    pp.push_back(b * 64000);
+                }
+                std::vector<int32_t> items((size_t)16 * 100000);
+                int32_t rows = 0, slots = 0, cut = 0;
+                const int32_t got = tkv_plan_prefill(&d, n, heads, ip.data(), pp.data(), units * heads, items.data(), 100000, &rows, &slots, &cut);
+                CHECK(got > 0 || got == TKV_ERR_INVALID_ARG);
+                if (got < 0) continue;
+                ++returned;
+                Prefill c;
+                c.d = d;
+                c.n_q_heads = heads;
+                c.n_tokens = n * 256;
+                c.n_prefix = n * 64000;
+                c.q_stride = c.k_stride = c.v_stride = (int64_t)heads * 128;
+                c.p = {rows, got, slots, cut, c.p.items};
+                c.bytes = tkv_prefill_workspace_bytes(&d, slots, rows);
+                CHECK(c.call() == TKV_OK);
+            }
+    CHECK(returned > 0);
+    return 0;
+}
+
 int main()
 {
+    if (plan_and_call(65535, 512, TKV_OK) || plan_and_call(65535, 513, TKV_ERR_INVALID_ARG)) return 1;      // 2^25 - 1 workgroups are 512 times 65535 and some
+    if (plan_and_call(1024, 32767, TKV_OK) || plan_and_call(1024, 32768, TKV_ERR_INVALID_ARG)) return 1;
+    if (plan_and_call(65536, 1, TKV_ERR_BAD_SHAPE)) return 1;
+    if (rows_as_long_as_strides() || rows_of_all_sequences() || plans_of_many_heads()) return 1;
     const float nan = std::numeric_limits<float>::quiet_NaN(), inf = std::numeric_limits<float>::infinity();
     if (workspace_of_distortions()) return 1;
 
