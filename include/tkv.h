@@ -761,7 +761,8 @@ size_t tkv_prefill_workspace_bytes(const tkv_desc *desc, int32_t n_slots, int32_
  * q . k (for bf16 queries over fp16 keys also sm_scale times the row's largest
  * |q|) must be finite in 32 bits, and sm_scale * q . k * log2 e below 2^26 in
  * magnitude, where the rounding of a row's reference still leaves its weights
- * in the range of fp16; a row that goes beyond is NaN or off.  A row of q that
+ * in the range of fp16; a row that goes beyond is NaN or off.  256 times the sum
+ * of |v| over the keys that a row sees must be finite in 32 bits.  A row of q that
  * holds NaN or infinities gives NaN and leaves the others alone; what
  * stands in keys and values that a token does not see does not reach it, an
  * infinite or NaN value that it sees makes that channel infinite or NaN.

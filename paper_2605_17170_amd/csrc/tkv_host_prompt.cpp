@@ -98,7 +98,7 @@ int32_t tkv_plan_prefill(const tkv_desc *desc, int32_t batch, int32_t n_q_heads,
                     longest = std::max(longest, keys);
                 }
                 // the first tile's keys and values come from memory, most of the next three tiles' from the caches (4 chunks of 16 tokens of 64 heads
-                // behind 2000 to 6000 38.6 us with 32 rows, which the plan took without this, 33.8 with 128)
+                // behind 2000 to 6000 38.6 us with 32 rows, which the plan took without this, 33.8 with 128); 0.13 of the bytes for each, fitted with the constants above
                 if (rows > 0) bytes += ((double)pre + n) * 4.0 * kHeadDim * (1.0 + 0.13 * std::min<double>(3.0, (double)(up(rows, kind.rows) - 1)));
             }
             if (mine.empty()) break;
@@ -112,13 +112,15 @@ int32_t tkv_plan_prefill(const tkv_desc *desc, int32_t batch, int32_t n_q_heads,
                     n += k;
                     if (k > 1) partial += (double)k * (double)std::min<int64_t>(kind.rows, ((int64_t)seq_indptr[t.seq + 1] - seq_indptr[t.seq]) * group - t.row);
                 }
+                // the chip's work and the longest chain of steps: the longer one, and of the shorter 0.16 that do not fall beside it (fitted likewise), less the more rounds there are
                 const double work = std::max((double)all * heads / target_cus * kind.step, bytes * heads / kBytesPerUs), line = (double)std::min(most, longest) * kind.alone + (crosses && most > 1 ? kCrossUs : 0.0);
                 const double rounds = std::max(1.0, (double)n * heads / (kind.resident * (double)target_cus));
                 return kind.begin + (rounds - 1.0) * kind.again + std::max(work, line) + 0.16 * std::min(work, line) / rounds +
                        (partial > 0.0 ? kMergeUs + partial * heads * 8.0 * (kHeadDim + 2) / kPartialBytesPerUs : 0.0);
             };
             auto parts = [&](int64_t most) { int64_t n = 0; for (const Tile &t : mine) n += up(t.keys, most); return n; };
-            // whole ranges, or as short ones as give no more workgroups than are resident at once, or a half, a quarter, ... as many
+            // whole ranges, or as short ones as give no more workgroups than are resident at once, or a half, a quarter, ... as many; whole ones without a look at others,
+            // where there are more tiles than that
             int64_t most = longest;
             double time = expect(longest);
             for (double share = 1.0; share > 0.05; share *= 0.5) {

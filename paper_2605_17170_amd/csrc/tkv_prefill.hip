@@ -11,10 +11,11 @@
 //
 // Workgroups of 32 rows (one wavefront, four of them on a compute unit: loads of many workgroups on the way), 128 (four wavefronts, two
 // workgroups: one takes the matrix cores while the other takes exponentials) and 256 (eight, one workgroup: keys and values are
-// read half as often).  One MI355X, us: 2048 tokens of 64 heads behind 30 000 with 128 rows 1954, with 256 1888, now 1813 (1149 TFLOP/s, MFMAs busy 62 % of the
-// cycles at the 1.4 to 1.7 GHz that power leaves; the library's bf16 product of 8192^3 runs at 1414); 8192 tokens 949 (1159 TFLOP/s); 16
-// single tokens of 64 heads behind 1500 to 5000 with 128 rows 63, with 32 41, now 38 (171 MB; 5.2 TB/s within the kernel).  In between, where there are
-// few workgroups, a step's chain bounds the call: logits 870 cycles, weights 600, values 900, fetches 350, maximum and reference 300.
+// read half as often).  One MI355X, us: 2048 tokens of 64 heads behind 30 000 with 128 rows 1954, with 256 1888, now 1820 (1144 TFLOP/s, MFMAs busy 62 % of the
+// cycles at the 1.4 to 1.7 GHz that power leaves; the library's bf16 product of 8192^3 runs at 1414); 8192 tokens 950 to 980 (1122 to 1157 TFLOP/s); 16
+// single tokens of 64 heads behind 1500 to 5000 with 128 rows 63, with 32 41, now 37 (171 MB; 5.3 TB/s within the kernel).  In between, where there are
+// few workgroups, the chain of a wavefront's steps bounds the call, each logits, weights and values of a tile: for a workgroup that has a compute unit to itself
+// 0.90 us (128 rows), 1.32 (256) or 0.79 (32).
 #include <hip/hip_runtime.h>
 
 #include <type_traits>
@@ -42,8 +43,8 @@ constexpr float kNone = -3.4028235e38f;   // reference of a row that has seen no
 // the row's largest is 2^kLift at least.  bf16 weights: 0 and 8 (8192 tokens of 64 heads 954 us, by every new maximum 1016; six ragged prompts 65.9, 68.8).  fp16
 // weights end at 2^16, are whole down to 2^-14 and nothing below 2^-25: 9 and 6 keep weights down to 2^-23 of the row's largest whole and drop those below 2^-34.
 // (0 and 8 dropped those below 2^-25: 60 000 keys, each e^-18 of a sink with a small value, made an output 6 % off.)  us, 0 and 8 / 7 and 8 / 9 and 6 / 11 and 4:
-// four prompts of 2000 fp16 tokens 291 / 291 / 292 / 295, 8192 1004 / 1014 / 1014 / 1026, 2048 behind 30 000 1799 / 1832 / 1824 / 1831, where weights that were zero
-// cost power now; calls that power does not bound the same to 0.5 %, with 11 and 4 to 2 %.
+// four prompts of 2000 fp16 tokens 291 / 291 / 292 / 295, 8192 1004 / 1014 / 1014 / 1026, 2048 behind 30 000 1799 / 1832 / 1824 / 1831 (these two
+// bound by power); other calls the same to 0.5 %, with 11 and 4 to 2 %.
 template <bool BF16> constexpr float kLift = BF16 ? 0.0f : 9.0f;
 template <bool BF16> constexpr float kSlack = BF16 ? 8.0f : 6.0f;
 
